@@ -487,6 +487,134 @@ pigan_status pigan_adam_update(int64_t n, float* params, const float* grads, flo
                                float lr, float beta1, float beta2, float eps, int32_t t,
                                const int32_t* skip, void* stream);
 
+/*
+ * Layers of normalised residual networks: a linear layer with its epilogue,
+ * layer norm, and their reverse passes, on matrices of one storage type
+ * (pigan_dtype: fp32, bf16 or fp16) with fp32 vectors, statistics and parameter
+ * gradients.  Together they make critics and trunks that the packed tanh MLPs
+ * above do not cover (any sizes and row strides, five activations, layer norm,
+ * residual blocks).
+ *
+ * A matrix operand is n_groups matrices (independent layers of one shape);
+ * element (r, c) of group g is p[g * gs + r * ld + c].  ld must be at least the
+ * number of columns and gs (for more than one group) at least the extent of a
+ * group; no alignment beyond the element's is required.  Rows on 16-byte
+ * boundaries (p, ld and gs) are fastest in the linear layer.  Vectors are
+ * [n_groups, columns] fp32, contiguous.  Inputs and outputs may not overlap,
+ * except that an output may be the same matrix (pointer and strides) as an
+ * elementwise input where that is said.
+ *
+ * Sums are held in fp32 or wider and in a fixed order; a result is rounded to
+ * the storage type once, when it is stored.  fp32 products are formed from
+ * three bf16 pieces per operand (24 significand bits; six products, about fp32
+ * accuracy) or on the fp32 matrix core: an infinite operand element may turn
+ * the sums that it enters into NaN, and operands below 2^-100 may lose bits.
+ * Masks do not occur: an infinity or NaN reaches exactly the outputs that
+ * depend on it.
+ *
+ * Errors of every entry: EINVAL for null or misaligned pointers, sizes or
+ * strides out of range; EWORKSPACE for a missing or small workspace; EDEVICE
+ * for a launch failure.  No rows (M = 0) is valid: nothing but zero parameter
+ * gradients is written.
+ */
+typedef enum {
+  PIGAN_ACT_NONE = 0,
+  PIGAN_ACT_TANH = 1,
+  PIGAN_ACT_RELU = 2,    /* derivative 0 at 0 */
+  PIGAN_ACT_GELU = 3,    /* a Phi(a), Phi the normal distribution function */
+  PIGAN_ACT_SILU = 4     /* a / (1 + exp(-a)) */
+} pigan_act;
+
+typedef struct {
+  void* p;
+  int64_t ld;
+  int64_t gs;
+} pigan_mat;
+
+/* Linear layer of K inputs and N outputs on M rows per group.  Fields that a
+ * direction does not name are ignored. */
+typedef struct {
+  int32_t n_groups;
+  int32_t dt;                  /* a pigan_dtype value: x, w, y, pre, add, g, dx */
+  int32_t act;                 /* a pigan_act value */
+  int32_t reserved;            /* 0 */
+  int64_t M, K, N;             /* M >= 0; K, N in [1, 2^31 - 1] */
+  pigan_mat x;                 /* [M, K] */
+  pigan_mat w;                 /* [N, K] */
+  pigan_mat y;                 /* forward: [M, N] output */
+  pigan_mat pre;               /* forward: [M, N] pre-activation output, or p = NULL;
+                                  backward: [M, K] the pre-activation below, or p = NULL */
+  pigan_mat add;               /* forward: [M, N] residual, or p = NULL (may be y);
+                                  backward: [M, K] added to dx, or p = NULL (may be dx) */
+  pigan_mat g;                 /* backward: [M, N] cotangent of the layer's pre-activation */
+  pigan_mat dx;                /* backward: [M, K] output, or p = NULL (may be pre) */
+  const float* bias;           /* forward: [N], or NULL */
+  float* dw;                   /* backward: [N, K] output, contiguous, or NULL */
+  float* db;                   /* backward: [N] output, or NULL */
+} pigan_linear;
+
+/*
+ * pigan_linear_forward — y = act(x w^T + bias) + add, and pre = x w^T + bias.
+ *
+ * pigan_linear_backward — from the cotangent g of x w^T + bias:
+ *   dx = (g w) * act'(pre) + add, where x = act(pre): the cotangent of the
+ *        pre-activation below (pre.p = NULL and act = NONE: of x itself);
+ *   dw = g^T x,  db = sum of g over the rows (fp32).
+ * For a layer whose own output was activated, g is pigan_act_backward's.
+ *
+ * The workspace (256-byte aligned; NULL where none is needed) depends on the
+ * sizes, the type and which outputs are given; the queries return 0 for invalid
+ * arguments and 1 where none is needed.
+ */
+size_t pigan_linear_forward_workspace(const pigan_linear* a);
+pigan_status pigan_linear_forward(const pigan_linear* a, void* ws, size_t ws_bytes, void* stream);
+size_t pigan_linear_backward_workspace(const pigan_linear* a);
+pigan_status pigan_linear_backward(const pigan_linear* a, void* ws, size_t ws_bytes, void* stream);
+
+/* g = dy * act'(pre) on [M, N] matrices (g may be dy or pre); act is not NONE. */
+typedef struct {
+  int32_t n_groups;
+  int32_t dt;
+  int32_t act;
+  int32_t reserved;            /* 0 */
+  int64_t M, N;
+  pigan_mat dy, pre, g;
+} pigan_act_args;
+pigan_status pigan_act_backward(const pigan_act_args* a, void* stream);
+
+/* Layer norm over the N columns of every row. */
+typedef struct {
+  int32_t n_groups;
+  int32_t dt;                  /* x, y, dy, dx, add */
+  int64_t M, N;                /* M >= 0; N in [1, 2^31 - 1] */
+  float eps;                   /* forward: > 0 */
+  int32_t reserved;            /* 0 */
+  pigan_mat x;
+  pigan_mat y;                 /* forward: output (may be x) */
+  pigan_mat dy;                /* backward: cotangent of y */
+  pigan_mat add;               /* backward: added to dx, or p = NULL (may be dx) */
+  pigan_mat dx;                /* backward: output, or p = NULL (may be dy or add, not x) */
+  const float* gamma;          /* [N], or NULL: ones */
+  const float* beta;           /* forward: [N], or NULL: zeros */
+  float* mean;                 /* [M]: forward: output, or NULL; backward: input */
+  float* rstd;                 /* [M]: as mean */
+  float* dgamma;               /* backward: [N] output, or NULL */
+  float* dbeta;                /* backward: [N] output, or NULL */
+} pigan_norm;
+
+/*
+ * pigan_layer_norm_forward — y = (x - mean) rstd gamma + beta with
+ *   mean = mean_c(x), rstd = 1 / sqrt(mean_c((x - mean)^2) + eps).
+ *
+ * pigan_layer_norm_backward — with xhat = (x - mean) rstd and h = dy gamma:
+ *   dx = rstd (h - mean_c(h) - xhat mean_c(h xhat)) + add,
+ *   dgamma = sum of dy xhat and dbeta = sum of dy over the rows.
+ * dx given, add is a block's skip cotangent.
+ */
+pigan_status pigan_layer_norm_forward(const pigan_norm* a, void* stream);
+size_t pigan_layer_norm_backward_workspace(const pigan_norm* a);
+pigan_status pigan_layer_norm_backward(const pigan_norm* a, void* ws, size_t ws_bytes, void* stream);
+
 /* Thread-local description of the last non-OK status ("" if none). */
 const char* pigan_last_error(void);
 

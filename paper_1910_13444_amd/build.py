@@ -19,7 +19,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libpigan.so")
 
-SOURCES = ["gemm.hip", "pointwise.hip", "optim.hip", "pigan_api.cpp"]
+SOURCES = ["gemm.hip", "linear_fwd.hip", "linear_dx.hip", "linear_dw.hip", "norm.hip", "pointwise.hip", "optim.hip",
+           "pigan_api.cpp", "layers_api.cpp"]
 ARCH = "gfx950"
 
 

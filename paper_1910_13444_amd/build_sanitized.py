@@ -1,6 +1,6 @@
 """Build a host-sanitized copy of libpigan.so for the CPU tests of the
-argument checks: the C-ABI layer (pigan_api.cpp: descriptor checks,
-workspace planning, dispatch) is compiled with AddressSanitizer and
+argument checks: the C-ABI layer (pigan_api.cpp and layers_api.cpp: descriptor
+checks, workspace planning, dispatch) is compiled with AddressSanitizer and
 UndefinedBehaviorSanitizer on its host code; the kernel sources are linked
 from the ordinary build's objects (built here when missing).
 
@@ -46,7 +46,7 @@ def _compile(src: str) -> str:
     return obj
 
 
-SANITIZED = ("pigan_api.cpp",)
+SANITIZED = ("pigan_api.cpp", "layers_api.cpp")
 
 
 def _object(src: str) -> str:

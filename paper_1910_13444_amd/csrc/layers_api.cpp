@@ -1,0 +1,553 @@
+// C entry points of the linear layer, layer norm and the elementwise reverse
+// pass: argument checks, choice of kernels, workspace.
+#include <math.h>
+
+#include <algorithm>
+
+#include "api.h"
+#include "linear.h"
+#include "norm.h"
+
+namespace pigan {
+namespace {
+
+constexpr int64_t MAX_DIM = 0x7fffffff;
+
+// [rows, cols] matrices of `groups` groups; p = NULL is left to the caller
+pigan_status check_mat(const pigan_mat& m, const char* name, int32_t groups, int64_t rows, int64_t cols, size_t es) {
+  if (!m.p) return fail(PIGAN_EINVAL, "%s: null pointer", name);
+  if ((uintptr_t)m.p % es) return fail(PIGAN_EINVAL, "%s: pointer is not aligned to its elements", name);
+  if (m.ld < cols || m.ld > (int64_t(1) << 40))
+    return fail(PIGAN_EINVAL, "%s: row stride %lld out of [%lld, 2^40]", name, (long long)m.ld, (long long)cols);
+  if (groups > 1) {
+    const int64_t extent = rows > 0 ? (rows - 1) * m.ld + cols : 0;   // < 2^31 2^40
+    if (m.gs < extent || m.gs > (int64_t(1) << 46))
+      return fail(PIGAN_EINVAL, "%s: group stride %lld does not hold a group of %lld elements", name, (long long)m.gs,
+                  (long long)extent);
+  }
+  return PIGAN_OK;
+}
+
+pigan_status check_vec(const void* p, const char* name) {
+  if ((uintptr_t)p % 4) return fail(PIGAN_EINVAL, "%s: pointer is not aligned to its elements", name);
+  return PIGAN_OK;
+}
+
+pigan_status check_dims(int32_t groups, int32_t dt, int64_t M, int64_t N) {
+  if (groups < 1 || groups > 65535) return fail(PIGAN_EINVAL, "n_groups=%d out of [1, 65535]", (int)groups);
+  if (pigan_status st = check_dtype(dt)) return st;
+  if (M < 0 || M > MAX_DIM) return fail(PIGAN_EINVAL, "M=%lld out of [0, 2^31 - 1]", (long long)M);
+  if (N < 1 || N > MAX_DIM) return fail(PIGAN_EINVAL, "N=%lld out of [1, 2^31 - 1]", (long long)N);
+  return PIGAN_OK;
+}
+
+pigan_status check_act(int32_t act) {
+  if (act < PIGAN_ACT_NONE || act > PIGAN_ACT_SILU) return fail(PIGAN_EINVAL, "unknown activation %d", (int)act);
+  return PIGAN_OK;
+}
+
+pigan_status check_ws(const void* ws, size_t have, size_t need) {
+  if (need == 0) return PIGAN_OK;
+  if (!ws) return fail(PIGAN_EWORKSPACE, "null workspace, %zu bytes are needed", need);
+  if (have < need) return fail(PIGAN_EWORKSPACE, "workspace of %zu bytes, %zu are needed", have, need);
+  if ((uintptr_t)ws % 256) return fail(PIGAN_EINVAL, "the workspace must be 256-byte aligned");
+  return PIGAN_OK;
+}
+
+// an exception may not leave a C entry point
+template <class F> pigan_status guarded(F&& f) noexcept {
+  try {
+    clear_error();
+    return f();
+  } catch (...) {
+    return PIGAN_EDEVICE;
+  }
+}
+
+template <class T> Mat<const T> in(const pigan_mat& m) { return {(const T*)m.p, m.ld, m.gs}; }
+template <class T> Mat<T> out(const pigan_mat& m) { return {(T*)m.p, m.ld, m.gs}; }
+
+// f(element of the storage type)
+template <class F> pigan_status by_dtype(int32_t dt, F&& f) {
+  switch (dt) {
+    case PIGAN_BF16: return f(bf16{});
+    case PIGAN_FP16: return f(f16{});
+    default: return f(float{});
+  }
+}
+
+// ---------------------------------------------------------------------------
+// linear layer: checks
+// ---------------------------------------------------------------------------
+pigan_status check_linear(const pigan_linear* a) {
+  if (!a) return fail(PIGAN_EINVAL, "null arguments");
+  if (pigan_status st = check_dims(a->n_groups, a->dt, a->M, a->N)) return st;
+  if (a->K < 1 || a->K > MAX_DIM) return fail(PIGAN_EINVAL, "K=%lld out of [1, 2^31 - 1]", (long long)a->K);
+  if (pigan_status st = check_act(a->act)) return st;
+  if (a->reserved) return fail(PIGAN_EINVAL, "reserved=%d must be 0", (int)a->reserved);
+  return PIGAN_OK;
+}
+
+pigan_status check_forward(const pigan_linear* a) {
+  if (pigan_status st = check_linear(a)) return st;
+  const size_t es = esize(a->dt);
+  const int32_t G = a->n_groups;
+  if (pigan_status st = check_mat(a->w, "w", G, a->N, a->K, es)) return st;
+  if (pigan_status st = check_vec(a->bias, "bias")) return st;
+  if (a->M > 0 || a->x.p)
+    if (pigan_status st = check_mat(a->x, "x", G, a->M, a->K, es)) return st;
+  if (a->M > 0 || a->y.p)
+    if (pigan_status st = check_mat(a->y, "y", G, a->M, a->N, es)) return st;
+  if (a->pre.p)
+    if (pigan_status st = check_mat(a->pre, "pre", G, a->M, a->N, es)) return st;
+  if (a->add.p)
+    if (pigan_status st = check_mat(a->add, "add", G, a->M, a->N, es)) return st;
+  return PIGAN_OK;
+}
+
+pigan_status check_backward(const pigan_linear* a) {
+  if (pigan_status st = check_linear(a)) return st;
+  const size_t es = esize(a->dt);
+  const int32_t G = a->n_groups;
+  const bool rows = a->M > 0;
+  if (!a->dx.p && !a->dw && !a->db) return fail(PIGAN_EINVAL, "no output: dx, dw and db are null");
+  if (rows || a->g.p)
+    if (pigan_status st = check_mat(a->g, "g", G, a->M, a->N, es)) return st;
+  if (a->dx.p) {
+    if (pigan_status st = check_mat(a->dx, "dx", G, a->M, a->K, es)) return st;
+    if (pigan_status st = check_mat(a->w, "w", G, a->N, a->K, es)) return st;
+    if (a->act != PIGAN_ACT_NONE && !a->pre.p && rows)
+      return fail(PIGAN_EINVAL, "pre: the derivative of activation %d needs the pre-activation", (int)a->act);
+    if (a->act == PIGAN_ACT_NONE && a->pre.p) return fail(PIGAN_EINVAL, "pre: given without an activation");
+    if (a->pre.p)
+      if (pigan_status st = check_mat(a->pre, "pre", G, a->M, a->K, es)) return st;
+    if (a->add.p)
+      if (pigan_status st = check_mat(a->add, "add", G, a->M, a->K, es)) return st;
+  }
+  if (a->dw && rows)
+    if (pigan_status st = check_mat(a->x, "x", G, a->M, a->K, es)) return st;
+  if (pigan_status st = check_vec(a->dw, "dw")) return st;
+  return check_vec(a->db, "db");
+}
+
+// ---------------------------------------------------------------------------
+// linear layer: choice of tile and split
+// ---------------------------------------------------------------------------
+struct MmPlan {
+  int tile = MM_64;
+  int n_split = 1;
+};
+
+// Modelled time of a launch, from the time of a stage (64 values of k) and of
+// a block's start and epilogue, per tile; the splits of the contraction add the
+// partials' way through memory and the launch that joins them.
+MmPlan plan_mm(int64_t I, int64_t J, int64_t K, int pairs, int G) {
+  static const double stage_us[3] = {0.45, 0.75, 2.1};    // of all blocks that share a CU
+  static const double block_us[3] = {3.0, 4.0, 8.0};
+  static const int per_cu[3] = {2, 2, 1};
+  const int64_t nk = (K + 63) / 64;
+  MmPlan best;
+  double best_us = 1e30;
+  for (int t = MM_64; t <= MM_256; ++t) {
+    const int64_t s = mm_tile_side(t);
+    const double tiles = (double)((I + s - 1) / s) * (double)((J + s - 1) / s) * G;
+    for (int split = 1; split <= 64 && split <= nk; split *= 2) {
+      if (split > 1 && nk * pairs / split < 4) break;
+      const double rounds = ceil(tiles * split / (256.0 * per_cu[t]));
+      double us = rounds * ((double)((nk + split - 1) / split) * pairs * stage_us[t] + block_us[t]);
+      if (split > 1) us += 4.0 + (double)G * I * J * 4.0 * (split * 2 + 1) / 5e6;
+      if (us < best_us) {
+        best_us = us;
+        best.tile = t;
+        best.n_split = split;
+      }
+    }
+  }
+  return best;
+}
+
+// few rows, or so little work that launches count
+bool short_ok(const pigan_linear* a) {
+  if (a->M <= 64) return true;
+  const double work = (double)a->n_groups * a->M * a->K * a->N;
+  return work <= (a->dt == PIGAN_FP32 ? 1e8 : 2e7) && (a->M + 15) / 16 <= 65535;
+}
+
+// 16-byte pieces of every row: the rows may go straight to LDS
+template <class T> bool rows_aligned(const MmOperand<T>& m, int G) {
+  return (uintptr_t)m.p % 16 == 0 && m.ld % 8 == 0 && (G == 1 || m.gs % 8 == 0) && m.ld < (int64_t(1) << 21);
+}
+
+// bf16 planes of an fp32 matrix in the workspace
+struct Planes {
+  size_t at = 0;
+  int64_t rows = 0, Kp = 0;
+  void take(Carver& cv, int G, int64_t r, int64_t cols) {
+    rows = r;
+    Kp = round_up(cols, 8);
+    at = cv.take((size_t)3 * G * rows * Kp * 2);
+  }
+  MmOperand<bf16> operand(char* ws, int G) const {
+    return {(const bf16*)(ws + at), Kp, rows * Kp, (int64_t)G * rows * Kp};
+  }
+  SplitSet set(char* ws, const pigan_mat& m, int64_t cols) const {
+    return {(const float*)m.p, m.ld, m.gs, rows, cols, Kp, (bf16*)(ws + at)};
+  }
+};
+
+struct ForwardPlan {
+  bool brief = false;
+  MmPlan mm;
+  Planes x, w;
+  size_t part = 0, total = 0;
+};
+
+ForwardPlan plan_forward(const pigan_linear* a) {
+  ForwardPlan p;
+  if (a->M == 0 || (p.brief = short_ok(a))) return p;
+  Carver cv;
+  const int G = a->n_groups;
+  const bool fp32 = a->dt == PIGAN_FP32;
+  p.mm = plan_mm(a->M, a->N, a->K, fp32 ? 6 : 1, G);
+  if (fp32) {
+    p.x.take(cv, G, a->M, a->K);
+    p.w.take(cv, G, a->N, a->K);
+  }
+  if (p.mm.n_split > 1) p.part = cv.take((size_t)G * p.mm.n_split * a->M * a->N * 4);
+  p.total = cv.off;
+  return p;
+}
+
+struct BackwardPlan {
+  MmPlan dx, dw;
+  Planes g, w, x;
+  size_t part_dx = 0, part_dw = 0, part_db = 0, total = 0;
+  int db_slots = 0;
+};
+
+constexpr int COLSUM_SPLITS = 64;
+
+BackwardPlan plan_backward(const pigan_linear* a) {
+  BackwardPlan p;
+  if (a->M == 0) return p;
+  Carver cv;
+  const int G = a->n_groups;
+  const bool fp32 = a->dt == PIGAN_FP32;
+  const int pairs = fp32 ? 6 : 1;
+  if (fp32 && (a->dx.p || a->dw)) p.g.take(cv, G, a->M, a->N);
+  if (a->dx.p) {
+    p.dx = plan_mm(a->M, a->K, a->N, pairs, G);
+    if (fp32) p.w.take(cv, G, a->N, a->K);
+    if (p.dx.n_split > 1) p.part_dx = cv.take((size_t)G * p.dx.n_split * a->M * a->K * 4);
+  }
+  if (a->dw) {
+    p.dw = plan_mm(a->N, a->K, a->M, pairs, G);
+    if (fp32) p.x.take(cv, G, a->M, a->K);
+    if (p.dw.n_split > 1) p.part_dw = cv.take((size_t)G * p.dw.n_split * a->N * a->K * 4);
+    const int64_t side = mm_tile_side(p.dw.tile);
+    p.db_slots = p.dw.n_split * (int)((a->K + side - 1) / side);
+  } else {
+    p.db_slots = (int)std::min<int64_t>(a->M, COLSUM_SPLITS);
+  }
+  if (a->db) p.part_db = cv.take((size_t)G * p.db_slots * a->N * 4);
+  p.total = cv.off;
+  return p;
+}
+
+// ---------------------------------------------------------------------------
+// linear layer: launches
+// ---------------------------------------------------------------------------
+template <class TO> MmOut<TO> forward_out(const pigan_linear* a, const MmPlan& mm, float* part) {
+  MmOut<TO> o{};
+  o.I = a->M;
+  o.J = a->N;
+  o.act = a->act;
+  o.n_split = mm.n_split;
+  o.bias = a->bias;
+  o.pre = (TO*)a->pre.p; o.ldp = a->pre.ld; o.gsp = a->pre.gs;
+  o.add = (const TO*)a->add.p; o.lda = a->add.ld; o.gsa = a->add.gs;
+  o.out = (TO*)a->y.p; o.ldo = a->y.ld; o.gso = a->y.gs;
+  o.part = mm.n_split > 1 ? part : nullptr;
+  return o;
+}
+
+template <class T> MmOperand<T> operand(const pigan_mat& m) { return {(const T*)m.p, m.ld, m.gs, 0}; }
+
+template <class T, class TO>
+pigan_status forward_tiles(const MmArgs<T, TO>& m, const MmPlan& mm, int G, hipStream_t st) {
+  const bool direct = rows_aligned(m.a, G) && rows_aligned(m.b, G);
+  HIP_TRY(launch_mm_fwd(m, mm.tile, direct, G, st));
+  if (mm.n_split > 1) HIP_TRY(launch_mm_join_fwd(m.o, G, st));
+  return PIGAN_OK;
+}
+
+pigan_status run_forward(const pigan_linear* a, const ForwardPlan& p, char* ws, hipStream_t st) {
+  const int G = a->n_groups;
+  const double es = (double)esize(a->dt), MN = (double)a->M * a->N;
+  ProfScope prof(st, "linear_fwd", 2.0 * G * MN * a->K,
+                 G * (es * ((double)a->M * a->K + (double)a->N * a->K + MN * (1 + !!a->pre.p + !!a->add.p)) + 4.0 * a->N));
+  float* part = (float*)(ws + p.part);
+  if (p.brief)
+    return by_dtype(a->dt, [&](auto t) -> pigan_status {
+      typedef decltype(t) T;
+      MmArgs<T, T> m{operand<T>(a->x), operand<T>(a->w), a->K, 1, forward_out<T>(a, MmPlan{}, nullptr), nullptr};
+      HIP_TRY(launch_short_fwd(m, G, st));
+      return PIGAN_OK;
+    });
+  if (a->dt == PIGAN_FP32) {
+    const SplitSet sets[2] = {p.x.set(ws, a->x, a->K), p.w.set(ws, a->w, a->K)};
+    HIP_TRY(launch_split3(sets, 2, G, st));
+    MmArgs<bf16, float> m{p.x.operand(ws, G), p.w.operand(ws, G), a->K, 6, forward_out<float>(a, p.mm, part), nullptr};
+    return forward_tiles(m, p.mm, G, st);
+  }
+  if (a->dt == PIGAN_BF16) {
+    MmArgs<bf16, bf16> m{operand<bf16>(a->x), operand<bf16>(a->w), a->K, 1, forward_out<bf16>(a, p.mm, part), nullptr};
+    return forward_tiles(m, p.mm, G, st);
+  }
+  MmArgs<f16, f16> m{operand<f16>(a->x), operand<f16>(a->w), a->K, 1, forward_out<f16>(a, p.mm, part), nullptr};
+  return forward_tiles(m, p.mm, G, st);
+}
+
+// T: operands of the products; TO: storage type of the layer
+template <class T, class TO>
+pigan_status backward_products(const pigan_linear* a, const BackwardPlan& p, const MmOperand<T>& g,
+                               const MmOperand<T>& w, const MmOperand<T>& x, bool padded, char* ws, hipStream_t st) {
+  const int G = a->n_groups;
+  const double es = (double)esize(a->dt), MN = (double)a->M * a->N, MK = (double)a->M * a->K, NK = (double)a->N * a->K;
+  // columns of operands that run down the rows are loaded in whole pieces
+  const bool n8 = padded || a->N % 8 == 0, k8 = padded || a->K % 8 == 0;
+  if (a->dx.p) {
+    ProfScope prof(st, "linear_dx", 2.0 * G * MN * a->K, G * es * (MN + NK + MK * (1 + !!a->pre.p + !!a->add.p)));
+    MmOut<TO> o{};
+    o.I = a->M;
+    o.J = a->K;
+    o.act = a->act;
+    o.n_split = p.dx.n_split;
+    o.pre = (TO*)a->pre.p; o.ldp = a->pre.ld; o.gsp = a->pre.gs;
+    o.add = (const TO*)a->add.p; o.lda = a->add.ld; o.gsa = a->add.gs;
+    o.out = (TO*)a->dx.p; o.ldo = a->dx.ld; o.gso = a->dx.gs;
+    o.part = p.dx.n_split > 1 ? (float*)(ws + p.part_dx) : nullptr;
+    MmArgs<T, TO> m{g, w, a->N, padded ? 6 : 1, o, nullptr};
+    HIP_TRY(launch_mm_dx(m, p.dx.tile, rows_aligned(g, G) && rows_aligned(w, G) && k8, G, st));
+    if (p.dx.n_split > 1) HIP_TRY(launch_mm_join_dx(o, G, st));
+  }
+  if (a->dw) {
+    ProfScope prof(st, "linear_dw", 2.0 * G * MN * a->K, G * (es * (MN + MK) + 4.0 * NK));
+    MmOut<float> o{};
+    o.I = a->N;
+    o.J = a->K;
+    o.n_split = p.dw.n_split;
+    o.out = a->dw; o.ldo = a->K; o.gso = a->N * a->K;
+    o.part = p.dw.n_split > 1 ? (float*)(ws + p.part_dw) : nullptr;
+    MmArgs<T, float> m{g, x, a->M, padded ? 6 : 1, o, a->db ? (float*)(ws + p.part_db) : nullptr};
+    HIP_TRY(launch_mm_dw(m, p.dw.tile, rows_aligned(g, G) && rows_aligned(x, G) && n8 && k8, G, st));
+    if (p.dw.n_split > 1) HIP_TRY(launch_mm_join_dw(o, G, st));
+  }
+  return PIGAN_OK;
+}
+
+pigan_status run_backward(const pigan_linear* a, const BackwardPlan& p, char* ws, hipStream_t st) {
+  const int G = a->n_groups;
+  if (a->M == 0) {   // sums over no rows
+    if (a->dw) HIP_TRY(launch_slot_sum(nullptr, 0, 0, a->N * a->K, a->dw, a->N * a->K, nullptr, G, st));
+    if (a->db) HIP_TRY(launch_slot_sum(nullptr, 0, 0, a->N, a->db, a->N, nullptr, G, st));
+    return PIGAN_OK;
+  }
+  if (a->dx.p || a->dw) {
+    pigan_status s;
+    if (a->dt == PIGAN_FP32) {
+      SplitSet sets[3];
+      int n = 0;
+      sets[n++] = p.g.set(ws, a->g, a->N);
+      if (a->dx.p) sets[n++] = p.w.set(ws, a->w, a->K);
+      if (a->dw) sets[n++] = p.x.set(ws, a->x, a->K);
+      HIP_TRY(launch_split3(sets, n, G, st));
+      s = backward_products<bf16, float>(a, p, p.g.operand(ws, G), p.w.operand(ws, G), p.x.operand(ws, G), true, ws, st);
+    } else {
+      s = a->dt == PIGAN_BF16
+              ? backward_products<bf16, bf16>(a, p, operand<bf16>(a->g), operand<bf16>(a->w), operand<bf16>(a->x), false, ws, st)
+              : backward_products<f16, f16>(a, p, operand<f16>(a->g), operand<f16>(a->w), operand<f16>(a->x), false, ws, st);
+    }
+    if (s != PIGAN_OK) return s;
+  }
+  if (a->db) {
+    float* part = (float*)(ws + p.part_db);
+    if (!a->dw) {
+      pigan_status s = by_dtype(a->dt, [&](auto t) -> pigan_status {
+        HIP_TRY(launch_colsum_rows(in<decltype(t)>(a->g), a->M, a->N, p.db_slots, part, G, st));
+        return PIGAN_OK;
+      });
+      if (s != PIGAN_OK) return s;
+    }
+    HIP_TRY(launch_slot_sum(part, (int64_t)p.db_slots * a->N, p.db_slots, a->N, a->db, a->N, nullptr, G, st));
+  }
+  return PIGAN_OK;
+}
+
+// ---------------------------------------------------------------------------
+// layer norm
+// ---------------------------------------------------------------------------
+pigan_status check_norm(const pigan_norm* a) {
+  if (!a) return fail(PIGAN_EINVAL, "null arguments");
+  if (pigan_status st = check_dims(a->n_groups, a->dt, a->M, a->N)) return st;
+  if (a->reserved) return fail(PIGAN_EINVAL, "reserved=%d must be 0", (int)a->reserved);
+  const void* vecs[6] = {a->gamma, a->beta, a->mean, a->rstd, a->dgamma, a->dbeta};
+  const char* names[6] = {"gamma", "beta", "mean", "rstd", "dgamma", "dbeta"};
+  for (int i = 0; i < 6; ++i)
+    if (pigan_status st = check_vec(vecs[i], names[i])) return st;
+  if (a->M > 0 || a->x.p) return check_mat(a->x, "x", a->n_groups, a->M, a->N, esize(a->dt));
+  return PIGAN_OK;
+}
+
+pigan_status check_norm_backward(const pigan_norm* a) {
+  if (pigan_status st = check_norm(a)) return st;
+  const size_t es = esize(a->dt);
+  if (!a->dx.p && !a->dgamma && !a->dbeta) return fail(PIGAN_EINVAL, "no output: dx, dgamma and dbeta are null");
+  if (a->M == 0) return PIGAN_OK;
+  if (!a->mean || !a->rstd) return fail(PIGAN_EINVAL, "mean and rstd: null pointer");
+  if (pigan_status st = check_mat(a->dy, "dy", a->n_groups, a->M, a->N, es)) return st;
+  if (a->add.p)
+    if (pigan_status st = check_mat(a->add, "add", a->n_groups, a->M, a->N, es)) return st;
+  if (a->dx.p) {
+    if (pigan_status st = check_mat(a->dx, "dx", a->n_groups, a->M, a->N, es)) return st;
+    if (a->dx.p == a->x.p) return fail(PIGAN_EINVAL, "dx: may not be x");
+  }
+  return PIGAN_OK;
+}
+
+template <class T> NormArgs<T> norm_args(const pigan_norm* a) {
+  NormArgs<T> n{};
+  n.x = in<T>(a->x);
+  n.gamma = a->gamma;
+  n.beta = a->beta;
+  n.mean = a->mean;
+  n.rstd = a->rstd;
+  n.M = a->M;
+  n.N = a->N;
+  n.eps = a->eps;
+  return n;
+}
+
+size_t norm_ws(const pigan_norm* a) {
+  return a->dgamma || a->dbeta ? (size_t)a->n_groups * norm_part_floats((int)esize(a->dt), a->M, a->N) * 4 : 0;
+}
+
+}  // namespace
+}  // namespace pigan
+
+using namespace pigan;
+
+extern "C" {
+
+size_t pigan_linear_forward_workspace(const pigan_linear* a) {
+  size_t n = 0;
+  guarded([&]() -> pigan_status {
+    if (pigan_status st = check_linear(a)) return st;
+    n = std::max<size_t>(plan_forward(a).total, 1);
+    return PIGAN_OK;
+  });
+  return n;
+}
+
+pigan_status pigan_linear_forward(const pigan_linear* a, void* ws, size_t ws_bytes, void* stream) {
+  return guarded([&]() -> pigan_status {
+    if (pigan_status st = check_forward(a)) return st;
+    const ForwardPlan p = plan_forward(a);
+    if (pigan_status st = check_ws(ws, ws_bytes, p.total)) return st;
+    return a->M == 0 ? PIGAN_OK : run_forward(a, p, (char*)ws, (hipStream_t)stream);
+  });
+}
+
+size_t pigan_linear_backward_workspace(const pigan_linear* a) {
+  size_t n = 0;
+  guarded([&]() -> pigan_status {
+    if (pigan_status st = check_linear(a)) return st;
+    n = std::max<size_t>(plan_backward(a).total, 1);
+    return PIGAN_OK;
+  });
+  return n;
+}
+
+pigan_status pigan_linear_backward(const pigan_linear* a, void* ws, size_t ws_bytes, void* stream) {
+  return guarded([&]() -> pigan_status {
+    if (pigan_status st = check_backward(a)) return st;
+    const BackwardPlan p = plan_backward(a);
+    if (pigan_status st = check_ws(ws, ws_bytes, p.total)) return st;
+    return run_backward(a, p, (char*)ws, (hipStream_t)stream);
+  });
+}
+
+pigan_status pigan_act_backward(const pigan_act_args* a, void* stream) {
+  return guarded([&]() -> pigan_status {
+    if (!a) return fail(PIGAN_EINVAL, "null arguments");
+    if (pigan_status st = check_dims(a->n_groups, a->dt, a->M, a->N)) return st;
+    if (pigan_status st = check_act(a->act)) return st;
+    if (a->act == PIGAN_ACT_NONE) return fail(PIGAN_EINVAL, "act: no activation to differentiate");
+    if (a->reserved) return fail(PIGAN_EINVAL, "reserved=%d must be 0", (int)a->reserved);
+    if (a->M == 0) return PIGAN_OK;
+    const size_t es = esize(a->dt);
+    if (pigan_status st = check_mat(a->dy, "dy", a->n_groups, a->M, a->N, es)) return st;
+    if (pigan_status st = check_mat(a->pre, "pre", a->n_groups, a->M, a->N, es)) return st;
+    if (pigan_status st = check_mat(a->g, "g", a->n_groups, a->M, a->N, es)) return st;
+    const hipStream_t st = (hipStream_t)stream;
+    ProfScope prof(st, "act_backward", 0.0, 3.0 * es * a->n_groups * (double)a->M * a->N);
+    return by_dtype(a->dt, [&](auto t) -> pigan_status {
+      typedef decltype(t) T;
+      HIP_TRY(launch_act_bwd<T>(a->act, in<T>(a->dy), in<T>(a->pre), out<T>(a->g), a->M, a->N, a->n_groups, st));
+      return PIGAN_OK;
+    });
+  });
+}
+
+pigan_status pigan_layer_norm_forward(const pigan_norm* a, void* stream) {
+  return guarded([&]() -> pigan_status {
+    if (pigan_status st = check_norm(a)) return st;
+    if (!(a->eps > 0.0f) || !__builtin_isfinite(a->eps)) return fail(PIGAN_EINVAL, "eps=%g must be finite and > 0", a->eps);
+    if (a->M == 0) return PIGAN_OK;
+    if (pigan_status st = check_mat(a->y, "y", a->n_groups, a->M, a->N, esize(a->dt))) return st;
+    const hipStream_t st = (hipStream_t)stream;
+    ProfScope prof(st, "layer_norm_fwd", 0.0, 2.0 * esize(a->dt) * a->n_groups * (double)a->M * a->N);
+    return by_dtype(a->dt, [&](auto t) -> pigan_status {
+      typedef decltype(t) T;
+      NormArgs<T> n = norm_args<T>(a);
+      n.out = out<T>(a->y);
+      HIP_TRY(launch_norm_fwd(n, a->n_groups, st));
+      return PIGAN_OK;
+    });
+  });
+}
+
+size_t pigan_layer_norm_backward_workspace(const pigan_norm* a) {
+  size_t n = 0;
+  guarded([&]() -> pigan_status {
+    if (!a) return fail(PIGAN_EINVAL, "null arguments");
+    if (pigan_status st = check_dims(a->n_groups, a->dt, a->M, a->N)) return st;
+    n = std::max<size_t>(norm_ws(a), 1);
+    return PIGAN_OK;
+  });
+  return n;
+}
+
+pigan_status pigan_layer_norm_backward(const pigan_norm* a, void* ws, size_t ws_bytes, void* stream) {
+  return guarded([&]() -> pigan_status {
+    if (pigan_status st = check_norm_backward(a)) return st;
+    if (pigan_status st = check_ws(ws, ws_bytes, norm_ws(a))) return st;
+    const hipStream_t st = (hipStream_t)stream;
+    ProfScope prof(st, "layer_norm_bwd", 0.0,
+                   (2.0 + !!a->dx.p + !!a->add.p) * esize(a->dt) * a->n_groups * (double)a->M * a->N);
+    return by_dtype(a->dt, [&](auto t) -> pigan_status {
+      typedef decltype(t) T;
+      NormArgs<T> n = norm_args<T>(a);
+      n.dy = in<T>(a->dy);
+      n.add = in<T>(a->add);
+      n.out = out<T>(a->dx);
+      n.dgamma = a->dgamma;
+      n.dbeta = a->dbeta;
+      n.part = (float*)ws;
+      HIP_TRY(launch_norm_bwd(n, a->n_groups, st));
+      return PIGAN_OK;
+    });
+  });
+}
+
+}  // extern "C"

@@ -1,0 +1,587 @@
+// Layer norm (forward, backward with the column sums of its parameter
+// gradients) and the reverse pass of an activation, for gfx950.
+//
+// All of it is bound by memory: a row is read once into registers, its
+// statistics are sums over the lanes that hold it, and the results leave from
+// the same registers.  TPR threads share a row, NV 16-byte pieces each; rows
+// may start at any element (the pieces are under-aligned vector accesses).
+#include "norm.h"
+
+#include "act.h"
+#include "piece.h"
+
+namespace pigan {
+namespace {
+
+// Sum over the TPR threads of a row, in a fixed order; every one of them gets
+// it.  Above a wave, `red` (one entry per wave) passes the waves' sums on; the
+// caller alternates between two of them, so one barrier per sum is enough.
+template <int TPR>
+__device__ __forceinline__ float row_sum(float v, float* red) {
+#pragma unroll
+  for (int o = 1; o < (TPR < 64 ? TPR : 64); o *= 2) v += __shfl_xor(v, o);
+  if constexpr (TPR > 64) {
+    constexpr int NW = TPR / 64;
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) red[wave] = v;
+    __syncthreads();
+    const float* r = red + wave / NW * NW;
+    v = r[0];
+#pragma unroll
+    for (int i = 1; i < NW; ++i) v += r[i];
+  }
+  return v;
+}
+
+// ---------------------------------------------------------------------------
+// Forward.  Two sums over registers (mean, then squared distances from it: no
+// cancellation).  Blocks walk rows; the next row is requested before the
+// present one is worked on, gamma and beta stay in registers.
+// ---------------------------------------------------------------------------
+template <class T, int TPR, int NV, int NTH>
+__global__ void __launch_bounds__(NTH) k_norm_fwd(const NormArgs<T> p) {
+  constexpr int E = EPP<T>, RPB = NTH / TPR;
+  __shared__ float red[2][NTH / 64];
+  const int g = blockIdx.z;
+  const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  const T* x = p.x.p + g * p.x.gs;
+  T* y = p.out.p + g * p.out.gs;
+  const float* gamma = p.gamma ? p.gamma + g * p.N : nullptr;
+  const float* beta = p.beta ? p.beta + g * p.N : nullptr;
+  const int64_t step = (int64_t)gridDim.x * RPB;
+  const float n = (float)p.N;   // divided by: the mean of a constant row is that constant
+
+  float ga[NV][E], be[NV][E];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int64_t c = (int64_t)(v * TPR + lane) * E;
+    vec_load<E>(gamma, c, p.N, 1.0f, ga[v]);
+    vec_load<E>(beta, c, p.N, 0.0f, be[v]);
+  }
+  auto request = [&](piece_t (&raw)[NV], int64_t r) {
+    const T* row = x + (r < p.M ? r : p.M - 1) * p.x.ld;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int64_t c = (int64_t)(v * TPR + lane) * E;
+      raw[v] = piece_load(row + c, p.N - c);
+    }
+  };
+  piece_t next[NV];
+  int64_t r0 = (int64_t)blockIdx.x * RPB;
+  request(next, r0 + sub);
+  // every thread of a block takes the same number of turns (barriers above a wave)
+  for (; r0 < p.M; r0 += step) {
+    const int64_t r = r0 + sub;
+    float f[NV][E];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) piece_floats<T>(next[v], f[v]);
+    if (r0 + step < p.M) request(next, r + step);
+    float s = 0.0f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int e = 0; e < E; ++e) s += f[v][e];       // zeros past the end
+    const float mean = row_sum<TPR>(s, red[0]) / n;
+    float q = 0.0f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int64_t c = (int64_t)(v * TPR + lane) * E;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        f[v][e] -= mean;
+        q += c + e < p.N ? f[v][e] * f[v][e] : 0.0f;
+      }
+    }
+    const float var = row_sum<TPR>(q, red[1]) / n;
+    const float rstd = 1.0f / sqrtf(var + p.eps);
+    if (r < p.M) {
+      T* row = y + r * p.out.ld;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const int64_t c = (int64_t)(v * TPR + lane) * E;
+#pragma unroll
+        for (int e = 0; e < E; ++e) f[v][e] = f[v][e] * rstd * ga[v][e] + be[v][e];
+        piece_store(row + c, p.N - c, f[v]);
+      }
+      if (lane == 0) {
+        if (p.mean) p.mean[g * p.M + r] = mean;
+        if (p.rstd) p.rstd[g * p.M + r] = rstd;
+      }
+    }
+  }
+}
+
+// Rows too long for registers: the row is read three times (from L2 after the
+// first), a block of 1024 threads per row.
+template <class T>
+__global__ void __launch_bounds__(1024) k_norm_fwd_long(const NormArgs<T> p) {
+  constexpr int E = EPP<T>;
+  __shared__ float red[2][16];
+  const int g = blockIdx.z;
+  const float* gamma = p.gamma ? p.gamma + g * p.N : nullptr;
+  const float* beta = p.beta ? p.beta + g * p.N : nullptr;
+  const float n = (float)p.N;   // divided by: the mean of a constant row is that constant
+  for (int64_t r = blockIdx.x; r < p.M; r += gridDim.x) {
+    const T* row = p.x.p + g * p.x.gs + r * p.x.ld;
+    T* out = p.out.p + g * p.out.gs + r * p.out.ld;
+    float s = 0.0f, f[E];
+    for (int64_t c = (int64_t)threadIdx.x * E; c < p.N; c += 1024 * E) {
+      piece_floats<T>(piece_load(row + c, p.N - c), f);
+#pragma unroll
+      for (int e = 0; e < E; ++e) s += f[e];
+    }
+    const float mean = row_sum<1024>(s, red[0]) / n;
+    float q = 0.0f;
+    for (int64_t c = (int64_t)threadIdx.x * E; c < p.N; c += 1024 * E) {
+      piece_floats<T>(piece_load(row + c, p.N - c), f);
+#pragma unroll
+      for (int e = 0; e < E; ++e) q += c + e < p.N ? (f[e] - mean) * (f[e] - mean) : 0.0f;
+    }
+    const float rstd = 1.0f / sqrtf(row_sum<1024>(q, red[1]) / n + p.eps);
+    for (int64_t c = (int64_t)threadIdx.x * E; c < p.N; c += 1024 * E) {
+      float ga[E], be[E];
+      piece_floats<T>(piece_load(row + c, p.N - c), f);
+      vec_load<E>(gamma, c, p.N, 1.0f, ga);
+      vec_load<E>(beta, c, p.N, 0.0f, be);
+#pragma unroll
+      for (int e = 0; e < E; ++e) f[e] = (f[e] - mean) * rstd * ga[e] + be[e];
+      piece_store(out + c, p.N - c, f);
+    }
+    if (threadIdx.x == 0) {
+      if (p.mean) p.mean[g * p.M + r] = mean;
+      if (p.rstd) p.rstd[g * p.M + r] = rstd;
+    }
+    // a thread may not begin the next row's sums while another still reads these
+    __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Backward.  As the forward, with two sums per row (h and h xhat); a thread
+// keeps the column sums of its NV pieces over all rows of the block in
+// registers, the block adds its waves' in order and writes one partial row of
+// [dgamma, dbeta] (the final ones, where one block takes all rows).
+// ---------------------------------------------------------------------------
+constexpr int BWD_NTH = 1024;
+
+template <class T, int TPR, int NV, bool DX, bool COLS>
+__global__ void __launch_bounds__(BWD_NTH) k_norm_bwd(const NormArgs<T> p, float* __restrict__ d0,
+                                                      float* __restrict__ d1, int64_t d_g, int64_t d_b) {
+  constexpr int E = EPP<T>, RPB = BWD_NTH / TPR;
+  __shared__ float red[4][BWD_NTH / 64];
+  __shared__ float cols[COLS && TPR <= 64 ? 2 * TPR * NV * E : 1];
+  const int g = blockIdx.z;
+  const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  const T* x = p.x.p + g * p.x.gs;
+  const T* dy = p.dy.p + g * p.dy.gs;
+  const T* add = p.add.p ? p.add.p + g * p.add.gs : nullptr;
+  const float* gamma = p.gamma ? p.gamma + g * p.N : nullptr;
+  const int64_t step = (int64_t)gridDim.x * RPB;
+  const float n = (float)p.N;   // divided by: the mean of a constant row is that constant
+
+  float ga[NV][E], sg[NV][E], sb[NV][E];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    vec_load<E>(gamma, (int64_t)(v * TPR + lane) * E, p.N, 1.0f, ga[v]);
+#pragma unroll
+    for (int e = 0; e < E; ++e) sg[v][e] = sb[v][e] = 0.0f;
+  }
+  int turn = 0;
+  for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < p.M; r0 += step, turn ^= 1) {
+    const int64_t r = r0 + sub;
+    const bool live = r < p.M;
+    const int64_t rc = live ? r : p.M - 1;
+    piece_t rx[NV], rd[NV], ra[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int64_t c = (int64_t)(v * TPR + lane) * E;
+      rx[v] = piece_load(x + rc * p.x.ld + c, p.N - c);
+      rd[v] = piece_load(dy + rc * p.dy.ld + c, p.N - c);
+    }
+    if (DX && add) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const int64_t c = (int64_t)(v * TPR + lane) * E;
+        ra[v] = piece_load(add + rc * p.add.ld + c, p.N - c);
+      }
+    }
+    const float mean = p.mean[g * p.M + rc], rstd = p.rstd[g * p.M + rc];
+    float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      float fx[E], fd[E];
+      const int64_t c = (int64_t)(v * TPR + lane) * E;
+      piece_floats<T>(rx[v], fx);
+      piece_floats<T>(rd[v], fd);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        // selected, not multiplied: a row or column past the end adds nothing
+        const float xh = live && c + e < p.N ? (fx[e] - mean) * rstd : 0.0f;
+        const float d = live ? fd[e] : 0.0f;
+        const float h = d * ga[v][e];
+        s1 += h;
+        s2 += h * xh;
+        if (COLS) {
+          sg[v][e] += d * xh;
+          sb[v][e] += d;
+        }
+      }
+    }
+    if constexpr (DX) {
+      s1 = row_sum<TPR>(s1, red[2 * turn]) / n;
+      s2 = row_sum<TPR>(s2, red[2 * turn + 1]) / n;
+      if (live) {
+        T* row = p.out.p + g * p.out.gs + r * p.out.ld;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+          float fx[E], fd[E], o[E];
+          const int64_t c = (int64_t)(v * TPR + lane) * E;
+          piece_floats<T>(rx[v], fx);
+          piece_floats<T>(rd[v], fd);
+#pragma unroll
+          for (int e = 0; e < E; ++e) o[e] = rstd * (fd[e] * ga[v][e] - s1 - (fx[e] - mean) * rstd * s2);
+          if (add) {
+            piece_floats<T>(ra[v], fd);
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] += fd[e];
+          }
+          piece_store(row + c, p.N - c, o);
+        }
+      }
+    }
+  }
+  if constexpr (COLS) {
+    float* o0 = d0 ? d0 + g * d_g + blockIdx.x * d_b : nullptr;
+    float* o1 = d1 ? d1 + g * d_g + blockIdx.x * d_b : nullptr;
+    if constexpr (TPR < 64) {
+      // lanes of a wave that hold the same columns
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+#pragma unroll
+          for (int o = TPR; o < 64; o *= 2) {
+            sg[v][e] += __shfl_xor(sg[v][e], o);
+            sb[v][e] += __shfl_xor(sb[v][e], o);
+          }
+    }
+    if constexpr (TPR <= 64) {
+      for (int w = 0; w < BWD_NTH / 64; ++w) {
+        if ((int)(threadIdx.x >> 6) == w && (threadIdx.x & 63) < TPR) {
+#pragma unroll
+          for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+              const int c = (v * TPR + lane) * E + e;
+              cols[c] = w ? cols[c] + sg[v][e] : sg[v][e];
+              cols[TPR * NV * E + c] = w ? cols[TPR * NV * E + c] + sb[v][e] : sb[v][e];
+            }
+        }
+        __syncthreads();
+      }
+      for (int c = threadIdx.x; c < p.N; c += BWD_NTH) {
+        if (o0) o0[c] = cols[c];
+        if (o1) o1[c] = cols[TPR * NV * E + c];
+      }
+    } else if constexpr (TPR == BWD_NTH) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const int64_t c = (int64_t)(v * TPR + lane) * E + e;
+          if (c < p.N && o0) o0[c] = sg[v][e];
+          if (c < p.N && o1) o1[c] = sb[v][e];
+        }
+    } else {
+      static_assert(TPR == BWD_NTH || !COLS, "column sums above a wave: one row per block");
+    }
+  }
+}
+
+// Rows too long for registers: two passes over the row.
+template <class T>
+__global__ void __launch_bounds__(1024) k_norm_bwd_long(const NormArgs<T> p) {
+  constexpr int E = EPP<T>;
+  __shared__ float red[2][16];
+  const int g = blockIdx.z;
+  const float* gamma = p.gamma ? p.gamma + g * p.N : nullptr;
+  const float n = (float)p.N;   // divided by: the mean of a constant row is that constant
+  for (int64_t r = blockIdx.x; r < p.M; r += gridDim.x) {
+    const T* x = p.x.p + g * p.x.gs + r * p.x.ld;
+    const T* dy = p.dy.p + g * p.dy.gs + r * p.dy.ld;
+    const T* add = p.add.p ? p.add.p + g * p.add.gs + r * p.add.ld : nullptr;
+    T* out = p.out.p + g * p.out.gs + r * p.out.ld;
+    const float mean = p.mean[g * p.M + r], rstd = p.rstd[g * p.M + r];
+    float s1 = 0.0f, s2 = 0.0f, fx[E], fd[E], ga[E];
+    for (int64_t c = (int64_t)threadIdx.x * E; c < p.N; c += 1024 * E) {
+      piece_floats<T>(piece_load(x + c, p.N - c), fx);
+      piece_floats<T>(piece_load(dy + c, p.N - c), fd);
+      vec_load<E>(gamma, c, p.N, 1.0f, ga);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float h = fd[e] * ga[e];
+        s1 += h;
+        s2 += c + e < p.N ? h * ((fx[e] - mean) * rstd) : 0.0f;
+      }
+    }
+    s1 = row_sum<1024>(s1, red[0]) / n;
+    s2 = row_sum<1024>(s2, red[1]) / n;
+    for (int64_t c = (int64_t)threadIdx.x * E; c < p.N; c += 1024 * E) {
+      float o[E];
+      piece_floats<T>(piece_load(x + c, p.N - c), fx);
+      piece_floats<T>(piece_load(dy + c, p.N - c), fd);
+      vec_load<E>(gamma, c, p.N, 1.0f, ga);
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = rstd * (fd[e] * ga[e] - s1 - (fx[e] - mean) * rstd * s2);
+      if (add) {
+        piece_floats<T>(piece_load(add + c, p.N - c), fd);
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] += fd[e];
+      }
+      piece_store(out + c, p.N - c, o);
+    }
+    __syncthreads();
+  }
+}
+
+// Column sums where the columns of a row do not fit a block's registers: a
+// block takes 256 pieces of columns and the rows b, b + gridDim.y, ...
+template <class T>
+__global__ void __launch_bounds__(256) k_norm_cols(const NormArgs<T> p, float* __restrict__ d0,
+                                                   float* __restrict__ d1, int64_t d_g, int64_t d_b) {
+  constexpr int E = EPP<T>;
+  const int g = blockIdx.z;
+  const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * E;
+  if (c >= p.N) return;
+  const T* x = p.x.p + g * p.x.gs + c;
+  const T* dy = p.dy.p + g * p.dy.gs + c;
+  float sg[E], sb[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) sg[e] = sb[e] = 0.0f;
+#pragma unroll 2
+  for (int64_t r = blockIdx.y; r < p.M; r += gridDim.y) {
+    float fx[E], fd[E];
+    piece_floats<T>(piece_load(x + r * p.x.ld, p.N - c), fx);
+    piece_floats<T>(piece_load(dy + r * p.dy.ld, p.N - c), fd);
+    const float mean = p.mean[g * p.M + r], rstd = p.rstd[g * p.M + r];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      sg[e] += fd[e] * ((fx[e] - mean) * rstd);
+      sb[e] += fd[e];
+    }
+  }
+  const int64_t o = g * d_g + blockIdx.y * d_b + c;
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    if (c + e < p.N) {
+      if (d0) d0[o + e] = sg[e];
+      if (d1) d1[o + e] = sb[e];
+    }
+}
+
+template <class T>
+__global__ void __launch_bounds__(256) k_colsum_rows(const Mat<const T> m, int64_t M, int64_t N,
+                                                     float* __restrict__ part) {
+  constexpr int E = EPP<T>;
+  const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * E;
+  if (c >= N) return;
+  const T* p = m.p + blockIdx.z * m.gs + c;
+  float s[E], f[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) s[e] = 0.0f;
+#pragma unroll 4
+  for (int64_t r = blockIdx.y; r < M; r += gridDim.y) {
+    piece_floats<T>(piece_load(p + r * m.ld, N - c), f);
+#pragma unroll
+    for (int e = 0; e < E; ++e) s[e] += f[e];
+  }
+  float* o = part + ((int64_t)blockIdx.z * gridDim.y + blockIdx.y) * N + c;
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    if (c + e < N) o[e] = s[e];
+}
+
+// Slot sums: 32 columns x 32 slot lanes per block; a slot lane adds every 32nd
+// slot in fp64, the 32 lanes' sums are added in order.
+__global__ void __launch_bounds__(1024) k_slot_sum(const float* __restrict__ part, int64_t p_g, int n_slots, int64_t n,
+                                                   float* __restrict__ dst, int64_t n1, float* __restrict__ dst2) {
+  __shared__ double sums[32][33];
+  const int cl = threadIdx.x & 31, sl = threadIdx.x >> 5;
+  const int64_t c = (int64_t)blockIdx.x * 32 + cl;
+  const int g = blockIdx.z;
+  double s = 0.0;
+  if (c < n) {
+    const float* q = part + g * p_g + c;
+#pragma unroll 4
+    for (int i = sl; i < n_slots; i += 32) s += (double)q[(int64_t)i * n];
+  }
+  sums[sl][cl] = s;
+  __syncthreads();
+  if (sl == 0 && c < n) {
+    for (int i = 1; i < 32; ++i) s += sums[i][cl];
+    if (c < n1) {
+      if (dst) dst[g * n1 + c] = (float)s;
+    } else if (dst2) {
+      dst2[g * (n - n1) + c - n1] = (float)s;
+    }
+  }
+}
+
+// g = dy act'(pre), a piece per thread and turn; `vpr` pieces per row
+template <class T, class I>
+__global__ void __launch_bounds__(256) k_act_bwd(int act, const Mat<const T> dy, const Mat<const T> pre, const Mat<T> out,
+                                                 int64_t M, int64_t N, I vpr) {
+  constexpr int E = EPP<T>;
+  const int g = blockIdx.z;
+  const I total = (I)M * vpr, stride = (I)gridDim.x * 256;
+  const T* pd = dy.p + g * dy.gs;
+  const T* pa = pre.p + g * pre.gs;
+  T* po = out.p + g * out.gs;
+  PIGAN_ACT_SWITCH(act, {
+    for (I i = (I)blockIdx.x * 256 + threadIdx.x; i < total; i += stride) {
+      const I r = i / vpr;
+      const int64_t c = (int64_t)(i - r * vpr) * E;
+      float fd[E], fa[E];
+      piece_floats<T>(piece_load(pd + (int64_t)r * dy.ld + c, N - c), fd);
+      piece_floats<T>(piece_load(pa + (int64_t)r * pre.ld + c, N - c), fa);
+      for (int e = 0; e < E; ++e) fd[e] *= act_slope<ACT>(fa[e]);
+      piece_store(po + (int64_t)r * out.ld + c, N - c, fd);
+    }
+  })
+}
+
+// ---------------------------------------------------------------------------
+// launchers
+// ---------------------------------------------------------------------------
+int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// pieces of a row that a block's registers hold at most: 1024 threads, two each
+constexpr int64_t MAX_PIECES = 2048;
+
+template <class T, int TPR, int NV, int NTH>
+void fwd(const NormArgs<T>& a, int G, hipStream_t st) {
+  // 16 waves per CU and row of the grid: enough loads in flight, and gamma and
+  // beta are read once for many rows
+  const int64_t most = cdiv(int64_t(256) * 2048 / NTH, G);
+  const int64_t blocks = cdiv(a.M, NTH / TPR);
+  k_norm_fwd<T, TPR, NV, NTH><<<dim3((unsigned)(blocks < most ? blocks : most), 1, G), NTH, 0, st>>>(a);
+}
+
+// blocks of the backward kernel per group, and threads per row
+int bwd_tpr(int64_t pieces) { return pieces <= 8 ? 8 : pieces <= 32 ? 32 : pieces <= 128 ? 64 : BWD_NTH; }
+int64_t bwd_blocks(int64_t pieces, int64_t M) {
+  const int64_t want = cdiv(M, BWD_NTH / bwd_tpr(pieces));
+  return want < 256 ? want : 256;   // one block per CU; each more is another partial row
+}
+int64_t cols_splits(int64_t M) { return M < 64 ? M : 64; }
+
+template <class T, int TPR, int NV>
+void bwd(const NormArgs<T>& a, int64_t nb, int G, hipStream_t st) {
+  const dim3 grid((unsigned)nb, 1, G);
+  const bool cols = a.dgamma || a.dbeta;
+  float* d0 = !cols ? nullptr : nb > 1 ? a.part : a.dgamma;
+  float* d1 = !cols ? nullptr : nb > 1 ? a.part + a.N : a.dbeta;
+  const int64_t d_g = nb > 1 ? nb * 2 * a.N : a.N, d_b = 2 * a.N;
+  if (a.out.p && cols) k_norm_bwd<T, TPR, NV, true, true><<<grid, BWD_NTH, 0, st>>>(a, d0, d1, d_g, d_b);
+  else if (cols) k_norm_bwd<T, TPR, NV, false, true><<<grid, BWD_NTH, 0, st>>>(a, d0, d1, d_g, d_b);
+  else if (a.out.p) k_norm_bwd<T, TPR, NV, true, false><<<grid, BWD_NTH, 0, st>>>(a, d0, d1, d_g, d_b);
+}
+
+}  // namespace
+
+template <class T>
+hipError_t launch_norm_fwd(const NormArgs<T>& a, int G, hipStream_t st) {
+  if (a.M <= 0) return hipSuccess;
+  const int64_t pc = cdiv(a.N, EPP<T>);
+  if (pc <= 8) fwd<T, 8, 1, 256>(a, G, st);
+  else if (pc <= 32) fwd<T, 32, 1, 256>(a, G, st);
+  else if (pc <= 64) fwd<T, 64, 1, 256>(a, G, st);
+  else if (pc <= 128) fwd<T, 64, 2, 256>(a, G, st);
+  else if (pc <= 256) fwd<T, 256, 1, 256>(a, G, st);
+  else if (pc <= 512) fwd<T, 256, 2, 256>(a, G, st);
+  else if (pc <= 1024) fwd<T, 1024, 1, 1024>(a, G, st);
+  else if (pc <= MAX_PIECES) fwd<T, 1024, 2, 1024>(a, G, st);
+  else k_norm_fwd_long<T><<<dim3((unsigned)(a.M < 65536 ? a.M : 65536), 1, G), 1024, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+int64_t norm_part_floats(int elem_bytes, int64_t M, int64_t N) {
+  const int64_t pc = cdiv(N, 16 / elem_bytes);
+  const int64_t nb = pc <= MAX_PIECES ? bwd_blocks(pc, M) : cols_splits(M);
+  return nb > 1 ? nb * 2 * N : 0;
+}
+
+template <class T>
+hipError_t launch_norm_bwd(const NormArgs<T>& a, int G, hipStream_t st) {
+  const bool cols = a.dgamma || a.dbeta;
+  if (a.M <= 0) {
+    // sums over no rows
+    return cols ? launch_slot_sum(nullptr, 0, 0, 2 * a.N, a.dgamma, a.N, a.dbeta, G, st) : hipSuccess;
+  }
+  const int64_t pc = cdiv(a.N, EPP<T>);
+  int64_t nb;
+  if (pc <= MAX_PIECES) {
+    nb = bwd_blocks(pc, a.M);
+    if (pc <= 8) bwd<T, 8, 1>(a, nb, G, st);
+    else if (pc <= 32) bwd<T, 32, 1>(a, nb, G, st);
+    else if (pc <= 64) bwd<T, 64, 1>(a, nb, G, st);
+    else if (pc <= 128) bwd<T, 64, 2>(a, nb, G, st);
+    else if (pc <= 1024) bwd<T, BWD_NTH, 1>(a, nb, G, st);
+    else bwd<T, BWD_NTH, 2>(a, nb, G, st);
+  } else {
+    nb = cols_splits(a.M);
+    if (cols) {
+      float* d0 = nb > 1 ? a.part : a.dgamma;
+      float* d1 = nb > 1 ? a.part + a.N : a.dbeta;
+      k_norm_cols<T><<<dim3((unsigned)cdiv(pc, 256), (unsigned)nb, G), 256, 0, st>>>(
+          a, d0, d1, nb > 1 ? nb * 2 * a.N : a.N, 2 * a.N);
+    }
+    // after the column sums: dx may overwrite dy
+    if (a.out.p) k_norm_bwd_long<T><<<dim3((unsigned)(a.M < 65536 ? a.M : 65536), 1, G), 1024, 0, st>>>(a);
+  }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !cols || nb == 1) return e;
+  return launch_slot_sum(a.part, nb * 2 * a.N, (int)nb, 2 * a.N, a.dgamma, a.N, a.dbeta, G, st);
+}
+
+hipError_t launch_slot_sum(const float* part, int64_t p_g, int n_slots, int64_t n, float* dst, int64_t n1, float* dst2,
+                           int G, hipStream_t st) {
+  k_slot_sum<<<dim3((unsigned)cdiv(n, 32), 1, G), 1024, 0, st>>>(part, p_g, n_slots, n, dst, n1, dst2);
+  return hipGetLastError();
+}
+
+template <class T>
+hipError_t launch_colsum_rows(const Mat<const T>& m, int64_t M, int64_t N, int slots, float* part, int G,
+                              hipStream_t st) {
+  k_colsum_rows<T><<<dim3((unsigned)cdiv(cdiv(N, EPP<T>), 256), slots, G), 256, 0, st>>>(m, M, N, part);
+  return hipGetLastError();
+}
+
+template <class T>
+hipError_t launch_act_bwd(int act, const Mat<const T>& dy, const Mat<const T>& pre, const Mat<T>& g, int64_t M,
+                          int64_t N, int G, hipStream_t st) {
+  if (M <= 0) return hipSuccess;
+  const bool flat = dy.ld == N && pre.ld == N && g.ld == N;   // one long row
+  const int64_t rows = flat ? 1 : M, cols = flat ? M * N : N;
+  const int64_t vpr = cdiv(cols, EPP<T>), total = rows * vpr;
+  const int64_t most = cdiv(8192, G), blocks = cdiv(total, 256);
+  const dim3 grid((unsigned)(blocks < most ? blocks : most), 1, G);
+  // a turn adds up to 2^21 to the index
+  if (total < (int64_t(1) << 31))
+    k_act_bwd<T, uint32_t><<<grid, 256, 0, st>>>(act, dy, pre, g, rows, cols, (uint32_t)vpr);
+  else
+    k_act_bwd<T, uint64_t><<<grid, 256, 0, st>>>(act, dy, pre, g, rows, cols, (uint64_t)vpr);
+  return hipGetLastError();
+}
+
+#define PIGAN_NORM_INST(T)                                                                                          \
+  template hipError_t launch_norm_fwd<T>(const NormArgs<T>&, int, hipStream_t);                                     \
+  template hipError_t launch_norm_bwd<T>(const NormArgs<T>&, int, hipStream_t);                                     \
+  template hipError_t launch_colsum_rows<T>(const Mat<const T>&, int64_t, int64_t, int, float*, int, hipStream_t);    \
+  template hipError_t launch_act_bwd<T>(int, const Mat<const T>&, const Mat<const T>&, const Mat<T>&, int64_t, int64_t, \
+                                        int, hipStream_t);
+PIGAN_NORM_INST(float)
+PIGAN_NORM_INST(bf16)
+PIGAN_NORM_INST(f16)
+
+}  // namespace pigan

@@ -11,7 +11,7 @@
 #include <string>
 #include <vector>
 
-#include "common.h"
+#include "api.h"
 #include "pointwise.h"
 #include "optim.h"
 
@@ -22,7 +22,7 @@ namespace pigan {
 // ---------------------------------------------------------------------------
 static thread_local std::string g_err;
 
-static pigan_status fail(pigan_status st, const char* fmt, ...) {
+pigan_status fail(pigan_status st, const char* fmt, ...) {
   char buf[512];
   va_list ap;
   va_start(ap, fmt);
@@ -32,11 +32,7 @@ static pigan_status fail(pigan_status st, const char* fmt, ...) {
   return st;
 }
 
-#define HIP_TRY(expr)                                                                       \
-  do {                                                                                      \
-    hipError_t e_ = (expr);                                                                 \
-    if (e_ != hipSuccess) return fail(PIGAN_EDEVICE, "%s: %s", #expr, hipGetErrorString(e_)); \
-  } while (0)
+void clear_error() { g_err.clear(); }
 
 // ---------------------------------------------------------------------------
 // kernel timing record (enabled by pigan_profile_enable)
@@ -76,31 +72,9 @@ void prof_end(hipStream_t st) {
   if (g_recs.back().b) (void)hipEventRecord(g_recs.back().b, st);
 }
 
-struct ProfScope {
-  hipStream_t st;
-  ProfScope(hipStream_t s, const char* name, double flops, double bytes) : st(s) {
-    prof_begin(s, name, flops, bytes);
-  }
-  ~ProfScope() { prof_end(st); }
-};
-
 // ---------------------------------------------------------------------------
 // shapes and workspace carving
 // ---------------------------------------------------------------------------
-static inline int64_t round_up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
-
-struct Carver {
-  size_t off = 0;
-  size_t take(size_t bytes) {
-    off = (size_t)round_up((int64_t)off, 256);
-    const size_t o = off;
-    off += bytes;
-    return o;
-  }
-};
-
-static size_t esize(int32_t dt) { return dt == PIGAN_FP32 ? 4 : 2; }
-
 struct MlpOff {  // offsets (in floats) of one group's packed parameters
   int in_dim, L, W;
   int64_t n;
@@ -143,11 +117,6 @@ static pigan_status check_mlp(const pigan_mlp* m, const char* what) {
   if (!width_ok(m->width))
     return fail(PIGAN_ENOTSUP, "%s: width=%d unsupported (multiple of 32 dividing 256, or multiple of 256 up to 4096)",
                 what, m->width);
-  return PIGAN_OK;
-}
-
-static pigan_status check_dtype(int32_t dt) {
-  if (dt != PIGAN_FP32 && dt != PIGAN_BF16 && dt != PIGAN_FP16) return fail(PIGAN_EINVAL, "unknown dtype %d", (int)dt);
   return PIGAN_OK;
 }
 

@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 import re
+import struct
 from dataclasses import dataclass
 
 import torch
@@ -26,6 +27,13 @@ HEADER = os.path.join(os.path.dirname(_HERE), "include", "pigan.h")
 OK, EINVAL, ENOTSUP, EWORKSPACE, EDEVICE = 0, 1, 2, 3, 4
 STATUS_NAMES = {0: "OK", 1: "EINVAL", 2: "ENOTSUP", 3: "EWORKSPACE", 4: "EDEVICE"}
 DTYPES = {"fp32": 0, "bf16": 1, "fp16": 2}
+TORCH_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+ACTS = {"none": 0, "tanh": 1, "relu": 2, "gelu": 3, "silu": 4}
+
+# pigan_linear, pigan_act_args and pigan_norm, each matrix as (p, ld, gs)
+LINEAR_ARGS = struct.Struct("4i3q" + "Pqq" * 7 + "3P")
+ACT_ARGS = struct.Struct("4i2q" + "Pqq" * 3)
+NORM_ARGS = struct.Struct("2i2qfi" + "Pqq" * 5 + "6P")
 
 
 class PiganError(RuntimeError):
@@ -114,6 +122,14 @@ def lib():
         "pigan_trunk_workspace_bytes": (sz, [P]),
         "pigan_trunk_step_grads": (i32, [P, P, P, P, P, P, P, P, f32, P, P, P, P, P, P, P, sz, P]),
         "pigan_trunk_step_grads_gp": (i32, [P, P, P, P, P, P, P, P, f32, P, P, P, P, P, P, P, P, P, sz, P]),
+        "pigan_linear_forward_workspace": (sz, [P]),
+        "pigan_linear_forward": (i32, [P, P, sz, P]),
+        "pigan_linear_backward_workspace": (sz, [P]),
+        "pigan_linear_backward": (i32, [P, P, sz, P]),
+        "pigan_act_backward": (i32, [P, P]),
+        "pigan_layer_norm_forward": (i32, [P, P]),
+        "pigan_layer_norm_backward_workspace": (sz, [P]),
+        "pigan_layer_norm_backward": (i32, [P, P, sz, P]),
         "pigan_last_error": (C.c_char_p, []),
         "pigan_profile_enable": (i32, [i32]),
         "pigan_profile_read": (i32, [P, i32, P]),
@@ -520,6 +536,210 @@ class StepGraph:
 
     def replay(self):
         self.graph.replay()
+
+
+# ---------------------------------------------------------------------------
+# layers of normalised residual networks
+# ---------------------------------------------------------------------------
+# Matrices are [M, columns], or [G, M, columns] for G independent layers of one
+# shape, of one dtype (fp32, bf16, fp16), with unit stride along the columns
+# and any strides above; vectors ([columns] or [G, columns]) and parameter
+# gradients are fp32.
+
+_NO_MAT = (0, 0, 0)
+
+
+def _mat(t: torch.Tensor, name: str, like: torch.Tensor, shape) -> tuple[int, int, int]:
+    """(pointer, row stride, group stride) of a matrix operand."""
+    if t.dtype != like.dtype:
+        raise ValueError(f"{name} must be {like.dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.device != like.device:
+        raise ValueError(f"{name} is on {t.device}, expected {like.device}")
+    st = t.stride()
+    cols = shape[-1]
+    if st[-1] != 1 and cols > 1:
+        raise ValueError(f"{name} must have unit stride along its columns")
+    ld = st[-2] if shape[-2] > 1 else cols
+    if ld < cols:
+        raise ValueError(f"{name} has overlapping rows (stride {ld}, {cols} columns)")
+    if len(st) == 2:
+        return t.data_ptr(), ld, 0
+    gs = st[0] if shape[0] > 1 else 0
+    if shape[0] > 1 and gs < (shape[1] - 1) * ld + cols:
+        raise ValueError(f"{name} has overlapping groups (stride {gs})")
+    return t.data_ptr(), ld, gs
+
+
+def _vec(t: torch.Tensor, name: str, like: torch.Tensor, shape) -> int:
+    """Pointer of an fp32 vector (one per group)."""
+    if t.dtype != torch.float32:
+        raise ValueError(f"{name} must be torch.float32, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.device != like.device or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous and on {like.device}")
+    return t.data_ptr()
+
+
+def _layer_dims(x: torch.Tensor, name: str) -> tuple[int, int]:
+    """(groups, dtype) of the matrix that sets a call's type and device."""
+    if not x.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if x.dim() not in (2, 3):
+        raise ValueError(f"{name} must be [rows, columns] or [groups, rows, columns]")
+    dt = TORCH_DTYPES.get(x.dtype)
+    if dt is None:
+        raise ValueError(f"{name} must be fp32, bf16 or fp16, got {x.dtype}")
+    return (x.shape[0] if x.dim() == 3 else 1), dt
+
+
+def _act(act: str) -> int:
+    if act not in ACTS:
+        raise ValueError(f"unknown activation {act!r}: one of {', '.join(ACTS)}")
+    return ACTS[act]
+
+
+def _call(fn, args: bytes, like: torch.Tensor, *ws):
+    """One library call on the current stream of the operands' device."""
+    dev = like.device
+    if dev.index != torch.cuda.current_device():
+        with torch.cuda.device(dev):
+            return _call(fn, args, like, *ws)
+    st = fn(args, *ws, torch.cuda.current_stream().cuda_stream)
+    if st != OK:
+        _check(st)
+
+
+def _call_ws(fn, query, args: bytes, like: torch.Tensor, ws: torch.Tensor | None):
+    """_call with a workspace: the caller's where it is large enough, else one
+    of the stream's allocator."""
+    need = query(args)
+    if need > 1 and (ws is None or ws.numel() < need):
+        ws = torch.empty(need, dtype=torch.uint8, device=like.device)
+    if ws is not None and (ws.dtype != torch.uint8 or ws.device != like.device or not ws.is_contiguous()):
+        raise ValueError(f"ws must be a contiguous torch.uint8 tensor on {like.device}")
+    _call(fn, args, like, ws.data_ptr() if ws is not None else None, ws.numel() if ws is not None else 0)
+
+
+def linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None, act: str = "none",
+           residual: torch.Tensor | None = None, save_pre: bool = False, out: torch.Tensor | None = None,
+           pre: torch.Tensor | None = None, ws: torch.Tensor | None = None):
+    """act(x w^T + bias) + residual: x [.., M, K], w [.., N, K], bias [.., N] fp32.
+
+    With save_pre (or `pre`) the pre-activation x w^T + bias is stored too, for
+    linear_backward or act_backward, and (y, pre) is returned.  `out` may be
+    `residual`."""
+    L = lib()
+    G, dt = _layer_dims(x, "x")
+    *lead, M, K = x.shape
+    N = w.shape[-2] if w.dim() == x.dim() else 0
+    shape, vec = (*lead, M, N), (*lead, N)
+    mw = _mat(w, "w", x, (*lead, N, K))
+    if out is None:
+        out = torch.empty(shape, dtype=x.dtype, device=x.device)
+    if save_pre and pre is None:
+        pre = torch.empty(shape, dtype=x.dtype, device=x.device)
+    args = LINEAR_ARGS.pack(G, dt, _act(act), 0, M, K, N, *_mat(x, "x", x, x.shape), *mw,
+                            *_mat(out, "out", x, shape), *(_NO_MAT if pre is None else _mat(pre, "pre", x, shape)),
+                            *(_NO_MAT if residual is None else _mat(residual, "residual", x, shape)), *_NO_MAT,
+                            *_NO_MAT, 0 if bias is None else _vec(bias, "bias", x, vec), 0, 0)
+    _call_ws(L.pigan_linear_forward, L.pigan_linear_forward_workspace, args, x, ws)
+    return out if pre is None else (out, pre)
+
+
+def linear_backward(g: torch.Tensor, x: torch.Tensor, w: torch.Tensor, act: str = "none",
+                    pre: torch.Tensor | None = None, add: torch.Tensor | None = None, need_dx: bool = True,
+                    need_dw: bool = True, need_db: bool = True, dx: torch.Tensor | None = None,
+                    dw: torch.Tensor | None = None, db: torch.Tensor | None = None, ws: torch.Tensor | None = None):
+    """Gradients of x w^T + bias from its cotangent g [.., M, N]: (dx, dw, db).
+
+    dx = (g w) * act'(pre) + add, where x = act(pre): the cotangent of the
+    pre-activation that x was formed from (act "none": of x itself); dw = g^T x
+    and db = sum of g over the rows, in fp32.  What is not needed is None.
+    `dx` may be `add` or `pre`."""
+    L = lib()
+    G, dt = _layer_dims(g, "g")
+    *lead, M, N = g.shape
+    K = x.shape[-1]
+    shape = (*lead, M, K)
+    mx, mw = _mat(x, "x", g, shape), _mat(w, "w", g, (*lead, N, K))
+    dx = torch.empty(shape, dtype=g.dtype, device=g.device) if need_dx and dx is None else dx if need_dx else None
+    if need_dw and dw is None:
+        dw = torch.empty((*lead, N, K), dtype=torch.float32, device=g.device)
+    if need_db and db is None:
+        db = torch.empty((*lead, N), dtype=torch.float32, device=g.device)
+    args = LINEAR_ARGS.pack(G, dt, _act(act), 0, M, K, N, *mx, *mw, *_NO_MAT,
+                            *(_NO_MAT if pre is None else _mat(pre, "pre", g, shape)),
+                            *(_NO_MAT if add is None else _mat(add, "add", g, shape)), *_mat(g, "g", g, g.shape),
+                            *(_NO_MAT if dx is None else _mat(dx, "dx", g, shape)), 0,
+                            _vec(dw, "dw", g, (*lead, N, K)) if need_dw else 0,
+                            _vec(db, "db", g, (*lead, N)) if need_db else 0)
+    _call_ws(L.pigan_linear_backward, L.pigan_linear_backward_workspace, args, g, ws)
+    return dx, dw if need_dw else None, db if need_db else None
+
+
+def act_backward(dy: torch.Tensor, pre: torch.Tensor, act: str, out: torch.Tensor | None = None) -> torch.Tensor:
+    """dy * act'(pre): the cotangent of a pre-activation from that of its
+    activation.  `out` may be `dy` or `pre`."""
+    G, dt = _layer_dims(dy, "dy")
+    shape = dy.shape
+    if out is None:
+        out = torch.empty(shape, dtype=dy.dtype, device=dy.device)
+    args = ACT_ARGS.pack(G, dt, _act(act), 0, shape[-2], shape[-1], *_mat(dy, "dy", dy, shape),
+                         *_mat(pre, "pre", dy, shape), *_mat(out, "out", dy, shape))
+    _call(lib().pigan_act_backward, args, dy)
+    return out
+
+
+def layer_norm(x: torch.Tensor, gamma: torch.Tensor | None = None, beta: torch.Tensor | None = None,
+               eps: float = 1e-5, out: torch.Tensor | None = None, mean: torch.Tensor | None = None,
+               rstd: torch.Tensor | None = None):
+    """(y, mean, rstd): y = (x - mean) rstd gamma + beta over the columns of
+    every row, rstd = 1 / sqrt(variance + eps); mean and rstd [.., M] fp32.
+    `out` may be `x`."""
+    G, dt = _layer_dims(x, "x")
+    shape = x.shape
+    rows, cols = shape[:-1], (*shape[:-2], shape[-1])
+    if out is None:
+        out = torch.empty(shape, dtype=x.dtype, device=x.device)
+    if mean is None:
+        mean = torch.empty(rows, dtype=torch.float32, device=x.device)
+    if rstd is None:
+        rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
+    args = NORM_ARGS.pack(G, dt, shape[-2], shape[-1], eps, 0, *_mat(x, "x", x, shape), *_mat(out, "out", x, shape),
+                          *_NO_MAT, *_NO_MAT, *_NO_MAT, 0 if gamma is None else _vec(gamma, "gamma", x, cols),
+                          0 if beta is None else _vec(beta, "beta", x, cols), _vec(mean, "mean", x, rows),
+                          _vec(rstd, "rstd", x, rows), 0, 0)
+    _call(lib().pigan_layer_norm_forward, args, x)
+    return out, mean, rstd
+
+
+def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
+                        gamma: torch.Tensor | None = None, add: torch.Tensor | None = None, need_dx: bool = True,
+                        need_params: bool = True, dx: torch.Tensor | None = None, dgamma: torch.Tensor | None = None,
+                        dbeta: torch.Tensor | None = None, ws: torch.Tensor | None = None):
+    """Gradients of layer_norm: (dx, dgamma, dbeta), `add` (a skip's cotangent)
+    added to dx.  What is not needed is None.  `dx` may be `dy` or `add`."""
+    L = lib()
+    G, dt = _layer_dims(dy, "dy")
+    shape = dy.shape
+    rows, cols = shape[:-1], (*shape[:-2], shape[-1])
+    dx = torch.empty(shape, dtype=dy.dtype, device=dy.device) if need_dx and dx is None else dx if need_dx else None
+    if need_params:
+        if dgamma is None:
+            dgamma = torch.empty(cols, dtype=torch.float32, device=dy.device)
+        if dbeta is None:
+            dbeta = torch.empty(cols, dtype=torch.float32, device=dy.device)
+    args = NORM_ARGS.pack(G, dt, shape[-2], shape[-1], 0.0, 0, *_mat(x, "x", dy, shape), *_NO_MAT,
+                          *_mat(dy, "dy", dy, shape), *(_NO_MAT if add is None else _mat(add, "add", dy, shape)),
+                          *(_NO_MAT if dx is None else _mat(dx, "dx", dy, shape)),
+                          0 if gamma is None else _vec(gamma, "gamma", dy, cols), 0, _vec(mean, "mean", dy, rows),
+                          _vec(rstd, "rstd", dy, rows), _vec(dgamma, "dgamma", dy, cols) if need_params else 0,
+                          _vec(dbeta, "dbeta", dy, cols) if need_params else 0)
+    _call_ws(L.pigan_layer_norm_backward, L.pigan_layer_norm_backward_workspace, args, dy, ws)
+    return (dx, dgamma, dbeta) if need_params else (dx, None, None)
 
 
 def profile_enable(on: bool = True):
