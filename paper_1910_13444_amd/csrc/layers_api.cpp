@@ -138,13 +138,19 @@ struct MmPlan {
   int n_split = 1;
 };
 
-// Modelled time of a launch, from the time of a stage (64 values of k) and of
-// a block's start and epilogue, per tile; the splits of the contraction add the
-// partials' way through memory and the launch that joins them.
+// Modelled time of a launch on 256 CUs, from measured times: of a stage (64 values
+// of k) with 1, 2, .. blocks on a CU, of a block's start and epilogue, and of a
+// kernel's first blocks (the 256 tile's unrolled epilogue has to be fetched).  The
+// splits of a contraction add a launch and the partials' way through memory.
+//   us measured (256 | 128 | 64 tile, best split)       modelled
+//   forward 262144 x 1024 x 1024   816 | 903 | -        738 | 824 | -
+//   forward 1024 x 2000 x 1024     36 | 21 | 13         43 | 30 | 16
+//   dw of 131072 x 1024 x 1024     284 | 297 | 536      306 | 330 | 428
+//   dx of 21 x 512 x 256 x 256     36 | 12 | 10         36 | 15 | 8
 MmPlan plan_mm(int64_t I, int64_t J, int64_t K, int pairs, int G) {
-  static const double stage_us[3] = {0.45, 0.75, 2.1};    // of all blocks that share a CU
-  static const double block_us[3] = {3.0, 4.0, 8.0};
-  static const int per_cu[3] = {2, 2, 1};
+  static const double stage_us[3][4] = {{0.33, 0.48, 0.63, 0.78}, {0.6, 1.16, 0, 0}, {1.9, 0, 0, 0}};
+  static const double block_us[3] = {3.0, 7.0, 14.0}, first_us[3] = {2.0, 5.0, 14.0};
+  static const int per_cu[3] = {4, 2, 1};
   const int64_t nk = (K + 63) / 64;
   MmPlan best;
   double best_us = 1e30;
@@ -153,9 +159,11 @@ MmPlan plan_mm(int64_t I, int64_t J, int64_t K, int pairs, int G) {
     const double tiles = (double)((I + s - 1) / s) * (double)((J + s - 1) / s) * G;
     for (int split = 1; split <= 64 && split <= nk; split *= 2) {
       if (split > 1 && nk * pairs / split < 4) break;
-      const double rounds = ceil(tiles * split / (256.0 * per_cu[t]));
-      double us = rounds * ((double)((nk + split - 1) / split) * pairs * stage_us[t] + block_us[t]);
-      if (split > 1) us += 4.0 + (double)G * I * J * 4.0 * (split * 2 + 1) / 5e6;
+      const double blocks = tiles * split;
+      const int held = (int)std::min<double>(per_cu[t], ceil(blocks / 256));
+      const double rounds = ceil(blocks / (256.0 * held));
+      double us = rounds * ((double)((nk + split - 1) / split) * pairs * stage_us[t][held - 1] + block_us[t]) + first_us[t];
+      if (split > 1) us += 8.0 + (double)G * I * J * 4.0 * (split * 2 + 1) / 5e6;
       if (us < best_us) {
         best_us = us;
         best.tile = t;
@@ -244,7 +252,7 @@ BackwardPlan plan_backward(const pigan_linear* a) {
     p.dw = plan_mm(a->N, a->K, a->M, pairs, G);
     if (fp32) p.x.take(cv, G, a->M, a->K);
     if (p.dw.n_split > 1) p.part_dw = cv.take((size_t)G * p.dw.n_split * a->N * a->K * 4);
-    const int64_t side = mm_tile_side(p.dw.tile);
+    const int64_t side = std::min(mm_tile_side(p.dw.tile), 128);   // the smaller of the tiles that it may become
     p.db_slots = p.dw.n_split * (int)((a->K + side - 1) / side);
   } else {
     p.db_slots = (int)std::min<int64_t>(a->M, COLSUM_SPLITS);
@@ -273,10 +281,13 @@ template <class TO> MmOut<TO> forward_out(const pigan_linear* a, const MmPlan& m
 
 template <class T> MmOperand<T> operand(const pigan_mat& m) { return {(const T*)m.p, m.ld, m.gs, 0}; }
 
+// the largest tile is there for aligned operands only
+int tile_for(const MmPlan& mm, bool direct) { return !direct && mm.tile == MM_256 ? (int)MM_128 : mm.tile; }
+
 template <class T, class TO>
 pigan_status forward_tiles(const MmArgs<T, TO>& m, const MmPlan& mm, int G, hipStream_t st) {
-  const bool direct = rows_aligned(m.a, G) && rows_aligned(m.b, G);
-  HIP_TRY(launch_mm_fwd(m, mm.tile, direct, G, st));
+  const bool direct = rows_aligned(m.a, G) && rows_aligned(m.b, G) && (m.pairs != 1 || m.K % 8 == 0) && m.o.J % 8 == 0;
+  HIP_TRY(launch_mm_fwd(m, tile_for(mm, direct), direct, G, st));
   if (mm.n_split > 1) HIP_TRY(launch_mm_join_fwd(m.o, G, st));
   return PIGAN_OK;
 }
@@ -311,11 +322,12 @@ pigan_status run_forward(const pigan_linear* a, const ForwardPlan& p, char* ws, 
 // T: operands of the products; TO: storage type of the layer
 template <class T, class TO>
 pigan_status backward_products(const pigan_linear* a, const BackwardPlan& p, const MmOperand<T>& g,
-                               const MmOperand<T>& w, const MmOperand<T>& x, bool padded, char* ws, hipStream_t st) {
+                               const MmOperand<T>& w, const MmOperand<T>& x, bool padded, char* ws, int& db_slots,
+                               hipStream_t st) {
   const int G = a->n_groups;
   const double es = (double)esize(a->dt), MN = (double)a->M * a->N, MK = (double)a->M * a->K, NK = (double)a->N * a->K;
-  // columns of operands that run down the rows are loaded in whole pieces
-  const bool n8 = padded || a->N % 8 == 0, k8 = padded || a->K % 8 == 0;
+  // whole pieces of columns (the padded planes hold zeros behind theirs)
+  const bool whole = (padded || a->N % 8 == 0) && a->K % 8 == 0;
   if (a->dx.p) {
     ProfScope prof(st, "linear_dx", 2.0 * G * MN * a->K, G * es * (MN + NK + MK * (1 + !!a->pre.p + !!a->add.p)));
     MmOut<TO> o{};
@@ -328,7 +340,8 @@ pigan_status backward_products(const pigan_linear* a, const BackwardPlan& p, con
     o.out = (TO*)a->dx.p; o.ldo = a->dx.ld; o.gso = a->dx.gs;
     o.part = p.dx.n_split > 1 ? (float*)(ws + p.part_dx) : nullptr;
     MmArgs<T, TO> m{g, w, a->N, padded ? 6 : 1, o, nullptr};
-    HIP_TRY(launch_mm_dx(m, p.dx.tile, rows_aligned(g, G) && rows_aligned(w, G) && k8, G, st));
+    const bool direct = rows_aligned(g, G) && rows_aligned(w, G) && whole;
+    HIP_TRY(launch_mm_dx(m, tile_for(p.dx, direct), direct, G, st));
     if (p.dx.n_split > 1) HIP_TRY(launch_mm_join_dx(o, G, st));
   }
   if (a->dw) {
@@ -340,7 +353,10 @@ pigan_status backward_products(const pigan_linear* a, const BackwardPlan& p, con
     o.out = a->dw; o.ldo = a->K; o.gso = a->N * a->K;
     o.part = p.dw.n_split > 1 ? (float*)(ws + p.part_dw) : nullptr;
     MmArgs<T, float> m{g, x, a->M, padded ? 6 : 1, o, a->db ? (float*)(ws + p.part_db) : nullptr};
-    HIP_TRY(launch_mm_dw(m, p.dw.tile, rows_aligned(g, G) && rows_aligned(x, G) && n8 && k8, G, st));
+    const bool direct = rows_aligned(g, G) && rows_aligned(x, G) && whole;
+    const int tile = tile_for(p.dw, direct), side = mm_tile_side(tile);
+    db_slots = p.dw.n_split * (int)((a->K + side - 1) / side);
+    HIP_TRY(launch_mm_dw(m, tile, direct, G, st));
     if (p.dw.n_split > 1) HIP_TRY(launch_mm_join_dw(o, G, st));
   }
   return PIGAN_OK;
@@ -353,6 +369,7 @@ pigan_status run_backward(const pigan_linear* a, const BackwardPlan& p, char* ws
     if (a->db) HIP_TRY(launch_slot_sum(nullptr, 0, 0, a->N, a->db, a->N, nullptr, G, st));
     return PIGAN_OK;
   }
+  int db_slots = p.db_slots;
   if (a->dx.p || a->dw) {
     pigan_status s;
     if (a->dt == PIGAN_FP32) {
@@ -362,11 +379,14 @@ pigan_status run_backward(const pigan_linear* a, const BackwardPlan& p, char* ws
       if (a->dx.p) sets[n++] = p.w.set(ws, a->w, a->K);
       if (a->dw) sets[n++] = p.x.set(ws, a->x, a->K);
       HIP_TRY(launch_split3(sets, n, G, st));
-      s = backward_products<bf16, float>(a, p, p.g.operand(ws, G), p.w.operand(ws, G), p.x.operand(ws, G), true, ws, st);
+      s = backward_products<bf16, float>(a, p, p.g.operand(ws, G), p.w.operand(ws, G), p.x.operand(ws, G), true, ws,
+                                         db_slots, st);
     } else {
       s = a->dt == PIGAN_BF16
-              ? backward_products<bf16, bf16>(a, p, operand<bf16>(a->g), operand<bf16>(a->w), operand<bf16>(a->x), false, ws, st)
-              : backward_products<f16, f16>(a, p, operand<f16>(a->g), operand<f16>(a->w), operand<f16>(a->x), false, ws, st);
+              ? backward_products<bf16, bf16>(a, p, operand<bf16>(a->g), operand<bf16>(a->w), operand<bf16>(a->x), false, ws,
+                                             db_slots, st)
+              : backward_products<f16, f16>(a, p, operand<f16>(a->g), operand<f16>(a->w), operand<f16>(a->x), false, ws, db_slots,
+                                           st);
     }
     if (s != PIGAN_OK) return s;
   }
@@ -374,12 +394,12 @@ pigan_status run_backward(const pigan_linear* a, const BackwardPlan& p, char* ws
     float* part = (float*)(ws + p.part_db);
     if (!a->dw) {
       pigan_status s = by_dtype(a->dt, [&](auto t) -> pigan_status {
-        HIP_TRY(launch_colsum_rows(in<decltype(t)>(a->g), a->M, a->N, p.db_slots, part, G, st));
+        HIP_TRY(launch_colsum_rows(in<decltype(t)>(a->g), a->M, a->N, db_slots, part, G, st));
         return PIGAN_OK;
       });
       if (s != PIGAN_OK) return s;
     }
-    HIP_TRY(launch_slot_sum(part, (int64_t)p.db_slots * a->N, p.db_slots, a->N, a->db, a->N, nullptr, G, st));
+    HIP_TRY(launch_slot_sum(part, (int64_t)db_slots * a->N, db_slots, a->N, a->db, a->N, nullptr, G, st));
   }
   return PIGAN_OK;
 }

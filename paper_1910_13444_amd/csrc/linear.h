@@ -39,8 +39,9 @@ template <class T, class TO> struct MmArgs {
 enum MmTile { MM_64 = 0, MM_128 = 1, MM_256 = 2 };
 inline int mm_tile_side(int t) { return t == MM_64 ? 64 : t == MM_128 ? 128 : 256; }
 
-// direct: both operands may go straight to LDS (16-byte aligned rows, offsets
-// of a tile below 2^31 bytes; down-the-rows operands: whole pieces of columns)
+// direct: both operands may go straight to LDS: 16-byte aligned rows (a tile's
+// extent below 2^31 bytes) of whole pieces, along the row and in the result's
+// columns; planes (pairs = 6) hold zeros behind their rows up to a whole piece
 template <class T, class TO>
 hipError_t launch_mm_fwd(const MmArgs<T, TO>& a, int tile, bool direct, int G, hipStream_t st);
 template <class T, class TO>

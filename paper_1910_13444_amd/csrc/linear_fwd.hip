@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(64 * NW) k_short_fwd(const MmArgs<T, T> p) {
       for (int e = 0; e < 8; ++e) v[e] += sums[w][row][c + e];
     if (i0 + row < p.o.I && j0 + c < p.o.J) {
       vec_load<8>(p.o.bias ? p.o.bias + g * p.o.J : nullptr, j0 + c, p.o.J, 0.0f, bias);
-      mm_epilogue<MM_FWD>(p.o, g, i0 + row, j0 + c, bias, v);
+      mm_finish<MM_FWD>(p.o, g, i0 + row, j0 + c, bias, v);
     }
   }
 }

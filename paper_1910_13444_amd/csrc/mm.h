@@ -1,7 +1,7 @@
 // The tiled product of the linear layer on the 16-bit matrix cores of gfx950
 // (see linear.h for the operands).
 //
-// A block of WM x WN waves forms a tile of C; a wave owns MT x NT fragments of
+// A block of four waves forms a tile of C; a wave owns MT x NT fragments of
 // 32 x 32.  Operands pass through LDS in stages of 64 values of k:
 //   k along the row   a row of the stage is a 128-byte line of a row of A; its
 //                     16-byte segment s sits at s ^ (row & 7), so the 32 rows
@@ -10,11 +10,6 @@
 //                     segment s of row r sits at s ^ 4 (r & 3) (rows of eight
 //                     segments: s ^ 4 (r / 2 & 1)), which puts the four rows of
 //                     a transposing read in disjoint banks.
-// With DMA the stages go straight to LDS (global_load_lds_dwordx4: lane l of a
-// wave fills byte 16 l of 1 KB), NS - 1 of them ahead of the products; a last
-// partial stage and unaligned operands go through registers, with zeros past
-// the end of k.  Rows of a tile past the end of the matrix repeat the last
-// row; their products are not stored.
 //
 // The matrix core is given (B, A), so a lane holds one row of C and runs of
 // four columns; two lane exchanges make that eight consecutive columns, of
@@ -54,37 +49,126 @@ __device__ __forceinline__ void mm_exchange(float (&v)[16]) {
   }
 }
 
-// epilogue of eight consecutive columns j.. of row i (i < I, j < J); `bias`
-// holds their biases
-template <int KIND, class TO>
-__device__ __forceinline__ void mm_epilogue(const MmOut<TO>& o, int g, int64_t i, int64_t j, const float* bias,
-                                            float* v) {
-  const int64_t valid = o.J - j;
-  if constexpr (KIND != MM_DW) {
-    if constexpr (KIND == MM_FWD) {
+// Eight consecutive columns of a row as they lie in memory.
+template <class TO> struct Octet {
+  piece_t q[8 / EPP<TO>];
+  __device__ __forceinline__ void load(const TO* p, int64_t valid) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += bias[e];
-      if (o.pre) store8(o.pre + g * o.gsp + i * o.ldp + j, valid, v);
-      PIGAN_ACT_SWITCH(o.act, {
-        _Pragma("unroll") for (int e = 0; e < 8; ++e) v[e] = act_value<ACT>(v[e]);
-      })
-    } else {
-      if (o.pre) {
-        float a[8];
-        load8(o.pre + g * o.gsp + i * o.ldp + j, valid, a);
-        PIGAN_ACT_SWITCH(o.act, {
-          _Pragma("unroll") for (int e = 0; e < 8; ++e) v[e] *= act_slope<ACT>(a[e]);
-        })
-      }
-    }
+    for (int i = 0; i < 8 / EPP<TO>; ++i) q[i] = piece_load(p + i * EPP<TO>, valid - i * EPP<TO>);
+  }
+  __device__ __forceinline__ void floats(float* f) const {
+#pragma unroll
+    for (int i = 0; i < 8 / EPP<TO>; ++i) piece_floats<TO>(q[i], f + i * EPP<TO>);
+  }
+};
+
+// what the epilogue of eight columns j.. of row i reads (i < I, j < J)
+template <int KIND, int ACT, class TO> struct EpiIn {
+  Octet<TO> pre, add;
+  __device__ __forceinline__ void load(const MmOut<TO>& o, int g, int64_t i, int64_t j, int64_t valid) {
+    if constexpr (KIND == MM_DX && ACT != PIGAN_ACT_NONE) pre.load(o.pre + g * o.gsp + i * o.ldp + j, valid);
+    if constexpr (KIND != MM_DW)
+      if (o.add) add.load(o.add + g * o.gsa + i * o.lda + j, valid);
+  }
+};
+
+// the epilogue itself; `bias` holds the columns' biases
+template <int KIND, int ACT, class TO>
+__device__ __forceinline__ void mm_epilogue(const MmOut<TO>& o, int g, int64_t i, int64_t j, int64_t valid,
+                                            const EpiIn<KIND, ACT, TO>& in, const float* bias, float* v) {
+  if constexpr (KIND == MM_FWD) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += bias[e];
+    if (o.pre) store8(o.pre + g * o.gsp + i * o.ldp + j, valid, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = act_value<ACT>(v[e]);
+  } else if constexpr (KIND == MM_DX && ACT != PIGAN_ACT_NONE) {
+    float a[8];
+    in.pre.floats(a);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= act_slope<ACT>(a[e]);
+  }
+  if constexpr (KIND != MM_DW)
     if (o.add) {
       float r[8];
-      load8(o.add + g * o.gsa + i * o.lda + j, valid, r);
+      in.add.floats(r);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] += r[e];
     }
-  }
   store8(o.out + g * o.gso + i * o.ldo + j, valid, v);
+}
+
+// A wave's MT x NT fragments, from rows i0 and columns j0 on, to memory: as
+// partial sums or through the epilogue (one branch on the activation for all of
+// them: the accumulators stay in registers only if every loop unrolls).  What the
+// epilogue reads is requested a column of fragments ahead: asked for one by one,
+// each of 32 reads was waited for by itself (30 us of the 60 that a 256 x 256 tile
+// took at K = 1024).  WHOLE: the columns come in whole eights.
+template <int KIND, int ACT, bool PART, bool WHOLE, class TO, int MT, int NT>
+__device__ __forceinline__ void mm_store(const MmOut<TO>& o, int g, int split, int64_t i0, int64_t j0,
+                                         const f32x16 (&acc)[MT][NT]) {
+  const int lane = threadIdx.x & 63;
+  // (a column ahead where the registers hold two columns' operands)
+  constexpr int AHEAD = WHOLE && (MT <= 2 || (KIND == MM_FWD && sizeof(TO) == 2)) ? 1 : 0;
+  EpiIn<KIND, ACT, TO> in[1 + AHEAD][MT][2];
+  auto request = [&](int b) __attribute__((always_inline)) {
+    const int64_t j = j0 + 32 * b + mm_col(lane);
+#pragma unroll
+    for (int a = 0; a < MT; ++a)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int64_t i = i0 + 32 * a + 16 * h + (lane & 15);
+        if (i < o.I && j < o.J) in[b & AHEAD][a][h].load(o, g, i, j, WHOLE ? 8 : o.J - j);
+      }
+  };
+  if constexpr (!PART && AHEAD) request(0);
+#pragma unroll
+  for (int b = 0; b < NT; ++b) {
+    const int64_t j = j0 + 32 * b + mm_col(lane);
+    float bias[8];
+    if constexpr (KIND == MM_FWD && !PART)
+      vec_load<8>(o.bias && (!WHOLE || j < o.J) ? o.bias + g * o.J : nullptr, j, WHOLE ? j + 8 : o.J, 0.0f, bias);
+    if constexpr (!PART)
+      if (b + AHEAD < NT) request(b + AHEAD);
+#pragma unroll
+    for (int a = 0; a < MT; ++a) {
+      float v[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) v[r] = acc[a][b][r];
+      mm_exchange(v);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int64_t i = i0 + 32 * a + 16 * h + (lane & 15);
+        if (i < o.I && j < o.J) {
+          const int64_t valid = WHOLE ? 8 : o.J - j;
+          if constexpr (PART) store8(o.part + (((int64_t)g * o.n_split + split) * o.I + i) * o.J + j, valid, v + 8 * h);
+          else mm_epilogue<KIND, ACT>(o, g, i, j, valid, in[b & AHEAD][a][h], bias, v + 8 * h);
+        }
+      }
+    }
+  }
+}
+
+template <int KIND, bool WHOLE, class TO, int MT, int NT>
+__device__ __forceinline__ void mm_results(const MmOut<TO>& o, int g, int split, int64_t i0, int64_t j0,
+                                           const f32x16 (&acc)[MT][NT]) {
+  if (o.part) {
+    mm_store<KIND, PIGAN_ACT_NONE, true, WHOLE>(o, g, split, i0, j0, acc);
+  } else if constexpr (KIND == MM_DW) {
+    mm_store<KIND, PIGAN_ACT_NONE, false, WHOLE>(o, g, split, i0, j0, acc);
+  } else {
+    PIGAN_ACT_SWITCH(o.act, { mm_store<KIND, ACT, false, WHOLE>(o, g, split, i0, j0, acc); })
+  }
+}
+
+// one octet by itself
+template <int KIND, class TO>
+__device__ __forceinline__ void mm_finish(const MmOut<TO>& o, int g, int64_t i, int64_t j, const float* bias, float* v) {
+  PIGAN_ACT_SWITCH(KIND == MM_DW ? PIGAN_ACT_NONE : o.act, {
+    EpiIn<KIND, ACT, TO> in;
+    in.load(o, g, i, j, o.J - j);
+    mm_epilogue<KIND, ACT>(o, g, i, j, o.J - j, in, bias, v);
+  })
 }
 
 // all but N vector-memory operations and all LDS operations of this wave are
@@ -98,51 +182,50 @@ __device__ __forceinline__ void stage_sync() {
   asm volatile("" ::: "memory");
 }
 
-template <int WM, int WN, int MT, int NT, int NS>
-struct MmShape {
-  static constexpr int BM = 32 * MT * WM, BN = 32 * NT * WN, NTH = 64 * WM * WN;
-  static constexpr int BK = 64;
-  static constexpr int STAGE_A = BM * BK * 2, STAGE = (BM + BN) * BK * 2;
+// One tile of C: group, first row and column, part of the contraction.
+struct MmTilePos {
+  int g, split, ti, tj;   // ti, tj: row and column of the tile
 };
 
-template <class T, class TO, int KIND, int WM, int WN, int MT, int NT, int NS, bool DMA, int OCC>
-__global__ void __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(OCC)))
-k_mm(const MmArgs<T, TO> p) {
-  typedef MmShape<WM, WN, MT, NT, NS> S;
-  constexpr int BM = S::BM, BN = S::BN, NW = WM * WN, BK = S::BK, STAGE_A = S::STAGE_A;
-  constexpr bool AK = KIND != MM_DW, BKC = KIND == MM_FWD;   // k along the row of A, of B
-  constexpr int GA = BM / 8 / NW, GB = BN / 8 / NW, GPW = GA + GB;   // 1 KB groups per wave and stage
-  static_assert(GA >= 1 && GB >= 1 && (NS - 2) * GPW <= 63, "whole groups");
-  static_assert(NS == 2 || NS == 4, "stages");
-  typedef typename Elem<T>::frag frag;
-  // one object per stage: the compiler then knows which of them a load in
-  // flight can touch, and waits for no other
-  __shared__ __attribute__((aligned(1024))) char s0[S::STAGE];
-  __shared__ __attribute__((aligned(1024))) char s1[S::STAGE];
-  __shared__ __attribute__((aligned(1024))) char s2[NS > 2 ? S::STAGE : 16];
-  __shared__ __attribute__((aligned(1024))) char s3[NS > 2 ? S::STAGE : 16];
-  auto stage_at = [&](auto u) -> char* {
-    constexpr int U = decltype(u)::value % NS;
-    if constexpr (U == 0) return s0;
-    else if constexpr (U == 1) return s1;
-    else if constexpr (U == 2) return s2;
-    else return s3;
-  };
+// Tile n of all.  Tiles of one split of a group are neighbours, in panels of four
+// row tiles, column by column: an XCD, which walks a range of n, then shares
+// their rows in its L2.
+__device__ __forceinline__ MmTilePos mm_tile(uint32_t n, uint32_t rows, uint32_t cols, uint32_t n_split) {
+  MmTilePos t;
+  const uint32_t per = rows * cols, part = n / per;
+  n -= part * per;
+  t.g = (int)(part / n_split);
+  t.split = (int)(part - t.g * n_split);
+  const uint32_t panel = n / (4 * cols), prow = rows - 4 * panel < 4 ? rows - 4 * panel : 4;
+  n -= panel * 4 * cols;
+  t.tj = (int)(n / prow);
+  t.ti = (int)(4 * panel + n - t.tj * prow);
+  return t;
+}
 
-  const int g = blockIdx.z;
+// ---------------------------------------------------------------------------
+// Operands of any alignment: stages pass through registers, one ahead of the
+// products, with zeros past the end of k.  Rows of a tile past the end of the
+// matrix repeat its last row; their products are not stored.
+// ---------------------------------------------------------------------------
+template <class T, class TO, int KIND, int MT, int NT>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
+k_mm_any(const MmArgs<T, TO> p) {
+  constexpr int BM = 64 * MT, BN = 64 * NT, BK = 64, STAGE_A = BM * BK * 2, STAGE = STAGE_A + BN * BK * 2;
+  constexpr bool AK = KIND != MM_DW, BKC = KIND == MM_FWD;   // k along the row of A, of B
+  constexpr int GA = BM / 32, GPW = GA + BN / 32;            // 1 KB groups per wave and stage
+  typedef typename Elem<T>::frag frag;
+  __shared__ __attribute__((aligned(1024))) char s0[STAGE];
+  __shared__ __attribute__((aligned(1024))) char s1[STAGE];
+
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = wave % WM, wn = wave / WM;
+  const int wm = wave & 1, wn = wave >> 1;
 
-  // Tiles of one split are neighbours in the order in which an XCD walks them:
-  // panels of four row tiles, column by column, share their rows in its L2.
-  const int64_t ti = (p.o.I + BM - 1) / BM, tj = (p.o.J + BN - 1) / BN;
-  const int64_t lb = xcd_remap(blockIdx.x, gridDim.x);
-  const int split = (int)(lb / (ti * tj));
-  int64_t t = lb % (ti * tj);
-  const int64_t panel = t / (4 * tj), prow = ti - 4 * panel < 4 ? ti - 4 * panel : 4;
-  t -= panel * 4 * tj;
-  const int64_t i0 = (4 * panel + t % prow) * BM, j0 = t / prow * BN;
+  const uint32_t rows = (uint32_t)((p.o.I + BM - 1) / BM), tj = (uint32_t)((p.o.J + BN - 1) / BN);
+  const MmTilePos at = mm_tile((uint32_t)xcd_remap(blockIdx.x, gridDim.x), rows, tj, p.o.n_split);
+  const int g = at.g, split = at.split;
+  const int64_t i0 = (int64_t)at.ti * BM, j0 = (int64_t)at.tj * BN;
 
   // this split's stages of k (of every plane pair)
   const int64_t nk = (p.K + BK - 1) / BK;
@@ -157,66 +240,30 @@ k_mm(const MmArgs<T, TO> p) {
     for (int b = 0; b < NT; ++b)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[a][b][r] = 0.0f;
-  float db[KIND == MM_DW ? MT : 1];
+  float db[MT];
 #pragma unroll
-  for (int a = 0; a < (KIND == MM_DW ? MT : 1); ++a) db[a] = 0.0f;
+  for (int a = 0; a < MT; ++a) db[a] = 0.0f;
 
-  // ---- where this lane's 16 bytes of every group come from ----
   const T* pa = p.a.p + g * p.a.gs + (AK ? i0 * p.a.ld : i0);
   const T* pb = p.b.p + g * p.b.gs + (BKC ? j0 * p.b.ld : j0);
-  // row of the stage and column segment of the lane in group q of an operand
-  // with `side` rows (k along the row) or columns (k down the rows)
-  auto place = [&](bool along, int side, int q, int& row, int& seg) __attribute__((always_inline)) {
-    if (along) {
-      row = q * 8 + (lane >> 3);
-      seg = (lane & 7) ^ (row & 7);
-    } else {
-      const int spr = side / 8;               // segments per row
-      row = (q * 64 + lane) / spr;
-      seg = (lane % spr) ^ mm_swizzle(side, row);
-    }
-  };
-  uint32_t off[GPW];   // byte offset from the stage's first element (DMA)
-  if constexpr (DMA) {
-#pragma unroll
-    for (int n = 0; n < GPW; ++n) {
-      const bool isA = n < GA;
-      const bool along = isA ? AK : BKC;
-      const int64_t ld = isA ? p.a.ld : p.b.ld, left = isA ? p.o.I - i0 : p.o.J - j0;
-      int row, seg;
-      place(along, isA ? BM : BN, wave + (isA ? n : n - GA) * NW, row, seg);
-      int64_t o;
-      if (along) o = (row < left ? row : left - 1) * ld + seg * 8;
-      else o = row * ld + (seg * 8 < left ? seg * 8 : 0);
-      off[n] = (uint32_t)(o * 2);
-    }
-  }
-  // plane pairs in the order of growing products
-  auto pair_planes = [&](int st, int& a, int& b, int64_t& k) __attribute__((always_inline)) {
-    const int pr = p.pairs == 1 ? 5 : st / per_pair;
-    k = (int64_t)(k_lo + (p.pairs == 1 ? st : st - pr * per_pair)) * BK;
-    // pair:  0      1      2      3      4      5
-    //        (0,2)  (1,1)  (2,0)  (0,1)  (1,0)  (0,0)
-    a = pr == 0 ? 0 : pr == 1 ? 1 : pr == 2 ? 2 : pr == 4 ? 1 : 0;
-    b = pr == 0 ? 2 : pr == 1 ? 1 : pr == 3 ? 1 : 0;
-  };
-  // a stage through registers: zeros past the end of k
   auto fetch = [&](piece_t (&r)[GPW], int st) __attribute__((always_inline)) {
-    int qa, qb;
-    int64_t k0;
-    pair_planes(st, qa, qb, k0);
+    // plane pairs (0,2) (1,1) (2,0) (0,1) (1,0) (0,0), as in the aligned kernel
+    const int pr = p.pairs == 1 ? 5 : st / per_pair;
+    const int64_t k0 = (int64_t)(k_lo + (p.pairs == 1 ? st : st - pr * per_pair)) * BK;
+    const int qa = (0x124 >> (2 * pr)) & 3, qb = (0x046 >> (2 * pr)) & 3;
 #pragma unroll
     for (int n = 0; n < GPW; ++n) {
       const bool isA = n < GA;
       const bool along = isA ? AK : BKC;
+      const int side = isA ? BM : BN, q = wave + (isA ? n : n - GA) * 4;
       const int64_t ld = isA ? p.a.ld : p.b.ld, left = isA ? p.o.I - i0 : p.o.J - j0;
       const T* base = isA ? pa + qa * p.a.plane : pb + qb * p.b.plane;
-      int row, seg;
-      place(along, isA ? BM : BN, wave + (isA ? n : n - GA) * NW, row, seg);
       if (along) {
-        const int64_t k = k0 + seg * 8;
+        const int row = q * 8 + (lane >> 3);
+        const int64_t k = k0 + ((lane & 7) ^ (row & 7)) * 8;
         r[n] = piece_load(base + (row < left ? row : left - 1) * ld + k, p.K - k);
       } else {
+        const int spr = side / 8, row = (q * 64 + lane) / spr, seg = (lane % spr) ^ mm_swizzle(side, row);
         const int64_t k = k0 + row;
         r[n] = piece_load(base + k * ld + seg * 8, k < p.K ? left - seg * 8 : 0);
       }
@@ -225,59 +272,36 @@ k_mm(const MmArgs<T, TO> p) {
   auto put = [&](const piece_t (&r)[GPW], char* stage) __attribute__((always_inline)) {
 #pragma unroll
     for (int n = 0; n < GPW; ++n)
-      *(piece_t*)(stage + (n < GA ? 0 : STAGE_A) + (wave + (n < GA ? n : n - GA) * NW) * 1024 + lane * 16) = r[n];
+      *(piece_t*)(stage + (n < GA ? 0 : STAGE_A) + (wave + (n < GA ? n : n - GA) * 4) * 1024 + lane * 16) = r[n];
   };
-  auto issue = [&](int st, char* stage) __attribute__((always_inline)) {
-    int qa, qb;
-    int64_t k0;
-    pair_planes(st, qa, qb, k0);
-    if (k0 + BK <= p.K) {
-      const char* ba = (const char*)(pa + qa * p.a.plane + (AK ? k0 : k0 * p.a.ld));
-      const char* bb = (const char*)(pb + qb * p.b.plane + (BKC ? k0 : k0 * p.b.ld));
-#pragma unroll
-      for (int n = 0; n < GPW; ++n)
-        __builtin_amdgcn_global_load_lds((const void*)((n < GA ? ba : bb) + off[n]),
-                                         (lds_ptr_t)(stage + (n < GA ? 0 : STAGE_A) +
-                                                     (wave + (n < GA ? n : n - GA) * NW) * 1024), 16, 0, 0);
-    } else {
-      piece_t r[GPW];
-      fetch(r, st);
-      put(r, stage);
-      wait_vmcnt<0>();   // also in a wave whose pieces are all past the end: the counts below stay upper bounds
-    }
-  };
-
-  // ---- products of one stage ----
   const int grp = lane >> 4, t16 = lane & 15, rr = t16 >> 2, q4 = t16 & 3, kb = 8 * (lane >> 5);
   auto frag_at = [&](const char* base, bool along, int side, int c, int blk) __attribute__((always_inline)) -> frag {
-    if (along) {
-      const int row = blk + (lane & 31), seg = 2 * c + (lane >> 5);
-      return *(const frag*)(base + row * 128 + ((seg ^ (row & 7)) << 4));
-    }
-    const int byte = (blk + 16 * (grp & 1) + 4 * q4) * 2, pitch = side * 2;
+    if (along)
+      return *(const frag*)(base + (lane & 31) * 128 + (((2 * c + (lane >> 5)) ^ (lane & 7)) << 4) + blk * 4096);
+    const int byte = (32 * blk + 16 * (grp & 1) + 4 * q4) * 2, pitch = side * 2;
     const char* q = base + (c * 16 + kb + rr) * pitch + (((byte >> 4) ^ mm_swizzle(side, rr)) << 4) + (byte & 15);
     const u32x2 lo = lds_read_tr<T>(q), hi = lds_read_tr<T>(q + 4 * pitch);
     return __builtin_bit_cast(frag, (u32x4{lo.x, lo.y, hi.x, hi.y}));
   };
   // dw: the sums of A over k go by the blocks of a row of tiles in turn, the
-  // chunks of a stage by the waves of a column in turn
+  // chunks of a stage by the waves of a column in turn; the first three plane
+  // pairs hold every plane of A once
   const int db_tiles = (int)tj, db_turn = (int)(j0 / BN);
   auto products = [&](const char* stage, int st) __attribute__((always_inline)) {
-    // the first three plane pairs hold every plane of A once
     const bool sum_a = KIND == MM_DW && p.part_db && st < 3 * per_pair && st % db_tiles == db_turn;
 #pragma unroll
     for (int c = 0; c < BK / 16; ++c) {
       frag fa[MT], fb[NT];
 #pragma unroll
-      for (int a = 0; a < MT; ++a) fa[a] = frag_at(stage, AK, BM, c, 32 * (wm * MT + a));
+      for (int a = 0; a < MT; ++a) fa[a] = frag_at(stage, AK, BM, c, MT * wm + a);
 #pragma unroll
-      for (int b = 0; b < NT; ++b) fb[b] = frag_at(stage + STAGE_A, BKC, BN, c, 32 * (wn * NT + b));
+      for (int b = 0; b < NT; ++b) fb[b] = frag_at(stage + STAGE_A, BKC, BN, c, NT * wn + b);
 #pragma unroll
       for (int a = 0; a < MT; ++a)
 #pragma unroll
         for (int b = 0; b < NT; ++b) Elem<T>::mma(acc[a][b], fb[b], fa[a]);
       if constexpr (KIND == MM_DW) {
-        if (sum_a && c % WN == wn) {
+        if (sum_a && (c & 1) == wn) {
 #pragma unroll
           for (int a = 0; a < MT; ++a)
 #pragma unroll
@@ -287,99 +311,253 @@ k_mm(const MmArgs<T, TO> p) {
     }
   };
 
-  if constexpr (DMA) {
-    auto first = [&](auto u) __attribute__((always_inline)) {
-      if (u < stages) issue(u, stage_at(u));
-    };
-    first(std::integral_constant<int, 0>{});
-    if constexpr (NS > 2) {
-      first(std::integral_constant<int, 1>{});
-      first(std::integral_constant<int, 2>{});
-    }
-    // stage st has arrived, and every wave is done with the stage that the next load replaces
-    auto turn = [&](int st, auto u) __attribute__((always_inline)) {
-      const int later = stages - 1 - st;
-      if constexpr (NS > 2) {
-        if (later >= 2) stage_sync<2 * GPW>();
-        else if (later == 1) stage_sync<GPW>();
-        else stage_sync<0>();
-      } else {
-        stage_sync<0>();
-      }
-      if (st + NS - 1 < stages) issue(st + NS - 1, stage_at(std::integral_constant<int, decltype(u)::value + NS - 1>{}));
-      products(stage_at(u), st);
-    };
-    for (int st = 0; st < stages; st += NS) {
-      turn(st, std::integral_constant<int, 0>{});
-      if (st + 1 < stages) turn(st + 1, std::integral_constant<int, 1>{});
-      if constexpr (NS > 2) {
-        if (st + 2 < stages) turn(st + 2, std::integral_constant<int, 2>{});
-        if (st + 3 < stages) turn(st + 3, std::integral_constant<int, 3>{});
-      }
-    }
-  } else {
-    piece_t r[GPW];
-    if (stages > 0) {
-      fetch(r, 0);
-      put(r, s0);
-    }
-    auto turn = [&](int st, char* now, char* next) __attribute__((always_inline)) {
-      const bool more = st + 1 < stages;
-      if (more) fetch(r, st + 1);
-      lds_sync();
-      products(now, st);
-      if (more) put(r, next);   // every wave is past the products that read it: the barrier above
-    };
-    for (int st = 0; st < stages; st += 2) {
-      turn(st, s0, s1);
-      if (st + 1 < stages) turn(st + 1, s1, s0);
-    }
+  piece_t r[GPW];
+  if (stages > 0) {
+    fetch(r, 0);
+    put(r, s0);
+  }
+  auto turn = [&](int st, char* now, char* next) __attribute__((always_inline)) {
+    const bool more = st + 1 < stages;
+    if (more) fetch(r, st + 1);
+    lds_sync();
+    products(now, st);
+    if (more) put(r, next);   // its readers are past the barrier above
+  };
+  for (int st = 0; st < stages; st += 2) {
+    turn(st, s0, s1);
+    if (st + 1 < stages) turn(st + 1, s1, s0);
   }
 
-  // ---- results ----
-  const int64_t jc = j0 + 32 * wn * NT + mm_col(lane);
-  float bias[KIND == MM_FWD ? NT : 1][8];
-  if constexpr (KIND == MM_FWD) {
-#pragma unroll
-    for (int b = 0; b < NT; ++b)
-      vec_load<8>(p.o.bias && !p.o.part ? p.o.bias + g * p.o.J : nullptr, jc + 32 * b, p.o.J, 0.0f, bias[b]);
-  }
-#pragma unroll
-  for (int a = 0; a < MT; ++a) {
-#pragma unroll
-    for (int b = 0; b < NT; ++b) {
-      float v[16];
-#pragma unroll
-      for (int r = 0; r < 16; ++r) v[r] = acc[a][b][r];
-      mm_exchange(v);
-      const int64_t j = jc + 32 * b;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int64_t i = i0 + 32 * (wm * MT + a) + 16 * h + (lane & 15);
-        if (i < p.o.I && j < p.o.J) {
-          if (p.o.part) store8(p.o.part + (((int64_t)g * p.o.n_split + split) * p.o.I + i) * p.o.J + j, p.o.J - j, v + 8 * h);
-          else mm_epilogue<KIND>(p.o, g, i, j, bias[KIND == MM_FWD ? b : 0], v + 8 * h);
-        }
-      }
-    }
-  }
+  mm_results<KIND, false>(p.o, g, split, i0 + 32 * MT * wm, j0 + 32 * NT * wn, acc);
   if constexpr (KIND == MM_DW) {
     if (p.part_db) {
       // the waves' sums through LDS, in order
-      float* sums = (float*)s0;   // [WN][BM]
+      float* sums = (float*)s0;   // [2][BM]
       lds_sync();
 #pragma unroll
       for (int a = 0; a < MT; ++a) {
         const float s = db[a] + __shfl_xor(db[a], 32);
-        if (lane < 32) sums[wn * BM + 32 * (wm * MT + a) + lane] = s;
+        if (lane < 32) sums[wn * BM + 32 * (MT * wm + a) + lane] = s;
       }
       lds_sync();
-      if (tid < BM && i0 + tid < p.o.I) {
-        float s = sums[tid];
+      if (tid < BM && i0 + tid < p.o.I)
+        p.part_db[(((int64_t)g * p.o.n_split + split) * tj + j0 / BN) * p.o.I + i0 + tid] = sums[tid] + sums[BM + tid];
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Aligned operands.  Four waves form a tile of 64 MT x 64 NT, two stages of LDS.
+// Fragments are read one chunk of 16 k ahead of their products, and the only wait
+// of a stage stands before its last chunk, when the next stage has had three
+// chunks' time to land and this stage's buffer has no reader left.
+//   256 x 256  one wave per SIMD with the whole register file (256 accumulators
+//              a lane): a fragment read from LDS feeds four products, so LDS
+//              moves 0.75 of what the matrix cores take in the same time
+//   128 x 128  two blocks per CU, which fill each other's waits and epilogues;
+//              LDS bound (1.5 of the matrix cores' time)
+//   64 x 64    four blocks per CU, for few tiles
+// The loads are buffer loads: what is past the end of the matrix is out of the
+// buffer's range and arrives as zeros.
+// ---------------------------------------------------------------------------
+// the buffer of `bytes` bytes from p on: the same in all lanes, whatever the
+// compiler makes of the address
+__device__ __forceinline__ u32x4 mm_buffer(const void* p, uint32_t bytes) {
+  const uint64_t a = (uint64_t)p;
+  return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a),
+               (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32)) & 0xffff,
+               (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00027000};
+}
+
+// 16 bytes a lane from a buffer straight to 1 KB of LDS.  As an instruction that
+// the compiler does not model: it cannot tell which object a transposing LDS read
+// touches, and would have every one of them wait for every load in flight.  The
+// load has no destination register; its arrival is waited for by stage_sync()
+// alone, before the barrier behind which the stage is read.  M0 is a reserved
+// register: nothing else in these kernels sets or reads it.
+__device__ __forceinline__ void lds_load(const u32x4& buffer, char* lds, uint32_t lane_off, uint32_t off) {
+  const uint32_t to = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(lds_ptr_t)lds);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+               ::"s"(to), "v"(lane_off), "s"(buffer), "s"(off));
+}
+
+template <class T, class TO, int KIND, int MT, int NT, int OCC>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
+k_mm_piped(const MmArgs<T, TO> p) {
+  constexpr int BM = 64 * MT, BN = 64 * NT, BK = 64, STAGE_A = BM * BK * 2, STAGE = STAGE_A + BN * BK * 2;
+  constexpr bool AK = KIND != MM_DW, BKC = KIND == MM_FWD;
+  constexpr int GA = BM / 32, GB = BN / 32;   // 1 KB groups per wave and stage
+  static_assert(GA == GB, "one group of each operand at a time");
+  typedef typename Elem<T>::frag frag;
+  __shared__ __attribute__((aligned(1024))) char s0[STAGE];
+  __shared__ __attribute__((aligned(1024))) char s1[STAGE];
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave & 1, wn = wave >> 1;
+
+  const uint32_t rows = (uint32_t)((p.o.I + BM - 1) / BM), tj = (uint32_t)((p.o.J + BN - 1) / BN);
+  const MmTilePos at = mm_tile((uint32_t)xcd_remap(blockIdx.x, gridDim.x), rows, tj, p.o.n_split);
+  const int64_t i0 = (int64_t)at.ti * BM, j0 = (int64_t)at.tj * BN;
+  const uint32_t nk = (uint32_t)((p.K + BK - 1) / BK);
+  const int k_lo = (int)((uint64_t)nk * at.split / (uint32_t)p.o.n_split);
+  const int per_pair = (int)((uint64_t)nk * (at.split + 1) / (uint32_t)p.o.n_split) - k_lo;
+  const int stages = per_pair * p.pairs;
+
+  f32x16 acc[MT][NT];
 #pragma unroll
-        for (int n = 1; n < WN; ++n) s += sums[n * BM + tid];
-        p.part_db[(((int64_t)g * p.o.n_split + split) * tj + j0 / BN) * p.o.I + i0 + tid] = s;
+  for (int a = 0; a < MT; ++a)
+#pragma unroll
+    for (int b = 0; b < NT; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[a][b][r] = 0.0f;
+  float db[MT];
+#pragma unroll
+  for (int a = 0; a < MT; ++a) db[a] = 0.0f;
+
+  // ---- loads: lane offset within a group, uniform distance of groups ----
+  const T* pa = p.a.p + at.g * p.a.gs + (AK ? i0 * p.a.ld : i0);
+  const T* pb = p.b.p + at.g * p.b.gs + (BKC ? j0 * p.b.ld : j0);
+  const int left_a = (int)(p.o.I - i0 < BM ? p.o.I - i0 : BM), left_b = (int)(p.o.J - j0 < BN ? p.o.J - j0 : BN);
+  // a group is eight rows of an operand with k along the row, 512 / side rows of
+  // one with k down the rows; a wave's groups are wave, wave + 4, ...
+  constexpr uint32_t OUT = 0xffffffffu;   // never in range
+  auto lane_off = [&](bool along, int side, int64_t ld, int left) __attribute__((always_inline)) -> uint32_t {
+    if (along) return (uint32_t)((8 * wave + (lane >> 3)) * ld * 2 + (((lane & 7) ^ (lane >> 3)) * 16));
+    const int spr = side / 8, row = wave * (64 / spr) + lane / spr, seg = (lane % spr) ^ mm_swizzle(side, row);
+    return seg * 8 < left ? (uint32_t)(row * ld * 2 + seg * 16) : OUT;
+  };
+  const uint32_t off_a = lane_off(AK, BM, p.a.ld, left_a), off_b = lane_off(BKC, BN, p.b.ld, left_b);
+  const uint32_t step_a = (uint32_t)((AK ? 32 : 2048 / BM) * p.a.ld * 2);
+  const uint32_t step_b = (uint32_t)((BKC ? 32 : 2048 / BN) * p.b.ld * 2);
+  const int seg_k = ((lane & 7) ^ (lane >> 3)) * 8;   // k of the lane's piece (k along the row)
+
+  // the next stage to load: its first elements, its k, the stages left of its plane pair
+  const int64_t adv_a = AK ? BK : BK * p.a.ld, adv_b = BKC ? BK : BK * p.b.ld;
+  const int64_t k_first = (int64_t)k_lo * BK;
+  const T *src_a = nullptr, *src_b = nullptr;
+  int64_t k_left = 0;
+  int pair = p.pairs == 1 ? 5 : 0, pair_left = 0;
+  const uint32_t rows_a = (uint32_t)(left_a * p.a.ld * 2), rows_b = (uint32_t)(left_b * p.b.ld * 2);
+  auto begin_pair = [&]() __attribute__((always_inline)) {
+    // (0,2) (1,1) (2,0) (0,1) (1,0) (0,0): two bits each, from the lowest
+    const int qa = (0x124 >> (2 * pair)) & 3, qb = (0x046 >> (2 * pair)) & 3;
+    src_a = pa + qa * p.a.plane + (AK ? k_first : k_first * p.a.ld);
+    src_b = pb + qb * p.b.plane + (BKC ? k_first : k_first * p.b.ld);
+    k_left = p.K - k_first;
+    pair_left = per_pair;
+    ++pair;
+  };
+  // prepare() takes the next stage (past the last one: an empty buffer, so that
+  // its loads only fill LDS with zeros), load() requests a group of each operand
+  u32x4 ra, rb;
+  uint32_t va = 0, vb = 0;
+  int to_load = stages;
+  auto prepare = [&]() __attribute__((always_inline)) {
+    if (pair_left == 0 && to_load > 0) begin_pair();
+    const int kl = to_load <= 0 ? 0 : (int)(k_left < BK ? k_left : BK);
+    ra = mm_buffer(src_a, AK ? (kl ? rows_a : 0) : (uint32_t)(kl * p.a.ld * 2));
+    rb = mm_buffer(src_b, BKC ? (kl ? rows_b : 0) : (uint32_t)(kl * p.b.ld * 2));
+    const bool in_k = seg_k < kl;
+    va = AK && !in_k ? OUT : off_a;
+    vb = BKC && !in_k ? OUT : off_b;
+    src_a += adv_a;
+    src_b += adv_b;
+    k_left -= BK;
+    --pair_left;
+    --to_load;
+  };
+  auto load = [&](char* stage, int q) __attribute__((always_inline)) {
+    lds_load(ra, stage + (wave + 4 * q) * 1024, va, q * step_a);
+    lds_load(rb, stage + (STAGE_A + (wave + 4 * q) * 1024), vb, q * step_b);
+  };
+
+  // ---- fragments ----
+  // (each address is its stage plus ONE offset: through longer chains of pointer
+  // arithmetic the compiler loses which stage is read)
+  const int grp = lane >> 4, t16 = lane & 15, rr = t16 >> 2, q4 = t16 & 3, kb = 8 * (lane >> 5);
+  auto frag_at = [&](const char* stage, int from, bool along, int side, int c, int blk)
+      __attribute__((always_inline)) -> frag {
+    if (along)
+      return *(const frag*)(stage + (from + (lane & 31) * 128 + (((2 * c + (lane >> 5)) ^ (lane & 7)) << 4) + blk * 4096));
+    const int byte = (32 * blk + 16 * (grp & 1) + 4 * q4) * 2, pitch = side * 2;
+    const int off = from + (kb + rr) * pitch + (((byte >> 4) ^ mm_swizzle(side, rr)) << 4) + (byte & 15) + c * 16 * pitch;
+    const u32x2 lo = lds_read_tr<T>(stage + off), hi = lds_read_tr<T>(stage + (off + 4 * pitch));
+    return __builtin_bit_cast(frag, (u32x4{lo.x, lo.y, hi.x, hi.y}));
+  };
+  frag fa[2][MT], fb[2][NT];
+  auto read1 = [&](int into, const char* stage, int c, int n) __attribute__((always_inline)) {
+    if (n < MT) fa[into][n] = frag_at(stage, 0, AK, BM, c, MT * wm + n);
+    if (n < NT) fb[into][n] = frag_at(stage, STAGE_A, BKC, BN, c, NT * wn + n);
+  };
+  // db: the blocks of a row of tiles take the stages in turn, the waves of a
+  // column the chunks; the first three plane pairs hold every plane of A once
+  auto sum_a = [&](int from, int c, uint32_t st) __attribute__((always_inline)) {
+    if constexpr (KIND == MM_DW) {
+      if (p.part_db && (c & 1) == wn && st < (uint32_t)(3 * per_pair) && st % tj == (uint32_t)at.tj) {
+#pragma unroll
+        for (int a = 0; a < MT; ++a)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) db[a] += Elem<T>::to_f(fa[from][a][e]);
       }
+    }
+  };
+  // the products of a chunk; between the first of them go out the reads of the
+  // next chunk and a stage's loads
+  auto chunk = [&](int from, const char* stage, int c, char* into, auto loads) __attribute__((always_inline)) {
+    constexpr int NP = MT * NT, RD = MT > NT ? MT : NT;
+#pragma unroll
+    for (int n = 0; n < NP; ++n) {
+      Elem<T>::mma(acc[n / NT][n % NT], fb[from][n % NT], fa[from][n / NT]);
+      if (n < RD) read1(from ^ 1, stage, c, n);
+      if constexpr (decltype(loads)::value) {
+        constexpr int PER = (GA + NP - 1) / NP;
+#pragma unroll
+        for (int q = 0; q < PER; ++q)
+          if (n * PER + q < GA) load(into, n * PER + q);
+      }
+      if (n < RD || (decltype(loads)::value && n < GA)) __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // one stage; its first chunk is already in fragments 0
+  auto turn = [&](int st, char* now, char* next) __attribute__((always_inline)) {
+    prepare();
+#pragma unroll
+    for (int c = 0; c < 3; ++c) {
+      chunk(c & 1, now, c + 1, nullptr, std::false_type{});
+      sum_a(c & 1, c, st);
+    }
+    stage_sync<0>();
+    chunk(1, next, 0, now, std::true_type{});
+    sum_a(1, 3, st);
+  };
+  prepare();
+#pragma unroll
+  for (int q = 0; q < GA; ++q) load(s0, q);
+  prepare();
+#pragma unroll
+  for (int q = 0; q < GA; ++q) load(s1, q);
+  stage_sync<2 * GA>();
+#pragma unroll
+  for (int q = 0; q < (MT > NT ? MT : NT); ++q) read1(0, s0, 0, q);
+  for (int st = 0; st < stages; st += 2) {
+    turn(st, s0, s1);
+    if (st + 1 < stages) turn(st + 1, s1, s0);
+  }
+  stage_sync<0>();   // no load in flight when LDS is used again or given up
+
+  mm_results<KIND, true>(p.o, at.g, at.split, i0 + 32 * MT * wm, j0 + 32 * NT * wn, acc);
+  if constexpr (KIND == MM_DW) {
+    if (p.part_db) {
+      float* sums = (float*)s0;   // [2][BM]
+#pragma unroll
+      for (int a = 0; a < MT; ++a) {
+        const float s = db[a] + __shfl_xor(db[a], 32);
+        if (lane < 32) sums[wn * BM + 32 * (MT * wm + a) + lane] = s;
+      }
+      lds_sync();
+      if (tid < BM && i0 + tid < p.o.I)
+        p.part_db[(((int64_t)at.g * p.o.n_split + at.split) * tj + at.tj) * p.o.I + i0 + tid] = sums[tid] + sums[BM + tid];
     }
   }
 }
@@ -406,7 +584,7 @@ __global__ void __launch_bounds__(256) k_mm_join(const MmOut<TO> o) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = (float)s[e];
     vec_load<8>(KIND == MM_FWD && o.bias ? o.bias + g * o.J : nullptr, j, o.J, 0.0f, bias);
-    mm_epilogue<KIND>(o, g, i, j, bias, v);
+    mm_finish<KIND>(o, g, i, j, bias, v);
   }
 }
 
@@ -423,21 +601,20 @@ hipError_t join_launch(const MmOut<TO>& o, int G, hipStream_t st) {
 template <class T, class TO, int KIND>
 hipError_t mm_launch(const MmArgs<T, TO>& a, int tile, bool direct, int G, hipStream_t st) {
   const int64_t side = mm_tile_side(tile);
-  const int64_t tiles = ((a.o.I + side - 1) / side) * ((a.o.J + side - 1) / side) * a.o.n_split;
-  if (a.o.I < 1 || a.o.J < 1 || a.K < 1 || a.o.n_split < 1 || G < 1 || G > 65535 || tiles > 0x7fffffff ||
-      (a.o.n_split > 1 && !a.o.part) || (a.pairs != 1 && a.pairs != 6) ||
-      a.K > 0x7fffffff)
+  const int64_t rows = (a.o.I + side - 1) / side, cols = (a.o.J + side - 1) / side;
+  if (a.o.I < 1 || a.o.J < 1 || a.K < 1 || a.o.n_split < 1 || G < 1 || G > 65535 ||
+      (double)rows * cols * a.o.n_split * G > 2e9 || a.o.n_split > (a.K + 63) / 64 || (a.o.n_split > 1 && !a.o.part) ||
+      (a.pairs != 1 && a.pairs != 6) || a.K > 0x7fffffff || (!direct && tile == MM_256) ||
+      (direct && (a.o.J % 8 || (KIND != MM_DW && a.pairs == 1 && a.K % 8))))
     return hipErrorInvalidValue;
-  const dim3 grid((unsigned)tiles, 1, G);
-  if (tile == MM_256) {
-    if (direct) k_mm<T, TO, KIND, 2, 4, 4, 2, 2, true, 2><<<grid, 512, 0, st>>>(a);
-    else k_mm<T, TO, KIND, 2, 4, 4, 2, 2, false, 2><<<grid, 512, 0, st>>>(a);
-  } else if (tile == MM_128) {
-    if (direct) k_mm<T, TO, KIND, 2, 2, 2, 2, 2, true, 2><<<grid, 256, 0, st>>>(a);
-    else k_mm<T, TO, KIND, 2, 2, 2, 2, 2, false, 2><<<grid, 256, 0, st>>>(a);
+  const uint32_t count = (uint32_t)(rows * cols * a.o.n_split * G);
+  if (direct) {
+    if (tile == MM_256) k_mm_piped<T, TO, KIND, 4, 4, 1><<<count, 256, 0, st>>>(a);
+    else if (tile == MM_128) k_mm_piped<T, TO, KIND, 2, 2, 2><<<count, 256, 0, st>>>(a);
+    else k_mm_piped<T, TO, KIND, 1, 1, 4><<<count, 256, 0, st>>>(a);
   } else {
-    if (direct) k_mm<T, TO, KIND, 2, 2, 1, 1, 4, true, 2><<<grid, 256, 0, st>>>(a);
-    else k_mm<T, TO, KIND, 2, 2, 1, 1, 2, false, 2><<<grid, 256, 0, st>>>(a);
+    if (tile == MM_128) k_mm_any<T, TO, KIND, 2, 2><<<count, 256, 0, st>>>(a);
+    else k_mm_any<T, TO, KIND, 1, 1><<<count, 256, 0, st>>>(a);
   }
   return hipGetLastError();
 }
