@@ -13,24 +13,51 @@
 namespace pigan {
 namespace {
 
-// Sum over the TPR threads of a row, in a fixed order; every one of them gets
-// it.  Above a wave, `red` (one entry per wave) passes the waves' sums on; the
-// caller alternates between two of them, so one barrier per sum is enough.
-template <int TPR>
-__device__ __forceinline__ float row_sum(float v, float* red) {
+// A piece of a row of N columns from column c on.  WHOLE: the columns come in whole
+// pieces, so a piece is all there or not at all.
+template <bool WHOLE, class T>
+__device__ __forceinline__ piece_t row_load(const T* p, int64_t c, int64_t N) {
+  if constexpr (!WHOLE) return piece_load(p + c, N - c);
+  piece_t v = {0, 0, 0, 0};
+  if (c < N) v = *(const piece_u*)(p + c);
+  return v;
+}
+template <bool WHOLE, class T>
+__device__ __forceinline__ void row_store(T* p, int64_t c, int64_t N, const float* f) {
+  if constexpr (!WHOLE) piece_store(p + c, N - c, f);
+  else if (c < N) piece_store(p + c, EPP<T>, f);
+}
+
+// Sums over the TPR threads of a row, in a fixed order; every one of them gets
+// them.  Above a wave, `red` (K entries per wave) passes the waves' sums on; the
+// caller alternates between two of them, so one barrier is enough.
+template <int TPR, int K>
+__device__ __forceinline__ void row_sums(float (&v)[K], float* red) {
 #pragma unroll
-  for (int o = 1; o < (TPR < 64 ? TPR : 64); o *= 2) v += __shfl_xor(v, o);
+  for (int o = 1; o < (TPR < 64 ? TPR : 64); o *= 2)
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], o);
   if constexpr (TPR > 64) {
     constexpr int NW = TPR / 64;
     const int wave = threadIdx.x >> 6;
-    if ((threadIdx.x & 63) == 0) red[wave] = v;
-    __syncthreads();
-    const float* r = red + wave / NW * NW;
-    v = r[0];
+    if ((threadIdx.x & 63) == 0)
 #pragma unroll
-    for (int i = 1; i < NW; ++i) v += r[i];
+      for (int k = 0; k < K; ++k) red[wave * K + k] = v[k];
+    __syncthreads();
+    const float* r = red + wave / NW * NW * K;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      v[k] = r[k];
+#pragma unroll
+      for (int i = 1; i < NW; ++i) v[k] += r[i * K + k];
+    }
   }
-  return v;
+}
+template <int TPR>
+__device__ __forceinline__ float row_sum(float v, float* red) {
+  float s[1] = {v};
+  row_sums<TPR>(s, red);
+  return s[0];
 }
 
 // ---------------------------------------------------------------------------
@@ -38,7 +65,7 @@ __device__ __forceinline__ float row_sum(float v, float* red) {
 // cancellation).  Blocks walk rows; the next row is requested before the
 // present one is worked on, gamma and beta stay in registers.
 // ---------------------------------------------------------------------------
-template <class T, int TPR, int NV, int NTH>
+template <class T, int TPR, int NV, int NTH, bool WHOLE>
 __global__ void __launch_bounds__(NTH) k_norm_fwd(const NormArgs<T> p) {
   constexpr int E = EPP<T>, RPB = NTH / TPR;
   __shared__ float red[2][NTH / 64];
@@ -63,7 +90,7 @@ __global__ void __launch_bounds__(NTH) k_norm_fwd(const NormArgs<T> p) {
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int64_t c = (int64_t)(v * TPR + lane) * E;
-      raw[v] = piece_load(row + c, p.N - c);
+      raw[v] = row_load<WHOLE>(row, c, p.N);
     }
   };
   piece_t next[NV];
@@ -89,7 +116,7 @@ __global__ void __launch_bounds__(NTH) k_norm_fwd(const NormArgs<T> p) {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         f[v][e] -= mean;
-        q += c + e < p.N ? f[v][e] * f[v][e] : 0.0f;
+        if (WHOLE ? c < p.N : c + e < p.N) q += f[v][e] * f[v][e];
       }
     }
     const float var = row_sum<TPR>(q, red[1]) / n;
@@ -101,7 +128,7 @@ __global__ void __launch_bounds__(NTH) k_norm_fwd(const NormArgs<T> p) {
         const int64_t c = (int64_t)(v * TPR + lane) * E;
 #pragma unroll
         for (int e = 0; e < E; ++e) f[v][e] = f[v][e] * rstd * ga[v][e] + be[v][e];
-        piece_store(row + c, p.N - c, f[v]);
+        row_store<WHOLE>(row, c, p.N, f[v]);
       }
       if (lane == 0) {
         if (p.mean) p.mean[g * p.M + r] = mean;
@@ -162,92 +189,106 @@ __global__ void __launch_bounds__(1024) k_norm_fwd_long(const NormArgs<T> p) {
 // registers, the block adds its waves' in order and writes one partial row of
 // [dgamma, dbeta] (the final ones, where one block takes all rows).
 // ---------------------------------------------------------------------------
-constexpr int BWD_NTH = 1024;
+// Threads of a block: 1024, which leaves few partial rows, but 256 where a thread
+// holds two 16-bit pieces (sixteen columns): that needs more registers than 1024
+// threads have (131,072 x 1024 with a skip: 312 us spilling, see launch_norm_bwd).
+template <class T, int TPR, int NV> constexpr int bwd_nth() { return TPR <= 64 && sizeof(T) == 2 && NV == 2 ? 256 : 1024; }
 
-template <class T, int TPR, int NV, bool DX, bool COLS>
-__global__ void __launch_bounds__(BWD_NTH) k_norm_bwd(const NormArgs<T> p, float* __restrict__ d0,
+// Nothing is masked by element: past the end of a row dy is loaded as zero, and
+// with it everything that a column there adds.
+template <class T, int TPR, int NV, bool DX, bool COLS, bool WHOLE>
+__global__ void __launch_bounds__((bwd_nth<T, TPR, NV>())) k_norm_bwd(const NormArgs<T> p, float* __restrict__ d0,
                                                       float* __restrict__ d1, int64_t d_g, int64_t d_b) {
-  constexpr int E = EPP<T>, RPB = BWD_NTH / TPR;
-  __shared__ float red[4][BWD_NTH / 64];
+  constexpr int E = EPP<T>, BWD_NTH = bwd_nth<T, TPR, NV>(), RPB = BWD_NTH / TPR;
+  __shared__ float red[2][2 * BWD_NTH / 64];
   __shared__ float cols[COLS && TPR <= 64 ? 2 * TPR * NV * E : 1];
+  __shared__ __attribute__((aligned(16))) float ga[TPR * NV * E];
   const int g = blockIdx.z;
   const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
   const T* x = p.x.p + g * p.x.gs;
   const T* dy = p.dy.p + g * p.dy.gs;
-  const T* add = p.add.p ? p.add.p + g * p.add.gs : nullptr;
+  const T* add = DX && p.add.p ? p.add.p + g * p.add.gs : nullptr;
   const float* gamma = p.gamma ? p.gamma + g * p.N : nullptr;
   const int64_t step = (int64_t)gridDim.x * RPB;
-  const float n = (float)p.N;   // divided by: the mean of a constant row is that constant
+  const float n = (float)p.N;
 
-  float ga[NV][E], sg[NV][E], sb[NV][E];
+  // gamma waits in LDS: beside the column sums it would not fit the registers
+  for (int c = threadIdx.x; c < TPR * NV * E; c += BWD_NTH) ga[c] = gamma && c < p.N ? gamma[c] : 1.0f;
+  __syncthreads();
+  float sg[NV][E], sb[NV][E];
 #pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    vec_load<E>(gamma, (int64_t)(v * TPR + lane) * E, p.N, 1.0f, ga[v]);
+  for (int v = 0; v < NV; ++v)
 #pragma unroll
     for (int e = 0; e < E; ++e) sg[v][e] = sb[v][e] = 0.0f;
-  }
+  piece_t rx[NV], rd[NV], ra[NV];
+  float mean = 0.0f, rstd = 0.0f;
+  auto request = [&](int64_t r) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int64_t c = (int64_t)(v * TPR + lane) * E;
+      rx[v] = row_load<WHOLE>(x + r * p.x.ld, c, p.N);
+      rd[v] = row_load<WHOLE>(dy + r * p.dy.ld, c, p.N);
+    }
+    mean = p.mean[g * p.M + r];
+    rstd = p.rstd[g * p.M + r];
+  };
+  auto request_add = [&](int64_t r) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int64_t c = (int64_t)(v * TPR + lane) * E;
+      ra[v] = row_load<WHOLE>(add + r * p.add.ld, c, p.N);
+    }
+  };
   int turn = 0;
-  for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < p.M; r0 += step, turn ^= 1) {
-    const int64_t r = r0 + sub;
-    const bool live = r < p.M;
-    const int64_t rc = live ? r : p.M - 1;
-    piece_t rx[NV], rd[NV], ra[NV];
+  int64_t r = (int64_t)blockIdx.x * RPB + sub;
+  if (r < p.M) {
+    request(r);
+    if (add) request_add(r);
+  }
+  // (rows above a wave take the whole block: its threads leave together)
+  for (; r < p.M; r += step, turn ^= 1) {
+    asm volatile("" ::: "memory");   // gamma is read again for every row
+    float xh[NV][E], h[NV][E], s[2] = {0.0f, 0.0f};
+    const float mu = mean, rs = rstd;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int64_t c = (int64_t)(v * TPR + lane) * E;
-      rx[v] = piece_load(x + rc * p.x.ld + c, p.N - c);
-      rd[v] = piece_load(dy + rc * p.dy.ld + c, p.N - c);
+      piece_floats<T>(rx[v], xh[v]);
+      piece_floats<T>(rd[v], h[v]);
     }
-    if (DX && add) {
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        const int64_t c = (int64_t)(v * TPR + lane) * E;
-        ra[v] = piece_load(add + rc * p.add.ld + c, p.N - c);
-      }
-    }
-    const float mean = p.mean[g * p.M + rc], rstd = p.rstd[g * p.M + rc];
-    float s1 = 0.0f, s2 = 0.0f;
+    // the next row is on its way while this one is worked on
+    if (r + step < p.M) request(r + step);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      float fx[E], fd[E];
-      const int64_t c = (int64_t)(v * TPR + lane) * E;
-      piece_floats<T>(rx[v], fx);
-      piece_floats<T>(rd[v], fd);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        // selected, not multiplied: a row or column past the end adds nothing
-        const float xh = live && c + e < p.N ? (fx[e] - mean) * rstd : 0.0f;
-        const float d = live ? fd[e] : 0.0f;
-        const float h = d * ga[v][e];
-        s1 += h;
-        s2 += h * xh;
+        xh[v][e] = (xh[v][e] - mu) * rs;
         if (COLS) {
-          sg[v][e] += d * xh;
-          sb[v][e] += d;
+          sg[v][e] += h[v][e] * xh[v][e];
+          sb[v][e] += h[v][e];
         }
+        h[v][e] *= ga[(v * TPR + lane) * E + e];
+        s[0] += h[v][e];
+        s[1] += h[v][e] * xh[v][e];
       }
     }
     if constexpr (DX) {
-      s1 = row_sum<TPR>(s1, red[2 * turn]) / n;
-      s2 = row_sum<TPR>(s2, red[2 * turn + 1]) / n;
-      if (live) {
-        T* row = p.out.p + g * p.out.gs + r * p.out.ld;
+      row_sums<TPR>(s, red[turn]);
+      const float s1 = s[0] / n, s2 = s[1] / n;
+      T* row = p.out.p + g * p.out.gs + r * p.out.ld;
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-          float fx[E], fd[E], o[E];
-          const int64_t c = (int64_t)(v * TPR + lane) * E;
-          piece_floats<T>(rx[v], fx);
-          piece_floats<T>(rd[v], fd);
+      for (int v = 0; v < NV; ++v) {
+        const int64_t c = (int64_t)(v * TPR + lane) * E;
 #pragma unroll
-          for (int e = 0; e < E; ++e) o[e] = rstd * (fd[e] * ga[v][e] - s1 - (fx[e] - mean) * rstd * s2);
-          if (add) {
-            piece_floats<T>(ra[v], fd);
+        for (int e = 0; e < E; ++e) h[v][e] = rs * (h[v][e] - s1 - xh[v][e] * s2);
+        if (add) {
+          float res[E];
+          piece_floats<T>(ra[v], res);
 #pragma unroll
-            for (int e = 0; e < E; ++e) o[e] += fd[e];
-          }
-          piece_store(row + c, p.N - c, o);
+          for (int e = 0; e < E; ++e) h[v][e] += res[e];
         }
+        row_store<WHOLE>(row, c, p.N, h[v]);
       }
+      if (add && r + step < p.M) request_add(r + step);
     }
   }
   if constexpr (COLS) {
@@ -302,17 +343,17 @@ __global__ void __launch_bounds__(BWD_NTH) k_norm_bwd(const NormArgs<T> p, float
 template <class T>
 __global__ void __launch_bounds__(1024) k_norm_bwd_long(const NormArgs<T> p) {
   constexpr int E = EPP<T>;
-  __shared__ float red[2][16];
+  __shared__ float red[32];
   const int g = blockIdx.z;
   const float* gamma = p.gamma ? p.gamma + g * p.N : nullptr;
-  const float n = (float)p.N;   // divided by: the mean of a constant row is that constant
+  const float n = (float)p.N;
   for (int64_t r = blockIdx.x; r < p.M; r += gridDim.x) {
     const T* x = p.x.p + g * p.x.gs + r * p.x.ld;
     const T* dy = p.dy.p + g * p.dy.gs + r * p.dy.ld;
     const T* add = p.add.p ? p.add.p + g * p.add.gs + r * p.add.ld : nullptr;
     T* out = p.out.p + g * p.out.gs + r * p.out.ld;
     const float mean = p.mean[g * p.M + r], rstd = p.rstd[g * p.M + r];
-    float s1 = 0.0f, s2 = 0.0f, fx[E], fd[E], ga[E];
+    float s[2] = {0.0f, 0.0f}, fx[E], fd[E], ga[E];
     for (int64_t c = (int64_t)threadIdx.x * E; c < p.N; c += 1024 * E) {
       piece_floats<T>(piece_load(x + c, p.N - c), fx);
       piece_floats<T>(piece_load(dy + c, p.N - c), fd);
@@ -320,12 +361,12 @@ __global__ void __launch_bounds__(1024) k_norm_bwd_long(const NormArgs<T> p) {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const float h = fd[e] * ga[e];
-        s1 += h;
-        s2 += c + e < p.N ? h * ((fx[e] - mean) * rstd) : 0.0f;
+        s[0] += h;
+        s[1] += h * ((fx[e] - mean) * rstd);
       }
     }
-    s1 = row_sum<1024>(s1, red[0]) / n;
-    s2 = row_sum<1024>(s2, red[1]) / n;
+    row_sums<1024>(s, red);
+    const float s1 = s[0] / n, s2 = s[1] / n;
     for (int64_t c = (int64_t)threadIdx.x * E; c < p.N; c += 1024 * E) {
       float o[E];
       piece_floats<T>(piece_load(x + c, p.N - c), fx);
@@ -464,27 +505,38 @@ void fwd(const NormArgs<T>& a, int G, hipStream_t st) {
   // beta are read once for many rows
   const int64_t most = cdiv(int64_t(256) * 2048 / NTH, G);
   const int64_t blocks = cdiv(a.M, NTH / TPR);
-  k_norm_fwd<T, TPR, NV, NTH><<<dim3((unsigned)(blocks < most ? blocks : most), 1, G), NTH, 0, st>>>(a);
+  const dim3 grid((unsigned)(blocks < most ? blocks : most), 1, G);
+  if (a.N % EPP<T> == 0) k_norm_fwd<T, TPR, NV, NTH, true><<<grid, NTH, 0, st>>>(a);
+  else k_norm_fwd<T, TPR, NV, NTH, false><<<grid, NTH, 0, st>>>(a);
 }
 
-// blocks of the backward kernel per group, and threads per row
-int bwd_tpr(int64_t pieces) { return pieces <= 8 ? 8 : pieces <= 32 ? 32 : pieces <= 128 ? 64 : BWD_NTH; }
-int64_t bwd_blocks(int64_t pieces, int64_t M) {
-  const int64_t want = cdiv(M, BWD_NTH / bwd_tpr(pieces));
-  return want < 256 ? want : 256;   // one block per CU; each more is another partial row
+// blocks of the backward kernel per group: each is another partial row, so no
+// more than fill the CUs (one of 1024 threads, three of 256)
+int64_t bwd_blocks(int elem_bytes, int64_t pieces, int64_t M) {
+  const int tpr = pieces <= 8 ? 8 : pieces <= 32 ? 32 : pieces <= 128 ? 64 : 1024;
+  const bool small = pieces > 64 && pieces <= 128 && elem_bytes == 2;
+  const int64_t most = small ? 768 : 256, want = cdiv(M, (small ? 256 : 1024) / tpr);
+  return want < most ? want : most;
 }
 int64_t cols_splits(int64_t M) { return M < 64 ? M : 64; }
 
-template <class T, int TPR, int NV>
-void bwd(const NormArgs<T>& a, int64_t nb, int G, hipStream_t st) {
+template <class T, int TPR, int NV, bool WHOLE>
+void bwd_of(const NormArgs<T>& a, int64_t nb, int G, hipStream_t st) {
+  constexpr int BWD_NTH = bwd_nth<T, TPR, NV>();
   const dim3 grid((unsigned)nb, 1, G);
   const bool cols = a.dgamma || a.dbeta;
   float* d0 = !cols ? nullptr : nb > 1 ? a.part : a.dgamma;
   float* d1 = !cols ? nullptr : nb > 1 ? a.part + a.N : a.dbeta;
   const int64_t d_g = nb > 1 ? nb * 2 * a.N : a.N, d_b = 2 * a.N;
-  if (a.out.p && cols) k_norm_bwd<T, TPR, NV, true, true><<<grid, BWD_NTH, 0, st>>>(a, d0, d1, d_g, d_b);
-  else if (cols) k_norm_bwd<T, TPR, NV, false, true><<<grid, BWD_NTH, 0, st>>>(a, d0, d1, d_g, d_b);
-  else if (a.out.p) k_norm_bwd<T, TPR, NV, true, false><<<grid, BWD_NTH, 0, st>>>(a, d0, d1, d_g, d_b);
+  if (a.out.p && cols) k_norm_bwd<T, TPR, NV, true, true, WHOLE><<<grid, BWD_NTH, 0, st>>>(a, d0, d1, d_g, d_b);
+  else if (cols) k_norm_bwd<T, TPR, NV, false, true, WHOLE><<<grid, BWD_NTH, 0, st>>>(a, d0, d1, d_g, d_b);
+  else if (a.out.p) k_norm_bwd<T, TPR, NV, true, false, WHOLE><<<grid, BWD_NTH, 0, st>>>(a, d0, d1, d_g, d_b);
+}
+
+template <class T, int TPR, int NV>
+void bwd(const NormArgs<T>& a, int64_t nb, int G, hipStream_t st) {
+  if (a.N % EPP<T> == 0) bwd_of<T, TPR, NV, true>(a, nb, G, st);
+  else bwd_of<T, TPR, NV, false>(a, nb, G, st);
 }
 
 }  // namespace
@@ -507,7 +559,7 @@ hipError_t launch_norm_fwd(const NormArgs<T>& a, int G, hipStream_t st) {
 
 int64_t norm_part_floats(int elem_bytes, int64_t M, int64_t N) {
   const int64_t pc = cdiv(N, 16 / elem_bytes);
-  const int64_t nb = pc <= MAX_PIECES ? bwd_blocks(pc, M) : cols_splits(M);
+  const int64_t nb = pc <= MAX_PIECES ? bwd_blocks(elem_bytes, pc, M) : cols_splits(M);
   return nb > 1 ? nb * 2 * N : 0;
 }
 
@@ -521,13 +573,13 @@ hipError_t launch_norm_bwd(const NormArgs<T>& a, int G, hipStream_t st) {
   const int64_t pc = cdiv(a.N, EPP<T>);
   int64_t nb;
   if (pc <= MAX_PIECES) {
-    nb = bwd_blocks(pc, a.M);
+    nb = bwd_blocks((int)sizeof(T), pc, a.M);
     if (pc <= 8) bwd<T, 8, 1>(a, nb, G, st);
     else if (pc <= 32) bwd<T, 32, 1>(a, nb, G, st);
     else if (pc <= 64) bwd<T, 64, 1>(a, nb, G, st);
     else if (pc <= 128) bwd<T, 64, 2>(a, nb, G, st);
-    else if (pc <= 1024) bwd<T, BWD_NTH, 1>(a, nb, G, st);
-    else bwd<T, BWD_NTH, 2>(a, nb, G, st);
+    else if (pc <= 1024) bwd<T, 1024, 1>(a, nb, G, st);
+    else bwd<T, 1024, 2>(a, nb, G, st);
   } else {
     nb = cols_splits(a.M);
     if (cols) {
