@@ -583,6 +583,17 @@ def _vec(t: torch.Tensor, name: str, like: torch.Tensor, shape) -> int:
     return t.data_ptr()
 
 
+def _new(shape, like: torch.Tensor) -> tuple[torch.Tensor, tuple[int, int, int]]:
+    """A matrix for a result, and its operand."""
+    t = torch.empty(shape, dtype=like.dtype, device=like.device)
+    return t, (t.data_ptr(), shape[-1], shape[-2] * shape[-1])
+
+
+def _new_vec(shape, like: torch.Tensor) -> tuple[torch.Tensor, int]:
+    t = torch.empty(shape, dtype=torch.float32, device=like.device)
+    return t, t.data_ptr()
+
+
 def _layer_dims(x: torch.Tensor, name: str) -> tuple[int, int]:
     """(groups, dtype) of the matrix that sets a call's type and device."""
     if not x.is_cuda:
@@ -593,6 +604,19 @@ def _layer_dims(x: torch.Tensor, name: str) -> tuple[int, int]:
     if dt is None:
         raise ValueError(f"{name} must be fp32, bf16 or fp16, got {x.dtype}")
     return (x.shape[0] if x.dim() == 3 else 1), dt
+
+
+def _result(need: bool, t: torch.Tensor | None, name: str, like: torch.Tensor, shape):
+    """(tensor, operand) of a result: the caller's, a new one, or none."""
+    if not need:
+        return None, _NO_MAT
+    return _new(shape, like) if t is None else (t, _mat(t, name, like, shape))
+
+
+def _result_vec(need: bool, t: torch.Tensor | None, name: str, like: torch.Tensor, shape):
+    if not need:
+        return None, 0
+    return _new_vec(shape, like) if t is None else (t, _vec(t, name, like, shape))
 
 
 def _act(act: str) -> int:
@@ -607,7 +631,9 @@ def _call(fn, args: bytes, like: torch.Tensor, *ws):
     if dev.index != torch.cuda.current_device():
         with torch.cuda.device(dev):
             return _call(fn, args, like, *ws)
-    st = fn(args, *ws, torch.cuda.current_stream().cuda_stream)
+    # the current stream's handle; torch.cuda.current_stream() builds an object
+    # around it, which takes as long as the launch of a kernel
+    st = fn(args, *ws, torch._C._cuda_getCurrentRawStream(dev.index))
     if st != OK:
         _check(st)
 
@@ -620,7 +646,10 @@ def _call_ws(fn, query, args: bytes, like: torch.Tensor, ws: torch.Tensor | None
         ws = torch.empty(need, dtype=torch.uint8, device=like.device)
     if ws is not None and (ws.dtype != torch.uint8 or ws.device != like.device or not ws.is_contiguous()):
         raise ValueError(f"ws must be a contiguous torch.uint8 tensor on {like.device}")
-    _call(fn, args, like, ws.data_ptr() if ws is not None else None, ws.numel() if ws is not None else 0)
+    if ws is None:
+        _call(fn, args, like, None, 0)
+    else:
+        _call(fn, args, like, ws.data_ptr(), ws.numel())
 
 
 def linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None, act: str = "none",
@@ -637,12 +666,13 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None, a
     N = w.shape[-2] if w.dim() == x.dim() else 0
     shape, vec = (*lead, M, N), (*lead, N)
     mw = _mat(w, "w", x, (*lead, N, K))
-    if out is None:
-        out = torch.empty(shape, dtype=x.dtype, device=x.device)
-    if save_pre and pre is None:
-        pre = torch.empty(shape, dtype=x.dtype, device=x.device)
-    args = LINEAR_ARGS.pack(G, dt, _act(act), 0, M, K, N, *_mat(x, "x", x, x.shape), *mw,
-                            *_mat(out, "out", x, shape), *(_NO_MAT if pre is None else _mat(pre, "pre", x, shape)),
+    mx = _mat(x, "x", x, x.shape)
+    out, my = _new(shape, x) if out is None else (out, _mat(out, "out", x, shape))
+    if pre is not None:
+        mp = _mat(pre, "pre", x, shape)
+    else:
+        pre, mp = _new(shape, x) if save_pre else (None, _NO_MAT)
+    args = LINEAR_ARGS.pack(G, dt, _act(act), 0, M, K, N, *mx, *mw, *my, *mp,
                             *(_NO_MAT if residual is None else _mat(residual, "residual", x, shape)), *_NO_MAT,
                             *_NO_MAT, 0 if bias is None else _vec(bias, "bias", x, vec), 0, 0)
     _call_ws(L.pigan_linear_forward, L.pigan_linear_forward_workspace, args, x, ws)
@@ -665,19 +695,15 @@ def linear_backward(g: torch.Tensor, x: torch.Tensor, w: torch.Tensor, act: str 
     K = x.shape[-1]
     shape = (*lead, M, K)
     mx, mw = _mat(x, "x", g, shape), _mat(w, "w", g, (*lead, N, K))
-    dx = torch.empty(shape, dtype=g.dtype, device=g.device) if need_dx and dx is None else dx if need_dx else None
-    if need_dw and dw is None:
-        dw = torch.empty((*lead, N, K), dtype=torch.float32, device=g.device)
-    if need_db and db is None:
-        db = torch.empty((*lead, N), dtype=torch.float32, device=g.device)
+    dx, mdx = _result(need_dx, dx, "dx", g, shape)
+    dw, pdw = _result_vec(need_dw, dw, "dw", g, (*lead, N, K))
+    db, pdb = _result_vec(need_db, db, "db", g, (*lead, N))
     args = LINEAR_ARGS.pack(G, dt, _act(act), 0, M, K, N, *mx, *mw, *_NO_MAT,
                             *(_NO_MAT if pre is None else _mat(pre, "pre", g, shape)),
-                            *(_NO_MAT if add is None else _mat(add, "add", g, shape)), *_mat(g, "g", g, g.shape),
-                            *(_NO_MAT if dx is None else _mat(dx, "dx", g, shape)), 0,
-                            _vec(dw, "dw", g, (*lead, N, K)) if need_dw else 0,
-                            _vec(db, "db", g, (*lead, N)) if need_db else 0)
+                            *(_NO_MAT if add is None else _mat(add, "add", g, shape)), *_mat(g, "g", g, g.shape), *mdx, 0,
+                            pdw, pdb)
     _call_ws(L.pigan_linear_backward, L.pigan_linear_backward_workspace, args, g, ws)
-    return dx, dw if need_dw else None, db if need_db else None
+    return dx, dw, db
 
 
 def act_backward(dy: torch.Tensor, pre: torch.Tensor, act: str, out: torch.Tensor | None = None) -> torch.Tensor:
@@ -685,10 +711,9 @@ def act_backward(dy: torch.Tensor, pre: torch.Tensor, act: str, out: torch.Tenso
     activation.  `out` may be `dy` or `pre`."""
     G, dt = _layer_dims(dy, "dy")
     shape = dy.shape
-    if out is None:
-        out = torch.empty(shape, dtype=dy.dtype, device=dy.device)
-    args = ACT_ARGS.pack(G, dt, _act(act), 0, shape[-2], shape[-1], *_mat(dy, "dy", dy, shape),
-                         *_mat(pre, "pre", dy, shape), *_mat(out, "out", dy, shape))
+    md, mp = _mat(dy, "dy", dy, shape), _mat(pre, "pre", dy, shape)
+    out, mo = _result(True, out, "out", dy, shape)
+    args = ACT_ARGS.pack(G, dt, _act(act), 0, shape[-2], shape[-1], *md, *mp, *mo)
     _call(lib().pigan_act_backward, args, dy)
     return out
 
@@ -702,16 +727,13 @@ def layer_norm(x: torch.Tensor, gamma: torch.Tensor | None = None, beta: torch.T
     G, dt = _layer_dims(x, "x")
     shape = x.shape
     rows, cols = shape[:-1], (*shape[:-2], shape[-1])
-    if out is None:
-        out = torch.empty(shape, dtype=x.dtype, device=x.device)
-    if mean is None:
-        mean = torch.empty(rows, dtype=torch.float32, device=x.device)
-    if rstd is None:
-        rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
-    args = NORM_ARGS.pack(G, dt, shape[-2], shape[-1], eps, 0, *_mat(x, "x", x, shape), *_mat(out, "out", x, shape),
-                          *_NO_MAT, *_NO_MAT, *_NO_MAT, 0 if gamma is None else _vec(gamma, "gamma", x, cols),
-                          0 if beta is None else _vec(beta, "beta", x, cols), _vec(mean, "mean", x, rows),
-                          _vec(rstd, "rstd", x, rows), 0, 0)
+    mx = _mat(x, "x", x, shape)
+    out, mo = _result(True, out, "out", x, shape)
+    mean, pm = _result_vec(True, mean, "mean", x, rows)
+    rstd, pr = _result_vec(True, rstd, "rstd", x, rows)
+    args = NORM_ARGS.pack(G, dt, shape[-2], shape[-1], eps, 0, *mx, *mo, *_NO_MAT, *_NO_MAT, *_NO_MAT,
+                          0 if gamma is None else _vec(gamma, "gamma", x, cols),
+                          0 if beta is None else _vec(beta, "beta", x, cols), pm, pr, 0, 0)
     _call(lib().pigan_layer_norm_forward, args, x)
     return out, mean, rstd
 
@@ -726,20 +748,15 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, r
     G, dt = _layer_dims(dy, "dy")
     shape = dy.shape
     rows, cols = shape[:-1], (*shape[:-2], shape[-1])
-    dx = torch.empty(shape, dtype=dy.dtype, device=dy.device) if need_dx and dx is None else dx if need_dx else None
-    if need_params:
-        if dgamma is None:
-            dgamma = torch.empty(cols, dtype=torch.float32, device=dy.device)
-        if dbeta is None:
-            dbeta = torch.empty(cols, dtype=torch.float32, device=dy.device)
+    dx, mdx = _result(need_dx, dx, "dx", dy, shape)
+    dgamma, pg = _result_vec(need_params, dgamma, "dgamma", dy, cols)
+    dbeta, pb = _result_vec(need_params, dbeta, "dbeta", dy, cols)
     args = NORM_ARGS.pack(G, dt, shape[-2], shape[-1], 0.0, 0, *_mat(x, "x", dy, shape), *_NO_MAT,
                           *_mat(dy, "dy", dy, shape), *(_NO_MAT if add is None else _mat(add, "add", dy, shape)),
-                          *(_NO_MAT if dx is None else _mat(dx, "dx", dy, shape)),
-                          0 if gamma is None else _vec(gamma, "gamma", dy, cols), 0, _vec(mean, "mean", dy, rows),
-                          _vec(rstd, "rstd", dy, rows), _vec(dgamma, "dgamma", dy, cols) if need_params else 0,
-                          _vec(dbeta, "dbeta", dy, cols) if need_params else 0)
+                          *mdx, 0 if gamma is None else _vec(gamma, "gamma", dy, cols), 0,
+                          _vec(mean, "mean", dy, rows), _vec(rstd, "rstd", dy, rows), pg, pb)
     _call_ws(L.pigan_layer_norm_backward, L.pigan_layer_norm_backward_workspace, args, dy, ws)
-    return (dx, dgamma, dbeta) if need_params else (dx, None, None)
+    return dx, dgamma, dbeta
 
 
 def profile_enable(on: bool = True):
