@@ -6,9 +6,15 @@ namespace pigan {
 namespace {
 
 // ---------------------------------------------------------------------------
-// Few rows.  A block forms 16 x 16 results; its waves take chunks of k in turn
-// and read both operands' fragments from memory (w streams through once, 16
-// bytes a lane), U chunks in flight.  Their sums meet in LDS, in order.
+// Few rows.  A block forms a strip of 16 / P columns for up to 16 / P rows at a
+// time; its waves take chunks of k in turn and read both operands' fragments
+// straight from memory, U chunks in flight, so w streams through once and no wave
+// waits for another before the end.  With P > 1 the 16 rows and columns of the
+// matrix instruction hold P chunks of k at once, 16 / P rows and columns each:
+// only the blocks on its diagonal, which pair a chunk with itself, are used.  The
+// lanes of a load then cover 64 P consecutive bytes of a row of w, and there are P
+// times as many blocks.  The waves' sums meet in LDS, in order.
+// Bound by the bytes of w (one row of x, 8192 -> 2048 bf16: P = 1 15.6 us).
 // ---------------------------------------------------------------------------
 template <class T> struct ShortMma;
 template <> struct ShortMma<bf16> {
@@ -33,51 +39,52 @@ template <> struct ShortMma<float> {
   }
 };
 
-template <class T, int NW, int U>
+template <class T, int P, int NW, int U>
 __global__ void __launch_bounds__(64 * NW) k_short_fwd(const MmArgs<T, T> p) {
-  constexpr int CK = ShortMma<T>::CK;
+  constexpr int CK = ShortMma<T>::CK, S = 16 / P, TURN = NW * P * CK;   // k per turn of all waves
   __shared__ float sums[NW][16][17];
   const int g = blockIdx.z;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t i0 = (int64_t)blockIdx.y * 16, j0 = (int64_t)blockIdx.x * 16;
-  const int64_t i = i0 + (lane & 15), j = j0 + (lane & 15);
+  const int64_t i0 = (int64_t)blockIdx.y * S, j0 = (int64_t)blockIdx.x * S;
+  const int64_t i = i0 + (lane & (S - 1)), j = j0 + (lane & (S - 1));
   // rows past the end repeat the last one; their results are not stored
-  const T* pa = p.a.p + g * p.a.gs + (i < p.o.I ? i : p.o.I - 1) * p.a.ld;
-  const T* pb = p.b.p + g * p.b.gs + (j < p.o.J ? j : p.o.J - 1) * p.b.ld;
-  const int kl = (lane >> 4) * EPP<T>;
+  const int64_t kl = (wave * P + ((lane & 15) / S)) * CK + (lane >> 4) * EPP<T>;
+  const T* pa = p.a.p + g * p.a.gs + (i < p.o.I ? i : p.o.I - 1) * p.a.ld + kl;
+  const T* pb = p.b.p + g * p.b.gs + (j < p.o.J ? j : p.o.J - 1) * p.b.ld + kl;
   f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-  // whole turns of U chunks for every wave, then the rest with zeros past the end
-  const int64_t whole = p.K / (NW * CK * U) * (NW * CK * U);
-  pa += wave * CK + kl;
-  pb += wave * CK + kl;
-  for (int64_t k0 = 0; k0 < whole; k0 += NW * CK * U) {
+  // turns of U chunks that are whole for every wave, then the rest with zeros past the end
+  const int64_t whole = p.K / (TURN * U) * (TURN * U);
+  for (int64_t k0 = 0; k0 < whole; k0 += TURN * U) {
     piece_t a[U], b[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      b[u] = *(const piece_u*)(pb + k0 + u * NW * CK);
-      a[u] = *(const piece_u*)(pa + k0 + u * NW * CK);
-    }
+    for (int u = 0; u < U; ++u) b[u] = *(const piece_u*)(pb + k0 + u * TURN);
+#pragma unroll
+    for (int u = 0; u < U; ++u) a[u] = *(const piece_u*)(pa + k0 + u * TURN);
 #pragma unroll
     for (int u = 0; u < U; ++u) acc = ShortMma<T>::mma(b[u], a[u], acc);
   }
-  for (int64_t k0 = whole; k0 < p.K; k0 += NW * CK) {
-    const int64_t left = p.K - k0 - wave * CK - kl;
+  for (int64_t k0 = whole; k0 < p.K; k0 += TURN) {
+    const int64_t left = p.K - k0 - kl;
     acc = ShortMma<T>::mma(piece_load(pb + k0, left), piece_load(pa + k0, left), acc);
   }
 #pragma unroll
   for (int r = 0; r < 4; ++r) sums[wave][lane & 15][4 * (lane >> 4) + r] = acc[r];
   __syncthreads();
-  if (threadIdx.x < 32) {
-    const int row = threadIdx.x >> 1, c = 8 * (threadIdx.x & 1);
+  constexpr int OC = S < 8 ? 1 : S / 8;   // octets per row of the strip
+  if (threadIdx.x < S * OC) {
+    const int row = threadIdx.x / OC, c = 8 * (threadIdx.x % OC);
     float v[8], bias[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = sums[0][row][c + e];
-    for (int w = 1; w < NW; ++w)
+    for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+    for (int w = 0; w < NW; ++w)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += sums[w][row][c + e];
-    if (i0 + row < p.o.I && j0 + c < p.o.J) {
+      for (int q = 0; q < P; ++q)
+#pragma unroll
+        for (int e = 0; e < (S < 8 ? S : 8); ++e) v[e] += sums[w][q * S + row][q * S + c + e];
+    const int64_t left = p.o.J - j0 - c, valid = left < S - c ? left : S - c;
+    if (i0 + row < p.o.I && valid > 0) {
       vec_load<8>(p.o.bias ? p.o.bias + g * p.o.J : nullptr, j0 + c, p.o.J, 0.0f, bias);
-      mm_finish<MM_FWD>(p.o, g, i0 + row, j0 + c, bias, v);
+      mm_finish<MM_FWD>(p.o, g, i0 + row, j0 + c, valid < 8 ? valid : 8, bias, v);
     }
   }
 }
@@ -119,14 +126,22 @@ __global__ void __launch_bounds__(256) k_split3(const SplitSets sets, int G) {
 
 }  // namespace
 
+template <class T, int P>
+void short_of(const MmArgs<T, T>& a, int G, hipStream_t st) {
+  constexpr int S = 16 / P;
+  const dim3 grid((unsigned)((a.o.J + S - 1) / S), (unsigned)((a.o.I + S - 1) / S), G);
+  // waves for the length of k, so that all of a row is in flight at once up to 8192
+  if (a.K > 2048) k_short_fwd<T, P, 8, 8><<<grid, 512, 0, st>>>(a);
+  else k_short_fwd<T, P, 4, 4><<<grid, 256, 0, st>>>(a);
+}
+
 template <class T>
 hipError_t launch_short_fwd(const MmArgs<T, T>& a, int G, hipStream_t st) {
-  const int64_t bx = (a.o.J + 15) / 16, by = (a.o.I + 15) / 16;
-  if (a.o.I < 1 || a.o.J < 1 || a.K < 1 || by > 65535 || bx > 0x7fffffff || G < 1 || G > 65535)
+  if (a.o.I < 1 || a.o.J < 1 || a.K < 1 || a.o.J > 0x7fffffff || (a.o.I + 15) / 16 > 65535 || G < 1 || G > 65535)
     return hipErrorInvalidValue;
-  const dim3 grid((unsigned)bx, (unsigned)by, G);
-  if (a.K > 1024) k_short_fwd<T, 16, 4><<<grid, 1024, 0, st>>>(a);
-  else k_short_fwd<T, 4, 2><<<grid, 256, 0, st>>>(a);
+  if (a.o.I <= 4) short_of<T, 4>(a, G, st);
+  else if (a.o.I <= 8) short_of<T, 2>(a, G, st);
+  else short_of<T, 1>(a, G, st);
   return hipGetLastError();
 }
 

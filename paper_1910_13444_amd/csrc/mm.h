@@ -161,13 +161,14 @@ __device__ __forceinline__ void mm_results(const MmOut<TO>& o, int g, int split,
   }
 }
 
-// one octet by itself
+// the first `valid` columns of an octet by itself
 template <int KIND, class TO>
-__device__ __forceinline__ void mm_finish(const MmOut<TO>& o, int g, int64_t i, int64_t j, const float* bias, float* v) {
+__device__ __forceinline__ void mm_finish(const MmOut<TO>& o, int g, int64_t i, int64_t j, int64_t valid,
+                                          const float* bias, float* v) {
   PIGAN_ACT_SWITCH(KIND == MM_DW ? PIGAN_ACT_NONE : o.act, {
     EpiIn<KIND, ACT, TO> in;
-    in.load(o, g, i, j, o.J - j);
-    mm_epilogue<KIND, ACT>(o, g, i, j, o.J - j, in, bias, v);
+    in.load(o, g, i, j, valid);
+    mm_epilogue<KIND, ACT>(o, g, i, j, valid, in, bias, v);
   })
 }
 
@@ -584,7 +585,7 @@ __global__ void __launch_bounds__(256) k_mm_join(const MmOut<TO> o) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = (float)s[e];
     vec_load<8>(KIND == MM_FWD && o.bias ? o.bias + g * o.J : nullptr, j, o.J, 0.0f, bias);
-    mm_finish<KIND>(o, g, i, j, bias, v);
+    mm_finish<KIND>(o, g, i, j, o.J - j, bias, v);
   }
 }
 
