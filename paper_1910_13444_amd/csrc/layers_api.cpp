@@ -136,6 +136,7 @@ pigan_status check_backward(const pigan_linear* a) {
 struct MmPlan {
   int tile = MM_64;
   int n_split = 1;
+  double us = 1e30;   // modelled
 };
 
 // Modelled time of a launch on 256 CUs, from measured times: of a stage (64 values
@@ -147,31 +148,63 @@ struct MmPlan {
 //   forward 1024 x 2000 x 1024     36 | 21 | 13         43 | 30 | 16
 //   dw of 131072 x 1024 x 1024     284 | 297 | 536      306 | 330 | 428
 //   dx of 21 x 512 x 256 x 256     36 | 12 | 10         36 | 15 | 8
-MmPlan plan_mm(int64_t I, int64_t J, int64_t K, int pairs, int G) {
-  static const double stage_us[3][4] = {{0.33, 0.48, 0.63, 0.78}, {0.6, 1.16, 0, 0}, {1.9, 0, 0, 0}};
-  static const double block_us[3] = {3.0, 7.0, 14.0}, first_us[3] = {2.0, 5.0, 14.0};
-  static const int per_cu[3] = {4, 2, 1};
+// (64 tile with k down the rows of an operand: 8192^3 in 2066 and 2275 us, forward 1605)
+constexpr double STAGE_FWD[3][4] = {{0.33, 0.48, 0.63, 0.78}, {0.6, 1.16, 0, 0}, {1.9, 0, 0, 0}};
+constexpr double STAGE_BWD[3][4] = {{0.42, 0.63, 0.84, 1.05}, {0.6, 1.16, 0, 0}, {1.9, 0, 0, 0}};
+constexpr double BLOCK_US[3] = {3.0, 7.0, 14.0}, FIRST_US[3] = {2.0, 5.0, 14.0};
+constexpr int PER_CU[3] = {4, 2, 1};
+
+double tiles_of(int64_t I, int64_t J, int G, int t) {
+  const int64_t s = mm_tile_side(t);
+  return (double)((I + s - 1) / s) * (double)((J + s - 1) / s) * G;
+}
+double split_us(int64_t I, int64_t J, int G, int split) {
+  return split > 1 ? 8.0 + (double)G * I * J * 4.0 * (split * 2 + 1) / 5e6 : 0.0;
+}
+
+MmPlan plan_mm(const double (&STAGE_US)[3][4], int64_t I, int64_t J, int64_t K, int pairs, int G) {
   const int64_t nk = (K + 63) / 64;
   MmPlan best;
-  double best_us = 1e30;
   for (int t = MM_64; t <= MM_256; ++t) {
-    const int64_t s = mm_tile_side(t);
-    const double tiles = (double)((I + s - 1) / s) * (double)((J + s - 1) / s) * G;
+    const double tiles = tiles_of(I, J, G, t);
     for (int split = 1; split <= 64 && split <= nk; split *= 2) {
       if (split > 1 && nk * pairs / split < 4) break;
       const double blocks = tiles * split;
-      const int held = (int)std::min<double>(per_cu[t], ceil(blocks / 256));
+      const int held = (int)std::min<double>(PER_CU[t], ceil(blocks / 256));
       const double rounds = ceil(blocks / (256.0 * held));
-      double us = rounds * ((double)((nk + split - 1) / split) * pairs * stage_us[t][held - 1] + block_us[t]) + first_us[t];
-      if (split > 1) us += 8.0 + (double)G * I * J * 4.0 * (split * 2 + 1) / 5e6;
-      if (us < best_us) {
-        best_us = us;
-        best.tile = t;
-        best.n_split = split;
-      }
+      const double us = rounds * ((double)((nk + split - 1) / split) * pairs * STAGE_US[t][held - 1] + BLOCK_US[t]) +
+                        FIRST_US[t] + split_us(I, J, G, split);
+      if (us < best.us) best = {t, split, us};
     }
   }
   return best;
+}
+
+// Both products of a reverse pass in one launch, dx on whole contractions: the
+// time is that of the longest block, or of all of them spread over the chip.
+// Taken where it is shorter than one launch after the other (2 us between them).
+bool plan_both(int64_t M, int64_t N, int64_t K, int pairs, int G, MmPlan& dx, MmPlan& dw) {
+  const auto& STAGE_US = STAGE_BWD;
+  const int64_t nx = (N + 63) / 64, nw = (M + 63) / 64;
+  double best = dx.us + dw.us + 2.0;
+  bool both = false;
+  for (int t = MM_64; t <= MM_128; ++t)
+    for (int split = 1; split <= 64 && split <= nw; split *= 2) {
+      if (split > 1 && nw * pairs / split < 4) break;
+      const double b1 = tiles_of(M, K, G, t), b2 = tiles_of(N, K, G, t) * split;
+      const double load = std::min<double>(PER_CU[t], std::max(1.0, (b1 + b2) / 256));
+      const int lo = (int)load, hi = std::min(lo + 1, PER_CU[t]);
+      const double stage = STAGE_US[t][lo - 1] + (load - lo) * (STAGE_US[t][hi - 1] - STAGE_US[t][lo - 1]);
+      const double t1 = nx * pairs * stage + BLOCK_US[t], t2 = (double)((nw + split - 1) / split) * pairs * stage + BLOCK_US[t];
+      const double us = std::max(std::max(t1, t2), (b1 * t1 + b2 * t2) / (256.0 * load)) + FIRST_US[t] + split_us(N, K, G, split);
+      if (us < best) {
+        best = us;
+        both = true;
+        dx = {t, 1, t1};
+        dw = {t, split, t2};
+      }
+    }
+  return both;
 }
 
 // few rows, or so little work that launches count
@@ -216,7 +249,7 @@ ForwardPlan plan_forward(const pigan_linear* a) {
   Carver cv;
   const int G = a->n_groups;
   const bool fp32 = a->dt == PIGAN_FP32;
-  p.mm = plan_mm(a->M, a->N, a->K, fp32 ? 6 : 1, G);
+  p.mm = plan_mm(STAGE_FWD, a->M, a->N, a->K, fp32 ? 6 : 1, G);
   if (fp32) {
     p.x.take(cv, G, a->M, a->K);
     p.w.take(cv, G, a->N, a->K);
@@ -231,6 +264,7 @@ struct BackwardPlan {
   Planes g, w, x;
   size_t part_dx = 0, part_dw = 0, part_db = 0, total = 0;
   int db_slots = 0;
+  bool both = false;   // dx and dw in one launch
 };
 
 constexpr int COLSUM_SPLITS = 64;
@@ -243,13 +277,15 @@ BackwardPlan plan_backward(const pigan_linear* a) {
   const bool fp32 = a->dt == PIGAN_FP32;
   const int pairs = fp32 ? 6 : 1;
   if (fp32 && (a->dx.p || a->dw)) p.g.take(cv, G, a->M, a->N);
+  // tiles and splits do not depend on which gradients are wanted: the same sums for each of them
+  p.dx = plan_mm(STAGE_BWD, a->M, a->K, a->N, pairs, G);
+  p.dw = plan_mm(STAGE_BWD, a->N, a->K, a->M, pairs, G);
+  p.both = plan_both(a->M, a->N, a->K, pairs, G, p.dx, p.dw) && a->dx.p && a->dw;
   if (a->dx.p) {
-    p.dx = plan_mm(a->M, a->K, a->N, pairs, G);
     if (fp32) p.w.take(cv, G, a->N, a->K);
     if (p.dx.n_split > 1) p.part_dx = cv.take((size_t)G * p.dx.n_split * a->M * a->K * 4);
   }
   if (a->dw) {
-    p.dw = plan_mm(a->N, a->K, a->M, pairs, G);
     if (fp32) p.x.take(cv, G, a->M, a->K);
     if (p.dw.n_split > 1) p.part_dw = cv.take((size_t)G * p.dw.n_split * a->N * a->K * 4);
     const int64_t side = std::min(mm_tile_side(p.dw.tile), 128);   // the smaller of the tiles that it may become
@@ -257,7 +293,7 @@ BackwardPlan plan_backward(const pigan_linear* a) {
   } else {
     p.db_slots = (int)std::min<int64_t>(a->M, COLSUM_SPLITS);
   }
-  if (a->db) p.part_db = cv.take((size_t)G * p.db_slots * a->N * 4);
+  if (a->db && (!a->dw || p.dw.n_split > 1)) p.part_db = cv.take((size_t)G * p.db_slots * a->N * 4);
   p.total = cv.off;
   return p;
 }
@@ -322,42 +358,53 @@ pigan_status run_forward(const pigan_linear* a, const ForwardPlan& p, char* ws, 
 // T: operands of the products; TO: storage type of the layer
 template <class T, class TO>
 pigan_status backward_products(const pigan_linear* a, const BackwardPlan& p, const MmOperand<T>& g,
-                               const MmOperand<T>& w, const MmOperand<T>& x, bool padded, char* ws, int& db_slots,
-                               hipStream_t st) {
+                               const MmOperand<T>& w, const MmOperand<T>& x, bool padded, char* ws, hipStream_t st) {
   const int G = a->n_groups;
   const double es = (double)esize(a->dt), MN = (double)a->M * a->N, MK = (double)a->M * a->K, NK = (double)a->N * a->K;
   // whole pieces of columns (the padded planes hold zeros behind theirs)
   const bool whole = (padded || a->N % 8 == 0) && a->K % 8 == 0;
+  const bool direct_dx = rows_aligned(g, G) && rows_aligned(w, G) && whole;
+  const bool direct_dw = rows_aligned(g, G) && rows_aligned(x, G) && whole;
+  const int pairs = padded ? 6 : 1;
+  MmArgs<T, TO> dx{g, w, a->N, pairs, {}, nullptr};
+  MmArgs<T, float> dw{g, x, a->M, pairs, {}, nullptr};
+  const int tile_dw = tile_for(p.dw, direct_dw), side = mm_tile_side(tile_dw);
+  const int slots = p.dw.n_split * (int)((a->K + side - 1) / side);
   if (a->dx.p) {
-    ProfScope prof(st, "linear_dx", 2.0 * G * MN * a->K, G * es * (MN + NK + MK * (1 + !!a->pre.p + !!a->add.p)));
-    MmOut<TO> o{};
-    o.I = a->M;
-    o.J = a->K;
-    o.act = a->act;
-    o.n_split = p.dx.n_split;
-    o.pre = (TO*)a->pre.p; o.ldp = a->pre.ld; o.gsp = a->pre.gs;
-    o.add = (const TO*)a->add.p; o.lda = a->add.ld; o.gsa = a->add.gs;
-    o.out = (TO*)a->dx.p; o.ldo = a->dx.ld; o.gso = a->dx.gs;
-    o.part = p.dx.n_split > 1 ? (float*)(ws + p.part_dx) : nullptr;
-    MmArgs<T, TO> m{g, w, a->N, padded ? 6 : 1, o, nullptr};
-    const bool direct = rows_aligned(g, G) && rows_aligned(w, G) && whole;
-    HIP_TRY(launch_mm_dx(m, tile_for(p.dx, direct), direct, G, st));
-    if (p.dx.n_split > 1) HIP_TRY(launch_mm_join_dx(o, G, st));
+    dx.o.I = a->M;
+    dx.o.J = a->K;
+    dx.o.act = a->act;
+    dx.o.n_split = p.dx.n_split;
+    dx.o.pre = (TO*)a->pre.p; dx.o.ldp = a->pre.ld; dx.o.gsp = a->pre.gs;
+    dx.o.add = (const TO*)a->add.p; dx.o.lda = a->add.ld; dx.o.gsa = a->add.gs;
+    dx.o.out = (TO*)a->dx.p; dx.o.ldo = a->dx.ld; dx.o.gso = a->dx.gs;
+    dx.o.part = p.dx.n_split > 1 ? (float*)(ws + p.part_dx) : nullptr;
   }
   if (a->dw) {
-    ProfScope prof(st, "linear_dw", 2.0 * G * MN * a->K, G * (es * (MN + MK) + 4.0 * NK));
-    MmOut<float> o{};
-    o.I = a->N;
-    o.J = a->K;
-    o.n_split = p.dw.n_split;
-    o.out = a->dw; o.ldo = a->K; o.gso = a->N * a->K;
-    o.part = p.dw.n_split > 1 ? (float*)(ws + p.part_dw) : nullptr;
-    MmArgs<T, float> m{g, x, a->M, padded ? 6 : 1, o, a->db ? (float*)(ws + p.part_db) : nullptr};
-    const bool direct = rows_aligned(g, G) && rows_aligned(x, G) && whole;
-    const int tile = tile_for(p.dw, direct), side = mm_tile_side(tile);
-    db_slots = p.dw.n_split * (int)((a->K + side - 1) / side);
-    HIP_TRY(launch_mm_dw(m, tile, direct, G, st));
-    if (p.dw.n_split > 1) HIP_TRY(launch_mm_join_dw(o, G, st));
+    dw.o.I = a->N;
+    dw.o.J = a->K;
+    dw.o.n_split = p.dw.n_split;
+    dw.o.out = a->dw; dw.o.ldo = a->K; dw.o.gso = a->N * a->K;
+    dw.o.part = p.dw.n_split > 1 ? (float*)(ws + p.part_dw) : nullptr;
+    dw.part_db = !a->db ? nullptr : p.dw.n_split == 1 ? a->db : (float*)(ws + p.part_db);
+  }
+  const double fl = 2.0 * G * MN * a->K, bx = G * es * (MN + NK + MK * (1 + !!a->pre.p + !!a->add.p));
+  const double bw = G * (es * (MN + MK) + 4.0 * NK);
+  if (p.both && direct_dx && direct_dw) {
+    ProfScope prof(st, "linear_bwd", 2 * fl, bx + bw);
+    HIP_TRY(launch_mm_both(dx, dw, p.dx.tile, p.dw.us > p.dx.us, G, st));
+    if (p.dw.n_split > 1) HIP_TRY(launch_mm_join_dw(dw.o, dw.part_db, slots, a->db, G, st));
+    return PIGAN_OK;
+  }
+  if (a->dx.p) {
+    ProfScope prof(st, "linear_dx", fl, bx);
+    HIP_TRY(launch_mm_dx(dx, tile_for(p.dx, direct_dx), direct_dx, G, st));
+    if (p.dx.n_split > 1) HIP_TRY(launch_mm_join_dx(dx.o, G, st));
+  }
+  if (a->dw) {
+    ProfScope prof(st, "linear_dw", fl, bw);
+    HIP_TRY(launch_mm_dw(dw, tile_dw, direct_dw, G, st));
+    if (p.dw.n_split > 1) HIP_TRY(launch_mm_join_dw(dw.o, dw.part_db, slots, a->db, G, st));
   }
   return PIGAN_OK;
 }
@@ -369,7 +416,6 @@ pigan_status run_backward(const pigan_linear* a, const BackwardPlan& p, char* ws
     if (a->db) HIP_TRY(launch_slot_sum(nullptr, 0, 0, a->N, a->db, a->N, nullptr, G, st));
     return PIGAN_OK;
   }
-  int db_slots = p.db_slots;
   if (a->dx.p || a->dw) {
     pigan_status s;
     if (a->dt == PIGAN_FP32) {
@@ -379,27 +425,22 @@ pigan_status run_backward(const pigan_linear* a, const BackwardPlan& p, char* ws
       if (a->dx.p) sets[n++] = p.w.set(ws, a->w, a->K);
       if (a->dw) sets[n++] = p.x.set(ws, a->x, a->K);
       HIP_TRY(launch_split3(sets, n, G, st));
-      s = backward_products<bf16, float>(a, p, p.g.operand(ws, G), p.w.operand(ws, G), p.x.operand(ws, G), true, ws,
-                                         db_slots, st);
+      s = backward_products<bf16, float>(a, p, p.g.operand(ws, G), p.w.operand(ws, G), p.x.operand(ws, G), true, ws, st);
     } else {
       s = a->dt == PIGAN_BF16
-              ? backward_products<bf16, bf16>(a, p, operand<bf16>(a->g), operand<bf16>(a->w), operand<bf16>(a->x), false, ws,
-                                             db_slots, st)
-              : backward_products<f16, f16>(a, p, operand<f16>(a->g), operand<f16>(a->w), operand<f16>(a->x), false, ws, db_slots,
-                                           st);
+              ? backward_products<bf16, bf16>(a, p, operand<bf16>(a->g), operand<bf16>(a->w), operand<bf16>(a->x), false, ws, st)
+              : backward_products<f16, f16>(a, p, operand<f16>(a->g), operand<f16>(a->w), operand<f16>(a->x), false, ws, st);
     }
     if (s != PIGAN_OK) return s;
   }
-  if (a->db) {
+  if (a->db && !a->dw) {   // by themselves
     float* part = (float*)(ws + p.part_db);
-    if (!a->dw) {
-      pigan_status s = by_dtype(a->dt, [&](auto t) -> pigan_status {
-        HIP_TRY(launch_colsum_rows(in<decltype(t)>(a->g), a->M, a->N, db_slots, part, G, st));
-        return PIGAN_OK;
-      });
-      if (s != PIGAN_OK) return s;
-    }
-    HIP_TRY(launch_slot_sum(part, (int64_t)db_slots * a->N, db_slots, a->N, a->db, a->N, nullptr, G, st));
+    pigan_status s = by_dtype(a->dt, [&](auto t) -> pigan_status {
+      HIP_TRY(launch_colsum_rows(in<decltype(t)>(a->g), a->M, a->N, p.db_slots, part, G, st));
+      return PIGAN_OK;
+    });
+    if (s != PIGAN_OK) return s;
+    HIP_TRY(launch_slot_sum(part, (int64_t)p.db_slots * a->N, p.db_slots, a->N, a->db, a->N, nullptr, G, st));
   }
   return PIGAN_OK;
 }

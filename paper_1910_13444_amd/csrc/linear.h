@@ -33,7 +33,7 @@ template <class T, class TO> struct MmArgs {
   int64_t K;
   int32_t pairs;            // 1; 6: three bf16 planes per operand (fp32 products)
   MmOut<TO> o;
-  float* part_db;           // dw: sums of A over k, [G][n_split * column tiles][I], or null
+  float* part_db;           // dw: sums of A over k, [G][I], with splits [G][n_split * column tiles][I]; or null
 };
 
 enum MmTile { MM_64 = 0, MM_128 = 1, MM_256 = 2 };
@@ -49,10 +49,16 @@ hipError_t launch_mm_dx(const MmArgs<T, TO>& a, int tile, bool direct, int G, hi
 template <class T>
 hipError_t launch_mm_dw(const MmArgs<T, float>& a, int tile, bool direct, int G, hipStream_t st);
 
+// dx and dw of aligned operands in one launch (tiles of 64 and 128)
+template <class T, class TO>
+hipError_t launch_mm_both(const MmArgs<T, TO>& dx, const MmArgs<T, float>& dw, int tile, bool dw_first, int G,
+                          hipStream_t st);
+
 // sums the partials of split products in order and applies the epilogue
 template <class TO> hipError_t launch_mm_join_fwd(const MmOut<TO>& o, int G, hipStream_t st);
 template <class TO> hipError_t launch_mm_join_dx(const MmOut<TO>& o, int G, hipStream_t st);
-hipError_t launch_mm_join_dw(const MmOut<float>& o, int G, hipStream_t st);
+// (and of db, where it is wanted: [G][slots][I])
+hipError_t launch_mm_join_dw(const MmOut<float>& o, const float* part_db, int slots, float* db, int G, hipStream_t st);
 
 // forward on few rows or few outputs, no LDS stages
 template <class T> hipError_t launch_short_fwd(const MmArgs<T, T>& a, int G, hipStream_t st);

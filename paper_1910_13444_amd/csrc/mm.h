@@ -204,6 +204,15 @@ __device__ __forceinline__ MmTilePos mm_tile(uint32_t n, uint32_t rows, uint32_t
   return t;
 }
 
+// a block's sum of column i0 + n of A (n < 0: none): db itself, or a slot of the split
+template <class T, class TO>
+__device__ __forceinline__ void mm_store_db(const MmArgs<T, TO>& p, int g, int split, int tj, int tiles, int64_t i0,
+                                            int n, float sum) {
+  if (n < 0 || i0 + n >= p.o.I) return;
+  if (p.o.n_split > 1) p.part_db[(((int64_t)g * p.o.n_split + split) * tiles + tj) * p.o.I + i0 + n] = sum;
+  else if (tj == 0) p.part_db[g * p.o.I + i0 + n] = sum;
+}
+
 // ---------------------------------------------------------------------------
 // Operands of any alignment: stages pass through registers, one ahead of the
 // products, with zeros past the end of k.  Rows of a tile past the end of the
@@ -284,12 +293,10 @@ k_mm_any(const MmArgs<T, TO> p) {
     const u32x2 lo = lds_read_tr<T>(q), hi = lds_read_tr<T>(q + 4 * pitch);
     return __builtin_bit_cast(frag, (u32x4{lo.x, lo.y, hi.x, hi.y}));
   };
-  // dw: the sums of A over k go by the blocks of a row of tiles in turn, the
-  // chunks of a stage by the waves of a column in turn; the first three plane
-  // pairs hold every plane of A once
-  const int db_tiles = (int)tj, db_turn = (int)(j0 / BN);
+  // db: as in the aligned kernel
   auto products = [&](const char* stage, int st) __attribute__((always_inline)) {
-    const bool sum_a = KIND == MM_DW && p.part_db && st < 3 * per_pair && st % db_tiles == db_turn;
+    const bool sum_a = KIND == MM_DW && p.part_db && st < 3 * per_pair &&
+                       (p.o.n_split == 1 ? at.tj == 0 : (uint32_t)st % tj == (uint32_t)at.tj);
 #pragma unroll
     for (int c = 0; c < BK / 16; ++c) {
       frag fa[MT], fb[NT];
@@ -341,8 +348,7 @@ k_mm_any(const MmArgs<T, TO> p) {
         if (lane < 32) sums[wn * BM + 32 * (MT * wm + a) + lane] = s;
       }
       lds_sync();
-      if (tid < BM && i0 + tid < p.o.I)
-        p.part_db[(((int64_t)g * p.o.n_split + split) * tj + j0 / BN) * p.o.I + i0 + tid] = sums[tid] + sums[BM + tid];
+      mm_store_db(p, g, split, at.tj, (int)tj, i0, tid < BM ? tid : -1, sums[tid % BM] + sums[BM + tid % BM]);
     }
   }
 }
@@ -382,23 +388,24 @@ __device__ __forceinline__ void lds_load(const u32x4& buffer, char* lds, uint32_
                ::"s"(to), "v"(lane_off), "s"(buffer), "s"(off));
 }
 
-template <class T, class TO, int KIND, int MT, int NT, int OCC>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
-k_mm_piped(const MmArgs<T, TO> p) {
-  constexpr int BM = 64 * MT, BN = 64 * NT, BK = 64, STAGE_A = BM * BK * 2, STAGE = STAGE_A + BN * BK * 2;
+// bytes of a stage
+template <int MT, int NT> constexpr int mm_stage() { return (64 * MT + 64 * NT) * 64 * 2; }
+
+// block n of `blocks` of the product, with two stages of LDS
+template <class T, class TO, int KIND, int MT, int NT>
+__device__ __forceinline__ void mm_piped(const MmArgs<T, TO>& p, uint32_t n, uint32_t blocks, char* s0, char* s1) {
+  constexpr int BM = 64 * MT, BN = 64 * NT, BK = 64, STAGE_A = BM * BK * 2;
   constexpr bool AK = KIND != MM_DW, BKC = KIND == MM_FWD;
   constexpr int GA = BM / 32, GB = BN / 32;   // 1 KB groups per wave and stage
   static_assert(GA == GB, "one group of each operand at a time");
   typedef typename Elem<T>::frag frag;
-  __shared__ __attribute__((aligned(1024))) char s0[STAGE];
-  __shared__ __attribute__((aligned(1024))) char s1[STAGE];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave & 1, wn = wave >> 1;
 
   const uint32_t rows = (uint32_t)((p.o.I + BM - 1) / BM), tj = (uint32_t)((p.o.J + BN - 1) / BN);
-  const MmTilePos at = mm_tile((uint32_t)xcd_remap(blockIdx.x, gridDim.x), rows, tj, p.o.n_split);
+  const MmTilePos at = mm_tile((uint32_t)xcd_remap(n, blocks), rows, tj, p.o.n_split);
   const int64_t i0 = (int64_t)at.ti * BM, j0 = (int64_t)at.tj * BN;
   const uint32_t nk = (uint32_t)((p.K + BK - 1) / BK);
   const int k_lo = (int)((uint64_t)nk * at.split / (uint32_t)p.o.n_split);
@@ -491,11 +498,13 @@ k_mm_piped(const MmArgs<T, TO> p) {
     if (n < MT) fa[into][n] = frag_at(stage, 0, AK, BM, c, MT * wm + n);
     if (n < NT) fb[into][n] = frag_at(stage, STAGE_A, BKC, BN, c, NT * wn + n);
   };
-  // db: the blocks of a row of tiles take the stages in turn, the waves of a
-  // column the chunks; the first three plane pairs hold every plane of A once
+  // db: the first block of a row of tiles sums (with splits, which are joined
+  // anyway, all blocks of the row take the stages in turn), the waves of a column
+  // take the chunks in turn; the first three plane pairs hold every plane of A once
   auto sum_a = [&](int from, int c, uint32_t st) __attribute__((always_inline)) {
     if constexpr (KIND == MM_DW) {
-      if (p.part_db && (c & 1) == wn && st < (uint32_t)(3 * per_pair) && st % tj == (uint32_t)at.tj) {
+      if (p.part_db && (c & 1) == wn && st < (uint32_t)(3 * per_pair) &&
+          (p.o.n_split == 1 ? at.tj == 0 : st % tj == (uint32_t)at.tj)) {
 #pragma unroll
         for (int a = 0; a < MT; ++a)
 #pragma unroll
@@ -557,20 +566,41 @@ k_mm_piped(const MmArgs<T, TO> p) {
         if (lane < 32) sums[wn * BM + 32 * (MT * wm + a) + lane] = s;
       }
       lds_sync();
-      if (tid < BM && i0 + tid < p.o.I)
-        p.part_db[(((int64_t)at.g * p.o.n_split + at.split) * tj + at.tj) * p.o.I + i0 + tid] = sums[tid] + sums[BM + tid];
+      mm_store_db(p, at.g, at.split, at.tj, (int)tj, i0, tid < BM ? tid : -1, sums[tid % BM] + sums[BM + tid % BM]);
     }
   }
+}
+
+template <class T, class TO, int KIND, int MT, int NT, int OCC>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
+k_mm_piped(const MmArgs<T, TO> p) {
+  __shared__ __attribute__((aligned(1024))) char s0[mm_stage<MT, NT>()];
+  __shared__ __attribute__((aligned(1024))) char s1[mm_stage<MT, NT>()];
+  mm_piped<T, TO, KIND, MT, NT>(p, blockIdx.x, gridDim.x, s0, s1);
 }
 
 // ---------------------------------------------------------------------------
 // sums of split products
 // ---------------------------------------------------------------------------
+// the last db_blocks blocks (dw) add the slots of db: [G][slots][I]
 template <int KIND, class TO>
-__global__ void __launch_bounds__(256) k_mm_join(const MmOut<TO> o) {
+__global__ void __launch_bounds__(256) k_mm_join(const MmOut<TO> o, const float* __restrict__ part_db, int slots,
+                                                 float* __restrict__ db, int db_blocks) {
   const int g = blockIdx.z;
+  const unsigned blocks = gridDim.x - db_blocks;
+  if constexpr (KIND == MM_DW) {
+    if (blockIdx.x >= blocks) {
+      const int64_t i = (int64_t)(blockIdx.x - blocks) * 256 + threadIdx.x;
+      if (i >= o.I) return;
+      double s = 0.0;
+#pragma unroll 8
+      for (int n = 0; n < slots; ++n) s += (double)part_db[((int64_t)g * slots + n) * o.I + i];
+      db[g * o.I + i] = (float)s;
+      return;
+    }
+  }
   const int64_t vpr = (o.J + 7) / 8, total = o.I * vpr;
-  for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < total; q += (int64_t)gridDim.x * 256) {
+  for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < total; q += (int64_t)blocks * 256) {
     const int64_t i = q / vpr, j = (q - i * vpr) * 8;
     float v[8], bias[8];
     double s[8];
@@ -590,25 +620,34 @@ __global__ void __launch_bounds__(256) k_mm_join(const MmOut<TO> o) {
 }
 
 template <int KIND, class TO>
-hipError_t join_launch(const MmOut<TO>& o, int G, hipStream_t st) {
-  const int64_t blocks = (o.I * ((o.J + 7) / 8) + 255) / 256;
-  k_mm_join<KIND, TO><<<dim3((unsigned)(blocks < 8192 ? blocks : 8192), 1, G), 256, 0, st>>>(o);
+hipError_t join_launch(const MmOut<TO>& o, int G, hipStream_t st, const float* part_db = nullptr, int slots = 0,
+                       float* db = nullptr) {
+  const int64_t blocks = (o.I * ((o.J + 7) / 8) + 255) / 256, more = db ? (o.I + 255) / 256 : 0;
+  k_mm_join<KIND, TO><<<dim3((unsigned)((blocks < 8192 ? blocks : 8192) + more), 1, G), 256, 0, st>>>(o, part_db, slots, db,
+                                                                                                      (int)more);
   return hipGetLastError();
 }
 
 // ---------------------------------------------------------------------------
 // launch of a tile
 // ---------------------------------------------------------------------------
+// blocks of a product, 0 where the kernels do not take it
 template <class T, class TO, int KIND>
-hipError_t mm_launch(const MmArgs<T, TO>& a, int tile, bool direct, int G, hipStream_t st) {
+uint32_t mm_blocks(const MmArgs<T, TO>& a, int tile, bool direct, int G) {
   const int64_t side = mm_tile_side(tile);
   const int64_t rows = (a.o.I + side - 1) / side, cols = (a.o.J + side - 1) / side;
   if (a.o.I < 1 || a.o.J < 1 || a.K < 1 || a.o.n_split < 1 || G < 1 || G > 65535 ||
-      (double)rows * cols * a.o.n_split * G > 2e9 || a.o.n_split > (a.K + 63) / 64 || (a.o.n_split > 1 && !a.o.part) ||
+      (double)rows * cols * a.o.n_split * G > 1e9 || a.o.n_split > (a.K + 63) / 64 || (a.o.n_split > 1 && !a.o.part) ||
       (a.pairs != 1 && a.pairs != 6) || a.K > 0x7fffffff || (!direct && tile == MM_256) ||
       (direct && (a.o.J % 8 || (KIND != MM_DW && a.pairs == 1 && a.K % 8))))
-    return hipErrorInvalidValue;
-  const uint32_t count = (uint32_t)(rows * cols * a.o.n_split * G);
+    return 0;
+  return (uint32_t)(rows * cols * a.o.n_split * G);
+}
+
+template <class T, class TO, int KIND>
+hipError_t mm_launch(const MmArgs<T, TO>& a, int tile, bool direct, int G, hipStream_t st) {
+  const uint32_t count = mm_blocks<T, TO, KIND>(a, tile, direct, G);
+  if (!count) return hipErrorInvalidValue;
   if (direct) {
     if (tile == MM_256) k_mm_piped<T, TO, KIND, 4, 4, 1><<<count, 256, 0, st>>>(a);
     else if (tile == MM_128) k_mm_piped<T, TO, KIND, 2, 2, 2><<<count, 256, 0, st>>>(a);
