@@ -177,6 +177,10 @@ MmPlan plan_mm(const double (&STAGE_US)[3][4], int64_t I, int64_t J, int64_t K, 
       if (us < best.us) best = {t, split, us};
     }
   }
+  // 64 tiles of four groups, one on a CU: a stage of each group in the time of four blocks' stages
+  const double us = ceil(tiles_of(I, J, G, MM_64) / 256) * ((double)((nk + 3) / 4) * pairs * STAGE_US[MM_64][3] + 4.0) +
+                    FIRST_US[MM_64];
+  if (nk >= 8 && us < best.us) best = {MM_64K, 1, us};
   return best;
 }
 
@@ -317,8 +321,10 @@ template <class TO> MmOut<TO> forward_out(const pigan_linear* a, const MmPlan& m
 
 template <class T> MmOperand<T> operand(const pigan_mat& m) { return {(const T*)m.p, m.ld, m.gs, 0}; }
 
-// the largest tile is there for aligned operands only
-int tile_for(const MmPlan& mm, bool direct) { return !direct && mm.tile == MM_256 ? (int)MM_128 : mm.tile; }
+// the largest tile and the shared one are there for aligned operands only
+int tile_for(const MmPlan& mm, bool direct) {
+  return direct ? mm.tile : mm.tile == MM_256 ? (int)MM_128 : mm.tile == MM_64K ? (int)MM_64 : mm.tile;
+}
 
 template <class T, class TO>
 pigan_status forward_tiles(const MmArgs<T, TO>& m, const MmPlan& mm, int G, hipStream_t st) {

@@ -36,8 +36,9 @@ template <class T, class TO> struct MmArgs {
   float* part_db;           // dw: sums of A over k, [G][I], with splits [G][n_split * column tiles][I]; or null
 };
 
-enum MmTile { MM_64 = 0, MM_128 = 1, MM_256 = 2 };
-inline int mm_tile_side(int t) { return t == MM_64 ? 64 : t == MM_128 ? 128 : 256; }
+// MM_64K: 64 with the contraction shared by four groups of waves
+enum MmTile { MM_64 = 0, MM_128 = 1, MM_256 = 2, MM_64K = 3 };
+inline int mm_tile_side(int t) { return t == MM_128 ? 128 : t == MM_256 ? 256 : 64; }
 
 // direct: both operands may go straight to LDS: 16-byte aligned rows (a tile's
 // extent below 2^31 bytes) of whole pieces, along the row and in the result's

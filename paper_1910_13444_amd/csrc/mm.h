@@ -363,7 +363,8 @@ k_mm_any(const MmArgs<T, TO> p) {
 //              moves 0.75 of what the matrix cores take in the same time
 //   128 x 128  two blocks per CU, which fill each other's waits and epilogues;
 //              LDS bound (1.5 of the matrix cores' time)
-//   64 x 64    four blocks per CU, for few tiles
+//   64 x 64    four blocks per CU, for few tiles; for very few, one block of four
+//              groups that share the contraction
 // The loads are buffer loads: what is past the end of the matrix is out of the
 // buffer's range and arrives as zeros.
 // ---------------------------------------------------------------------------
@@ -391,25 +392,41 @@ __device__ __forceinline__ void lds_load(const u32x4& buffer, char* lds, uint32_
 // bytes of a stage
 template <int MT, int NT> constexpr int mm_stage() { return (64 * MT + 64 * NT) * 64 * 2; }
 
-// block n of `blocks` of the product, with two stages of LDS
-template <class T, class TO, int KIND, int MT, int NT>
+// Block n of `blocks` of the product, with two stages of LDS for each of KG groups
+// of four waves: the groups share the contraction of the tile and meet in LDS, in
+// order, before the epilogue.
+template <class T, class TO, int KIND, int MT, int NT, int KG = 1>
 __device__ __forceinline__ void mm_piped(const MmArgs<T, TO>& p, uint32_t n, uint32_t blocks, char* s0, char* s1) {
+  static_assert(KG == 1 || MT * NT == 1, "groups: tiles of one fragment a wave");
   constexpr int BM = 64 * MT, BN = 64 * NT, BK = 64, STAGE_A = BM * BK * 2;
   constexpr bool AK = KIND != MM_DW, BKC = KIND == MM_FWD;
   constexpr int GA = BM / 32, GB = BN / 32;   // 1 KB groups per wave and stage
   static_assert(GA == GB, "one group of each operand at a time");
   typedef typename Elem<T>::frag frag;
 
-  const int tid = threadIdx.x, lane = tid & 63;
+  const int tid = threadIdx.x & 255, lane = tid & 63;
+  const int kg = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 8);
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave & 1, wn = wave >> 1;
+  if constexpr (KG > 1) {
+    s0 += kg * mm_stage<MT, NT>();
+    s1 += kg * mm_stage<MT, NT>();
+  }
 
   const uint32_t rows = (uint32_t)((p.o.I + BM - 1) / BM), tj = (uint32_t)((p.o.J + BN - 1) / BN);
   const MmTilePos at = mm_tile((uint32_t)xcd_remap(n, blocks), rows, tj, p.o.n_split);
   const int64_t i0 = (int64_t)at.ti * BM, j0 = (int64_t)at.tj * BN;
   const uint32_t nk = (uint32_t)((p.K + BK - 1) / BK);
-  const int k_lo = (int)((uint64_t)nk * at.split / (uint32_t)p.o.n_split);
-  const int per_pair = (int)((uint64_t)nk * (at.split + 1) / (uint32_t)p.o.n_split) - k_lo;
+  int k_lo = (int)((uint64_t)nk * at.split / (uint32_t)p.o.n_split);
+  int per_pair = (int)((uint64_t)nk * (at.split + 1) / (uint32_t)p.o.n_split) - k_lo;
+  int turns = per_pair * p.pairs;
+  if constexpr (KG > 1) {
+    // this group's part; all of them take the turns of the longest one
+    const int all = per_pair, lo = all * kg / KG;
+    per_pair = all * (kg + 1) / KG - lo;
+    k_lo += lo;
+    turns = (all + KG - 1) / KG * p.pairs;
+  }
   const int stages = per_pair * p.pairs;
 
   f32x16 acc[MT][NT];
@@ -550,12 +567,30 @@ __device__ __forceinline__ void mm_piped(const MmArgs<T, TO>& p, uint32_t n, uin
   stage_sync<2 * GA>();
 #pragma unroll
   for (int q = 0; q < (MT > NT ? MT : NT); ++q) read1(0, s0, 0, q);
-  for (int st = 0; st < stages; st += 2) {
+  for (int st = 0; st < turns; st += 2) {
     turn(st, s0, s1);
-    if (st + 1 < stages) turn(st + 1, s1, s0);
+    if (st + 1 < turns) turn(st + 1, s1, s0);
   }
   stage_sync<0>();   // no load in flight when LDS is used again or given up
 
+  if constexpr (KG > 1) {
+    // a group's sums: [wave][16][64] in its first stage, those of A in its second
+    float* mine = (float*)s0;
+    if (kg > 0) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mine[(wave * 16 + r) * 64 + lane] = acc[0][0][r];
+      if constexpr (KIND == MM_DW) ((float*)s1)[tid] = db[0];
+    }
+    lds_sync();
+    if (kg > 0) return;
+#pragma unroll
+    for (int q = 1; q < KG; ++q) {
+      const float* from = (const float*)(s0 + q * mm_stage<MT, NT>());
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[0][0][r] += from[(wave * 16 + r) * 64 + lane];
+      if constexpr (KIND == MM_DW) db[0] += ((const float*)(s1 + q * mm_stage<MT, NT>()))[tid];
+    }
+  }
   mm_results<KIND, true>(p.o, at.g, at.split, i0 + 32 * MT * wm, j0 + 32 * NT * wn, acc);
   if constexpr (KIND == MM_DW) {
     if (p.part_db) {
@@ -571,12 +606,12 @@ __device__ __forceinline__ void mm_piped(const MmArgs<T, TO>& p, uint32_t n, uin
   }
 }
 
-template <class T, class TO, int KIND, int MT, int NT, int OCC>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
+template <class T, class TO, int KIND, int MT, int NT, int OCC, int KG = 1>
+__global__ void __launch_bounds__(256 * KG) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
 k_mm_piped(const MmArgs<T, TO> p) {
-  __shared__ __attribute__((aligned(1024))) char s0[mm_stage<MT, NT>()];
-  __shared__ __attribute__((aligned(1024))) char s1[mm_stage<MT, NT>()];
-  mm_piped<T, TO, KIND, MT, NT>(p, blockIdx.x, gridDim.x, s0, s1);
+  __shared__ __attribute__((aligned(1024))) char s0[KG * mm_stage<MT, NT>()];
+  __shared__ __attribute__((aligned(1024))) char s1[KG * mm_stage<MT, NT>()];
+  mm_piped<T, TO, KIND, MT, NT, KG>(p, blockIdx.x, gridDim.x, s0, s1);
 }
 
 // ---------------------------------------------------------------------------
@@ -651,7 +686,8 @@ hipError_t mm_launch(const MmArgs<T, TO>& a, int tile, bool direct, int G, hipSt
   if (direct) {
     if (tile == MM_256) k_mm_piped<T, TO, KIND, 4, 4, 1><<<count, 256, 0, st>>>(a);
     else if (tile == MM_128) k_mm_piped<T, TO, KIND, 2, 2, 2><<<count, 256, 0, st>>>(a);
-    else k_mm_piped<T, TO, KIND, 1, 1, 4><<<count, 256, 0, st>>>(a);
+    else if (tile == MM_64) k_mm_piped<T, TO, KIND, 1, 1, 4><<<count, 256, 0, st>>>(a);
+    else k_mm_piped<T, TO, KIND, 1, 1, 4, 4><<<count, 1024, 0, st>>>(a);
   } else {
     if (tile == MM_128) k_mm_any<T, TO, KIND, 2, 2><<<count, 256, 0, st>>>(a);
     else k_mm_any<T, TO, KIND, 1, 1><<<count, 256, 0, st>>>(a);
