@@ -62,20 +62,11 @@ template <class TO> struct Octet {
   }
 };
 
-// what the epilogue of eight columns j.. of row i reads (i < I, j < J)
-template <int KIND, int ACT, class TO> struct EpiIn {
-  Octet<TO> pre, add;
-  __device__ __forceinline__ void load(const MmOut<TO>& o, int g, int64_t i, int64_t j, int64_t valid) {
-    if constexpr (KIND == MM_DX && ACT != PIGAN_ACT_NONE) pre.load(o.pre + g * o.gsp + i * o.ldp + j, valid);
-    if constexpr (KIND != MM_DW)
-      if (o.add) add.load(o.add + g * o.gsa + i * o.lda + j, valid);
-  }
-};
-
-// the epilogue itself; `bias` holds the columns' biases
+// The epilogue of eight columns j.. of row i (i < I, j < J): `bias` holds the
+// columns' biases, `pre` and `add` what it reads of those matrices.
 template <int KIND, int ACT, class TO>
 __device__ __forceinline__ void mm_epilogue(const MmOut<TO>& o, int g, int64_t i, int64_t j, int64_t valid,
-                                            const EpiIn<KIND, ACT, TO>& in, const float* bias, float* v) {
+                                            const Octet<TO>& pre, const Octet<TO>& add, const float* bias, float* v) {
   if constexpr (KIND == MM_FWD) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] += bias[e];
@@ -84,14 +75,14 @@ __device__ __forceinline__ void mm_epilogue(const MmOut<TO>& o, int g, int64_t i
     for (int e = 0; e < 8; ++e) v[e] = act_value<ACT>(v[e]);
   } else if constexpr (KIND == MM_DX && ACT != PIGAN_ACT_NONE) {
     float a[8];
-    in.pre.floats(a);
+    pre.floats(a);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] *= act_slope<ACT>(a[e]);
   }
   if constexpr (KIND != MM_DW)
     if (o.add) {
       float r[8];
-      in.add.floats(r);
+      add.floats(r);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] += r[e];
     }
@@ -101,35 +92,58 @@ __device__ __forceinline__ void mm_epilogue(const MmOut<TO>& o, int g, int64_t i
 // A wave's MT x NT fragments, from rows i0 and columns j0 on, to memory: as
 // partial sums or through the epilogue (one branch on the activation for all of
 // them: the accumulators stay in registers only if every loop unrolls).  What the
-// epilogue reads is requested a column of fragments ahead: asked for one by one,
-// each of 32 reads was waited for by itself (30 us of the 60 that a 256 x 256 tile
-// took at K = 1024).  WHOLE: the columns come in whole eights.
+// epilogue reads is requested columns of fragments ahead, as many as the registers
+// hold beside the accumulators (DP of pre, DA of add): asked for one by one, each
+// of 32 reads was waited for by itself, 30 us of the 60 that a 256 x 256 tile took
+// at K = 1024.  WHOLE: the columns come in whole eights.
 template <int KIND, int ACT, bool PART, bool WHOLE, class TO, int MT, int NT>
 __device__ __forceinline__ void mm_store(const MmOut<TO>& o, int g, int split, int64_t i0, int64_t j0,
                                          const f32x16 (&acc)[MT][NT]) {
   const int lane = threadIdx.x & 63;
-  // (a column ahead where the registers hold two columns' operands)
-  constexpr int AHEAD = WHOLE && (MT <= 2 || (KIND == MM_FWD && sizeof(TO) == 2)) ? 1 : 0;
-  EpiIn<KIND, ACT, TO> in[1 + AHEAD][MT][2];
-  auto request = [&](int b) __attribute__((always_inline)) {
+  constexpr bool PRE = !PART && KIND == MM_DX && ACT != PIGAN_ACT_NONE, ADD = !PART && KIND != MM_DW;
+  constexpr bool HALF = sizeof(TO) == 2;
+  constexpr int DP = !PRE || !WHOLE ? 1 : MT <= 2 ? NT : HALF ? 2 : 1;
+  constexpr int DA = !ADD || !WHOLE ? 1 : MT <= 2 ? NT : !HALF || PRE ? 1 : NT;
+  Octet<TO> pre[DP][MT][2], add[DA][MT][2];
+  auto each = [&](int b, auto f) __attribute__((always_inline)) {
     const int64_t j = j0 + 32 * b + mm_col(lane);
 #pragma unroll
     for (int a = 0; a < MT; ++a)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int64_t i = i0 + 32 * a + 16 * h + (lane & 15);
-        if (i < o.I && j < o.J) in[b & AHEAD][a][h].load(o, g, i, j, WHOLE ? 8 : o.J - j);
+        if (i < o.I && j < o.J) f(a, h, i, j, WHOLE ? (int64_t)8 : o.J - j);
       }
   };
-  if constexpr (!PART && AHEAD) request(0);
+  auto request_pre = [&](int b) __attribute__((always_inline)) {
+    each(b, [&](int a, int h, int64_t i, int64_t j, int64_t valid) __attribute__((always_inline)) {
+      pre[b % DP][a][h].load(o.pre + g * o.gsp + i * o.ldp + j, valid);
+    });
+  };
+  auto request_add = [&](int b) __attribute__((always_inline)) {
+    if (o.add)
+      each(b, [&](int a, int h, int64_t i, int64_t j, int64_t valid) __attribute__((always_inline)) {
+        add[b % DA][a][h].load(o.add + g * o.gsa + i * o.lda + j, valid);
+      });
+  };
+  // columns up to b + D - 1 are on their way when column b begins
+#pragma unroll
+  for (int b = 0; b < NT; ++b) {
+    if constexpr (PRE)
+      if (b < DP - 1) request_pre(b);
+    if constexpr (ADD)
+      if (b < DA - 1) request_add(b);
+  }
 #pragma unroll
   for (int b = 0; b < NT; ++b) {
     const int64_t j = j0 + 32 * b + mm_col(lane);
+    if constexpr (PRE)
+      if (b + DP - 1 < NT) request_pre(b + DP - 1);
+    if constexpr (ADD)
+      if (b + DA - 1 < NT) request_add(b + DA - 1);
     float bias[8];
     if constexpr (KIND == MM_FWD && !PART)
       vec_load<8>(o.bias && (!WHOLE || j < o.J) ? o.bias + g * o.J : nullptr, j, WHOLE ? j + 8 : o.J, 0.0f, bias);
-    if constexpr (!PART)
-      if (b + AHEAD < NT) request(b + AHEAD);
 #pragma unroll
     for (int a = 0; a < MT; ++a) {
       float v[16];
@@ -142,7 +156,7 @@ __device__ __forceinline__ void mm_store(const MmOut<TO>& o, int g, int split, i
         if (i < o.I && j < o.J) {
           const int64_t valid = WHOLE ? 8 : o.J - j;
           if constexpr (PART) store8(o.part + (((int64_t)g * o.n_split + split) * o.I + i) * o.J + j, valid, v + 8 * h);
-          else mm_epilogue<KIND, ACT>(o, g, i, j, valid, in[b & AHEAD][a][h], bias, v + 8 * h);
+          else mm_epilogue<KIND, ACT>(o, g, i, j, valid, pre[b % DP][a][h], add[b % DA][a][h], bias, v + 8 * h);
         }
       }
     }
@@ -166,9 +180,11 @@ template <int KIND, class TO>
 __device__ __forceinline__ void mm_finish(const MmOut<TO>& o, int g, int64_t i, int64_t j, int64_t valid,
                                           const float* bias, float* v) {
   PIGAN_ACT_SWITCH(KIND == MM_DW ? PIGAN_ACT_NONE : o.act, {
-    EpiIn<KIND, ACT, TO> in;
-    in.load(o, g, i, j, valid);
-    mm_epilogue<KIND, ACT>(o, g, i, j, valid, in, bias, v);
+    Octet<TO> pre, add;
+    if constexpr (KIND == MM_DX && ACT != PIGAN_ACT_NONE) pre.load(o.pre + g * o.gsp + i * o.ldp + j, valid);
+    if constexpr (KIND != MM_DW)
+      if (o.add) add.load(o.add + g * o.gsa + i * o.lda + j, valid);
+    mm_epilogue<KIND, ACT>(o, g, i, j, valid, pre, add, bias, v);
   })
 }
 
