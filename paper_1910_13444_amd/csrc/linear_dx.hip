@@ -10,11 +10,11 @@ namespace pigan {
 template <class T, class TO, int MT, int NT, int OCC>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
 k_mm_both(const MmArgs<T, TO> dx, const MmArgs<T, float> dw, uint32_t n_dx, uint32_t n_dw, int dw_first) {
-  __shared__ __attribute__((aligned(1024))) char s0[mm_stage<MT, NT>()];
-  __shared__ __attribute__((aligned(1024))) char s1[mm_stage<MT, NT>()];
+  __shared__ __attribute__((aligned(1024))) char s0[mm_stage<MT, NT, 2>()];
+  __shared__ __attribute__((aligned(1024))) char s1[mm_stage<MT, NT, 2>()];
   const uint32_t n = blockIdx.x, begin = dw_first ? n_dw : 0;
-  if (n >= begin && n - begin < n_dx) mm_piped<T, TO, MM_DX, MT, NT>(dx, n - begin, n_dx, s0, s1);
-  else mm_piped<T, float, MM_DW, MT, NT>(dw, dw_first ? n : n - n_dx, n_dw, s0, s1);
+  if (n >= begin && n - begin < n_dx) mm_piped<T, TO, MM_DX, MT, NT, 2>(dx, n - begin, n_dx, s0, s1);
+  else mm_piped<T, float, MM_DW, MT, NT, 2>(dw, dw_first ? n : n - n_dx, n_dw, s0, s1);
 }
 
 template <class T, class TO>

@@ -1,7 +1,7 @@
 // The tiled product of the linear layer on the 16-bit matrix cores of gfx950
 // (see linear.h for the operands).
 //
-// A block of four waves forms a tile of C; a wave owns MT x NT fragments of
+// A block of waves forms a tile of C; a wave owns MT x NT fragments of
 // 32 x 32.  Operands pass through LDS in stages of 64 values of k:
 //   k along the row   a row of the stage is a 128-byte line of a row of A; its
 //                     16-byte segment s sits at s ^ (row & 7), so the 32 rows
@@ -92,74 +92,56 @@ __device__ __forceinline__ void mm_epilogue(const MmOut<TO>& o, int g, int64_t i
 // A wave's MT x NT fragments, from rows i0 and columns j0 on, to memory: as
 // partial sums or through the epilogue (one branch on the activation for all of
 // them: the accumulators stay in registers only if every loop unrolls).  What the
-// epilogue reads is requested columns of fragments ahead, as many as the registers
-// hold beside the accumulators (DP of pre, DA of add): asked for one by one, each
-// of 32 reads was waited for by itself, 30 us of the 60 that a 256 x 256 tile took
-// at K = 1024.  WHOLE: the columns come in whole eights.
+// epilogue reads is requested D - 1 fragments ahead, as many as the registers hold
+// beside the accumulators: asked for one by one, each of 32 reads was waited for
+// by itself, 30 us of the 60 that a 256 x 256 tile took at K = 1024.  WHOLE: the
+// columns come in whole eights.
 template <int KIND, int ACT, bool PART, bool WHOLE, class TO, int MT, int NT>
 __device__ __forceinline__ void mm_store(const MmOut<TO>& o, int g, int split, int64_t i0, int64_t j0,
                                          const f32x16 (&acc)[MT][NT]) {
   const int lane = threadIdx.x & 63;
   constexpr bool PRE = !PART && KIND == MM_DX && ACT != PIGAN_ACT_NONE, ADD = !PART && KIND != MM_DW;
-  constexpr bool HALF = sizeof(TO) == 2;
-  constexpr int DP = !PRE || !WHOLE ? 1 : MT <= 2 ? NT : HALF ? 2 : 1;
-  constexpr int DA = !ADD || !WHOLE ? 1 : MT <= 2 ? NT : !HALF || PRE ? 1 : NT;
-  Octet<TO> pre[DP][MT][2], add[DA][MT][2];
-  auto each = [&](int b, auto f) __attribute__((always_inline)) {
-    const int64_t j = j0 + 32 * b + mm_col(lane);
+  constexpr int NF = MT * NT;
+  constexpr int WANT = !WHOLE ? 1 : sizeof(TO) == 4 ? 2 : PRE ? 4 : 6;
+  constexpr int D = WANT < NF ? WANT : NF;
+  Octet<TO> pre[PRE ? D : 1][2], add[ADD ? D : 1][2];
+  // f(half, row, column, columns that are there) of fragment n
+  auto each = [&](int n, auto f) __attribute__((always_inline)) {
+    const int64_t j = j0 + 32 * (n / MT) + mm_col(lane);
 #pragma unroll
-    for (int a = 0; a < MT; ++a)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int64_t i = i0 + 32 * a + 16 * h + (lane & 15);
-        if (i < o.I && j < o.J) f(a, h, i, j, WHOLE ? (int64_t)8 : o.J - j);
-      }
+    for (int h = 0; h < 2; ++h) {
+      const int64_t i = i0 + 32 * (n % MT) + 16 * h + (lane & 15);
+      if (i < o.I && j < o.J) f(h, i, j, WHOLE ? (int64_t)8 : o.J - j);
+    }
   };
-  auto request_pre = [&](int b) __attribute__((always_inline)) {
-    each(b, [&](int a, int h, int64_t i, int64_t j, int64_t valid) __attribute__((always_inline)) {
-      pre[b % DP][a][h].load(o.pre + g * o.gsp + i * o.ldp + j, valid);
+  auto request = [&](int n) __attribute__((always_inline)) {
+    each(n, [&](int h, int64_t i, int64_t j, int64_t valid) __attribute__((always_inline)) {
+      if constexpr (PRE) pre[n % D][h].load(o.pre + g * o.gsp + i * o.ldp + j, valid);
+      if constexpr (ADD)
+        if (o.add) add[n % D][h].load(o.add + g * o.gsa + i * o.lda + j, valid);
     });
   };
-  auto request_add = [&](int b) __attribute__((always_inline)) {
-    if (o.add)
-      each(b, [&](int a, int h, int64_t i, int64_t j, int64_t valid) __attribute__((always_inline)) {
-        add[b % DA][a][h].load(o.add + g * o.gsa + i * o.lda + j, valid);
-      });
-  };
-  // columns up to b + D - 1 are on their way when column b begins
+  if constexpr (PRE || ADD)
 #pragma unroll
-  for (int b = 0; b < NT; ++b) {
-    if constexpr (PRE)
-      if (b < DP - 1) request_pre(b);
-    if constexpr (ADD)
-      if (b < DA - 1) request_add(b);
-  }
+    for (int n = 0; n < D - 1; ++n) request(n);
+  float bias[8];
 #pragma unroll
-  for (int b = 0; b < NT; ++b) {
-    const int64_t j = j0 + 32 * b + mm_col(lane);
-    if constexpr (PRE)
-      if (b + DP - 1 < NT) request_pre(b + DP - 1);
-    if constexpr (ADD)
-      if (b + DA - 1 < NT) request_add(b + DA - 1);
-    float bias[8];
+  for (int n = 0; n < NF; ++n) {
+    if constexpr (PRE || ADD)
+      if (n + D - 1 < NF) request(n + D - 1);
     if constexpr (KIND == MM_FWD && !PART)
-      vec_load<8>(o.bias && (!WHOLE || j < o.J) ? o.bias + g * o.J : nullptr, j, WHOLE ? j + 8 : o.J, 0.0f, bias);
-#pragma unroll
-    for (int a = 0; a < MT; ++a) {
-      float v[16];
-#pragma unroll
-      for (int r = 0; r < 16; ++r) v[r] = acc[a][b][r];
-      mm_exchange(v);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int64_t i = i0 + 32 * a + 16 * h + (lane & 15);
-        if (i < o.I && j < o.J) {
-          const int64_t valid = WHOLE ? 8 : o.J - j;
-          if constexpr (PART) store8(o.part + (((int64_t)g * o.n_split + split) * o.I + i) * o.J + j, valid, v + 8 * h);
-          else mm_epilogue<KIND, ACT>(o, g, i, j, valid, pre[b % DP][a][h], add[b % DA][a][h], bias, v + 8 * h);
-        }
+      if (n % MT == 0) {
+        const int64_t j = j0 + 32 * (n / MT) + mm_col(lane);
+        vec_load<8>(o.bias && (!WHOLE || j < o.J) ? o.bias + g * o.J : nullptr, j, WHOLE ? j + 8 : o.J, 0.0f, bias);
       }
-    }
+    float v[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) v[r] = acc[n % MT][n / MT][r];
+    mm_exchange(v);
+    each(n, [&](int h, int64_t i, int64_t j, int64_t valid) __attribute__((always_inline)) {
+      if constexpr (PART) store8(o.part + (((int64_t)g * o.n_split + split) * o.I + i) * o.J + j, valid, v + 8 * h);
+      else mm_epilogue<KIND, ACT>(o, g, i, j, valid, pre[PRE ? n % D : 0][h], add[ADD ? n % D : 0][h], bias, v + 8 * h);
+    });
   }
 }
 
@@ -370,15 +352,15 @@ k_mm_any(const MmArgs<T, TO> p) {
 }
 
 // ---------------------------------------------------------------------------
-// Aligned operands.  Four waves form a tile of 64 MT x 64 NT, two stages of LDS.
+// Aligned operands.  2 x WN waves form a tile of 64 MT x 32 NT WN, two stages of LDS.
 // Fragments are read one chunk of 16 k ahead of their products, and the only wait
 // of a stage stands before its last chunk, when the next stage has had three
 // chunks' time to land and this stage's buffer has no reader left.
-//   256 x 256  one wave per SIMD with the whole register file (256 accumulators
-//              a lane): a fragment read from LDS feeds four products, so LDS
-//              moves 0.75 of what the matrix cores take in the same time
-//   128 x 128  two blocks per CU, which fill each other's waits and epilogues;
-//              LDS bound (1.5 of the matrix cores' time)
+//   256 x 256  eight waves of 128 x 64, two per SIMD.  (Four waves of 128 x 128 read
+//              a third less from LDS but leave the matrix cores idle at every wait
+//              and in the epilogue: 8192^3 bf16 1170 against 1267 TFLOP/s, 262,144 x
+//              1024 x 1024 with a residual 786 against 703 us.)
+//   128 x 128  two blocks of four waves per CU, which fill each other's waits
 //   64 x 64    four blocks per CU, for few tiles; for very few, one block of four
 //              groups that share the contraction
 // The loads are buffer loads: what is past the end of the matrix is out of the
@@ -399,34 +381,34 @@ __device__ __forceinline__ u32x4 mm_buffer(const void* p, uint32_t bytes) {
 // load has no destination register; its arrival is waited for by stage_sync()
 // alone, before the barrier behind which the stage is read.  M0 is a reserved
 // register: nothing else in these kernels sets or reads it.
-__device__ __forceinline__ void lds_load(const u32x4& buffer, char* lds, uint32_t lane_off, uint32_t off) {
-  const uint32_t to = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(lds_ptr_t)lds);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-               ::"s"(to), "v"(lane_off), "s"(buffer), "s"(off));
+__device__ __forceinline__ void lds_load(const u32x4& buffer, uint32_t lds, uint32_t more, uint32_t lane_off,
+                                         uint32_t off) {
+  asm volatile("s_add_u32 m0, %0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, %4 offen lds"
+               ::"s"(lds), "i"(more), "v"(lane_off), "s"(buffer), "s"(off) : "scc");
 }
 
 // bytes of a stage
-template <int MT, int NT> constexpr int mm_stage() { return (64 * MT + 64 * NT) * 64 * 2; }
+template <int MT, int NT, int WN> constexpr int mm_stage() { return (64 * MT + 32 * NT * WN) * 64 * 2; }
 
 // Block n of `blocks` of the product, with two stages of LDS for each of KG groups
-// of four waves: the groups share the contraction of the tile and meet in LDS, in
+// of 2 x WN waves: the groups share the contraction of the tile and meet in LDS, in
 // order, before the epilogue.
-template <class T, class TO, int KIND, int MT, int NT, int KG = 1>
+template <class T, class TO, int KIND, int MT, int NT, int WN, int KG = 1>
 __device__ __forceinline__ void mm_piped(const MmArgs<T, TO>& p, uint32_t n, uint32_t blocks, char* s0, char* s1) {
   static_assert(KG == 1 || MT * NT == 1, "groups: tiles of one fragment a wave");
-  constexpr int BM = 64 * MT, BN = 64 * NT, BK = 64, STAGE_A = BM * BK * 2;
+  constexpr int BM = 64 * MT, BN = 32 * NT * WN, BK = 64, STAGE_A = BM * BK * 2, NW = 2 * WN, NTH = 64 * NW;
   constexpr bool AK = KIND != MM_DW, BKC = KIND == MM_FWD;
-  constexpr int GA = BM / 32, GB = BN / 32;   // 1 KB groups per wave and stage
+  constexpr int GA = BM / 8 / NW, GB = BN / 8 / NW;   // 1 KB groups per wave and stage
   static_assert(GA == GB, "one group of each operand at a time");
   typedef typename Elem<T>::frag frag;
 
-  const int tid = threadIdx.x & 255, lane = tid & 63;
-  const int kg = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 8);
+  const int tid = KG == 1 ? (int)threadIdx.x : (int)threadIdx.x % NTH, lane = tid & 63;
+  const int kg = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / NTH);
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave & 1, wn = wave >> 1;
   if constexpr (KG > 1) {
-    s0 += kg * mm_stage<MT, NT>();
-    s1 += kg * mm_stage<MT, NT>();
+    s0 += kg * mm_stage<MT, NT, WN>();
+    s1 += kg * mm_stage<MT, NT, WN>();
   }
 
   const uint32_t rows = (uint32_t)((p.o.I + BM - 1) / BM), tj = (uint32_t)((p.o.J + BN - 1) / BN);
@@ -461,7 +443,7 @@ __device__ __forceinline__ void mm_piped(const MmArgs<T, TO>& p, uint32_t n, uin
   const T* pb = p.b.p + at.g * p.b.gs + (BKC ? j0 * p.b.ld : j0);
   const int left_a = (int)(p.o.I - i0 < BM ? p.o.I - i0 : BM), left_b = (int)(p.o.J - j0 < BN ? p.o.J - j0 : BN);
   // a group is eight rows of an operand with k along the row, 512 / side rows of
-  // one with k down the rows; a wave's groups are wave, wave + 4, ...
+  // one with k down the rows; a wave's groups are wave, wave + NW, ...
   constexpr uint32_t OUT = 0xffffffffu;   // never in range
   auto lane_off = [&](bool along, int side, int64_t ld, int left) __attribute__((always_inline)) -> uint32_t {
     if (along) return (uint32_t)((8 * wave + (lane >> 3)) * ld * 2 + (((lane & 7) ^ (lane >> 3)) * 16));
@@ -469,8 +451,8 @@ __device__ __forceinline__ void mm_piped(const MmArgs<T, TO>& p, uint32_t n, uin
     return seg * 8 < left ? (uint32_t)(row * ld * 2 + seg * 16) : OUT;
   };
   const uint32_t off_a = lane_off(AK, BM, p.a.ld, left_a), off_b = lane_off(BKC, BN, p.b.ld, left_b);
-  const uint32_t step_a = (uint32_t)((AK ? 32 : 2048 / BM) * p.a.ld * 2);
-  const uint32_t step_b = (uint32_t)((BKC ? 32 : 2048 / BN) * p.b.ld * 2);
+  const uint32_t step_a = (uint32_t)(NW * (AK ? 8 : 512 / BM) * p.a.ld * 2);
+  const uint32_t step_b = (uint32_t)(NW * (BKC ? 8 : 512 / BN) * p.b.ld * 2);
   const int seg_k = ((lane & 7) ^ (lane >> 3)) * 8;   // k of the lane's piece (k along the row)
 
   // the next stage to load: its first elements, its k, the stages left of its plane pair
@@ -508,9 +490,12 @@ __device__ __forceinline__ void mm_piped(const MmArgs<T, TO>& p, uint32_t n, uin
     --pair_left;
     --to_load;
   };
-  auto load = [&](char* stage, int q) __attribute__((always_inline)) {
-    lds_load(ra, stage + (wave + 4 * q) * 1024, va, q * step_a);
-    lds_load(rb, stage + (STAGE_A + (wave + 4 * q) * 1024), vb, q * step_b);
+  // where this wave's groups begin in either stage (LDS addresses in scalar registers)
+  const uint32_t lds0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(lds_ptr_t)s0) + wave * 1024;
+  const uint32_t lds1 = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(lds_ptr_t)s1) + wave * 1024;
+  auto load = [&](uint32_t lds, int q, int operand) __attribute__((always_inline)) {
+    if (operand == 0) lds_load(ra, lds, q * NW * 1024, va, q * step_a);
+    else lds_load(rb, lds, STAGE_A + q * NW * 1024, vb, q * step_b);
   };
 
   // ---- fragments ----
@@ -536,7 +521,7 @@ __device__ __forceinline__ void mm_piped(const MmArgs<T, TO>& p, uint32_t n, uin
   // take the chunks in turn; the first three plane pairs hold every plane of A once
   auto sum_a = [&](int from, int c, uint32_t st) __attribute__((always_inline)) {
     if constexpr (KIND == MM_DW) {
-      if (p.part_db && (c & 1) == wn && st < (uint32_t)(3 * per_pair) &&
+      if (p.part_db && c % WN == wn && st < (uint32_t)(3 * per_pair) &&
           (p.o.n_split == 1 ? at.tj == 0 : st % tj == (uint32_t)at.tj)) {
 #pragma unroll
         for (int a = 0; a < MT; ++a)
@@ -545,47 +530,47 @@ __device__ __forceinline__ void mm_piped(const MmArgs<T, TO>& p, uint32_t n, uin
       }
     }
   };
-  // the products of a chunk; between the first of them go out the reads of the
-  // next chunk and a stage's loads
-  auto chunk = [&](int from, const char* stage, int c, char* into, auto loads) __attribute__((always_inline)) {
-    constexpr int NP = MT * NT, RD = MT > NT ? MT : NT;
+  // the products of a chunk; the reads of the next chunk go out between the first
+  // of them, a stage's loads between all of them
+  auto chunk = [&](int from, const char* stage, int c, uint32_t into, auto loads) __attribute__((always_inline)) {
+    constexpr int NP = MT * NT, RD = MT > NT ? MT : NT, PER = (2 * GA + NP - 1) / NP;
+    constexpr bool LOADS = decltype(loads)::value;
 #pragma unroll
     for (int n = 0; n < NP; ++n) {
       Elem<T>::mma(acc[n / NT][n % NT], fb[from][n % NT], fa[from][n / NT]);
       if (n < RD) read1(from ^ 1, stage, c, n);
-      if constexpr (decltype(loads)::value) {
-        constexpr int PER = (GA + NP - 1) / NP;
+      if constexpr (LOADS) {
 #pragma unroll
-        for (int q = 0; q < PER; ++q)
-          if (n * PER + q < GA) load(into, n * PER + q);
+        for (int q = n * PER; q < (n + 1) * PER; ++q)
+          if (q < 2 * GA) load(into, q >> 1, q & 1);
       }
-      if (n < RD || (decltype(loads)::value && n < GA)) __builtin_amdgcn_sched_barrier(0);
+      if (n < RD || (LOADS && n * PER < 2 * GA)) __builtin_amdgcn_sched_barrier(0);
     }
   };
   // one stage; its first chunk is already in fragments 0
-  auto turn = [&](int st, char* now, char* next) __attribute__((always_inline)) {
+  auto turn = [&](int st, char* now, uint32_t lds_now, char* next) __attribute__((always_inline)) {
     prepare();
 #pragma unroll
     for (int c = 0; c < 3; ++c) {
-      chunk(c & 1, now, c + 1, nullptr, std::false_type{});
+      chunk(c & 1, now, c + 1, 0, std::false_type{});
       sum_a(c & 1, c, st);
     }
     stage_sync<0>();
-    chunk(1, next, 0, now, std::true_type{});
+    chunk(1, next, 0, lds_now, std::true_type{});
     sum_a(1, 3, st);
   };
   prepare();
 #pragma unroll
-  for (int q = 0; q < GA; ++q) load(s0, q);
+  for (int q = 0; q < 2 * GA; ++q) load(lds0, q >> 1, q & 1);
   prepare();
 #pragma unroll
-  for (int q = 0; q < GA; ++q) load(s1, q);
+  for (int q = 0; q < 2 * GA; ++q) load(lds1, q >> 1, q & 1);
   stage_sync<2 * GA>();
 #pragma unroll
   for (int q = 0; q < (MT > NT ? MT : NT); ++q) read1(0, s0, 0, q);
   for (int st = 0; st < turns; st += 2) {
-    turn(st, s0, s1);
-    if (st + 1 < turns) turn(st + 1, s1, s0);
+    turn(st, s0, lds0, s1);
+    if (st + 1 < turns) turn(st + 1, s1, lds1, s0);
   }
   stage_sync<0>();   // no load in flight when LDS is used again or given up
 
@@ -601,33 +586,36 @@ __device__ __forceinline__ void mm_piped(const MmArgs<T, TO>& p, uint32_t n, uin
     if (kg > 0) return;
 #pragma unroll
     for (int q = 1; q < KG; ++q) {
-      const float* from = (const float*)(s0 + q * mm_stage<MT, NT>());
+      const float* from = (const float*)(s0 + q * mm_stage<MT, NT, WN>());
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[0][0][r] += from[(wave * 16 + r) * 64 + lane];
-      if constexpr (KIND == MM_DW) db[0] += ((const float*)(s1 + q * mm_stage<MT, NT>()))[tid];
+      if constexpr (KIND == MM_DW) db[0] += ((const float*)(s1 + q * mm_stage<MT, NT, WN>()))[tid];
     }
   }
   mm_results<KIND, true>(p.o, at.g, at.split, i0 + 32 * MT * wm, j0 + 32 * NT * wn, acc);
   if constexpr (KIND == MM_DW) {
     if (p.part_db) {
-      float* sums = (float*)s0;   // [2][BM]
+      float* sums = (float*)s0;   // [WN][BM]
 #pragma unroll
       for (int a = 0; a < MT; ++a) {
         const float s = db[a] + __shfl_xor(db[a], 32);
         if (lane < 32) sums[wn * BM + 32 * (MT * wm + a) + lane] = s;
       }
       lds_sync();
-      mm_store_db(p, at.g, at.split, at.tj, (int)tj, i0, tid < BM ? tid : -1, sums[tid % BM] + sums[BM + tid % BM]);
+      float sum = sums[tid % BM];
+#pragma unroll
+      for (int n = 1; n < WN; ++n) sum += sums[n * BM + tid % BM];
+      mm_store_db(p, at.g, at.split, at.tj, (int)tj, i0, tid < BM ? tid : -1, sum);
     }
   }
 }
 
-template <class T, class TO, int KIND, int MT, int NT, int OCC, int KG = 1>
-__global__ void __launch_bounds__(256 * KG) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
+template <class T, class TO, int KIND, int MT, int NT, int WN, int OCC, int KG = 1>
+__global__ void __launch_bounds__(128 * WN * KG) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
 k_mm_piped(const MmArgs<T, TO> p) {
-  __shared__ __attribute__((aligned(1024))) char s0[KG * mm_stage<MT, NT>()];
-  __shared__ __attribute__((aligned(1024))) char s1[KG * mm_stage<MT, NT>()];
-  mm_piped<T, TO, KIND, MT, NT, KG>(p, blockIdx.x, gridDim.x, s0, s1);
+  __shared__ __attribute__((aligned(1024))) char s0[KG * mm_stage<MT, NT, WN>()];
+  __shared__ __attribute__((aligned(1024))) char s1[KG * mm_stage<MT, NT, WN>()];
+  mm_piped<T, TO, KIND, MT, NT, WN, KG>(p, blockIdx.x, gridDim.x, s0, s1);
 }
 
 // ---------------------------------------------------------------------------
@@ -700,10 +688,10 @@ hipError_t mm_launch(const MmArgs<T, TO>& a, int tile, bool direct, int G, hipSt
   const uint32_t count = mm_blocks<T, TO, KIND>(a, tile, direct, G);
   if (!count) return hipErrorInvalidValue;
   if (direct) {
-    if (tile == MM_256) k_mm_piped<T, TO, KIND, 4, 4, 1><<<count, 256, 0, st>>>(a);
-    else if (tile == MM_128) k_mm_piped<T, TO, KIND, 2, 2, 2><<<count, 256, 0, st>>>(a);
-    else if (tile == MM_64) k_mm_piped<T, TO, KIND, 1, 1, 4><<<count, 256, 0, st>>>(a);
-    else k_mm_piped<T, TO, KIND, 1, 1, 4, 4><<<count, 1024, 0, st>>>(a);
+    if (tile == MM_256) k_mm_piped<T, TO, KIND, 4, 2, 4, 2><<<count, 512, 0, st>>>(a);
+    else if (tile == MM_128) k_mm_piped<T, TO, KIND, 2, 2, 2, 2><<<count, 256, 0, st>>>(a);
+    else if (tile == MM_64) k_mm_piped<T, TO, KIND, 1, 1, 2, 4><<<count, 256, 0, st>>>(a);
+    else k_mm_piped<T, TO, KIND, 1, 1, 2, 4, 4><<<count, 1024, 0, st>>>(a);
   } else {
     if (tile == MM_128) k_mm_any<T, TO, KIND, 2, 2><<<count, 256, 0, st>>>(a);
     else k_mm_any<T, TO, KIND, 1, 1><<<count, 256, 0, st>>>(a);
