@@ -143,14 +143,16 @@ struct MmPlan {
 // of k) with 1, 2, .. blocks on a CU, of a block's start and epilogue, and of a
 // kernel's first blocks (the 256 tile's unrolled epilogue has to be fetched).  The
 // splits of a contraction add a launch and the partials' way through memory.
-//   us measured (256 | 128 | 64 tile, best split)       modelled
-//   forward 262144 x 1024 x 1024   816 | 903 | -        738 | 824 | -
-//   forward 1024 x 2000 x 1024     36 | 21 | 13         43 | 30 | 16
-//   dw of 131072 x 1024 x 1024     284 | 297 | 536      306 | 330 | 428
-//   dx of 21 x 512 x 256 x 256     36 | 12 | 10         36 | 15 | 8
-// (64 tile with k down the rows of an operand: 8192^3 in 2066 and 2275 us, forward 1605)
-constexpr double STAGE_FWD[3][4] = {{0.33, 0.48, 0.63, 0.78}, {0.6, 1.16, 0, 0}, {1.9, 0, 0, 0}};
-constexpr double STAGE_BWD[3][4] = {{0.42, 0.63, 0.84, 1.05}, {0.6, 1.16, 0, 0}, {1.9, 0, 0, 0}};
+//   M x K x N, us            taken, modelled | measured    the others measured
+//   fwd 4096 x 2048 x 2048   128    49 | 38                256: 53, 64: 56
+//   fwd 20000 x 1032 x 1000  128    85 | 81                256: 85, 64: 105
+//   fwd 512 x 2048 x 2048    64K    13 | 13                64: 13, 128: 20
+//   dx 32768 x 512 x 512     128    38 | 39                256: 40, 64: 45
+//   dw 20000 x 1032 x 1000   128/4  81 | 78                256/8: 75, 128/2: 118
+//   dw 32768 x 512 x 512     128/16 46 | 38                64/16: 45, 256: over 46
+// (64 with k down the rows of an operand: 8192^3 in 2066 and 2275 us, forward 1605)
+constexpr double STAGE_FWD[3][4] = {{0.33, 0.5, 0.68, 0.85}, {0.6, 1.16, 0, 0}, {1.7, 0, 0, 0}};
+constexpr double STAGE_BWD[3][4] = {{0.42, 0.63, 0.84, 1.05}, {0.6, 1.16, 0, 0}, {1.7, 0, 0, 0}};
 constexpr double BLOCK_US[3] = {3.0, 7.0, 14.0}, FIRST_US[3] = {2.0, 5.0, 14.0};
 constexpr int PER_CU[3] = {4, 2, 1};
 
@@ -162,21 +164,26 @@ double split_us(int64_t I, int64_t J, int G, int split) {
   return split > 1 ? 8.0 + (double)G * I * J * 4.0 * (split * 2 + 1) / 5e6 : 0.0;
 }
 
+// a stage with `blocks` blocks spread over the chip, and how full they make a CU
+double stage_of(const double (&stage)[3][4], int t, double blocks, double& load) {
+  load = std::min<double>(PER_CU[t], std::max(1.0, blocks / 256));
+  const int lo = (int)load, hi = std::min(lo + 1, PER_CU[t]);
+  return stage[t][lo - 1] + (load - lo) * (stage[t][hi - 1] - stage[t][lo - 1]);
+}
+
 MmPlan plan_mm(const double (&STAGE_US)[3][4], int64_t I, int64_t J, int64_t K, int pairs, int G) {
   const int64_t nk = (K + 63) / 64;
   MmPlan best;
-  for (int t = MM_64; t <= MM_256; ++t) {
-    const double tiles = tiles_of(I, J, G, t);
+  double load;
+  for (int t = MM_64; t <= MM_256; ++t)
     for (int split = 1; split <= 64 && split <= nk; split *= 2) {
       if (split > 1 && nk * pairs / split < 4) break;
-      const double blocks = tiles * split;
-      const int held = (int)std::min<double>(PER_CU[t], ceil(blocks / 256));
-      const double rounds = ceil(blocks / (256.0 * held));
-      const double us = rounds * ((double)((nk + split - 1) / split) * pairs * STAGE_US[t][held - 1] + BLOCK_US[t]) +
-                        FIRST_US[t] + split_us(I, J, G, split);
+      const double blocks = tiles_of(I, J, G, t) * split, rounds = ceil(blocks / (256.0 * PER_CU[t]));
+      const double stages = (double)((nk + split - 1) / split) * pairs;
+      const double us = rounds * (stages * stage_of(STAGE_US, t, blocks, load) + BLOCK_US[t]) + FIRST_US[t] +
+                        split_us(I, J, G, split);
       if (us < best.us) best = {t, split, us};
     }
-  }
   // 64 tiles of four groups, one on a CU: a stage of each group in the time of four blocks' stages
   const double us = ceil(tiles_of(I, J, G, MM_64) / 256) * ((double)((nk + 3) / 4) * pairs * STAGE_US[MM_64][3] + 4.0) +
                     FIRST_US[MM_64];
@@ -188,7 +195,6 @@ MmPlan plan_mm(const double (&STAGE_US)[3][4], int64_t I, int64_t J, int64_t K, 
 // time is that of the longest block, or of all of them spread over the chip.
 // Taken where it is shorter than one launch after the other (2 us between them).
 bool plan_both(int64_t M, int64_t N, int64_t K, int pairs, int G, MmPlan& dx, MmPlan& dw) {
-  const auto& STAGE_US = STAGE_BWD;
   const int64_t nx = (N + 63) / 64, nw = (M + 63) / 64;
   double best = dx.us + dw.us + 2.0;
   bool both = false;
@@ -196,9 +202,8 @@ bool plan_both(int64_t M, int64_t N, int64_t K, int pairs, int G, MmPlan& dx, Mm
     for (int split = 1; split <= 64 && split <= nw; split *= 2) {
       if (split > 1 && nw * pairs / split < 4) break;
       const double b1 = tiles_of(M, K, G, t), b2 = tiles_of(N, K, G, t) * split;
-      const double load = std::min<double>(PER_CU[t], std::max(1.0, (b1 + b2) / 256));
-      const int lo = (int)load, hi = std::min(lo + 1, PER_CU[t]);
-      const double stage = STAGE_US[t][lo - 1] + (load - lo) * (STAGE_US[t][hi - 1] - STAGE_US[t][lo - 1]);
+      double load;
+      const double stage = stage_of(STAGE_BWD, t, b1 + b2, load);
       const double t1 = nx * pairs * stage + BLOCK_US[t], t2 = (double)((nw + split - 1) / split) * pairs * stage + BLOCK_US[t];
       const double us = std::max(std::max(t1, t2), (b1 * t1 + b2 * t2) / (256.0 * load)) + FIRST_US[t] + split_us(N, K, G, split);
       if (us < best) {
