@@ -6,4 +6,4 @@ built from the HIP sources under ``csrc/``) and a thin ctypes binding
 library is opened on first use by :func:`paper_1910_13444_amd.pigan.lib`.
 """
 
-__all__ = ["configs", "inputs", "flops", "pigan"]
+__all__ = ["configs", "inputs", "flops", "pigan", "norm_critic"]
