@@ -190,18 +190,28 @@ __global__ void __launch_bounds__(1024) k_norm_fwd_long(const NormArgs<T> p) {
 // [dgamma, dbeta] (the final ones, where one block takes all rows).
 // ---------------------------------------------------------------------------
 // Threads of a block: 1024, which leaves few partial rows, but 256 where a thread
-// holds two 16-bit pieces (sixteen columns): that needs more registers than 1024
-// threads have (131,072 x 1024 with a skip: 312 us spilling, see launch_norm_bwd).
+// holds two 16-bit pieces (sixteen columns) of a wave's row: that needs more
+// registers than 1024 threads have (131,072 x 1024 with a skip: 312 us spilling,
+// 210 us without).  Rows of 8192 to 16384 such columns have no other way and spill
+// (17 registers; 16384 x 16384: 370 us, 4.4 TB/s).
 template <class T, int TPR, int NV> constexpr int bwd_nth() { return TPR <= 64 && sizeof(T) == 2 && NV == 2 ? 256 : 1024; }
 
 // Nothing is masked by element: past the end of a row dy is loaded as zero, and
 // with it everything that a column there adds.
+// Several rows of more than a wave in a block leave its loop together, for its
+// barriers: past the last row they work on zeros (ROWS_JOIN).
+//   bf16, us (TB/s)   no skip      with a skip     one row per 1024 threads
+//   262144 x 1024     319 (5.1)    424 (5.1)
+//   131072 x 2048     298 (5.4)    388 (5.5)       707, 741
+//   65536 x 4096      302 (5.3)    392 (5.5)       390, 449
+//   32768 x 8192      308 (5.2)    403 (5.3)
 template <class T, int TPR, int NV, bool DX, bool COLS, bool WHOLE>
 __global__ void __launch_bounds__((bwd_nth<T, TPR, NV>())) k_norm_bwd(const NormArgs<T> p, float* __restrict__ d0,
                                                       float* __restrict__ d1, int64_t d_g, int64_t d_b) {
   constexpr int E = EPP<T>, BWD_NTH = bwd_nth<T, TPR, NV>(), RPB = BWD_NTH / TPR;
+  constexpr bool ROWS_JOIN = TPR > 64 && RPB > 1;
   __shared__ float red[2][2 * BWD_NTH / 64];
-  __shared__ float cols[COLS && TPR <= 64 ? 2 * TPR * NV * E : 1];
+  __shared__ float cols[COLS && RPB > 1 ? 2 * TPR * NV * E : 1];
   __shared__ __attribute__((aligned(16))) float ga[TPR * NV * E];
   const int g = blockIdx.z;
   const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
@@ -223,30 +233,31 @@ __global__ void __launch_bounds__((bwd_nth<T, TPR, NV>())) k_norm_bwd(const Norm
   piece_t rx[NV], rd[NV], ra[NV];
   float mean = 0.0f, rstd = 0.0f;
   auto request = [&](int64_t r) {
+    const bool live = !ROWS_JOIN || r < p.M;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int64_t c = (int64_t)(v * TPR + lane) * E;
+      const int64_t c = live ? (int64_t)(v * TPR + lane) * E : p.N;
       rx[v] = row_load<WHOLE>(x + r * p.x.ld, c, p.N);
       rd[v] = row_load<WHOLE>(dy + r * p.dy.ld, c, p.N);
     }
-    mean = p.mean[g * p.M + r];
-    rstd = p.rstd[g * p.M + r];
+    mean = live ? p.mean[g * p.M + r] : 0.0f;
+    rstd = live ? p.rstd[g * p.M + r] : 0.0f;
   };
   auto request_add = [&](int64_t r) {
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int64_t c = (int64_t)(v * TPR + lane) * E;
+      const int64_t c = !ROWS_JOIN || r < p.M ? (int64_t)(v * TPR + lane) * E : p.N;
       ra[v] = row_load<WHOLE>(add + r * p.add.ld, c, p.N);
     }
   };
   int turn = 0;
+  const int64_t last = p.M + (ROWS_JOIN ? sub : 0);   // as far as this thread's rows go
   int64_t r = (int64_t)blockIdx.x * RPB + sub;
-  if (r < p.M) {
+  if (r < last) {
     request(r);
     if (add) request_add(r);
   }
-  // (rows above a wave take the whole block: its threads leave together)
-  for (; r < p.M; r += step, turn ^= 1) {
+  for (; r < last; r += step, turn ^= 1) {
     asm volatile("" ::: "memory");   // gamma is read again for every row
     float xh[NV][E], h[NV][E], s[2] = {0.0f, 0.0f};
     const float mu = mean, rs = rstd;
@@ -256,7 +267,7 @@ __global__ void __launch_bounds__((bwd_nth<T, TPR, NV>())) k_norm_bwd(const Norm
       piece_floats<T>(rd[v], h[v]);
     }
     // the next row is on its way while this one is worked on
-    if (r + step < p.M) request(r + step);
+    if (r + step < last) request(r + step);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
 #pragma unroll
@@ -277,7 +288,7 @@ __global__ void __launch_bounds__((bwd_nth<T, TPR, NV>())) k_norm_bwd(const Norm
       T* row = p.out.p + g * p.out.gs + r * p.out.ld;
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        const int64_t c = (int64_t)(v * TPR + lane) * E;
+        const int64_t c = !ROWS_JOIN || r < p.M ? (int64_t)(v * TPR + lane) * E : p.N;
 #pragma unroll
         for (int e = 0; e < E; ++e) h[v][e] = rs * (h[v][e] - s1 - xh[v][e] * s2);
         if (add) {
@@ -288,7 +299,7 @@ __global__ void __launch_bounds__((bwd_nth<T, TPR, NV>())) k_norm_bwd(const Norm
         }
         row_store<WHOLE>(row, c, p.N, h[v]);
       }
-      if (add && r + step < p.M) request_add(r + step);
+      if (add && r + step < last) request_add(r + step);
     }
   }
   if constexpr (COLS) {
@@ -306,9 +317,10 @@ __global__ void __launch_bounds__((bwd_nth<T, TPR, NV>())) k_norm_bwd(const Norm
             sb[v][e] += __shfl_xor(sb[v][e], o);
           }
     }
-    if constexpr (TPR <= 64) {
-      for (int w = 0; w < BWD_NTH / 64; ++w) {
-        if ((int)(threadIdx.x >> 6) == w && (threadIdx.x & 63) < TPR) {
+    if constexpr (RPB > 1) {
+      constexpr int UNIT = TPR < 64 ? 64 : TPR;   // threads that hold a set of sums
+      for (int w = 0; w < BWD_NTH / UNIT; ++w) {
+        if ((int)(threadIdx.x / UNIT) == w && threadIdx.x % UNIT < TPR) {
 #pragma unroll
           for (int v = 0; v < NV; ++v)
 #pragma unroll
@@ -324,7 +336,7 @@ __global__ void __launch_bounds__((bwd_nth<T, TPR, NV>())) k_norm_bwd(const Norm
         if (o0) o0[c] = cols[c];
         if (o1) o1[c] = cols[TPR * NV * E + c];
       }
-    } else if constexpr (TPR == BWD_NTH) {
+    } else {
 #pragma unroll
       for (int v = 0; v < NV; ++v)
 #pragma unroll
@@ -333,8 +345,6 @@ __global__ void __launch_bounds__((bwd_nth<T, TPR, NV>())) k_norm_bwd(const Norm
           if (c < p.N && o0) o0[c] = sg[v][e];
           if (c < p.N && o1) o1[c] = sb[v][e];
         }
-    } else {
-      static_assert(TPR == BWD_NTH || !COLS, "column sums above a wave: one row per block");
     }
   }
 }
@@ -513,7 +523,8 @@ void fwd(const NormArgs<T>& a, int G, hipStream_t st) {
 // blocks of the backward kernel per group: each is another partial row, so no
 // more than fill the CUs (one of 1024 threads, three of 256)
 int64_t bwd_blocks(int elem_bytes, int64_t pieces, int64_t M) {
-  const int tpr = pieces <= 8 ? 8 : pieces <= 32 ? 32 : pieces <= 128 ? 64 : 1024;
+  const int tpr = pieces <= 8 ? 8 : pieces <= 32 ? 32 : pieces <= 128 ? 64 : pieces <= 256 ? 256
+                  : pieces <= 512 ? 512 : 1024;
   const bool small = pieces > 64 && pieces <= 128 && elem_bytes == 2;
   const int64_t most = small ? 768 : 256, want = cdiv(M, (small ? 256 : 1024) / tpr);
   return want < most ? want : most;
@@ -578,6 +589,8 @@ hipError_t launch_norm_bwd(const NormArgs<T>& a, int G, hipStream_t st) {
     else if (pc <= 32) bwd<T, 32, 1>(a, nb, G, st);
     else if (pc <= 64) bwd<T, 64, 1>(a, nb, G, st);
     else if (pc <= 128) bwd<T, 64, 2>(a, nb, G, st);
+    else if (pc <= 256) bwd<T, 256, 1>(a, nb, G, st);
+    else if (pc <= 512) bwd<T, 512, 1>(a, nb, G, st);
     else if (pc <= 1024) bwd<T, 1024, 1>(a, nb, G, st);
     else bwd<T, 1024, 2>(a, nb, G, st);
   } else {
