@@ -563,8 +563,10 @@ typedef struct {
  * For a layer whose own output was activated, g is pigan_act_backward's.
  *
  * The workspace (256-byte aligned; NULL where none is needed) depends on the
- * sizes, the type and which outputs are given; the queries return 0 for invalid
- * arguments and 1 where none is needed.
+ * sizes, the type, which outputs are given and, in 16 bits, on which operands
+ * have rows of whole 16-byte aligned pieces of eight elements (the others may be
+ * copied to it): a query takes the call's own arguments.  The queries return 0
+ * for invalid arguments and 1 where none is needed.
  */
 size_t pigan_linear_forward_workspace(const pigan_linear* a);
 pigan_status pigan_linear_forward(const pigan_linear* a, void* ws, size_t ws_bytes, void* stream);

@@ -194,9 +194,9 @@ MmPlan plan_mm(const double (&STAGE_US)[3][4], int64_t I, int64_t J, int64_t K, 
 // Both products of a reverse pass in one launch, dx on whole contractions: the
 // time is that of the longest block, or of all of them spread over the chip.
 // Taken where it is shorter than one launch after the other (2 us between them).
-bool plan_both(int64_t M, int64_t N, int64_t K, int pairs, int G, MmPlan& dx, MmPlan& dw) {
+bool plan_both(int64_t M, int64_t N, int64_t K, int pairs, int G, MmPlan& dx, MmPlan& dw, double& best) {
   const int64_t nx = (N + 63) / 64, nw = (M + 63) / 64;
-  double best = dx.us + dw.us + 2.0;
+  best = dx.us + dw.us + 2.0;
   bool both = false;
   for (int t = MM_64; t <= MM_128; ++t)
     for (int split = 1; split <= 64 && split <= nw; split *= 2) {
@@ -223,32 +223,63 @@ bool short_ok(const pigan_linear* a) {
   return work <= (a->dt == PIGAN_FP32 ? 1e8 : 2e7) && (a->M + 15) / 16 <= 65535;
 }
 
-// 16-byte pieces of every row: the rows may go straight to LDS
-template <class T> bool rows_aligned(const MmOperand<T>& m, int G) {
-  return (uintptr_t)m.p % 16 == 0 && m.ld % 8 == 0 && (G == 1 || m.gs % 8 == 0) && m.ld < (int64_t(1) << 21);
+// A matrix of a product, or its form in the workspace: rows of whole, aligned
+// pieces, zeros behind them; of fp32 three bf16 planes.
+struct Operand {
+  const pigan_mat* m = nullptr;
+  int64_t rows = 0, cols = 0, Kp = 0;   // Kp > 0: in the workspace
+  size_t at = 0;
+  // as it is, its rows may go straight to LDS
+  bool whole(int G) const { return cols % 8 == 0 && mm_whole(MmOperand<bf16>{(const bf16*)m->p, m->ld, m->gs, 0}, cols, G); }
+  double bytes(int G) const { return 2.0 * G * rows * cols; }
+  void take(Carver& cv, int G, int planes) {
+    Kp = round_up(cols, 8);
+    at = cv.take((size_t)planes * G * rows * Kp * 2);
+  }
+  template <class T> MmOperand<T> get(char* ws, int G) const {
+    if (Kp) return {(const T*)(ws + at), Kp, rows * Kp, (int64_t)G * rows * Kp};
+    return {(const T*)m->p, m->ld, m->gs, 0};
+  }
+  bool direct(char* ws, int G) const { return Kp ? mm_whole(get<bf16>(ws, G), cols, G) : whole(G); }
+};
+
+// 16-bit operands that have to be read element by element or in unaligned pieces
+// are copied first where that costs less than it saves: `us` is what the products
+// take on aligned rows, `ratio` how much longer they take without.
+//   bf16, us: whole pieces | copied | as they are
+//   fwd 4096 x 4096 x 4096    109 | 121 | 193     bwd  230 | 250 | 415
+//   fwd 20000 x 1032 x 1000    70 |     |  83     bwd  120 | 140 | 351
+//   fwd 131072 x 1024 x 1024  324 |     | 474     bwd  570 | 773 | 913
+// (the second and third forward are not copied: x alone would take 20 and 120 us)
+constexpr double LOOSE_FWD = 1.35, LOOSE_BWD = 2.0;
+
+template <int N> void plan_copies(Operand* (&ops)[N], int G, double us, double ratio, Carver& cv) {
+  double cost = 4.0;
+  for (Operand* o : ops)
+    if (o->m && !o->whole(G)) cost += 2 * o->bytes(G) / 4.5e6;
+  if (cost == 4.0 || cost > us * (ratio - 1.0)) return;
+  for (Operand* o : ops)
+    if (o->m && !o->whole(G)) o->take(cv, G, 1);
 }
 
-// bf16 planes of an fp32 matrix in the workspace
-struct Planes {
-  size_t at = 0;
-  int64_t rows = 0, Kp = 0;
-  void take(Carver& cv, int G, int64_t r, int64_t cols) {
-    rows = r;
-    Kp = round_up(cols, 8);
-    at = cv.take((size_t)3 * G * rows * Kp * 2);
-  }
-  MmOperand<bf16> operand(char* ws, int G) const {
-    return {(const bf16*)(ws + at), Kp, rows * Kp, (int64_t)G * rows * Kp};
-  }
-  SplitSet set(char* ws, const pigan_mat& m, int64_t cols) const {
-    return {(const float*)m.p, m.ld, m.gs, rows, cols, Kp, (bf16*)(ws + at)};
-  }
-};
+// fills the workspace forms of the operands that have one
+template <int N> hipError_t fill_operands(const Operand* const (&ops)[N], bool fp32, int G, char* ws, hipStream_t st) {
+  SplitSet split[N];
+  PackSet pack[N];
+  int n = 0;
+  for (const Operand* o : ops)
+    if (o->Kp) {
+      split[n] = {(const float*)o->m->p, o->m->ld, o->m->gs, o->rows, o->cols, o->Kp, (bf16*)(ws + o->at)};
+      pack[n++] = {o->m->p, o->m->ld, o->m->gs, o->rows, o->cols, o->Kp, ws + o->at};
+    }
+  if (!n) return hipSuccess;
+  return fp32 ? launch_split3(split, n, G, st) : launch_pack(pack, n, G, st);
+}
 
 struct ForwardPlan {
   bool brief = false;
   MmPlan mm;
-  Planes x, w;
+  Operand x, w;
   size_t part = 0, total = 0;
 };
 
@@ -259,10 +290,11 @@ ForwardPlan plan_forward(const pigan_linear* a) {
   const int G = a->n_groups;
   const bool fp32 = a->dt == PIGAN_FP32;
   p.mm = plan_mm(STAGE_FWD, a->M, a->N, a->K, fp32 ? 6 : 1, G);
-  if (fp32) {
-    p.x.take(cv, G, a->M, a->K);
-    p.w.take(cv, G, a->N, a->K);
-  }
+  p.x = {&a->x, a->M, a->K};
+  p.w = {&a->w, a->N, a->K};
+  Operand* ops[2] = {&p.x, &p.w};
+  if (!fp32) plan_copies(ops, G, p.mm.us, LOOSE_FWD, cv);
+  else for (Operand* o : ops) o->take(cv, G, 3);
   if (p.mm.n_split > 1) p.part = cv.take((size_t)G * p.mm.n_split * a->M * a->N * 4);
   p.total = cv.off;
   return p;
@@ -270,7 +302,7 @@ ForwardPlan plan_forward(const pigan_linear* a) {
 
 struct BackwardPlan {
   MmPlan dx, dw;
-  Planes g, w, x;
+  Operand g, w, x;   // those that are used
   size_t part_dx = 0, part_dw = 0, part_db = 0, total = 0;
   int db_slots = 0;
   bool both = false;   // dx and dw in one launch
@@ -285,17 +317,21 @@ BackwardPlan plan_backward(const pigan_linear* a) {
   const int G = a->n_groups;
   const bool fp32 = a->dt == PIGAN_FP32;
   const int pairs = fp32 ? 6 : 1;
-  if (fp32 && (a->dx.p || a->dw)) p.g.take(cv, G, a->M, a->N);
   // tiles and splits do not depend on which gradients are wanted: the same sums for each of them
   p.dx = plan_mm(STAGE_BWD, a->M, a->K, a->N, pairs, G);
   p.dw = plan_mm(STAGE_BWD, a->N, a->K, a->M, pairs, G);
-  p.both = plan_both(a->M, a->N, a->K, pairs, G, p.dx, p.dw) && a->dx.p && a->dw;
+  double us;
+  p.both = plan_both(a->M, a->N, a->K, pairs, G, p.dx, p.dw, us) && a->dx.p && a->dw;
+  if (a->dx.p || a->dw) p.g = {&a->g, a->M, a->N};
+  if (a->dx.p) p.w = {&a->w, a->N, a->K};
+  if (a->dw) p.x = {&a->x, a->M, a->K};
+  Operand* ops[3] = {&p.g, &p.w, &p.x};
+  if (!fp32) plan_copies(ops, G, us, LOOSE_BWD, cv);
+  else for (Operand* o : ops) if (o->m) o->take(cv, G, 3);
   if (a->dx.p) {
-    if (fp32) p.w.take(cv, G, a->N, a->K);
     if (p.dx.n_split > 1) p.part_dx = cv.take((size_t)G * p.dx.n_split * a->M * a->K * 4);
   }
   if (a->dw) {
-    if (fp32) p.x.take(cv, G, a->M, a->K);
     if (p.dw.n_split > 1) p.part_dw = cv.take((size_t)G * p.dw.n_split * a->N * a->K * 4);
     const int64_t side = std::min(mm_tile_side(p.dw.tile), 128);   // the smaller of the tiles that it may become
     p.db_slots = p.dw.n_split * (int)((a->K + side - 1) / side);
@@ -331,11 +367,17 @@ int tile_for(const MmPlan& mm, bool direct) {
   return direct ? mm.tile : mm.tile == MM_256 ? (int)MM_128 : mm.tile == MM_64K ? (int)MM_64 : mm.tile;
 }
 
+// T: operands of the products; TO: storage type of the layer
 template <class T, class TO>
-pigan_status forward_tiles(const MmArgs<T, TO>& m, const MmPlan& mm, int G, hipStream_t st) {
-  const bool direct = rows_aligned(m.a, G) && rows_aligned(m.b, G) && (m.pairs != 1 || m.K % 8 == 0) && m.o.J % 8 == 0;
-  HIP_TRY(launch_mm_fwd(m, tile_for(mm, direct), direct, G, st));
-  if (mm.n_split > 1) HIP_TRY(launch_mm_join_fwd(m.o, G, st));
+pigan_status forward_tiles(const pigan_linear* a, const ForwardPlan& p, char* ws, hipStream_t st) {
+  const int G = a->n_groups;
+  const Operand* ops[2] = {&p.x, &p.w};
+  HIP_TRY(fill_operands(ops, sizeof(TO) == 4, G, ws, st));
+  const bool direct = p.x.direct(ws, G) && p.w.direct(ws, G);
+  MmArgs<T, TO> m{p.x.get<T>(ws, G), p.w.get<T>(ws, G), a->K, sizeof(TO) == 4 ? 6 : 1,
+                  forward_out<TO>(a, p.mm, (float*)(ws + p.part)), nullptr};
+  HIP_TRY(launch_mm_fwd(m, tile_for(p.mm, direct), direct, G, st));
+  if (p.mm.n_split > 1) HIP_TRY(launch_mm_join_fwd(m.o, G, st));
   return PIGAN_OK;
 }
 
@@ -344,7 +386,6 @@ pigan_status run_forward(const pigan_linear* a, const ForwardPlan& p, char* ws, 
   const double es = (double)esize(a->dt), MN = (double)a->M * a->N;
   ProfScope prof(st, "linear_fwd", 2.0 * G * MN * a->K,
                  G * (es * ((double)a->M * a->K + (double)a->N * a->K + MN * (1 + !!a->pre.p + !!a->add.p)) + 4.0 * a->N));
-  float* part = (float*)(ws + p.part);
   if (p.brief)
     return by_dtype(a->dt, [&](auto t) -> pigan_status {
       typedef decltype(t) T;
@@ -352,36 +393,31 @@ pigan_status run_forward(const pigan_linear* a, const ForwardPlan& p, char* ws, 
       HIP_TRY(launch_short_fwd(m, G, st));
       return PIGAN_OK;
     });
-  if (a->dt == PIGAN_FP32) {
-    const SplitSet sets[2] = {p.x.set(ws, a->x, a->K), p.w.set(ws, a->w, a->K)};
-    HIP_TRY(launch_split3(sets, 2, G, st));
-    MmArgs<bf16, float> m{p.x.operand(ws, G), p.w.operand(ws, G), a->K, 6, forward_out<float>(a, p.mm, part), nullptr};
-    return forward_tiles(m, p.mm, G, st);
-  }
-  if (a->dt == PIGAN_BF16) {
-    MmArgs<bf16, bf16> m{operand<bf16>(a->x), operand<bf16>(a->w), a->K, 1, forward_out<bf16>(a, p.mm, part), nullptr};
-    return forward_tiles(m, p.mm, G, st);
-  }
-  MmArgs<f16, f16> m{operand<f16>(a->x), operand<f16>(a->w), a->K, 1, forward_out<f16>(a, p.mm, part), nullptr};
-  return forward_tiles(m, p.mm, G, st);
+  return a->dt == PIGAN_FP32 ? forward_tiles<bf16, float>(a, p, ws, st)
+         : a->dt == PIGAN_BF16 ? forward_tiles<bf16, bf16>(a, p, ws, st)
+                               : forward_tiles<f16, f16>(a, p, ws, st);
 }
 
 // T: operands of the products; TO: storage type of the layer
 template <class T, class TO>
-pigan_status backward_products(const pigan_linear* a, const BackwardPlan& p, const MmOperand<T>& g,
-                               const MmOperand<T>& w, const MmOperand<T>& x, bool padded, char* ws, hipStream_t st) {
+pigan_status backward_products(const pigan_linear* a, const BackwardPlan& p, char* ws, hipStream_t st) {
   const int G = a->n_groups;
   const double es = (double)esize(a->dt), MN = (double)a->M * a->N, MK = (double)a->M * a->K, NK = (double)a->N * a->K;
-  // whole pieces of columns (the padded planes hold zeros behind theirs)
-  const bool whole = (padded || a->N % 8 == 0) && a->K % 8 == 0;
-  const bool direct_dx = rows_aligned(g, G) && rows_aligned(w, G) && whole;
-  const bool direct_dw = rows_aligned(g, G) && rows_aligned(x, G) && whole;
-  const int pairs = padded ? 6 : 1;
-  MmArgs<T, TO> dx{g, w, a->N, pairs, {}, nullptr};
-  MmArgs<T, float> dw{g, x, a->M, pairs, {}, nullptr};
+  const Operand* ops[3] = {&p.g, &p.w, &p.x};
+  HIP_TRY(fill_operands(ops, sizeof(TO) == 4, G, ws, st));
+  const bool direct_dx = a->dx.p && p.g.direct(ws, G) && p.w.direct(ws, G);
+  const bool direct_dw = a->dw && p.g.direct(ws, G) && p.x.direct(ws, G);
+  const int pairs = sizeof(TO) == 4 ? 6 : 1;
+  MmArgs<T, TO> dx{};
+  MmArgs<T, float> dw{};
+  dx.pairs = dw.pairs = pairs;
+  dx.a = dw.a = p.g.get<T>(ws, G);
+  dx.K = a->N;
+  dw.K = a->M;
   const int tile_dw = tile_for(p.dw, direct_dw), side = mm_tile_side(tile_dw);
   const int slots = p.dw.n_split * (int)((a->K + side - 1) / side);
   if (a->dx.p) {
+    dx.b = p.w.get<T>(ws, G);
     dx.o.I = a->M;
     dx.o.J = a->K;
     dx.o.act = a->act;
@@ -392,6 +428,7 @@ pigan_status backward_products(const pigan_linear* a, const BackwardPlan& p, con
     dx.o.part = p.dx.n_split > 1 ? (float*)(ws + p.part_dx) : nullptr;
   }
   if (a->dw) {
+    dw.b = p.x.get<T>(ws, G);
     dw.o.I = a->N;
     dw.o.J = a->K;
     dw.o.n_split = p.dw.n_split;
@@ -428,20 +465,9 @@ pigan_status run_backward(const pigan_linear* a, const BackwardPlan& p, char* ws
     return PIGAN_OK;
   }
   if (a->dx.p || a->dw) {
-    pigan_status s;
-    if (a->dt == PIGAN_FP32) {
-      SplitSet sets[3];
-      int n = 0;
-      sets[n++] = p.g.set(ws, a->g, a->N);
-      if (a->dx.p) sets[n++] = p.w.set(ws, a->w, a->K);
-      if (a->dw) sets[n++] = p.x.set(ws, a->x, a->K);
-      HIP_TRY(launch_split3(sets, n, G, st));
-      s = backward_products<bf16, float>(a, p, p.g.operand(ws, G), p.w.operand(ws, G), p.x.operand(ws, G), true, ws, st);
-    } else {
-      s = a->dt == PIGAN_BF16
-              ? backward_products<bf16, bf16>(a, p, operand<bf16>(a->g), operand<bf16>(a->w), operand<bf16>(a->x), false, ws, st)
-              : backward_products<f16, f16>(a, p, operand<f16>(a->g), operand<f16>(a->w), operand<f16>(a->x), false, ws, st);
-    }
+    const pigan_status s = a->dt == PIGAN_FP32   ? backward_products<bf16, float>(a, p, ws, st)
+                           : a->dt == PIGAN_BF16 ? backward_products<bf16, bf16>(a, p, ws, st)
+                                                 : backward_products<f16, f16>(a, p, ws, st);
     if (s != PIGAN_OK) return s;
   }
   if (a->db && !a->dw) {   // by themselves

@@ -41,8 +41,12 @@ enum MmTile { MM_64 = 0, MM_128 = 1, MM_256 = 2, MM_64K = 3 };
 inline int mm_tile_side(int t) { return t == MM_128 ? 128 : t == MM_256 ? 256 : 64; }
 
 // direct: both operands may go straight to LDS: 16-byte aligned rows (a tile's
-// extent below 2^31 bytes) of whole pieces, along the row and in the result's
-// columns; planes (pairs = 6) hold zeros behind their rows up to a whole piece
+// extent below 2^31 bytes) of whole pieces; copies (pack) and planes (split3), which
+// pairs = 6 needs, hold zeros behind their rows up to a whole piece
+template <class T> bool mm_whole(const MmOperand<T>& m, int64_t cols, int G) {
+  return (uintptr_t)m.p % 16 == 0 && m.ld % 8 == 0 && (G == 1 || m.gs % 8 == 0) && m.plane % 8 == 0 &&
+         (cols + 7) / 8 * 8 <= m.ld && m.ld < (int64_t(1) << 21);
+}
 template <class T, class TO>
 hipError_t launch_mm_fwd(const MmArgs<T, TO>& a, int tile, bool direct, int G, hipStream_t st);
 template <class T, class TO>
@@ -71,5 +75,13 @@ struct SplitSet {
   bf16* dst;                 // [3][G][rows][Kp]
 };
 hipError_t launch_split3(const SplitSet* sets, int n, int G, hipStream_t st);
+
+// 16-bit matrices with rows at any address to rows of whole, aligned pieces, zeros
+// behind them: up to three in one launch
+struct PackSet {
+  const void* src; int64_t ld, gs; int64_t rows, cols, Kp;
+  void* dst;                 // [G][rows][Kp]
+};
+hipError_t launch_pack(const PackSet* sets, int n, int G, hipStream_t st);
 
 }  // namespace pigan

@@ -124,6 +124,23 @@ __global__ void __launch_bounds__(256) k_split3(const SplitSets sets, int G) {
   }
 }
 
+struct PackSets {
+  PackSet s[3];
+};
+
+// Bound by memory; copies bits, so bf16 stands for either type.
+__global__ void __launch_bounds__(256) k_pack(const PackSets sets) {
+  const PackSet s = sets.s[blockIdx.y];
+  const int g = blockIdx.z;
+  const int64_t vpr = s.Kp / 8, total = s.rows * vpr;
+  const bf16* src = (const bf16*)s.src + g * s.gs;
+  bf16* dst = (bf16*)s.dst + g * s.rows * s.Kp;
+  for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < total; q += (int64_t)gridDim.x * 256) {
+    const int64_t r = q / vpr, c = (q - r * vpr) * 8;
+    *(piece_t*)(dst + r * s.Kp + c) = piece_load(src + r * s.ld + c, s.cols - c);
+  }
+}
+
 }  // namespace
 
 template <class T, int P>
@@ -145,17 +162,30 @@ hipError_t launch_short_fwd(const MmArgs<T, T>& a, int G, hipStream_t st) {
   return hipGetLastError();
 }
 
-hipError_t launch_split3(const SplitSet* sets, int n, int G, hipStream_t st) {
-  if (n < 1 || n > 3) return hipErrorInvalidValue;
-  SplitSets s{};
+// the sets of a launch, and blocks for the largest of them; 0 where one cannot be
+template <class Sets, class Set> unsigned sets_of(Sets& all, const Set* sets, int n) {
   int64_t most = 1;
+  if (n < 1 || n > 3) return 0;
   for (int i = 0; i < n; ++i) {
-    s.s[i] = sets[i];
+    all.s[i] = sets[i];
     const int64_t blocks = (sets[i].rows * (sets[i].Kp / 8) + 255) / 256;
-    if (sets[i].Kp % 8 || sets[i].Kp < sets[i].cols) return hipErrorInvalidValue;
+    if (sets[i].Kp % 8 || sets[i].Kp < sets[i].cols) return 0;
     if (blocks > most) most = blocks;
   }
-  k_split3<<<dim3((unsigned)(most < 4096 ? most : 4096), n, G), 256, 0, st>>>(s, G);
+  return (unsigned)(most < 4096 ? most : 4096);
+}
+hipError_t launch_split3(const SplitSet* sets, int n, int G, hipStream_t st) {
+  SplitSets s{};
+  const unsigned blocks = sets_of(s, sets, n);
+  if (!blocks) return hipErrorInvalidValue;
+  k_split3<<<dim3(blocks, n, G), 256, 0, st>>>(s, G);
+  return hipGetLastError();
+}
+hipError_t launch_pack(const PackSet* sets, int n, int G, hipStream_t st) {
+  PackSets s{};
+  const unsigned blocks = sets_of(s, sets, n);
+  if (!blocks) return hipErrorInvalidValue;
+  k_pack<<<dim3(blocks, n, G), 256, 0, st>>>(s);
   return hipGetLastError();
 }
 

@@ -393,7 +393,7 @@ template <int MT, int NT, int WN> constexpr int mm_stage() { return (64 * MT + 3
 // Block n of `blocks` of the product, with two stages of LDS for each of KG groups
 // of 2 x WN waves: the groups share the contraction of the tile and meet in LDS, in
 // order, before the epilogue.
-template <class T, class TO, int KIND, int MT, int NT, int WN, int KG = 1>
+template <class T, class TO, int KIND, int MT, int NT, int WN, bool WHOLE, int KG = 1>
 __device__ __forceinline__ void mm_piped(const MmArgs<T, TO>& p, uint32_t n, uint32_t blocks, char* s0, char* s1) {
   static_assert(KG == 1 || MT * NT == 1, "groups: tiles of one fragment a wave");
   constexpr int BM = 64 * MT, BN = 32 * NT * WN, BK = 64, STAGE_A = BM * BK * 2, NW = 2 * WN, NTH = 64 * NW;
@@ -592,7 +592,13 @@ __device__ __forceinline__ void mm_piped(const MmArgs<T, TO>& p, uint32_t n, uin
       if constexpr (KIND == MM_DW) db[0] += ((const float*)(s1 + q * mm_stage<MT, NT, WN>()))[tid];
     }
   }
-  mm_results<KIND, true>(p.o, at.g, at.split, i0 + 32 * MT * wm, j0 + 32 * NT * wn, acc);
+  // element by element only where a wave's columns reach over the edge (dw has no
+  // activation: both ways in one kernel)
+  const int64_t iw = i0 + 32 * MT * wm, jw = j0 + 32 * NT * wn;
+  if ((WHOLE && (KIND != MM_DW || p.o.J % 8 == 0)) || jw + 32 * NT <= p.o.J)
+    mm_results<KIND, true>(p.o, at.g, at.split, iw, jw, acc);
+  else
+    mm_results<KIND, false>(p.o, at.g, at.split, iw, jw, acc);
   if constexpr (KIND == MM_DW) {
     if (p.part_db) {
       float* sums = (float*)s0;   // [WN][BM]
@@ -610,12 +616,12 @@ __device__ __forceinline__ void mm_piped(const MmArgs<T, TO>& p, uint32_t n, uin
   }
 }
 
-template <class T, class TO, int KIND, int MT, int NT, int WN, int OCC, int KG = 1>
+template <class T, class TO, int KIND, int MT, int NT, int WN, int OCC, bool WHOLE, int KG = 1>
 __global__ void __launch_bounds__(128 * WN * KG) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
 k_mm_piped(const MmArgs<T, TO> p) {
   __shared__ __attribute__((aligned(1024))) char s0[KG * mm_stage<MT, NT, WN>()];
   __shared__ __attribute__((aligned(1024))) char s1[KG * mm_stage<MT, NT, WN>()];
-  mm_piped<T, TO, KIND, MT, NT, WN, KG>(p, blockIdx.x, gridDim.x, s0, s1);
+  mm_piped<T, TO, KIND, MT, NT, WN, WHOLE, KG>(p, blockIdx.x, gridDim.x, s0, s1);
 }
 
 // ---------------------------------------------------------------------------
@@ -677,10 +683,18 @@ uint32_t mm_blocks(const MmArgs<T, TO>& a, int tile, bool direct, int G) {
   const int64_t rows = (a.o.I + side - 1) / side, cols = (a.o.J + side - 1) / side;
   if (a.o.I < 1 || a.o.J < 1 || a.K < 1 || a.o.n_split < 1 || G < 1 || G > 65535 ||
       (double)rows * cols * a.o.n_split * G > 1e9 || a.o.n_split > (a.K + 63) / 64 || (a.o.n_split > 1 && !a.o.part) ||
-      (a.pairs != 1 && a.pairs != 6) || a.K > 0x7fffffff || (!direct && tile == MM_256) ||
-      (direct && (a.o.J % 8 || (KIND != MM_DW && a.pairs == 1 && a.K % 8))))
+      (a.pairs != 1 && a.pairs != 6) || a.K > 0x7fffffff || (!direct && (tile == MM_256 || tile == MM_64K)) ||
+      (direct && !(mm_whole(a.a, KIND == MM_DW ? a.o.I : a.K, G) && mm_whole(a.b, KIND == MM_FWD ? a.K : a.o.J, G))))
     return 0;
   return (uint32_t)(rows * cols * a.o.n_split * G);
+}
+
+template <class T, class TO, int KIND, bool WHOLE>
+void mm_direct(const MmArgs<T, TO>& a, int tile, uint32_t count, hipStream_t st) {
+  if (tile == MM_256) k_mm_piped<T, TO, KIND, 4, 2, 4, 2, WHOLE><<<count, 512, 0, st>>>(a);
+  else if (tile == MM_128) k_mm_piped<T, TO, KIND, 2, 2, 2, 2, WHOLE><<<count, 256, 0, st>>>(a);
+  else if (tile == MM_64) k_mm_piped<T, TO, KIND, 1, 1, 2, 4, WHOLE><<<count, 256, 0, st>>>(a);
+  else k_mm_piped<T, TO, KIND, 1, 1, 2, 4, WHOLE, 4><<<count, 1024, 0, st>>>(a);
 }
 
 template <class T, class TO, int KIND>
@@ -688,10 +702,8 @@ hipError_t mm_launch(const MmArgs<T, TO>& a, int tile, bool direct, int G, hipSt
   const uint32_t count = mm_blocks<T, TO, KIND>(a, tile, direct, G);
   if (!count) return hipErrorInvalidValue;
   if (direct) {
-    if (tile == MM_256) k_mm_piped<T, TO, KIND, 4, 2, 4, 2><<<count, 512, 0, st>>>(a);
-    else if (tile == MM_128) k_mm_piped<T, TO, KIND, 2, 2, 2, 2><<<count, 256, 0, st>>>(a);
-    else if (tile == MM_64) k_mm_piped<T, TO, KIND, 1, 1, 2, 4><<<count, 256, 0, st>>>(a);
-    else k_mm_piped<T, TO, KIND, 1, 1, 2, 4, 4><<<count, 1024, 0, st>>>(a);
+    if (KIND == MM_DW || a.o.J % 8 == 0) mm_direct<T, TO, KIND, true>(a, tile, count, st);
+    else if constexpr (KIND != MM_DW) mm_direct<T, TO, KIND, false>(a, tile, count, st);
   } else {
     if (tile == MM_128) k_mm_any<T, TO, KIND, 2, 2><<<count, 256, 0, st>>>(a);
     else k_mm_any<T, TO, KIND, 1, 1><<<count, 256, 0, st>>>(a);
