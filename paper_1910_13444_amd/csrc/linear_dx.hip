@@ -6,7 +6,7 @@ namespace pigan {
 
 // Both products of a small layer's reverse pass: neither fills the chip for long,
 // and side by side they fill each other's waits (21 layers of 512 x 256 x 256 fp16:
-// 10.4 us and 11.2 us apart).  The one with the longer blocks comes first.
+// 13 us; 10.4 us and 11.2 us apart).  The one with the longer blocks comes first.
 template <class T, class TO, int MT, int NT, int OCC, bool WHOLE>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
 k_mm_both(const MmArgs<T, TO> dx, const MmArgs<T, float> dw, uint32_t n_dx, uint32_t n_dw, int dw_first) {

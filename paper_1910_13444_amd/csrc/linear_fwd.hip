@@ -14,7 +14,8 @@ namespace {
 // only the blocks on its diagonal, which pair a chunk with itself, are used.  The
 // lanes of a load then cover 64 P consecutive bytes of a row of w, and there are P
 // times as many blocks.  The waves' sums meet in LDS, in order.
-// Bound by the bytes of w (one row of x, 8192 -> 2048 bf16: P = 1 15.6 us).
+// Bound by the bytes of w (one row of x, 8192 -> 2048 bf16: 10.3 us, 3.3 TB/s, of
+// which a launch by itself is 2; P = 1 15.6 us).
 // ---------------------------------------------------------------------------
 template <class T> struct ShortMma;
 template <> struct ShortMma<bf16> {
@@ -92,7 +93,8 @@ __global__ void __launch_bounds__(64 * NW) k_short_fwd(const MmArgs<T, T> p) {
 // ---------------------------------------------------------------------------
 // bf16 planes of fp32 matrices: x0 and x1 are x and the rest cut to eight
 // significand bits (towards zero, so that no plane overflows), x2 what is left:
-// all 24 bits.  An infinity or NaN goes to x0 alone.
+// all 24 bits.  An infinity or NaN goes to x0 alone.  Bound by memory: 4 bytes read
+// and 6 written per value (1001 x 2000, 513 x 2000 and 1001 x 513 in 7.5 us, 4.7 TB/s).
 // ---------------------------------------------------------------------------
 struct SplitSets {
   SplitSet s[3];
@@ -128,7 +130,8 @@ struct PackSets {
   PackSet s[3];
 };
 
-// Bound by memory; copies bits, so bf16 stands for either type.
+// Bound by memory; copies bits, so bf16 stands for either type (two of 4096 x 4096
+// in the 12 us between the product's 109 and 121).
 __global__ void __launch_bounds__(256) k_pack(const PackSets sets) {
   const PackSet s = sets.s[blockIdx.y];
   const int g = blockIdx.z;

@@ -214,7 +214,9 @@ __device__ __forceinline__ void mm_store_db(const MmArgs<T, TO>& p, int g, int s
 // ---------------------------------------------------------------------------
 // Operands of any alignment: stages pass through registers, one ahead of the
 // products, with zeros past the end of k.  Rows of a tile past the end of the
-// matrix repeat its last row; their products are not stored.
+// matrix repeat its last row; their products are not stored.  Bound by the waits
+// for those registers (bf16 20,000 x 1032 x 1000 with rows 3 elements apart: 83 us
+// where whole pieces take 70, 131,072 x 1024 x 1024 474 and 324).
 // ---------------------------------------------------------------------------
 template <class T, class TO, int KIND, int MT, int NT>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
@@ -360,9 +362,14 @@ k_mm_any(const MmArgs<T, TO> p) {
 //              a third less from LDS but leave the matrix cores idle at every wait
 //              and in the epilogue: 8192^3 bf16 1170 against 1267 TFLOP/s, 262,144 x
 //              1024 x 1024 with a residual 786 against 703 us.)
+//              Bound by the matrix cores' clock under load in the loop, by memory in
+//              the epilogue: 131,072 x 1024 x 1024 dw 235 us, 1170 TFLOP/s; dx with a
+//              gelu's slope 428 us, 640.
 //   128 x 128  two blocks of four waves per CU, which fill each other's waits
+//              (fp32 by six products, 1001 x 2000 x 513 dx and dw in one launch: 54 us)
 //   64 x 64    four blocks per CU, for few tiles; for very few, one block of four
-//              groups that share the contraction
+//              groups that share the contraction (1024 x 2000 x 1024 in 17 us, bound
+//              by its eight stages one after the other)
 // The loads are buffer loads: what is past the end of the matrix is out of the
 // buffer's range and arrives as zeros.
 // ---------------------------------------------------------------------------
