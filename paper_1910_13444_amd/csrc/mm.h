@@ -94,8 +94,10 @@ __device__ __forceinline__ void mm_epilogue(const MmOut<TO>& o, int g, int64_t i
 // them: the accumulators stay in registers only if every loop unrolls).  What the
 // epilogue reads is requested D - 1 fragments ahead, as many as the registers hold
 // beside the accumulators: asked for one by one, each of 32 reads was waited for
-// by itself, 30 us of the 60 that a 256 x 256 tile took at K = 1024.  WHOLE: the
-// columns come in whole eights.
+// by itself, 30 us of the 60 that a 256 x 256 tile took at K = 1024.  The fragments
+// of a row follow each other, so that the halves of a 128-byte line do (262,144 x
+// 1024 x 1024 with a residual: 1.36 GB read and 0.56 written; column by column of
+// fragments 1.57 and 0.67).  WHOLE: the columns come in whole eights.
 template <int KIND, int ACT, bool PART, bool WHOLE, class TO, int MT, int NT>
 __device__ __forceinline__ void mm_store(const MmOut<TO>& o, int g, int split, int64_t i0, int64_t j0,
                                          const f32x16 (&acc)[MT][NT]) {
@@ -107,10 +109,10 @@ __device__ __forceinline__ void mm_store(const MmOut<TO>& o, int g, int split, i
   Octet<TO> pre[PRE ? D : 1][2], add[ADD ? D : 1][2];
   // f(half, row, column, columns that are there) of fragment n
   auto each = [&](int n, auto f) __attribute__((always_inline)) {
-    const int64_t j = j0 + 32 * (n / MT) + mm_col(lane);
+    const int64_t j = j0 + 32 * (n % NT) + mm_col(lane);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int64_t i = i0 + 32 * (n % MT) + 16 * h + (lane & 15);
+      const int64_t i = i0 + 32 * (n / NT) + 16 * h + (lane & 15);
       if (i < o.I && j < o.J) f(h, i, j, WHOLE ? (int64_t)8 : o.J - j);
     }
   };
@@ -124,23 +126,24 @@ __device__ __forceinline__ void mm_store(const MmOut<TO>& o, int g, int split, i
   if constexpr (PRE || ADD)
 #pragma unroll
     for (int n = 0; n < D - 1; ++n) request(n);
-  float bias[8];
+  float bias[KIND == MM_FWD ? NT : 1][8];
+  if constexpr (KIND == MM_FWD && !PART)
+#pragma unroll
+    for (int b = 0; b < NT; ++b) {
+      const int64_t j = j0 + 32 * b + mm_col(lane);
+      vec_load<8>(o.bias && (!WHOLE || j < o.J) ? o.bias + g * o.J : nullptr, j, WHOLE ? j + 8 : o.J, 0.0f, bias[b]);
+    }
 #pragma unroll
   for (int n = 0; n < NF; ++n) {
     if constexpr (PRE || ADD)
       if (n + D - 1 < NF) request(n + D - 1);
-    if constexpr (KIND == MM_FWD && !PART)
-      if (n % MT == 0) {
-        const int64_t j = j0 + 32 * (n / MT) + mm_col(lane);
-        vec_load<8>(o.bias && (!WHOLE || j < o.J) ? o.bias + g * o.J : nullptr, j, WHOLE ? j + 8 : o.J, 0.0f, bias);
-      }
     float v[16];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) v[r] = acc[n % MT][n / MT][r];
+    for (int r = 0; r < 16; ++r) v[r] = acc[n / NT][n % NT][r];
     mm_exchange(v);
     each(n, [&](int h, int64_t i, int64_t j, int64_t valid) __attribute__((always_inline)) {
       if constexpr (PART) store8(o.part + (((int64_t)g * o.n_split + split) * o.I + i) * o.J + j, valid, v + 8 * h);
-      else mm_epilogue<KIND, ACT>(o, g, i, j, valid, pre[PRE ? n % D : 0][h], add[ADD ? n % D : 0][h], bias, v + 8 * h);
+      else mm_epilogue<KIND, ACT>(o, g, i, j, valid, pre[PRE ? n % D : 0][h], add[ADD ? n % D : 0][h], bias[KIND == MM_FWD ? n % NT : 0], v + 8 * h);
     });
   }
 }
