@@ -273,7 +273,7 @@ k_mm_any(const MmArgs<T, TO> p) {
       const T* base = isA ? pa + qa * p.a.plane : pb + qb * p.b.plane;
       if (along) {
         const int row = q * 8 + (lane >> 3);
-        const int64_t k = k0 + ((lane & 7) ^ (row & 7)) * 8;
+        const int64_t k = k0 + ((lane & 7) ^ ((row >> 1) & 7)) * 8;
         r[n] = piece_load(base + (row < left ? row : left - 1) * ld + k, p.K - k);
       } else {
         const int spr = side / 8, row = (q * 64 + lane) / spr, seg = (lane % spr) ^ mm_swizzle(side, row);
@@ -290,7 +290,7 @@ k_mm_any(const MmArgs<T, TO> p) {
   const int grp = lane >> 4, t16 = lane & 15, rr = t16 >> 2, q4 = t16 & 3, kb = 8 * (lane >> 5);
   auto frag_at = [&](const char* base, bool along, int side, int c, int blk) __attribute__((always_inline)) -> frag {
     if (along)
-      return *(const frag*)(base + (lane & 31) * 128 + (((2 * c + (lane >> 5)) ^ (lane & 7)) << 4) + blk * 4096);
+      return *(const frag*)(base + (lane & 31) * 128 + (((2 * c + (lane >> 5)) ^ ((lane >> 1) & 7)) << 4) + blk * 4096);
     const int byte = (32 * blk + 16 * (grp & 1) + 4 * q4) * 2, pitch = side * 2;
     const char* q = base + (c * 16 + kb + rr) * pitch + (((byte >> 4) ^ mm_swizzle(side, rr)) << 4) + (byte & 15);
     const u32x2 lo = lds_read_tr<T>(q), hi = lds_read_tr<T>(q + 4 * pitch);
@@ -455,15 +455,18 @@ __device__ __forceinline__ void mm_piped(const MmArgs<T, TO>& p, uint32_t n, uin
   // a group is eight rows of an operand with k along the row, 512 / side rows of
   // one with k down the rows; a wave's groups are wave, wave + NW, ...
   constexpr uint32_t OUT = 0xffffffffu;   // never in range
+  // k of the lane's piece (k along the row): a row's eight pieces are exchanged by
+  // half its number, so that 16 rows' pieces of one k lie in different banks (by the
+  // number itself, rows r and r + 8 share theirs)
+  const int seg_k = ((lane & 7) ^ (4 * (wave & 1) + (lane >> 4))) * 8;
   auto lane_off = [&](bool along, int side, int64_t ld, int left) __attribute__((always_inline)) -> uint32_t {
-    if (along) return (uint32_t)((8 * wave + (lane >> 3)) * ld * 2 + (((lane & 7) ^ (lane >> 3)) * 16));
+    if (along) return (uint32_t)((8 * wave + (lane >> 3)) * ld * 2 + seg_k * 2);
     const int spr = side / 8, row = wave * (64 / spr) + lane / spr, seg = (lane % spr) ^ mm_swizzle(side, row);
     return seg * 8 < left ? (uint32_t)(row * ld * 2 + seg * 16) : OUT;
   };
   const uint32_t off_a = lane_off(AK, BM, p.a.ld, left_a), off_b = lane_off(BKC, BN, p.b.ld, left_b);
   const uint32_t step_a = (uint32_t)(NW * (AK ? 8 : 512 / BM) * p.a.ld * 2);
   const uint32_t step_b = (uint32_t)(NW * (BKC ? 8 : 512 / BN) * p.b.ld * 2);
-  const int seg_k = ((lane & 7) ^ (lane >> 3)) * 8;   // k of the lane's piece (k along the row)
 
   // the next stage to load: its first elements, its k, the stages left of its plane pair
   const int64_t adv_a = AK ? BK : BK * p.a.ld, adv_b = BKC ? BK : BK * p.b.ld;
@@ -515,7 +518,7 @@ __device__ __forceinline__ void mm_piped(const MmArgs<T, TO>& p, uint32_t n, uin
   auto frag_at = [&](const char* stage, int from, bool along, int side, int c, int blk)
       __attribute__((always_inline)) -> frag {
     if (along)
-      return *(const frag*)(stage + (from + (lane & 31) * 128 + (((2 * c + (lane >> 5)) ^ (lane & 7)) << 4) + blk * 4096));
+      return *(const frag*)(stage + (from + (lane & 31) * 128 + (((2 * c + (lane >> 5)) ^ ((lane >> 1) & 7)) << 4) + blk * 4096));
     const int byte = (32 * blk + 16 * (grp & 1) + 4 * q4) * 2, pitch = side * 2;
     const int off = from + (kb + rr) * pitch + (((byte >> 4) ^ mm_swizzle(side, rr)) << 4) + (byte & 15) + c * 16 * pitch;
     const u32x2 lo = lds_read_tr<T>(stage + off), hi = lds_read_tr<T>(stage + (off + 4 * pitch));
