@@ -247,9 +247,9 @@ struct Operand {
 // are copied first where that costs less than it saves: `us` is what the products
 // take on aligned rows, `ratio` how much longer they take without.
 //   bf16, us: whole pieces | copied | as they are
-//   fwd 4096 x 4096 x 4096    109 | 121 | 193     bwd  230 | 250 | 415
-//   fwd 20000 x 1032 x 1000    70 |     |  83     bwd  120 | 140 | 351
-//   fwd 131072 x 1024 x 1024  324 |     | 474     bwd  570 | 773 | 913
+//   fwd 4096 x 4096 x 4096    107 | 118 | 193     bwd  227 | 247 | 415
+//   fwd 20000 x 1032 x 1000    70 |     |  83     bwd  122 | 140 | 351
+//   fwd 131072 x 1024 x 1024  284 |     | 466     bwd  529 | 736 | 913
 // (the second and third forward are not copied: x alone would take 20 and 120 us)
 constexpr double LOOSE_FWD = 1.35, LOOSE_BWD = 2.0;
 

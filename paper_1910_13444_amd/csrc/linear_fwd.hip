@@ -131,7 +131,7 @@ struct PackSets {
 };
 
 // Bound by memory; copies bits, so bf16 stands for either type (two of 4096 x 4096
-// in the 12 us between the product's 109 and 121).
+// in the 11 us between the product's 107 and 118).
 __global__ void __launch_bounds__(256) k_pack(const PackSets sets) {
   const PackSet s = sets.s[blockIdx.y];
   const int g = blockIdx.z;

@@ -219,7 +219,7 @@ __device__ __forceinline__ void mm_store_db(const MmArgs<T, TO>& p, int g, int s
 // products, with zeros past the end of k.  Rows of a tile past the end of the
 // matrix repeat its last row; their products are not stored.  Bound by the waits
 // for those registers (bf16 20,000 x 1032 x 1000 with rows 3 elements apart: 83 us
-// where whole pieces take 70, 131,072 x 1024 x 1024 474 and 324).
+// where whole pieces take 70, 131,072 x 1024 x 1024 466 and 284).
 // ---------------------------------------------------------------------------
 template <class T, class TO, int KIND, int MT, int NT>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
@@ -363,11 +363,12 @@ k_mm_any(const MmArgs<T, TO> p) {
 // chunks' time to land and this stage's buffer has no reader left.
 //   256 x 256  eight waves of 128 x 64, two per SIMD.  (Four waves of 128 x 128 read
 //              a third less from LDS but leave the matrix cores idle at every wait
-//              and in the epilogue: 8192^3 bf16 1170 against 1267 TFLOP/s, 262,144 x
-//              1024 x 1024 with a residual 786 against 703 us.)
+//              and in the epilogue: 8192^3 bf16 1170 against 1267 TFLOP/s before the
+//              pieces' banks were spread, which made it 1354; 262,144 x 1024 x 1024
+//              with a residual 786 against 703 us, then 674.)
 //              Bound by the matrix cores' clock under load in the loop, by memory in
-//              the epilogue: 131,072 x 1024 x 1024 dw 235 us, 1170 TFLOP/s; dx with a
-//              gelu's slope 428 us, 640.
+//              the epilogue: 131,072 x 1024 x 1024 dw 235 us, 1170 TFLOP/s; dx 330 us,
+//              with relu's slope 414 (pre is read), with gelu's 420 to 480.
 //   128 x 128  two blocks of four waves per CU, which fill each other's waits
 //              (fp32 by six products, 1001 x 2000 x 513 dx and dw in one launch: 54 us)
 //   64 x 64    four blocks per CU, for few tiles; for very few, one block of four
