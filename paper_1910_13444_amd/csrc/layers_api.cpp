@@ -110,7 +110,8 @@ pigan_status check_backward(const pigan_linear* a) {
   const size_t es = esize(a->dt);
   const int32_t G = a->n_groups;
   const bool rows = a->M > 0;
-  if (!a->dx.p && !a->dw && !a->db) return fail(PIGAN_EINVAL, "no output: dx, dw and db are null");
+  // without rows dx has no elements, and may have no address
+  if (rows && !a->dx.p && !a->dw && !a->db) return fail(PIGAN_EINVAL, "no output: dx, dw and db are null");
   if (rows || a->g.p)
     if (pigan_status st = check_mat(a->g, "g", G, a->M, a->N, es)) return st;
   if (a->dx.p) {
@@ -500,8 +501,8 @@ pigan_status check_norm(const pigan_norm* a) {
 pigan_status check_norm_backward(const pigan_norm* a) {
   if (pigan_status st = check_norm(a)) return st;
   const size_t es = esize(a->dt);
+  if (a->M == 0) return PIGAN_OK;   // dx has no elements, and may have no address
   if (!a->dx.p && !a->dgamma && !a->dbeta) return fail(PIGAN_EINVAL, "no output: dx, dgamma and dbeta are null");
-  if (a->M == 0) return PIGAN_OK;
   if (!a->mean || !a->rstd) return fail(PIGAN_EINVAL, "mean and rstd: null pointer");
   if (pigan_status st = check_mat(a->dy, "dy", a->n_groups, a->M, a->N, es)) return st;
   if (a->add.p)
