@@ -498,7 +498,7 @@ pigan_status pigan_adam_update(int64_t n, float* params, const float* grads, flo
  * A matrix operand is n_groups matrices (independent layers of one shape);
  * element (r, c) of group g is p[g * gs + r * ld + c].  ld must be at least the
  * number of columns and gs (for more than one group) at least the extent of a
- * group; no alignment beyond the element's is required.  Rows on 16-byte
+ * group, which is 2^46 elements at most; no alignment beyond the element's is required.  Rows on 16-byte
  * boundaries (p, ld and gs) are fastest in the linear layer.  Vectors are
  * [n_groups, columns] fp32, contiguous.  Inputs and outputs may not overlap,
  * except that an output may be the same matrix (pointer and strides) as an

@@ -19,12 +19,13 @@ pigan_status check_mat(const pigan_mat& m, const char* name, int32_t groups, int
   if ((uintptr_t)m.p % es) return fail(PIGAN_EINVAL, "%s: pointer is not aligned to its elements", name);
   if (m.ld < cols || m.ld > (int64_t(1) << 40))
     return fail(PIGAN_EINVAL, "%s: row stride %lld out of [%lld, 2^40]", name, (long long)m.ld, (long long)cols);
-  if (groups > 1) {
-    const int64_t extent = rows > 0 ? (rows - 1) * m.ld + cols : 0;   // < 2^31 2^40
-    if (m.gs < extent || m.gs > (int64_t(1) << 46))
-      return fail(PIGAN_EINVAL, "%s: group stride %lld does not hold a group of %lld elements", name, (long long)m.gs,
-                  (long long)extent);
-  }
+  // (rows - 1) ld may reach 2^71
+  const __int128 extent = rows > 0 ? (__int128)(rows - 1) * m.ld + cols : 0;
+  if (extent > (__int128(1) << 46)) return fail(PIGAN_EINVAL, "%s: %lld rows of stride %lld, more than 2^46 elements", name,
+                                                (long long)rows, (long long)m.ld);
+  if (groups > 1 && (m.gs < (int64_t)extent || m.gs > (int64_t(1) << 46)))
+    return fail(PIGAN_EINVAL, "%s: group stride %lld does not hold a group of %lld elements", name, (long long)m.gs,
+                (long long)extent);
   return PIGAN_OK;
 }
 

@@ -18,3 +18,17 @@ def test_no_rows_and_only_dx(dt):
     assert L.pigan_linear_backward(a, None, 0, None) == pigan.OK
     a = _norm(dt=dt, m=0, x=(0, N, 0), dy=(0, N, 0), dx=(0, N, 0), mean=0, rstd=0, dgamma=0, dbeta=0)
     assert L.pigan_layer_norm_backward(a, None, 0, None) == pigan.OK
+
+
+@needs_lib
+@pytest.mark.parametrize("rows,ld,gs", [((1 << 24) + 1, 1 << 40, 16), ((1 << 24) + 1, 1 << 40, 1 << 46),
+                                        ((1 << 31) - 1, 1 << 40, 1 << 46), ((1 << 23) + 1, 1 << 40, 1 << 40)])
+def test_groups_whose_extent_passes_63_bits(rows, ld, gs):
+    """(rows - 1) * ld wraps around: the group still does not fit its stride."""
+    L = pigan.lib()
+    far = (FAKE, ld, gs)
+    assert L.pigan_layer_norm_forward(_norm(G=2, m=rows, x=far, y=far), None) == pigan.EINVAL
+    assert L.pigan_linear_forward(_linear(G=2, m=rows, x=far, y=far), FAKE, 1 << 60, None) == pigan.EINVAL
+    one = (FAKE, ld, 0)
+    assert L.pigan_layer_norm_forward(_norm(m=1 << 6, x=one, y=one, eps=0.0), None) == pigan.EINVAL
+    assert b"eps" in L.pigan_last_error()   # the strides themselves are in range
