@@ -162,6 +162,8 @@ double tiles_of(int64_t I, int64_t J, int G, int t) {
   const int64_t s = mm_tile_side(t);
   return (double)((I + s - 1) / s) * (double)((J + s - 1) / s) * G;
 }
+// a launch's x dimension holds fewer than 2^32 threads
+bool grid_holds(double blocks, int t) { return blocks * mm_tile_threads(t) < 4294967296.0; }
 double split_us(int64_t I, int64_t J, int G, int split) {
   return split > 1 ? 8.0 + (double)G * I * J * 4.0 * (split * 2 + 1) / 5e6 : 0.0;
 }
@@ -181,6 +183,7 @@ MmPlan plan_mm(const double (&STAGE_US)[3][4], int64_t I, int64_t J, int64_t K, 
     for (int split = 1; split <= 64 && split <= nk; split *= 2) {
       if (split > 1 && nk * pairs / split < 4) break;
       const double blocks = tiles_of(I, J, G, t) * split, rounds = ceil(blocks / (256.0 * PER_CU[t]));
+      if (!grid_holds(blocks, t)) break;
       const double stages = (double)((nk + split - 1) / split) * pairs;
       const double us = rounds * (stages * stage_of(STAGE_US, t, blocks, load) + BLOCK_US[t]) + FIRST_US[t] +
                         split_us(I, J, G, split);
@@ -189,7 +192,7 @@ MmPlan plan_mm(const double (&STAGE_US)[3][4], int64_t I, int64_t J, int64_t K, 
   // 64 tiles of four groups, one on a CU: a stage of each group in the time of four blocks' stages
   const double us = ceil(tiles_of(I, J, G, MM_64) / 256) * ((double)((nk + 3) / 4) * pairs * STAGE_US[MM_64][3] + 4.0) +
                     FIRST_US[MM_64];
-  if (nk >= 8 && us < best.us) best = {MM_64K, 1, us};
+  if (nk >= 8 && us < best.us && grid_holds(tiles_of(I, J, G, MM_64), MM_64K)) best = {MM_64K, 1, us};
   return best;
 }
 
@@ -204,6 +207,7 @@ bool plan_both(int64_t M, int64_t N, int64_t K, int pairs, int G, MmPlan& dx, Mm
     for (int split = 1; split <= 64 && split <= nw; split *= 2) {
       if (split > 1 && nw * pairs / split < 4) break;
       const double b1 = tiles_of(M, K, G, t), b2 = tiles_of(N, K, G, t) * split;
+      if (!grid_holds(b1 + b2, t)) break;
       double load;
       const double stage = stage_of(STAGE_BWD, t, b1 + b2, load);
       const double t1 = nx * pairs * stage + BLOCK_US[t], t2 = (double)((nw + split - 1) / split) * pairs * stage + BLOCK_US[t];
@@ -462,8 +466,8 @@ pigan_status backward_products(const pigan_linear* a, const BackwardPlan& p, cha
 pigan_status run_backward(const pigan_linear* a, const BackwardPlan& p, char* ws, hipStream_t st) {
   const int G = a->n_groups;
   if (a->M == 0) {   // sums over no rows
-    if (a->dw) HIP_TRY(launch_slot_sum(nullptr, 0, 0, a->N * a->K, a->dw, a->N * a->K, nullptr, G, st));
-    if (a->db) HIP_TRY(launch_slot_sum(nullptr, 0, 0, a->N, a->db, a->N, nullptr, G, st));
+    if (a->dw) HIP_TRY(launch_zeros(a->dw, G * a->N * a->K, st));
+    if (a->db) HIP_TRY(launch_zeros(a->db, G * a->N, st));
     return PIGAN_OK;
   }
   if (a->dx.p || a->dw) {

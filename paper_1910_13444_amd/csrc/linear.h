@@ -40,6 +40,8 @@ template <class T, class TO> struct MmArgs {
 enum MmTile { MM_64 = 0, MM_128 = 1, MM_256 = 2, MM_64K = 3 };
 inline int mm_tile_side(int t) { return t == MM_128 ? 128 : t == MM_256 ? 256 : 64; }
 
+inline int mm_tile_threads(int t) { return t == MM_64K ? 1024 : t == MM_256 ? 512 : 256; }
+
 // direct: both operands may go straight to LDS: 16-byte aligned rows (a tile's
 // extent below 2^31 bytes) of whole pieces; copies (pack) and planes (split3), which
 // pairs = 6 needs, hold zeros behind their rows up to a whole piece

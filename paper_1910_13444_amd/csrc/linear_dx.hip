@@ -28,7 +28,7 @@ template <class T, class TO>
 hipError_t launch_mm_both(const MmArgs<T, TO>& dx, const MmArgs<T, float>& dw, int tile, bool dw_first, int G,
                           hipStream_t st) {
   const uint32_t n_dx = mm_blocks<T, TO, MM_DX>(dx, tile, true, G), n_dw = mm_blocks<T, float, MM_DW>(dw, tile, true, G);
-  if (!n_dx || !n_dw || dx.o.J != dw.o.J || (tile != MM_64 && tile != MM_128)) return hipErrorInvalidValue;
+  if (!n_dx || !n_dw || dx.o.J != dw.o.J || ((uint64_t)n_dx + n_dw) * 256 >> 32 || (tile != MM_64 && tile != MM_128)) return hipErrorInvalidValue;
   if (dx.o.J % 8 == 0) both_of<T, TO, true>(dx, dw, tile, n_dx, n_dw, dw_first, st);
   else both_of<T, TO, false>(dx, dw, tile, n_dx, n_dw, dw_first, st);
   return hipGetLastError();

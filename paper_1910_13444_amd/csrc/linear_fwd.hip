@@ -41,12 +41,18 @@ template <> struct ShortMma<float> {
 };
 
 template <class T, int P, int NW, int U>
-__global__ void __launch_bounds__(64 * NW) k_short_fwd(const MmArgs<T, T> p) {
+__global__ void __launch_bounds__(64 * NW) k_short_fwd(const MmArgs<T, T> p, uint32_t row_tiles, uint32_t ranges) {
   constexpr int CK = ShortMma<T>::CK, S = 16 / P, TURN = NW * P * CK;   // k per turn of all waves
   __shared__ float sums[NW][16][17];
   const int g = blockIdx.z;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t i0 = (int64_t)blockIdx.y * S, j0 = (int64_t)blockIdx.x * S;
+  // strips beyond a launch's x dimension: their range of gridDim.x strips is in y
+  uint32_t tile = blockIdx.y, range = 0;
+  if (ranges > 1) {
+    range = tile / row_tiles;
+    tile -= range * row_tiles;
+  }
+  const int64_t i0 = (int64_t)tile * S, j0 = ((int64_t)range * gridDim.x + blockIdx.x) * S;
   const int64_t i = i0 + (lane & (S - 1)), j = j0 + (lane & (S - 1));
   // rows past the end repeat the last one; their results are not stored
   const int64_t kl = (wave * P + ((lane & 15) / S)) * CK + (lane >> 4) * EPP<T>;
@@ -146,23 +152,27 @@ __global__ void __launch_bounds__(256) k_pack(const PackSets sets) {
 
 }  // namespace
 
-template <class T, int P>
-void short_of(const MmArgs<T, T>& a, int G, hipStream_t st) {
+// (a launch's x dimension holds fewer than 2^32 threads)
+template <class T, int P, int NW, int U>
+hipError_t short_of(const MmArgs<T, T>& a, int G, hipStream_t st) {
   constexpr int S = 16 / P;
-  const dim3 grid((unsigned)((a.o.J + S - 1) / S), (unsigned)((a.o.I + S - 1) / S), G);
+  constexpr int64_t MOST = (int64_t(1) << 32) / (64 * NW) - 1;
+  const int64_t strips = (a.o.J + S - 1) / S, tiles = (a.o.I + S - 1) / S, ranges = (strips + MOST - 1) / MOST;
+  if (tiles * ranges > 65535) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)((strips + ranges - 1) / ranges), (unsigned)(tiles * ranges), G);
+  k_short_fwd<T, P, NW, U><<<grid, 64 * NW, 0, st>>>(a, (uint32_t)tiles, (uint32_t)ranges);
+  return hipGetLastError();
+}
+template <class T, int P>
+hipError_t short_of(const MmArgs<T, T>& a, int G, hipStream_t st) {
   // waves for the length of k, so that all of a row is in flight at once up to 8192
-  if (a.K > 2048) k_short_fwd<T, P, 8, 8><<<grid, 512, 0, st>>>(a);
-  else k_short_fwd<T, P, 4, 4><<<grid, 256, 0, st>>>(a);
+  return a.K > 2048 ? short_of<T, P, 8, 8>(a, G, st) : short_of<T, P, 4, 4>(a, G, st);
 }
 
 template <class T>
 hipError_t launch_short_fwd(const MmArgs<T, T>& a, int G, hipStream_t st) {
-  if (a.o.I < 1 || a.o.J < 1 || a.K < 1 || a.o.J > 0x7fffffff || (a.o.I + 15) / 16 > 65535 || G < 1 || G > 65535)
-    return hipErrorInvalidValue;
-  if (a.o.I <= 4) short_of<T, 4>(a, G, st);
-  else if (a.o.I <= 8) short_of<T, 2>(a, G, st);
-  else short_of<T, 1>(a, G, st);
-  return hipGetLastError();
+  if (a.o.I < 1 || a.o.J < 1 || a.K < 1 || a.o.J > 0x7fffffff || G < 1 || G > 65535) return hipErrorInvalidValue;
+  return a.o.I <= 4 ? short_of<T, 4>(a, G, st) : a.o.I <= 8 ? short_of<T, 2>(a, G, st) : short_of<T, 1>(a, G, st);
 }
 
 // the sets of a launch, and blocks for the largest of them; 0 where one cannot be

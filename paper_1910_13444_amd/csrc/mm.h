@@ -695,8 +695,10 @@ template <class T, class TO, int KIND>
 uint32_t mm_blocks(const MmArgs<T, TO>& a, int tile, bool direct, int G) {
   const int64_t side = mm_tile_side(tile);
   const int64_t rows = (a.o.I + side - 1) / side, cols = (a.o.J + side - 1) / side;
+  // a launch's x dimension holds fewer than 2^32 threads
+  const double threads = (double)rows * cols * a.o.n_split * G * mm_tile_threads(tile);
   if (a.o.I < 1 || a.o.J < 1 || a.K < 1 || a.o.n_split < 1 || G < 1 || G > 65535 ||
-      (double)rows * cols * a.o.n_split * G > 1e9 || a.o.n_split > (a.K + 63) / 64 || (a.o.n_split > 1 && !a.o.part) ||
+      threads > 4294967295.0 || a.o.n_split > (a.K + 63) / 64 || (a.o.n_split > 1 && !a.o.part) ||
       (a.pairs != 1 && a.pairs != 6) || a.K > 0x7fffffff || (!direct && (tile == MM_256 || tile == MM_64K)) ||
       (direct && !(mm_whole(a.a, KIND == MM_DW ? a.o.I : a.K, G) && mm_whole(a.b, KIND == MM_FWD ? a.K : a.o.J, G))))
     return 0;

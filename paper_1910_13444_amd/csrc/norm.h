@@ -39,4 +39,7 @@ hipError_t launch_colsum_rows(const Mat<const T>& m, int64_t M, int64_t N, int s
 hipError_t launch_slot_sum(const float* part, int64_t p_g, int n_slots, int64_t n, float* dst, int64_t n1, float* dst2,
                            int G, hipStream_t st);
 
+// n zeros
+hipError_t launch_zeros(float* dst, int64_t n, hipStream_t st);
+
 }  // namespace pigan
