@@ -498,11 +498,15 @@ pigan_status pigan_adam_update(int64_t n, float* params, const float* grads, flo
  * A matrix operand is n_groups matrices (independent layers of one shape);
  * element (r, c) of group g is p[g * gs + r * ld + c].  ld must be at least the
  * number of columns and gs (for more than one group) at least the extent of a
- * group, which is 2^46 elements at most; no alignment beyond the element's is required.  Rows on 16-byte
- * boundaries (p, ld and gs) are fastest in the linear layer.  Vectors are
- * [n_groups, columns] fp32, contiguous.  Inputs and outputs may not overlap,
- * except that an output may be the same matrix (pointer and strides) as an
- * elementwise input where that is said.
+ * group, and all of it spans 2^46 elements at most; no alignment beyond the
+ * element's is required.  Rows on 16-byte boundaries (p, ld and gs) are fastest
+ * in the linear layer.  Vectors are [n_groups, columns] fp32, contiguous.
+ *
+ * An output may not overlap another output, the workspace or an input that the
+ * call reads, except that it may be the same matrix (pointer and strides) as an
+ * elementwise input where that is said.  Such calls are refused; an overlap of two
+ * matrices with gaps between their rows and different strides is noticed only
+ * where both begin at the same element.
  *
  * Sums are held in fp32 or wider and in a fixed order; a result is rounded to
  * the storage type once, when it is stored.  fp32 products are formed from

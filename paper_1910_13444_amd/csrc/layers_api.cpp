@@ -20,12 +20,12 @@ pigan_status check_mat(const pigan_mat& m, const char* name, int32_t groups, int
   if (m.ld < cols || m.ld > (int64_t(1) << 40))
     return fail(PIGAN_EINVAL, "%s: row stride %lld out of [%lld, 2^40]", name, (long long)m.ld, (long long)cols);
   // (rows - 1) ld may reach 2^71
-  const __int128 extent = rows > 0 ? (__int128)(rows - 1) * m.ld + cols : 0;
-  if (extent > (__int128(1) << 46)) return fail(PIGAN_EINVAL, "%s: %lld rows of stride %lld, more than 2^46 elements", name,
-                                                (long long)rows, (long long)m.ld);
-  if (groups > 1 && (m.gs < (int64_t)extent || m.gs > (int64_t(1) << 46)))
-    return fail(PIGAN_EINVAL, "%s: group stride %lld does not hold a group of %lld elements", name, (long long)m.gs,
-                (long long)extent);
+  const __int128 extent = rows > 0 ? (__int128)(rows - 1) * m.ld + cols : 0, most = __int128(1) << 46;
+  if (extent > most) return fail(PIGAN_EINVAL, "%s: %lld rows of stride %lld, more than 2^46 elements", name,
+                                 (long long)rows, (long long)m.ld);
+  if (groups > 1 && (m.gs < (int64_t)extent || (groups - 1) * (__int128)m.gs + extent > most))
+    return fail(PIGAN_EINVAL, "%s: group stride %lld does not hold a group of %lld elements, or %d of them pass 2^46", name,
+                (long long)m.gs, (long long)extent, (int)groups);
   return PIGAN_OK;
 }
 
@@ -52,6 +52,89 @@ pigan_status check_ws(const void* ws, size_t have, size_t need) {
   if (!ws) return fail(PIGAN_EWORKSPACE, "null workspace, %zu bytes are needed", need);
   if (have < need) return fail(PIGAN_EWORKSPACE, "workspace of %zu bytes, %zu are needed", have, need);
   if ((uintptr_t)ws % 256) return fail(PIGAN_EINVAL, "the workspace must be 256-byte aligned");
+  return PIGAN_OK;
+}
+
+// ---------------------------------------------------------------------------
+// Operands that share memory.  A kernel's blocks read their inputs while others
+// already store, so an output may be an input only where each element is read by
+// the thread that then stores it, and the two are the same matrix.
+// ---------------------------------------------------------------------------
+// in bytes: `groups` groups of `rows` pieces of `len`; p = 0: none
+struct Region {
+  const char* name;
+  int64_t p, len, rows, ld, groups, gs;
+  Region(const char* n, const pigan_mat& m, int64_t M, int64_t N, int32_t G, size_t es)
+      : name(n), p((int64_t)(uintptr_t)m.p), len(0), rows(1), ld(0), groups(1), gs(0) {
+    if (!p) return;
+    len = N * es; rows = M; ld = m.ld * es; groups = G; gs = G > 1 ? m.gs * es : 0;
+    // the fewest levels that say the same, so that equal memory has equal fields
+    if (rows == 1) { rows = groups; ld = gs; groups = 1; }
+    if (groups > 1 && gs == rows * ld) { rows *= groups; groups = 1; }
+    if (rows == 1 || (groups == 1 && ld == len)) { len *= rows; rows = 1; }
+    if (rows == 1) ld = len;
+    if (groups == 1) gs = 0;
+  }
+  Region(const char* n, const void* q, int64_t bytes) : Region(n, pigan_mat{(void*)q, bytes, 0}, 1, bytes, 1, 1) {}
+  __int128 end() const { return (__int128)(groups - 1) * gs + (__int128)(rows - 1) * ld + len + p; }
+  bool dense() const { return rows == 1 && groups == 1; }
+  bool same(const Region& o) const {
+    return p == o.p && len == o.len && rows == o.rows && ld == o.ld && groups == o.groups && gs == o.gs;
+  }
+};
+
+int64_t floor_div(int64_t a, int64_t b) { return a / b - (a % b < 0); }
+
+// pieces of a (from 0 on) and of b (from d on), both ld apart
+bool rows_meet(const Region& a, const Region& b, int64_t d) {
+  for (int64_t s = floor_div(-d, a.ld), n = 0; n < 2; ++n, ++s)   // row j of b, row j + s of a: |distance| < ld
+    if (s > -a.rows && s < b.rows && d + s * a.ld < a.len && -(d + s * a.ld) < b.len) return true;
+  return false;
+}
+
+// the interval [from, to) and the pieces of b; where it does not meet the last piece
+// that starts at or before `from`, it meets the next one or none
+bool interval_meets(__int128 from, __int128 to, const Region& b) {
+  const int64_t last_g = b.groups - 1, last_r = b.rows - 1;
+  for (int64_t n = 0; n < 2; ++n) {
+    int64_t g = b.groups > 1 ? (int64_t)((from - b.p) / b.gs) + n : 0;
+    g = std::min(std::max<int64_t>(from < b.p ? 0 : g, 0), last_g);
+    const __int128 at = (__int128)b.p + (__int128)g * b.gs;
+    for (int64_t m = 0; m < 2; ++m) {
+      __int128 r = from < at ? 0 : (from - at) / b.ld + m;
+      r = std::min<__int128>(r, last_r);
+      const __int128 q = at + r * b.ld;
+      if (q < to && from < q + b.len) return true;
+    }
+  }
+  return false;
+}
+
+// whether a and b have a byte in common; of two that are both apart in rows, by
+// different strides, it is only told where they begin at the same address
+bool share(const Region& a, const Region& b) {
+  if (!a.p || !b.p || a.end() <= b.p || b.end() <= a.p) return false;
+  if (a.dense()) return interval_meets(a.p, a.end(), b);
+  if (b.dense()) return interval_meets(b.p, b.end(), a);
+  if (a.ld != b.ld || a.gs != b.gs) return a.p == b.p;
+  const int64_t d = b.p - a.p;
+  if (a.groups == 1 && b.groups == 1) return rows_meet(a, b, d);
+  for (int64_t t = floor_div(-d, a.gs), n = 0; n < 2; ++n, ++t)
+    if (t > -a.groups && t < b.groups && rows_meet(a, b, d + t * a.gs)) return true;
+  return false;
+}
+
+// No output shares memory with another operand, but for the same matrix where
+// same_ok(output, input) says so.
+template <int NO, int NI, class F>
+pigan_status check_apart(const Region (&outs)[NO], const Region (&ins)[NI], F&& same_ok) {
+  for (int o = 0; o < NO; ++o) {
+    for (int q = 0; q < o; ++q)
+      if (share(outs[o], outs[q])) return fail(PIGAN_EINVAL, "%s overlaps %s", outs[o].name, outs[q].name);
+    for (int i = 0; i < NI; ++i)
+      if (share(outs[o], ins[i]) && !(same_ok(o, i) && outs[o].same(ins[i])))
+        return fail(PIGAN_EINVAL, "%s overlaps %s", outs[o].name, ins[i].name);
+  }
   return PIGAN_OK;
 }
 
@@ -128,8 +211,35 @@ pigan_status check_backward(const pigan_linear* a) {
   }
   if (a->dw && rows)
     if (pigan_status st = check_mat(a->x, "x", G, a->M, a->K, es)) return st;
+  if (a->dw && (__int128)a->N * a->K * G > (__int128(1) << 46))
+    return fail(PIGAN_EINVAL, "dw: %d of %lld x %lld, more than 2^46 elements", (int)G, (long long)a->N, (long long)a->K);
   if (pigan_status st = check_vec(a->dw, "dw")) return st;
   return check_vec(a->db, "db");
+}
+
+const pigan_mat NO_MAT = {};
+
+pigan_status check_forward_apart(const pigan_linear* a, const void* ws, size_t need) {
+  const size_t es = esize(a->dt);
+  const int32_t G = a->n_groups;
+  const Region outs[] = {{"y", a->y, a->M, a->N, G, es}, {"pre", a->pre, a->M, a->N, G, es},
+                         {"the workspace", need ? ws : nullptr, (int64_t)need}};
+  const Region ins[] = {{"add", a->add, a->M, a->N, G, es}, {"x", a->x, a->M, a->K, G, es}, {"w", a->w, a->N, a->K, G, es},
+                        {"bias", a->bias, G * a->N * 4}};
+  return check_apart(outs, ins, [](int o, int i) { return o == 0 && i == 0; });
+}
+
+// (what a call does not read may be anywhere)
+pigan_status check_backward_apart(const pigan_linear* a, const void* ws, size_t need) {
+  const size_t es = esize(a->dt);
+  const int32_t G = a->n_groups;
+  const bool dx = a->dx.p;
+  const Region outs[] = {{"dx", a->dx, a->M, a->K, G, es}, {"dw", a->dw, G * a->N * a->K * 4}, {"db", a->db, G * a->N * 4},
+                         {"the workspace", need ? ws : nullptr, (int64_t)need}};
+  const Region ins[] = {{"pre", dx ? a->pre : NO_MAT, a->M, a->K, G, es}, {"add", dx ? a->add : NO_MAT, a->M, a->K, G, es},
+                        {"g", a->g, a->M, a->N, G, es}, {"w", dx ? a->w : NO_MAT, a->N, a->K, G, es},
+                        {"x", a->dw ? a->x : NO_MAT, a->M, a->K, G, es}};
+  return check_apart(outs, ins, [](int o, int i) { return o == 0 && i < 2; });
 }
 
 // ---------------------------------------------------------------------------
@@ -514,9 +624,29 @@ pigan_status check_norm_backward(const pigan_norm* a) {
     if (pigan_status st = check_mat(a->add, "add", a->n_groups, a->M, a->N, es)) return st;
   if (a->dx.p) {
     if (pigan_status st = check_mat(a->dx, "dx", a->n_groups, a->M, a->N, es)) return st;
-    if (a->dx.p == a->x.p) return fail(PIGAN_EINVAL, "dx: may not be x");
   }
   return PIGAN_OK;
+}
+
+pigan_status check_norm_apart(const pigan_norm* a) {
+  const size_t es = esize(a->dt);
+  const int32_t G = a->n_groups;
+  const int64_t cols = G * a->N * 4, rows = G * a->M * 4;
+  const Region outs[] = {{"y", a->y, a->M, a->N, G, es}, {"mean", a->mean, rows}, {"rstd", a->rstd, rows}};
+  const Region ins[] = {{"x", a->x, a->M, a->N, G, es}, {"gamma", a->gamma, cols}, {"beta", a->beta, cols}};
+  return check_apart(outs, ins, [](int o, int i) { return o == 0 && i == 0; });
+}
+
+pigan_status check_norm_backward_apart(const pigan_norm* a, const void* ws, size_t need) {
+  const size_t es = esize(a->dt);
+  const int32_t G = a->n_groups;
+  const int64_t cols = G * a->N * 4, rows = G * a->M * 4;
+  const Region outs[] = {{"dx", a->dx, a->M, a->N, G, es}, {"dgamma", a->dgamma, cols}, {"dbeta", a->dbeta, cols},
+                         {"the workspace", need ? ws : nullptr, (int64_t)need}};
+  const Region ins[] = {{"dy", a->dy, a->M, a->N, G, es}, {"add", a->dx.p ? a->add : NO_MAT, a->M, a->N, G, es},
+                        {"x", a->x, a->M, a->N, G, es}, {"gamma", a->gamma, cols}, {"mean", a->mean, rows},
+                        {"rstd", a->rstd, rows}};
+  return check_apart(outs, ins, [](int o, int i) { return o == 0 && i < 2; });
 }
 
 template <class T> NormArgs<T> norm_args(const pigan_norm* a) {
@@ -558,7 +688,9 @@ pigan_status pigan_linear_forward(const pigan_linear* a, void* ws, size_t ws_byt
     if (pigan_status st = check_forward(a)) return st;
     const ForwardPlan p = plan_forward(a);
     if (pigan_status st = check_ws(ws, ws_bytes, p.total)) return st;
-    return a->M == 0 ? PIGAN_OK : run_forward(a, p, (char*)ws, (hipStream_t)stream);
+    if (a->M == 0) return PIGAN_OK;
+    if (pigan_status st = check_forward_apart(a, ws, p.total)) return st;
+    return run_forward(a, p, (char*)ws, (hipStream_t)stream);
   });
 }
 
@@ -577,6 +709,8 @@ pigan_status pigan_linear_backward(const pigan_linear* a, void* ws, size_t ws_by
     if (pigan_status st = check_backward(a)) return st;
     const BackwardPlan p = plan_backward(a);
     if (pigan_status st = check_ws(ws, ws_bytes, p.total)) return st;
+    if (a->M > 0)
+      if (pigan_status st = check_backward_apart(a, ws, p.total)) return st;
     return run_backward(a, p, (char*)ws, (hipStream_t)stream);
   });
 }
@@ -593,6 +727,9 @@ pigan_status pigan_act_backward(const pigan_act_args* a, void* stream) {
     if (pigan_status st = check_mat(a->dy, "dy", a->n_groups, a->M, a->N, es)) return st;
     if (pigan_status st = check_mat(a->pre, "pre", a->n_groups, a->M, a->N, es)) return st;
     if (pigan_status st = check_mat(a->g, "g", a->n_groups, a->M, a->N, es)) return st;
+    const Region outs[] = {{"g", a->g, a->M, a->N, a->n_groups, es}};
+    const Region ins[] = {{"dy", a->dy, a->M, a->N, a->n_groups, es}, {"pre", a->pre, a->M, a->N, a->n_groups, es}};
+    if (pigan_status st = check_apart(outs, ins, [](int, int) { return true; })) return st;
     const hipStream_t st = (hipStream_t)stream;
     ProfScope prof(st, "act_backward", 0.0, 3.0 * es * a->n_groups * (double)a->M * a->N);
     return by_dtype(a->dt, [&](auto t) -> pigan_status {
@@ -609,6 +746,7 @@ pigan_status pigan_layer_norm_forward(const pigan_norm* a, void* stream) {
     if (!(a->eps > 0.0f) || !__builtin_isfinite(a->eps)) return fail(PIGAN_EINVAL, "eps=%g must be finite and > 0", a->eps);
     if (a->M == 0) return PIGAN_OK;
     if (pigan_status st = check_mat(a->y, "y", a->n_groups, a->M, a->N, esize(a->dt))) return st;
+    if (pigan_status st = check_norm_apart(a)) return st;
     const hipStream_t st = (hipStream_t)stream;
     ProfScope prof(st, "layer_norm_fwd", 0.0, 2.0 * esize(a->dt) * a->n_groups * (double)a->M * a->N);
     return by_dtype(a->dt, [&](auto t) -> pigan_status {
@@ -636,6 +774,8 @@ pigan_status pigan_layer_norm_backward(const pigan_norm* a, void* ws, size_t ws_
   return guarded([&]() -> pigan_status {
     if (pigan_status st = check_norm_backward(a)) return st;
     if (pigan_status st = check_ws(ws, ws_bytes, norm_ws(a))) return st;
+    if (a->M > 0)
+      if (pigan_status st = check_norm_backward_apart(a, ws, norm_ws(a))) return st;
     const hipStream_t st = (hipStream_t)stream;
     ProfScope prof(st, "layer_norm_bwd", 0.0,
                    (2.0 + !!a->dx.p + !!a->add.p) * esize(a->dt) * a->n_groups * (double)a->M * a->N);

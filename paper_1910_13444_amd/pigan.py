@@ -544,7 +544,8 @@ class StepGraph:
 # Matrices are [M, columns], or [G, M, columns] for G independent layers of one
 # shape, of one dtype (fp32, bf16, fp16), with unit stride along the columns
 # and any strides above; vectors ([columns] or [G, columns]) and parameter
-# gradients are fp32.
+# gradients are fp32.  A result given by the caller may share memory with another
+# operand only where its function says so: other overlaps raise PiganError.
 
 _NO_MAT = (0, 0, 0)
 

@@ -58,3 +58,58 @@ def test_column_sums_beyond_one_dimension_of_a_launch():
     assert torch.equal(dbeta, dy.float().sum(0)) and torch.equal(dgamma, (dy.float() * x.float()).sum(0))
     dbeta = pigan.linear_backward(dy, x[:, :1], _whole_numbers(N, 1), need_dx=False, need_dw=False)[2]
     assert torch.equal(dbeta, dy.float().sum(0))
+
+
+def test_overlaps_are_told_exactly():
+    """Random layouts of two matrices in one buffer against the elements that they
+    have: calls that share one are refused unless both are the same matrix, the
+    others run.  Of two matrices with gaps and different strides only a refusal of
+    elements that are apart would be wrong."""
+    import random
+    rng = random.Random(1)
+    buf = torch.zeros(4096, dtype=torch.bfloat16, device="cuda")
+    seen = {True: 0, False: 0}
+    for _ in range(4000):
+        G, M, N = rng.choice((1, 1, 2, 3)), rng.randint(1, 4), rng.randint(1, 6)
+        pad = rng.choice((0, 0, 1, 3, 9))
+        lay = []
+        for _ in range(2):
+            ld = N + (pad if rng.random() < 0.8 else rng.randint(0, 9))
+            gs = (M - 1) * ld + N + (rng.choice((0, ld - N, 20)))
+            lay.append((rng.randint(0, 60), ld, gs))
+        if rng.random() < 0.3:
+            lay[1] = (lay[0][0] + rng.choice((0, 0, 1, -1, N, -N, lay[0][1])), *lay[0][1:])
+            if lay[1][0] < 0:
+                continue
+        at = [{o + g * gs + r * ld + c for g in range(G) for r in range(M) for c in range(N)} for o, ld, gs in lay]
+        views = [buf.as_strided((G, M, N), (gs, ld, 1), o) for o, ld, gs in lay]
+        pre = torch.zeros((G, M, N), dtype=torch.bfloat16, device="cuda")
+        meet, order = bool(at[0] & at[1]), [o + g * gs + r * ld + c for g in range(G) for r in range(M) for c in range(N)
+                                            for o, ld, gs in lay]
+        bad = meet and order[::2] != order[1::2]
+        dense = [max(a) - min(a) + 1 == len(a) for a in at]
+        told = any(dense) or (lay[0][1:] == lay[1][1:])
+        try:
+            pigan.act_backward(views[0], pre, "tanh", out=views[1])
+            refused = False
+        except pigan.PiganError as e:
+            refused = True
+            assert "overlaps" in str(e)
+        assert refused == bad if told else not refused or bad, (G, M, N, lay)
+        seen[refused] += 1
+    assert min(seen.values()) > 500
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_overlapping_calls_are_refused(dtype):
+    x, w = torch.ones((300, 64), dtype=DT[dtype], device="cuda"), torch.ones((64, 64), dtype=DT[dtype], device="cuda")
+    for call in (lambda: pigan.linear(x, w, out=x), lambda: pigan.linear(x, w, residual=w.new_ones(300, 64), pre=x),
+                 lambda: pigan.linear_backward(x, w.new_ones(300, 64), w, dx=x),
+                 lambda: pigan.linear_backward(w.new_ones(300, 64), x, w, dx=x),
+                 lambda: pigan.layer_norm_backward(w.new_ones(300, 64), x, x.new_ones(300).float(), x.new_ones(300).float(), dx=x),
+                 lambda: pigan.layer_norm(x[1:], out=x[:-1])):
+        with pytest.raises(pigan.PiganError, match="overlaps"):
+            call()
+    # what a call does not read may be anywhere
+    dx, dw, db = pigan.linear_backward(w.new_ones(300, 64), x, w, need_dw=False, dx=x)
+    assert dx is x and torch.equal(x, torch.full_like(x, 64)) and dw is None and torch.equal(db, torch.full_like(db, 300))
