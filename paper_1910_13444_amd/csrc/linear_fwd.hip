@@ -97,16 +97,29 @@ __global__ void __launch_bounds__(64 * NW) k_short_fwd(const MmArgs<T, T> p, uin
 }
 
 // ---------------------------------------------------------------------------
-// bf16 planes of fp32 matrices: x0 and x1 are x and the rest cut to eight
-// significand bits (towards zero, so that no plane overflows), x2 what is left:
-// all 24 bits.  An infinity or NaN goes to x0 alone.  Bound by memory: 4 bytes read
-// and 6 written per value (1001 x 2000, 513 x 2000 and 1001 x 513 in 7.5 us, 4.7 TB/s).
+// bf16 planes of fp32 matrices: x0 and x1 are x and the rest rounded to eight
+// significand bits (to nearest; towards zero where x0 would overflow), x2 what is
+// left: all 24 bits.  With |x1| <= 2^-8 and |x2| <= 2^-17 for x in [1, 2), the three
+// products that are left out (x1 y2, x2 y1, x2 y2) are at most 2^-24 of x y, of either
+// sign.  (Planes cut towards zero lose up to 2^-21, always of the product's sign.)
+// An infinity or NaN goes to x0 alone.
+// Bound by memory: 4 bytes read and 6 written per value (1001 x 2000, 513 x 2000 and
+// 1001 x 513 in 7.5 us, 4.7 TB/s).
 // ---------------------------------------------------------------------------
 struct SplitSets {
   SplitSet s[3];
 };
 
-__device__ __forceinline__ float cut8(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
+__device__ __forceinline__ float nearest8(float x) { return (float)(bf16)x; }
+
+__device__ __forceinline__ void planes(float x, float& p0, float& p1, float& p2) {
+  const bool inf = fabsf(x) == __builtin_inff();
+  p0 = nearest8(x);
+  if (fabsf(p0) == __builtin_inff() && !inf) p0 = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+  const float rest = inf ? 0.0f : x - p0;
+  p1 = nearest8(rest);
+  p2 = rest - p1;
+}
 
 __global__ void __launch_bounds__(256) k_split3(const SplitSets sets, int G) {
   const SplitSet s = sets.s[blockIdx.y];
@@ -119,13 +132,7 @@ __global__ void __launch_bounds__(256) k_split3(const SplitSets sets, int G) {
     bf16* d = s.dst + (g * s.rows + r) * s.Kp + c;
     float p0[8], p1[8], p2[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const bool fin = __builtin_isfinite(f[e]);
-      p0[e] = fin ? cut8(f[e]) : f[e];
-      const float rest = fin ? f[e] - p0[e] : 0.0f;
-      p1[e] = cut8(rest);
-      p2[e] = rest - p1[e];
-    }
+    for (int e = 0; e < 8; ++e) planes(f[e], p0[e], p1[e], p2[e]);
     store8(d, 8, p0);
     store8(d + plane, 8, p1);
     store8(d + 2 * plane, 8, p2);

@@ -1,0 +1,96 @@
+"""fp32 products of the linear layer: every significand bit of the operands, every
+pair of planes in every tile and split."""
+import math
+
+import pytest
+import torch
+
+from paper_1910_13444_amd import pigan
+from _layers import EPS32, matrix
+from test_gpu_linear import _seed
+from test_gpu_linear_tiles import BACKWARD32, FORWARD32
+
+pytestmark = pytest.mark.gpu
+
+F32 = dict(device="cuda", dtype=torch.float32)
+
+
+def _planes(x):
+    """x as three bf16 values that add up to it, in 64 bits"""
+    x0 = x.bfloat16().float()
+    x1 = (x - x0).bfloat16().float()
+    return x0.double(), x1.double(), (x - x0 - x1).double()
+
+
+def _values(gen, n):
+    """significands with every bit in use, and those whose lower bits are largest"""
+    hard = [1 + 2.0 ** -7 - 2.0 ** -23, 1 + 2.0 ** -8, 1 + 2.0 ** -8 - 2.0 ** -23, 2 - 2.0 ** -23, 1 + 2.0 ** -8 + 2.0 ** -17,
+            1 + 2.0 ** -8 - 2.0 ** -17 + 2.0 ** -23, 1.0, 1.5]
+    v = torch.cat([torch.tensor(hard, dtype=torch.float32), torch.rand(n - len(hard), generator=gen, dtype=torch.float32) + 1])
+    return v * (torch.randint(0, 2, (n,), generator=gen) * 2 - 1)
+
+
+def test_single_products():
+    """Contractions of one element: a product loses at most 2^-24 of itself to the
+    pairs of planes that are left out, and two roundings of the sum of the six, each
+    at most a unit (2^-23) should the matrix core cut."""
+    gen = _seed(1)
+    a, b = _values(gen, 1011).cuda(), _values(gen, 777).cuda()
+    want = a.double()[:, None] * b.double()[None, :]
+    bound = (1 + 2 * 2) * EPS32 * want.abs()
+    dw = pigan.linear_backward(a[None, :], b[None, :], torch.zeros((1011, 777), **F32), need_dx=False)[1]
+    assert ((dw.double() - want).abs() <= bound).all()
+    dx = pigan.linear_backward(a[:, None], torch.zeros((1011, 777), **F32), b[None, :], need_dw=False)[0]
+    assert ((dx.double() - want).abs() <= bound).all()
+    # rows enough for the tiles
+    a = _values(gen, 150001).cuda()
+    y = pigan.linear(a[:, None], b[:, None])
+    want = a.double()[:, None] * b.double()[None, :]
+    assert ((y.double() - want).abs() <= (1 + 2 * 2) * EPS32 * want.abs()).all()
+
+
+def test_largest_values():
+    """A value whose nearest bf16 is infinite."""
+    big = torch.tensor([3.4028234663852886e38, -3.4028234663852886e38, 3.39e38], **F32)
+    dw = pigan.linear_backward(big[None, :], torch.full((1, 500), 0.375, **F32), torch.zeros((3, 500), **F32), need_dx=False)[1]
+    want = big.double()[:, None] * 0.375
+    assert ((dw.double() - want).abs() <= 5 * EPS32 * want.abs()).all()
+
+
+def _rms(t):
+    return t.square().mean().sqrt().item()
+
+
+def _judge(got, a, b, what):
+    """got = a b^T for unit normals.  A partial sum of k products is sqrt(k) in the
+    root mean square, and rounding it to nearest is off by 0.42 * 2^-24 of that: n
+    additions one by one by 0.3 n units of 2^-24, cut sums by half as much again at
+    sqrt(n) (their errors have both signs as the sums have); the final rounding and
+    the pairs left out by less than sqrt(n) together.  The pair (1, 1) left out as
+    well would show."""
+    n = a.shape[-1]
+    want = a.double() @ b.double().transpose(-1, -2).contiguous()
+    tol = (0.45 * n + math.sqrt(n)) * EPS32
+    err = _rms(got.double() - want)
+    assert err <= tol, f"{what}: {err / EPS32} units for at most {tol / EPS32}"
+    if n >= 100 and n <= 2000:
+        (_, a1, _), (_, b1, _) = _planes(a), _planes(b)
+        assert _rms(a1 @ b1.transpose(-1, -2).contiguous()) > tol, f"{what}: a missing pair would pass"
+
+
+@pytest.mark.parametrize("size", FORWARD32)
+def test_every_pair_forward(size):
+    G, M, K, N = size
+    gen = _seed(*size)
+    x, w = matrix(gen, G, M, K, "fp32"), matrix(gen, G, N, K, "fp32")
+    _judge(pigan.linear(x, w), x, w, "y")
+
+
+@pytest.mark.parametrize("size", BACKWARD32)
+def test_every_pair_backward(size):
+    G, M, K, N = size
+    gen = _seed(*size)
+    g, x, w = matrix(gen, G, M, N, "fp32"), matrix(gen, G, M, K, "fp32"), matrix(gen, G, N, K, "fp32")
+    dx, dw, _ = pigan.linear_backward(g, x, w)
+    _judge(dx, g, w.transpose(-1, -2), "dx")
+    _judge(dw, g.transpose(-1, -2), x.transpose(-1, -2), "dw")
