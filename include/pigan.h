@@ -511,9 +511,9 @@ pigan_status pigan_adam_update(int64_t n, float* params, const float* grads, flo
  * Sums are held in fp32 or wider and in a fixed order; a result is rounded to
  * the storage type once, when it is stored.  fp32 products are formed from
  * three bf16 pieces per operand (24 significand bits; six products, what is left
- * out is at most 2^-24 of a product, of either sign) or on the fp32 matrix core:
- * an infinite operand element may turn the sums that it enters into NaN, and
- * operands below 2^-100 may lose bits.
+ * out is at most 2^-24 of a product, of either sign) or on the fp32 matrix core;
+ * operands below 2^-100 may lose bits, and an infinity times one of those may be
+ * NaN.
  * Masks do not occur: an infinity or NaN reaches exactly the outputs that
  * depend on it.
  *
