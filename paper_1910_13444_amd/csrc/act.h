@@ -1,24 +1,31 @@
 // Activations of the linear layer: value and derivative with respect to the
-// pre-activation, in fp32.
-//   tanh   t,                   1 - t^2 (formed from exp, see tanh_ts)
+// pre-activation.
+//   tanh   t,                   1 - t^2 (formed from exp)
 //   relu   max(a, 0),           1 for a > 0, else 0
 //   gelu   a Phi(a),            Phi(a) + a phi(a)      (normal distribution)
 //   silu   a s, s = 1 / (1 + exp(-a)),   s + a s (1 - s)
+//
+// For 16-bit results in fp32 (errors of 1e-7 to 2e-6 relative, below), for fp32
+// results in fp64, rounded once: there the fp32 forms' errors would be two to three
+// times those of the rounding.
 #pragma once
 #include "common.h"
 
 namespace pigan {
 
-// exp(x) by the hardware base-2 exponential; the rounding of the scaled
-// argument leaves |x| 6e-8 relative, which the functions below meet only where
-// the exponential is a small part of their result
+// ---------------------------------------------------------------------------
+// in fp32
+// ---------------------------------------------------------------------------
+// exp(x) by the hardware base-2 exponential; the rounding of the scaled argument
+// leaves 6e-8 |x| relative: 2e-6 at x = -a^2 / 2 of a = -6, less than 2^-8 of a unit
+// of fp16 wherever the result is not below its range
 __device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.4426950408889634f); }
 
 // Normal distribution: Phi(a), and gauss = exp(-a^2 / 2).  With z = |a| / sqrt 2
 // and t = 1 / (1 + 0.4 z) the tail is erfc(z) = t Q(t) exp(-z^2), Q the
 // polynomial of degree 8 that is nearest to erfc(z) exp(z^2) / t on all of
 // z >= 0 (1.3e-7 relative, 2.6e-7 with the roundings of the fp32 evaluation).
-// The lower tail is therefore accurate in relative terms, where
+// The lower tail therefore has these errors and exp's in relative terms, where
 // 0.5 (1 + erf) would cancel.
 __device__ __forceinline__ float normal_cdf(float a, float& gauss) {
   const float z = fabsf(a) * 0.70710678118654752f;
@@ -45,41 +52,151 @@ __device__ __forceinline__ float logistic(float a, float& c) {
   return a < 0.0f ? e * r : r;
 }
 
-template <int ACT>
+// ---------------------------------------------------------------------------
+// in fp64 (1e-9 relative, a hundredth of an fp32 rounding)
+// ---------------------------------------------------------------------------
+// exp(x), x <= 0; a NaN stays one.  2^f on |f| <= 1/2 by its nearest polynomial of
+// degree 7 (4e-11 relative); the whole part of x / ln 2 is in the low bits of its
+// sum with 1.5 * 2^52.
+__device__ __forceinline__ double exp64(double x) {
+  const double y = (x < -800.0 ? -800.0 : x) * 1.4426950408889634;   // below 2^-1150: 0
+  const double sum = y + 6755399441055744.0, f = y - (sum - 6755399441055744.0);
+  double q = 1.5201918109007667e-05;
+  q = q * f + 0.00015469291112801776;
+  q = q * f + 0.001333392257928822;
+  q = q * f + 0.009618027253755258;
+  q = q * f + 0.0555041035342827;
+  q = q * f + 0.24022651198157235;
+  q = q * f + 0.6931471807284516;
+  q = q * f + 0.999999999961682;
+  return __builtin_ldexp(q, (int)(uint32_t)__builtin_bit_cast(uint64_t, sum));
+}
+
+// 1 / d for 1 <= d < 2^100: the fp32 reciprocal (2e-7) and a Newton step (4e-14)
+__device__ __forceinline__ double rcp64(double d) {
+  const double r = __builtin_amdgcn_rcpf((float)d);
+  return r + r * (1.0 - d * r);
+}
+
+// tanh and its slope, as tanh_ts
+__device__ __forceinline__ void tanh64(double a, double& t, double& s) {
+  const double ax = fabs(a), e = exp64(-2.0 * ax), r = rcp64(1.0 + e), a2 = a * a;
+  double q = 62.0 / 2835.0;
+  q = q * a2 - 17.0 / 315.0;
+  q = q * a2 + 2.0 / 15.0;
+  q = q * a2 - 1.0 / 3.0;
+  const double small = a + (a * a2) * q, big = copysign((1.0 - e) * r, a);
+  t = ax < 0.125 ? small : big;
+  s = 4.0 * e * (r * r);
+}
+
+// as normal_cdf, by the polynomial of degree 12 (4.4e-10 relative); beyond z = 40 the
+// tail is 0
+__device__ __forceinline__ double normal_cdf64(double a, double& gauss) {
+  const double ax = fabs(a), z = ax > 57.0 ? 40.0 : ax * 0.70710678118654752;
+  const double t = rcp64(1.0 + 0.4 * z);
+  double q = 0.018811505674425494;
+  q = q * t - 0.10729278008867346;
+  q = q * t + 0.2368782544815048;
+  q = q * t - 0.23579579003834877;
+  q = q * t + 0.09861019955377608;
+  q = q * t - 0.05597279960943107;
+  q = q * t + 0.026584252877690683;
+  q = q * t + 0.06602337594654571;
+  q = q * t + 0.1216543416565863;
+  q = q * t + 0.1715270196183585;
+  q = q * t + 0.20762072780160984;
+  q = q * t + 0.22567585925075515;
+  q = q * t + 0.22567583331895807;
+  gauss = exp64(-z * z);
+  const double tail = 0.5 * t * q * gauss;
+  return a < 0.0 ? tail : 1.0 - tail;
+}
+
+// as logistic
+__device__ __forceinline__ double logistic64(double a, double& c) {
+  const double e = exp64(-fabs(a)), r = rcp64(1.0 + e);
+  c = a < 0.0 ? r : e * r;
+  return a < 0.0 ? e * r : r;
+}
+
+// a, where it is beside a factor that is 0 beyond `most`
+__device__ __forceinline__ double bounded64(double a, double most) { return fabs(a) < most ? a : copysign(most, a); }
+
+// ---------------------------------------------------------------------------
+// of results of type TO
+// ---------------------------------------------------------------------------
+template <int ACT, class TO>
 __device__ __forceinline__ float act_value(float a) {
+  constexpr bool X64 = sizeof(TO) == 4;
   if constexpr (ACT == PIGAN_ACT_TANH) {
-    float t, s;
-    tanh_ts(a, t, s);
-    return t;
+    if constexpr (X64) {
+      double t, s;
+      tanh64(a, t, s);
+      return (float)t;
+    } else {
+      float t, s;
+      tanh_ts(a, t, s);
+      return t;
+    }
   } else if constexpr (ACT == PIGAN_ACT_RELU) {
     return a < 0.0f ? 0.0f : a;      // a NaN stays one
   } else if constexpr (ACT == PIGAN_ACT_GELU) {
-    float g;
-    return a * normal_cdf(a, g);
+    if constexpr (X64) {
+      double g;
+      return (float)(a * normal_cdf64(a, g));
+    } else {
+      float g;
+      return a * normal_cdf(a, g);
+    }
   } else if constexpr (ACT == PIGAN_ACT_SILU) {
-    float c;
-    return a * logistic(a, c);
+    if constexpr (X64) {
+      double c;
+      return (float)(a * logistic64(a, c));
+    } else {
+      float c;
+      return a * logistic(a, c);
+    }
   } else {
     return a;
   }
 }
 
-template <int ACT>
+template <int ACT, class TO>
 __device__ __forceinline__ float act_slope(float a) {
+  constexpr bool X64 = sizeof(TO) == 4;
   if constexpr (ACT == PIGAN_ACT_TANH) {
-    float t, s;
-    tanh_ts(a, t, s);
-    return s;
+    if constexpr (X64) {
+      double t, s;
+      tanh64(a, t, s);
+      return (float)s;
+    } else {
+      float t, s;
+      tanh_ts(a, t, s);
+      return s;
+    }
   } else if constexpr (ACT == PIGAN_ACT_RELU) {
     return a > 0.0f ? 1.0f : 0.0f;
   } else if constexpr (ACT == PIGAN_ACT_GELU) {
-    float g;
-    const float p = normal_cdf(a, g);
-    return p + a * g * 0.3989422804014327f;   // 1 / sqrt(2 pi)
+    if constexpr (X64) {
+      double g;
+      const double p = normal_cdf64(a, g);
+      return (float)(p + bounded64(a, 64.0) * g * 0.3989422804014327);   // 1 / sqrt(2 pi)
+    } else {
+      float g;
+      const float p = normal_cdf(a, g);
+      return p + a * g * 0.3989422804014327f;
+    }
   } else if constexpr (ACT == PIGAN_ACT_SILU) {
-    float c;
-    const float s = logistic(a, c);
-    return s + a * s * c;
+    if constexpr (X64) {
+      double c;
+      const double s = logistic64(a, c);
+      return (float)(s + bounded64(a, 1000.0) * s * c);
+    } else {
+      float c;
+      const float s = logistic(a, c);
+      return s + a * s * c;
+    }
   } else {
     return 1.0f;
   }

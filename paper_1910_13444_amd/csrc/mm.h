@@ -72,12 +72,12 @@ __device__ __forceinline__ void mm_epilogue(const MmOut<TO>& o, int g, int64_t i
     for (int e = 0; e < 8; ++e) v[e] += bias[e];
     if (o.pre) store8(o.pre + g * o.gsp + i * o.ldp + j, valid, v);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = act_value<ACT>(v[e]);
+    for (int e = 0; e < 8; ++e) v[e] = act_value<ACT, TO>(v[e]);
   } else if constexpr (KIND == MM_DX && ACT != PIGAN_ACT_NONE) {
     float a[8];
     pre.floats(a);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= act_slope<ACT>(a[e]);
+    for (int e = 0; e < 8; ++e) v[e] *= act_slope<ACT, TO>(a[e]);
   }
   if constexpr (KIND != MM_DW)
     if (o.add) {

@@ -509,7 +509,7 @@ __global__ void __launch_bounds__(256) k_act_bwd(int act, const Mat<const T> dy,
       float fd[E], fa[E];
       piece_floats<T>(piece_load(pd + (int64_t)r * dy.ld + c, N - c), fd);
       piece_floats<T>(piece_load(pa + (int64_t)r * pre.ld + c, N - c), fa);
-      for (int e = 0; e < E; ++e) fd[e] *= act_slope<ACT>(fa[e]);
+      for (int e = 0; e < E; ++e) fd[e] *= act_slope<ACT, T>(fa[e]);
       piece_store(po + (int64_t)r * out.ld + c, N - c, fd);
     }
   })
