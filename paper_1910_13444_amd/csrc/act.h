@@ -162,6 +162,8 @@ __device__ __forceinline__ float act_value(float a) {
   }
 }
 
+// An infinite a (an fp16 pre-activation beyond 65504 is stored as one) has the
+// slope's limit: a's size is bounded where the factors beside it have become 0.
 template <int ACT, class TO>
 __device__ __forceinline__ float act_slope(float a) {
   constexpr bool X64 = sizeof(TO) == 4;
@@ -185,7 +187,7 @@ __device__ __forceinline__ float act_slope(float a) {
     } else {
       float g;
       const float p = normal_cdf(a, g);
-      return p + a * g * 0.3989422804014327f;
+      return p + __builtin_amdgcn_fmed3f(a, -64.0f, 64.0f) * g * 0.3989422804014327f;
     }
   } else if constexpr (ACT == PIGAN_ACT_SILU) {
     if constexpr (X64) {
@@ -195,7 +197,7 @@ __device__ __forceinline__ float act_slope(float a) {
     } else {
       float c;
       const float s = logistic(a, c);
-      return s + a * s * c;
+      return s + __builtin_amdgcn_fmed3f(a, -200.0f, 200.0f) * s * c;
     }
   } else {
     return 1.0f;

@@ -1,13 +1,41 @@
-"""The activations of the linear layer over their range."""
+"""The activations of the linear layer at the edges of their range."""
 import math
 
 import pytest
 import torch
 
 from paper_1910_13444_amd import pigan
-from _layers import act64
+from _layers import DT, act64
 
 pytestmark = pytest.mark.gpu
+
+LIMITS = {"tanh": (0.0, 0.0), "relu": (0.0, 1.0), "gelu": (0.0, 1.0), "silu": (0.0, 1.0)}   # slopes at -inf, inf
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("act", list(LIMITS))
+def test_slopes_at_infinity(act, dtype):
+    """The limits, elementwise and in the epilogue of dx; a NaN stays one but for
+    relu, whose slope is 1 for a > 0 alone."""
+    a = torch.tensor([-math.inf, math.inf, math.nan, 0.0], dtype=DT[dtype], device="cuda")
+    far = torch.tensor([*LIMITS[act], 0.0 if act == "relu" else math.nan, {"tanh": 1.0, "relu": 0.0}.get(act, 0.5)])
+    g = pigan.act_backward(torch.ones_like(a)[None], a[None], act)[0].float().cpu()
+    assert torch.equal(g.nan_to_num(7.0), far.nan_to_num(7.0))
+    for M in (4, 300):   # dx = 1 * 2 * slope
+        x = a.repeat(M, 16)
+        dx = pigan.linear_backward(torch.ones_like(x[:, :1]), x, torch.full_like(x[:1], 2.0), act=act, pre=x, need_dw=False)[0]
+        assert torch.equal(dx.float().cpu().nan_to_num(7.0), (2 * far).repeat(M, 16).nan_to_num(7.0))
+
+
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+def test_overflowed_preactivations_keep_the_gradient_finite(act):
+    """fp16: a pre-activation of -1e5 is stored as -inf, while its activation is 0."""
+    x = torch.full((200, 64), -40.0, dtype=torch.float16, device="cuda")
+    w = torch.full((64, 64), 40.0, dtype=torch.float16, device="cuda")
+    y, pre = pigan.linear(x, w, act=act, save_pre=True)
+    assert not y.any() and torch.isneginf(pre).all()
+    assert not pigan.act_backward(torch.ones_like(pre), pre, act).any()
+
 
 def _range():
     """-100 .. 100, densely around 0, and the powers of two down to the smallest value"""
