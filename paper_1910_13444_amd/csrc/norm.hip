@@ -31,8 +31,8 @@ __device__ __forceinline__ void row_store(T* p, int64_t c, int64_t N, const floa
 // Sums over the TPR threads of a row, in a fixed order; every one of them gets
 // them.  Above a wave, `red` (K entries per wave) passes the waves' sums on; the
 // caller alternates between two of them, so one barrier is enough.
-template <int TPR, int K>
-__device__ __forceinline__ void row_sums(float (&v)[K], float* red) {
+template <int TPR, int K, class S>
+__device__ __forceinline__ void row_sums(S (&v)[K], S* red) {
 #pragma unroll
   for (int o = 1; o < (TPR < 64 ? TPR : 64); o *= 2)
 #pragma unroll
@@ -44,7 +44,7 @@ __device__ __forceinline__ void row_sums(float (&v)[K], float* red) {
 #pragma unroll
       for (int k = 0; k < K; ++k) red[wave * K + k] = v[k];
     __syncthreads();
-    const float* r = red + wave / NW * NW * K;
+    const S* r = red + wave / NW * NW * K;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       v[k] = r[k];
@@ -53,25 +53,33 @@ __device__ __forceinline__ void row_sums(float (&v)[K], float* red) {
     }
   }
 }
-template <int TPR>
-__device__ __forceinline__ float row_sum(float v, float* red) {
-  float s[1] = {v};
+template <int TPR, class S>
+__device__ __forceinline__ S row_sum(S v, S* red) {
+  S s[1] = {v};
   row_sums<TPR>(s, red);
   return s[0];
 }
 
 // ---------------------------------------------------------------------------
 // Forward.  Two sums over registers (mean, then squared distances from it: no
-// cancellation).  Blocks walk rows; the next row is requested before the
-// present one is worked on, gamma and beta stay in registers.
+// cancellation).  The mean is rounded once, so that a constant row's is that constant:
+// its sum is held in fp64 where fp32 does not hold up to MAX_PIECES pieces of one
+// value, which it does of 8 bits (bf16), and of 11 (fp16) in up to 8192 columns.
+// Blocks walk rows; the next row is requested before the present one is worked on,
+// gamma and beta stay in registers.
 //   bf16, us (TB/s)  524288 x 512: 230 (4.7), 131072 x 2048: 222 (4.8), 32768 x 8192:
 //                    215 (5.0), 16384 x 16384: 205 (5.2); 1250 of 2048 pieces a row
 //                    (26843 x 10000) 280 (3.8)
 // ---------------------------------------------------------------------------
+template <class T, int COLS>
+using MeanSum = std::conditional_t<sizeof(T) == 4 || (__is_same(T, f16) && COLS > 8192), double, float>;
+
 template <class T, int TPR, int NV, int NTH, bool WHOLE>
 __global__ void __launch_bounds__(NTH) k_norm_fwd(const NormArgs<T> p) {
   constexpr int E = EPP<T>, RPB = NTH / TPR;
-  __shared__ float red[2][NTH / 64];
+  typedef MeanSum<T, TPR * NV * E> Sum;
+  __shared__ Sum red0[NTH / 64];
+  __shared__ float red1[NTH / 64];
   const int g = blockIdx.z;
   const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
   const T* x = p.x.p + g * p.x.gs;
@@ -79,7 +87,7 @@ __global__ void __launch_bounds__(NTH) k_norm_fwd(const NormArgs<T> p) {
   const float* gamma = p.gamma ? p.gamma + g * p.N : nullptr;
   const float* beta = p.beta ? p.beta + g * p.N : nullptr;
   const int64_t step = (int64_t)gridDim.x * RPB;
-  const float n = (float)p.N;   // divided by: the mean of a constant row is that constant
+  const float n = (float)p.N;   // divided by: no rounding of 1 / n
 
   float ga[NV][E], be[NV][E];
 #pragma unroll
@@ -106,12 +114,12 @@ __global__ void __launch_bounds__(NTH) k_norm_fwd(const NormArgs<T> p) {
 #pragma unroll
     for (int v = 0; v < NV; ++v) piece_floats<T>(next[v], f[v]);
     if (r0 + step < p.M) request(next, r + step);
-    float s = 0.0f;
+    std::conditional_t<sizeof(T) == 4, double, float> s = 0;
 #pragma unroll
     for (int v = 0; v < NV; ++v)
 #pragma unroll
       for (int e = 0; e < E; ++e) s += f[v][e];       // zeros past the end
-    const float mean = row_sum<TPR>(s, red[0]) / n;
+    const float mean = (float)(row_sum<TPR>((Sum)s, red0) / (Sum)p.N);
     float q = 0.0f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -122,7 +130,7 @@ __global__ void __launch_bounds__(NTH) k_norm_fwd(const NormArgs<T> p) {
         if (WHOLE ? c < p.N : c + e < p.N) q += f[v][e] * f[v][e];
       }
     }
-    const float var = row_sum<TPR>(q, red[1]) / n;
+    const float var = row_sum<TPR>(q, red1) / n;
     const float rstd = 1.0f / sqrtf(var + p.eps);
     if (r < p.M) {
       T* row = y + r * p.out.ld;
@@ -142,32 +150,34 @@ __global__ void __launch_bounds__(NTH) k_norm_fwd(const NormArgs<T> p) {
 }
 
 // Rows too long for registers: the row is read three times (from L2 after the
-// first), a block of 1024 threads per row (bf16 16376 x 16392: 391 us, 2.7 TB/s).
+// first), a block of 1024 threads per row (bf16 16376 x 16392: 419 us, 2.6 TB/s).
 template <class T>
 __global__ void __launch_bounds__(1024) k_norm_fwd_long(const NormArgs<T> p) {
   constexpr int E = EPP<T>;
-  __shared__ float red[2][16];
+  __shared__ double red0[16];
+  __shared__ float red1[16];
   const int g = blockIdx.z;
   const float* gamma = p.gamma ? p.gamma + g * p.N : nullptr;
   const float* beta = p.beta ? p.beta + g * p.N : nullptr;
-  const float n = (float)p.N;   // divided by: the mean of a constant row is that constant
+  const float n = (float)p.N;
   for (int64_t r = blockIdx.x; r < p.M; r += gridDim.x) {
     const T* row = p.x.p + g * p.x.gs + r * p.x.ld;
     T* out = p.out.p + g * p.out.gs + r * p.out.ld;
-    float s = 0.0f, f[E];
+    double s = 0.0;
+    float f[E];
     for (int64_t c = (int64_t)threadIdx.x * E; c < p.N; c += 1024 * E) {
       piece_floats<T>(piece_load(row + c, p.N - c), f);
 #pragma unroll
       for (int e = 0; e < E; ++e) s += f[e];
     }
-    const float mean = row_sum<1024>(s, red[0]) / n;
+    const float mean = (float)(row_sum<1024>(s, red0) / (double)p.N);
     float q = 0.0f;
     for (int64_t c = (int64_t)threadIdx.x * E; c < p.N; c += 1024 * E) {
       piece_floats<T>(piece_load(row + c, p.N - c), f);
 #pragma unroll
       for (int e = 0; e < E; ++e) q += c + e < p.N ? (f[e] - mean) * (f[e] - mean) : 0.0f;
     }
-    const float rstd = 1.0f / sqrtf(row_sum<1024>(q, red[1]) / n + p.eps);
+    const float rstd = 1.0f / sqrtf(row_sum<1024>(q, red1) / n + p.eps);
     for (int64_t c = (int64_t)threadIdx.x * E; c < p.N; c += 1024 * E) {
       float ga[E], be[E];
       piece_floats<T>(piece_load(row + c, p.N - c), f);
@@ -525,7 +535,7 @@ constexpr int64_t MAX_PIECES = 2048;
 
 template <class T, int TPR, int NV, int NTH>
 void fwd(const NormArgs<T>& a, int G, hipStream_t st) {
-  // 16 waves per CU and row of the grid: enough loads in flight, and gamma and
+  // 32 waves per CU and row of the grid: enough loads in flight, and gamma and
   // beta are read once for many rows
   const int64_t most = cdiv(int64_t(256) * 2048 / NTH, G);
   const int64_t blocks = cdiv(a.M, NTH / TPR);
