@@ -135,6 +135,18 @@ class NormCritic:
         return pigan.linear_backward(g_in, x, w["w_in"], need_dx=need_dx, dw=g["w_in"], db=g["b_in"])[0]
 
 
+def _shares(n: int, scale: float, dtype: torch.dtype) -> torch.Tensor:
+    """n values of dtype that add up to `scale`: scale / n each, or its two
+    neighbours in turn.  Rounded alike they would all be off by the same part (up
+    to 2^-9 in bf16), and with them the balance of two sums of different n."""
+    v = scale / n
+    if dtype == torch.float32:
+        return torch.full((n,), v, dtype=dtype)
+    digits, least = (8, -133) if dtype == torch.bfloat16 else (11, -24)
+    unit = 2.0 ** max(math.frexp(v)[1] - digits, least)
+    return (torch.arange(n + 1, dtype=torch.float64) * (v / unit)).round().diff().mul(unit).to(dtype)
+
+
 class CriticTrainer:
     """Wasserstein updates of a NormCritic on batches of fake and real
     snapshots.  `clip` bounds every element of its matrices after an update
@@ -143,6 +155,17 @@ class CriticTrainer:
     def __init__(self, critic: NormCritic, lr: float = 1e-4, clip: float | None = None):
         self.critic, self.clip = critic, clip
         self.opt = Adam(critic.master, lr)
+        self._cotangents = {}   # of the scores, by batch sizes
+
+    def _cotangent(self, S: int, B: int) -> tuple[torch.Tensor, float]:
+        """(dscore [G, S + B, 1], its scale) of the loss.  fp16 has fewer bits
+        below 2^-14: there the shares of large batches are scaled to about 1."""
+        if (S, B) not in self._cotangents:
+            c = self.critic
+            scale = 2.0 ** (min(S, B).bit_length() - 1) if c.dtype == torch.float16 else 1.0
+            d = torch.cat([_shares(S, scale, c.dtype), -_shares(B, scale, c.dtype)])
+            self._cotangents[S, B] = d.to(c.master.device)[:, None].repeat(c.G, 1, 1), scale
+        return self._cotangents[S, B]
 
     def step(self, fake: torch.Tensor, real: torch.Tensor) -> torch.Tensor:
         """One update; returns the loss mean D(fake) - mean D(real) per critic
@@ -150,9 +173,10 @@ class CriticTrainer:
         c = self.critic
         S, B = fake.shape[1], real.shape[1]
         score, saved = c.forward(torch.cat([fake, real], 1).to(c.dtype))
-        dscore = torch.empty_like(score)
-        dscore[:, :S], dscore[:, S:] = 1.0 / S, -1.0 / B
+        dscore, scale = self._cotangent(S, B)
         c.backward(dscore, saved)
+        if scale != 1.0:
+            c.grads.mul_(1.0 / scale)
         self.opt.step(c.grads)
         if self.clip is not None:
             c.matrices.clamp_(-self.clip, self.clip)
