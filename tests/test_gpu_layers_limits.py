@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_1910_13444_amd import pigan
-from _layers import DT
+from _layers import DT, EPS32, sum_error
 
 pytestmark = pytest.mark.gpu
 
@@ -113,3 +113,16 @@ def test_overlapping_calls_are_refused(dtype):
     # what a call does not read may be anywhere
     dx, dw, db = pigan.linear_backward(w.new_ones(300, 64), x, w, need_dw=False, dx=x)
     assert dx is x and torch.equal(x, torch.full_like(x, 64)) and dw is None and torch.equal(db, torch.full_like(db, 300))
+
+
+def test_joins_larger_than_a_launch():
+    """dw in parts of more than 8192 blocks of 256 eights of columns."""
+    M, K, N = 16389, 4096, 4360
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    g = torch.randn((M, N), generator=gen, dtype=torch.bfloat16, device="cuda")
+    x = torch.randn((M, K), generator=gen, dtype=torch.bfloat16, device="cuda")
+    _, dw, db = pigan.linear_backward(g, x, torch.empty((N, K), dtype=torch.bfloat16, device="cuda"), need_dx=False)
+    g64, x64 = g.double().t().contiguous(), x.double()
+    want, rss = g64 @ x64, ((g64 * g64) @ (x64 * x64)).sqrt()
+    assert ((dw.double() - want).abs() <= sum_error(M, rss) + EPS32 * want.abs()).all()
+    assert ((db.double() - g64.sum(1)).abs() <= sum_error(M, g64.square().sum(1).sqrt())).all()

@@ -96,6 +96,22 @@ def test_every_pair_backward(size):
     _judge(dw, g.transpose(-1, -2), x.transpose(-1, -2), "dw")
 
 
+def test_fp32_rows_too_wide_for_buffers():
+    """Planes whose rows are 2^21 values and more apart."""
+    M, K, N = 70, 2 ** 21 + 3, 9
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    x = torch.randn((M, K), generator=gen, device="cuda")
+    w = torch.randn((N, K), generator=gen, device="cuda")
+    g = torch.randn((M, N), generator=gen, device="cuda")
+    _judge(pigan.linear(x, w), x, w, "y")
+    dx, dw, _ = pigan.linear_backward(g, x, w)
+    _judge(dx, g, w.t(), "dx")
+    _judge(dw, g.t(), x.t(), "dw")
+    # k along rows that wide: a layer of 9 inputs
+    dx = pigan.linear_backward(x, g, w.t().contiguous(), need_dw=False)[0]
+    _judge(dx, x, w, "dx of a wide cotangent")
+
+
 def _same(got, a, b, dtype, what):
     """as the formula: the same infinities and NaN, the other elements close"""
     want, _ = mm64(a, b)
