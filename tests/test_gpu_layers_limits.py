@@ -116,13 +116,32 @@ def test_overlapping_calls_are_refused(dtype):
 
 
 def test_joins_larger_than_a_launch():
-    """dw in parts of more than 8192 blocks of 256 eights of columns."""
-    M, K, N = 16389, 4096, 4360
+    """Results in parts, of more than 8192 blocks of 256 eights of columns: dw of a
+    long batch, the forward pass of a long contraction."""
     gen = torch.Generator(device="cuda").manual_seed(7)
-    g = torch.randn((M, N), generator=gen, dtype=torch.bfloat16, device="cuda")
-    x = torch.randn((M, K), generator=gen, dtype=torch.bfloat16, device="cuda")
-    _, dw, db = pigan.linear_backward(g, x, torch.empty((N, K), dtype=torch.bfloat16, device="cuda"), need_dx=False)
+
+    def normal(*shape):
+        return torch.randn(shape, generator=gen, dtype=torch.bfloat16, device="cuda")
+
+    def parts(query, M, K, N):
+        at = (4096, K, 0), (4096, K, 0), (4096, N, 0), (0, 0, 0), (0, 0, 0), (4096, N, 0), (0, 0, 0)
+        need = query(pigan.LINEAR_ARGS.pack(1, 1, 0, 0, M, K, N, *(v for m in at for v in m), 0, 4096, 4096))
+        return need / 4
+
+    M, K, N = 16384, 4096, 4160
+    assert N * K > 8192 * 256 * 8 and parts(pigan.lib().pigan_linear_backward_workspace, M, K, N) >= 2 * N * K
+    g, x = normal(M, N), normal(M, K)
+    _, dw, db = pigan.linear_backward(g, x, normal(N, K), need_dx=False)
     g64, x64 = g.double().t().contiguous(), x.double()
     want, rss = g64 @ x64, ((g64 * g64) @ (x64 * x64)).sqrt()
     assert ((dw.double() - want).abs() <= sum_error(M, rss) + EPS32 * want.abs()).all()
     assert ((db.double() - g64.sum(1)).abs() <= sum_error(M, g64.square().sum(1).sqrt())).all()
+
+    M, K, N = 4096, 8192, 4160
+    assert M * N > 8192 * 256 * 8 and parts(pigan.lib().pigan_linear_forward_workspace, M, K, N) >= 2 * M * N
+    x, w, add = normal(M, K), normal(N, K), normal(M, N)
+    y = pigan.linear(x, w, residual=add)
+    x64, w64 = x.double(), w.double().t().contiguous()
+    want, rss = x64 @ w64 + add.double(), ((x64 * x64) @ (w64 * w64)).sqrt()
+    error = sum_error(K, rss) + EPS32 * want.abs()
+    assert ((y.double() - want).abs() <= error + 2.0 ** -8 * (want.abs() + error)).all()
