@@ -14,6 +14,9 @@ namespace {
 // only the blocks on its diagonal, which pair a chunk with itself, are used.  The
 // lanes of a load then cover 64 P consecutive bytes of a row of w, and there are P
 // times as many blocks.  The waves' sums meet in LDS, in order.
+// Four waves and P = 1 (many strips) are held to the registers of eight waves per
+// SIMD: 2048 blocks are then on the chip at once (fp32 64 x 1024 x 8192 31 us, 34 with
+// seven).
 // Bound by the bytes of w (one row of x, 8192 -> 2048 bf16: 10.3 us, 3.3 TB/s, of
 // which a launch by itself is 2; P = 1 15.6 us).
 // ---------------------------------------------------------------------------
@@ -41,18 +44,21 @@ template <> struct ShortMma<float> {
 };
 
 template <class T, int P, int NW, int U>
-__global__ void __launch_bounds__(64 * NW) k_short_fwd(const MmArgs<T, T> p, uint32_t row_tiles, uint32_t ranges) {
+__global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(P == 1 && NW == 4 ? 8 : 2)))
+k_short_fwd(const MmArgs<T, T> p, uint32_t row_tiles, uint32_t ranges) {
   constexpr int CK = ShortMma<T>::CK, S = 16 / P, TURN = NW * P * CK;   // k per turn of all waves
   __shared__ float sums[NW][16][17];
   const int g = blockIdx.z;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   // strips beyond a launch's x dimension: their range of gridDim.x strips is in y
-  uint32_t tile = blockIdx.y, range = 0;
+  uint32_t tile = blockIdx.y;
+  int64_t strip = blockIdx.x;
   if (ranges > 1) {
-    range = tile / row_tiles;
+    const uint32_t range = tile / row_tiles;
     tile -= range * row_tiles;
+    strip += (int64_t)range * gridDim.x;
   }
-  const int64_t i0 = (int64_t)tile * S, j0 = ((int64_t)range * gridDim.x + blockIdx.x) * S;
+  const int64_t i0 = (int64_t)tile * S, j0 = strip * S;
   const int64_t i = i0 + (lane & (S - 1)), j = j0 + (lane & (S - 1));
   // rows past the end repeat the last one; their results are not stored
   const int64_t kl = (wave * P + ((lane & 15) / S)) * CK + (lane >> 4) * EPP<T>;
