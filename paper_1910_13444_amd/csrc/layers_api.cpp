@@ -332,11 +332,37 @@ bool plan_both(int64_t M, int64_t N, int64_t K, int pairs, int G, MmPlan& dx, Mm
   return both;
 }
 
-// few rows, or so little work that launches count
+// Strips (k_short_fwd) against tiles.  Up to 8 rows w is read once, and little work
+// is over before a tile is full: strips.  Up to 64 rows it is read by up to four
+// strips of 16 rows, and the shorter modelled time decides.
+//   us, strips | tiles (with their planes in fp32)
+//   M x K x N             bf16           fp32
+//   16 x 1024 x 1024      4.6 |  8.2     6.3 | 19.5
+//   64 x 1024 x 1024      4.8 |  8.4     6.4 | 20.8
+//   64 x 2048 x 2048      9.9 | 10.7    16.8 | 28.8
+//   16 x 8192 x 2048     17.1 | 17.0    30.4 | 69.7
+//   64 x 8192 x 2048     31.2 | 16.8    58.7 | 75.0
+//   16 x 1024 x 8192      6.3 |  8.2    10.0 | 36.0
+//   64 x 1024 x 8192     17.0 |  8.8    31.1 | 42.6
+//   19531 x 32 x 32       5.3 |  4.8     5.1 | 10.8    (work 2e7)
+//   1220 x 128 x 128      3.8 |  4.3     4.4 | 10.7    (2e7)
+//   24414 x 64 x 64       8.6 |  5.2     9.9 | 14.8    (1e8)
+//   3333 x 100 x 300      7.0 |  6.2     9.1 | 12.4    (1e8)
 bool short_ok(const pigan_linear* a) {
-  if (a->M <= 64) return true;
+  if (a->M <= 8) return true;
   const double work = (double)a->n_groups * a->M * a->K * a->N;
   return work <= (a->dt == PIGAN_FP32 ? 1e8 : 2e7) && (a->M + 15) / 16 <= 65535;
+}
+
+// Modelled time of strips of 16 rows and columns: a launch, and rounds of 256 blocks
+// that stream K values of their rows (64 x 8192 x 2048: 30 and 57 us)
+double short_us(const pigan_linear* a) {
+  const double blocks = (double)((a->M + 15) / 16) * (double)((a->N + 15) / 16) * a->n_groups;
+  const double round = std::max(0.23, 0.05 + (a->dt == PIGAN_FP32 ? 3.4 : 1.7) * a->K / 1024.0);
+  return 3.0 + std::max(1.0, blocks / 256) * round;
+}
+double split3_us(const pigan_linear* a) {
+  return 2.0 + 10.0 * a->n_groups * a->K * ((double)a->M + a->N) / 4.7e6;
 }
 
 // A matrix of a product, or its form in the workspace: rows of whole, aligned
@@ -406,6 +432,7 @@ ForwardPlan plan_forward(const pigan_linear* a) {
   const int G = a->n_groups;
   const bool fp32 = a->dt == PIGAN_FP32;
   p.mm = plan_mm(STAGE_FWD, a->M, a->N, a->K, fp32 ? 6 : 1, G);
+  if ((p.brief = a->M <= 64 && short_us(a) <= p.mm.us + (fp32 ? split3_us(a) : 0.0))) return p;
   p.x = {&a->x, a->M, a->K};
   p.w = {&a->w, a->N, a->K};
   Operand* ops[2] = {&p.x, &p.w};
