@@ -18,7 +18,8 @@ def test_slopes_at_infinity(act, dtype):
     """The limits, elementwise and in the epilogue of dx; a NaN stays one but for
     relu, whose slope is 1 for a > 0 alone."""
     a = torch.tensor([-math.inf, math.inf, math.nan, 0.0], dtype=DT[dtype], device="cuda")
-    far = torch.tensor([*LIMITS[act], 0.0 if act == "relu" else math.nan, {"tanh": 1.0, "relu": 0.0}.get(act, 0.5)])
+    far = torch.tensor([*LIMITS[act], 0.0 if act == "relu" else math.nan, {"tanh": 1.0, "relu": 0.0}.get(act, 0.5)],
+                       dtype=torch.float32)
     g = pigan.act_backward(torch.ones_like(a)[None], a[None], act)[0].float().cpu()
     assert torch.equal(g.nan_to_num(7.0), far.nan_to_num(7.0))
     for M in (4, 300):   # dx = 1 * 2 * slope

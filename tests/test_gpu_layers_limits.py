@@ -53,7 +53,7 @@ def test_column_sums_beyond_one_dimension_of_a_launch():
     """Sums of more than 2^26 columns: 32 of them by 1024 threads."""
     N = 2 ** 26 + 41
     dy, x = _whole_numbers(2, N), _whole_numbers(2, N).flip(1).contiguous()
-    mean, rstd = torch.zeros(2, device="cuda"), torch.ones(2, device="cuda")
+    mean, rstd = (torch.full((2,), v, dtype=torch.float32, device="cuda") for v in (0.0, 1.0))
     _, dgamma, dbeta = pigan.layer_norm_backward(dy, x, mean, rstd, need_dx=False)
     assert torch.equal(dbeta, dy.float().sum(0)) and torch.equal(dgamma, (dy.float() * x.float()).sum(0))
     dbeta = pigan.linear_backward(dy, x[:, :1], _whole_numbers(N, 1), need_dx=False, need_dw=False)[2]

@@ -100,9 +100,7 @@ def test_fp32_rows_too_wide_for_buffers():
     """Planes whose rows are 2^21 values and more apart."""
     M, K, N = 70, 2 ** 21 + 3, 9
     gen = torch.Generator(device="cuda").manual_seed(9)
-    x = torch.randn((M, K), generator=gen, device="cuda")
-    w = torch.randn((N, K), generator=gen, device="cuda")
-    g = torch.randn((M, N), generator=gen, device="cuda")
+    x, w, g = (torch.randn(shape, generator=gen, **F32) for shape in ((M, K), (N, K), (M, N)))
     _judge(pigan.linear(x, w), x, w, "y")
     dx, dw, _ = pigan.linear_backward(g, x, w)
     _judge(dx, g, w.t(), "dx")
