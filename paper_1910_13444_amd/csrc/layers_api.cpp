@@ -392,7 +392,9 @@ struct Operand {
 //   fwd 4096 x 4096 x 4096    107 | 118 | 193     bwd  227 | 247 | 415
 //   fwd 20000 x 1032 x 1000    70 |     |  83     bwd  122 | 140 | 351
 //   fwd 131072 x 1024 x 1024  284 |     | 466     bwd  529 | 736 | 913
-// (the second and third forward are not copied: x alone would take 20 and 120 us)
+// (the second and third forward are not copied: x alone would take 20 and 120 us.  The
+// ratios are those of the sizes that lose least: at the third, and at the first, where
+// the unaligned kernel takes 1.6 to 1.8 times as long, a copy would still pay)
 constexpr double LOOSE_FWD = 1.35, LOOSE_BWD = 2.0;
 
 template <int N> void plan_copies(Operand* (&ops)[N], int G, double us, double ratio, Carver& cv) {

@@ -4,8 +4,8 @@
 // A block of waves forms a tile of C; a wave owns MT x NT fragments of
 // 32 x 32.  Operands pass through LDS in stages of 64 values of k:
 //   k along the row   a row of the stage is a 128-byte line of a row of A; its
-//                     16-byte segment s sits at s ^ (row & 7), so the 32 rows
-//                     of a fragment read spread over all banks;
+//                     16-byte segment s sits at s ^ (row / 2 & 7), so 16 rows'
+//                     pieces of one k, read together, spread over all banks;
 //   k down the rows   a row of the stage holds the tile's columns of one k;
 //                     segment s of row r sits at s ^ 4 (r & 3) (rows of eight
 //                     segments: s ^ 4 (r / 2 & 1)), which puts the four rows of
