@@ -466,34 +466,35 @@ __global__ void __launch_bounds__(256) k_colsum_rows(const Mat<const T> m, int64
     if (c + e < N) o[e] = s[e];
 }
 
-// Slot sums: 32 columns x 32 slot lanes per block and turn; a slot lane adds every
-// 32nd slot in fp64, the 32 lanes' sums are added in order.  Bound by latency (256
-// slots of 16,382 columns: 5.8 us, 2.9 TB/s).
+// Slot sums: 32 columns x 32 slot lanes per block; a slot lane adds every 32nd slot
+// in fp64, the 32 lanes' sums are added in order.  Bound by latency (256 slots of
+// 16,382 columns: 5.8 us, 2.9 TB/s).  WIDE: more columns than a launch's x dimension
+// holds, 2^25 for every y (a kernel by itself: the blocks are so short that its
+// arithmetic shows; bf16 reverse of 16 x 4 x 7216 28.8 us, 32.1 with it).
+constexpr int64_t SLOT_RANGE = int64_t(1) << 25;
+
+template <bool WIDE>
 __global__ void __launch_bounds__(1024) k_slot_sum(const float* __restrict__ part, int64_t p_g, int n_slots, int64_t n,
                                                    float* __restrict__ dst, int64_t n1, float* __restrict__ dst2) {
   __shared__ double sums[32][33];
   const int cl = threadIdx.x & 31, sl = threadIdx.x >> 5;
+  const int64_t c = (WIDE ? blockIdx.y * SLOT_RANGE : 0) + (int64_t)blockIdx.x * 32 + cl;
   const int g = blockIdx.z;
-  const int64_t step = (int64_t)gridDim.x * 32;
-  for (int64_t c0 = (int64_t)blockIdx.x * 32; c0 < n; c0 += step) {
-    const int64_t c = c0 + cl;
-    double s = 0.0;
-    if (c < n) {
-      const float* q = part + g * p_g + c;
+  double s = 0.0;
+  if (c < n) {
+    const float* q = part + g * p_g + c;
 #pragma unroll 4
-      for (int i = sl; i < n_slots; i += 32) s += (double)q[(int64_t)i * n];
+    for (int i = sl; i < n_slots; i += 32) s += (double)q[(int64_t)i * n];
+  }
+  sums[sl][cl] = s;
+  __syncthreads();
+  if (sl == 0 && c < n) {
+    for (int i = 1; i < 32; ++i) s += sums[i][cl];
+    if (c < n1) {
+      if (dst) dst[g * n1 + c] = (float)s;
+    } else if (dst2) {
+      dst2[g * (n - n1) + c - n1] = (float)s;
     }
-    sums[sl][cl] = s;
-    __syncthreads();
-    if (sl == 0 && c < n) {
-      for (int i = 1; i < 32; ++i) s += sums[i][cl];
-      if (c < n1) {
-        if (dst) dst[g * n1 + c] = (float)s;
-      } else if (dst2) {
-        dst2[g * (n - n1) + c - n1] = (float)s;
-      }
-    }
-    if (c0 + step < n) __syncthreads();   // the sums are read before the next turn's are written
   }
 }
 
@@ -639,9 +640,12 @@ hipError_t launch_norm_bwd(const NormArgs<T>& a, int G, hipStream_t st) {
 hipError_t launch_slot_sum(const float* part, int64_t p_g, int n_slots, int64_t n, float* dst, int64_t n1, float* dst2,
                            int G, hipStream_t st) {
   // a launch's x dimension holds fewer than 2^32 threads
-  const int64_t most = int64_t(1) << 20, blocks = cdiv(n, 32);
-  const dim3 grid((unsigned)(blocks < most ? blocks : most), 1, G);
-  k_slot_sum<<<grid, 1024, 0, st>>>(part, p_g, n_slots, n, dst, n1, dst2);
+  const int64_t most = SLOT_RANGE / 32, blocks = cdiv(n, 32), ranges = cdiv(blocks, most);
+  if (ranges > 65535) return hipErrorInvalidValue;
+  if (ranges > 1)
+    k_slot_sum<true><<<dim3((unsigned)most, (unsigned)ranges, G), 1024, 0, st>>>(part, p_g, n_slots, n, dst, n1, dst2);
+  else
+    k_slot_sum<false><<<dim3((unsigned)blocks, 1, G), 1024, 0, st>>>(part, p_g, n_slots, n, dst, n1, dst2);
   return hipGetLastError();
 }
 
