@@ -28,15 +28,40 @@ __device__ __forceinline__ void row_store(T* p, int64_t c, int64_t N, const floa
   else if (c < N) piece_store(p + c, EPP<T>, f);
 }
 
+// v of the lane whose number differs in bit O, where the O lanes of each aligned group
+// have one value: any lane of the other group will do, and up to 16 lanes LDS is not
+// asked (__shfl_xor becomes a ds_bpermute; fp32 16 x 75,770 x 41 forward 153 us with
+// it, 142 without; the swaps of half rows and half waves for 16 and 32: 148).
+template <int O>
+__device__ __forceinline__ uint32_t other_group(uint32_t v) {
+  if constexpr (O == 1) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xb1, 0xf, 0xf, true);         // quad 1 0 3 2
+  else if constexpr (O == 2) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4e, 0xf, 0xf, true);    // quad 2 3 0 1
+  else if constexpr (O == 4) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xf, 0xf, true);   // 8 lanes mirrored
+  else if constexpr (O == 8) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x140, 0xf, 0xf, true);   // 16 lanes mirrored
+  else return (uint32_t)__shfl_xor((int)v, O);
+}
+template <int O>
+__device__ __forceinline__ float other_group(float v) { return __uint_as_float(other_group<O>(__float_as_uint(v))); }
+template <int O>
+__device__ __forceinline__ double other_group(double v) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, v);
+  return __builtin_bit_cast(double, (uint64_t)other_group<O>((uint32_t)b) | (uint64_t)other_group<O>((uint32_t)(b >> 32)) << 32);
+}
+
 // Sums over the TPR threads of a row, in a fixed order; every one of them gets
 // them.  Above a wave, `red` (K entries per wave) passes the waves' sums on; the
 // caller alternates between two of them, so one barrier is enough.
 template <int TPR, int K, class S>
 __device__ __forceinline__ void row_sums(S (&v)[K], S* red) {
 #pragma unroll
-  for (int o = 1; o < (TPR < 64 ? TPR : 64); o *= 2)
-#pragma unroll
-    for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], o);
+  for (int k = 0; k < K; ++k) {
+    v[k] += other_group<1>(v[k]);
+    v[k] += other_group<2>(v[k]);
+    v[k] += other_group<4>(v[k]);
+    if constexpr (TPR > 8) v[k] += other_group<8>(v[k]);
+    if constexpr (TPR > 16) v[k] += other_group<16>(v[k]);
+    if constexpr (TPR > 32) v[k] += other_group<32>(v[k]);
+  }
   if constexpr (TPR > 64) {
     constexpr int NW = TPR / 64;
     const int wave = threadIdx.x >> 6;
