@@ -18,6 +18,7 @@ template <class T> struct NormArgs {
   float* part;                                         // backward: partial column sums
   int64_t M, N;
   float eps;
+  double inv_n;                                        // forward: 1 / N, set by the launcher
 };
 
 template <class T> hipError_t launch_norm_fwd(const NormArgs<T>& a, int G, hipStream_t st);

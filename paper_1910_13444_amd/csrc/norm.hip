@@ -30,8 +30,8 @@ __device__ __forceinline__ void row_store(T* p, int64_t c, int64_t N, const floa
 
 // v of the lane whose number differs in bit O, where the O lanes of each aligned group
 // have one value: any lane of the other group will do, and up to 16 lanes LDS is not
-// asked (__shfl_xor becomes a ds_bpermute; fp32 16 x 75,770 x 41 forward 153 us with
-// it, 142 without; the swaps of half rows and half waves for 16 and 32: 148).
+// asked (__shfl_xor becomes a ds_bpermute: 7 % of fp32 16 x 75,770 x 41 forward; the
+// swaps of half rows and half waves for 16 and 32 are slower than theirs by 4 %).
 template <int O>
 __device__ __forceinline__ uint32_t other_group(uint32_t v) {
   if constexpr (O == 1) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xb1, 0xf, 0xf, true);         // quad 1 0 3 2
@@ -96,6 +96,9 @@ __device__ __forceinline__ S row_sum(S v, S* red) {
 //                    215 (5.0), 16384 x 16384: 205 (5.2); 1250 of 2048 pieces a row
 //                    (26843 x 10000) 280 (3.8)
 // ---------------------------------------------------------------------------
+__device__ __forceinline__ float mean_of(float sum, float n, double) { return sum / n; }   // no rounding of 1 / n
+__device__ __forceinline__ float mean_of(double sum, float, double inv_n) { return (float)(sum * inv_n); }
+
 template <class T, int COLS>
 using MeanSum = std::conditional_t<sizeof(T) == 4 || (__is_same(T, f16) && COLS > 8192), double, float>;
 
@@ -112,7 +115,7 @@ __global__ void __launch_bounds__(NTH) k_norm_fwd(const NormArgs<T> p) {
   const float* gamma = p.gamma ? p.gamma + g * p.N : nullptr;
   const float* beta = p.beta ? p.beta + g * p.N : nullptr;
   const int64_t step = (int64_t)gridDim.x * RPB;
-  const float n = (float)p.N;   // divided by: no rounding of 1 / n
+  const float n = (float)p.N;
 
   float ga[NV][E], be[NV][E];
 #pragma unroll
@@ -144,7 +147,7 @@ __global__ void __launch_bounds__(NTH) k_norm_fwd(const NormArgs<T> p) {
     for (int v = 0; v < NV; ++v)
 #pragma unroll
       for (int e = 0; e < E; ++e) s += f[v][e];       // zeros past the end
-    const float mean = (float)(row_sum<TPR>((Sum)s, red0) / (Sum)p.N);
+    const float mean = mean_of(row_sum<TPR>((Sum)s, red0), n, p.inv_n);
     float q = 0.0f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -195,7 +198,7 @@ __global__ void __launch_bounds__(1024) k_norm_fwd_long(const NormArgs<T> p) {
 #pragma unroll
       for (int e = 0; e < E; ++e) s += f[e];
     }
-    const float mean = (float)(row_sum<1024>(s, red0) / (double)p.N);
+    const float mean = mean_of(row_sum<1024>(s, red0), n, p.inv_n);
     float q = 0.0f;
     for (int64_t c = (int64_t)threadIdx.x * E; c < p.N; c += 1024 * E) {
       piece_floats<T>(piece_load(row + c, p.N - c), f);
@@ -603,8 +606,10 @@ void bwd(const NormArgs<T>& a, int64_t nb, int G, hipStream_t st) {
 }  // namespace
 
 template <class T>
-hipError_t launch_norm_fwd(const NormArgs<T>& a, int G, hipStream_t st) {
-  if (a.M <= 0) return hipSuccess;
+hipError_t launch_norm_fwd(const NormArgs<T>& args, int G, hipStream_t st) {
+  if (args.M <= 0) return hipSuccess;
+  NormArgs<T> a = args;
+  a.inv_n = 1.0 / (double)a.N;
   const int64_t pc = cdiv(a.N, EPP<T>);
   if (pc <= 8) fwd<T, 8, 1, 256>(a, G, st);
   else if (pc <= 32) fwd<T, 32, 1, 256>(a, G, st);
