@@ -55,11 +55,10 @@ __device__ __forceinline__ float logistic(float a, float& c) {
 // ---------------------------------------------------------------------------
 // in fp64 (1e-9 relative, a hundredth of an fp32 rounding)
 // ---------------------------------------------------------------------------
-// exp(x), x <= 0; a NaN stays one.  2^f on |f| <= 1/2 by its nearest polynomial of
-// degree 7 (4e-11 relative); the whole part of x / ln 2 is in the low bits of its
-// sum with 1.5 * 2^52.
-__device__ __forceinline__ double exp64(double x) {
-  const double y = (x < -800.0 ? -800.0 : x) * 1.4426950408889634;   // below 2^-1150: 0
+// 2^y for -2^20 < y <= 0; a NaN stays one.  2^f on |f| <= 1/2 by its nearest polynomial
+// of degree 7 (4e-11 relative); the whole part of y is in the low bits of its sum with
+// 1.5 * 2^52.
+__device__ __forceinline__ double exp2_64(double y) {
   const double sum = y + 6755399441055744.0, f = y - (sum - 6755399441055744.0);
   double q = 1.5201918109007667e-05;
   q = q * f + 0.00015469291112801776;
@@ -78,50 +77,48 @@ __device__ __forceinline__ double rcp64(double d) {
   return r + r * (1.0 - d * r);
 }
 
+// |a|, but `most` beyond it (where the exponentials below are 0); a NaN stays one
+__device__ __forceinline__ float size_to(float a, float most) { return fabsf(a) > most ? most : fabsf(a); }
+
 // tanh and its slope, as tanh_ts
-__device__ __forceinline__ void tanh64(double a, double& t, double& s) {
-  const double ax = fabs(a), e = exp64(-2.0 * ax), r = rcp64(1.0 + e), a2 = a * a;
+__device__ __forceinline__ void tanh64(float a, double& t, double& s) {
+  const double x = a, a2 = x * x, e = exp2_64(size_to(a, 400.0f) * -2.8853900817779268), r = rcp64(1.0 + e);   // -2 / ln 2
   double q = 62.0 / 2835.0;
   q = q * a2 - 17.0 / 315.0;
   q = q * a2 + 2.0 / 15.0;
   q = q * a2 - 1.0 / 3.0;
-  const double small = a + (a * a2) * q, big = copysign((1.0 - e) * r, a);
-  t = ax < 0.125 ? small : big;
+  const double small = x + (x * a2) * q, big = copysign((1.0 - e) * r, x);
+  t = fabsf(a) < 0.125f ? small : big;
   s = 4.0 * e * (r * r);
 }
 
-// as normal_cdf, by the polynomial of degree 12 (4.4e-10 relative); beyond z = 40 the
-// tail is 0
-__device__ __forceinline__ double normal_cdf64(double a, double& gauss) {
-  const double ax = fabs(a), z = ax > 57.0 ? 40.0 : ax * 0.70710678118654752;
-  const double t = rcp64(1.0 + 0.4 * z);
-  double q = 0.018811505674425494;
-  q = q * t - 0.10729278008867346;
-  q = q * t + 0.2368782544815048;
-  q = q * t - 0.23579579003834877;
-  q = q * t + 0.09861019955377608;
-  q = q * t - 0.05597279960943107;
-  q = q * t + 0.026584252877690683;
-  q = q * t + 0.06602337594654571;
-  q = q * t + 0.1216543416565863;
-  q = q * t + 0.1715270196183585;
-  q = q * t + 0.20762072780160984;
-  q = q * t + 0.22567585925075515;
-  q = q * t + 0.22567583331895807;
-  gauss = exp64(-z * z);
-  const double tail = 0.5 * t * q * gauss;
-  return a < 0.0 ? tail : 1.0 - tail;
+// as normal_cdf, by half the polynomial of degree 12 (4.4e-10 relative)
+__device__ __forceinline__ double normal_cdf64(float a, double& gauss) {
+  const double x = size_to(a, 57.0f), t = rcp64(1.0 + 0.28284271247461901 * x);   // 0.4 / sqrt 2
+  double q = 0.009405752837212747;
+  q = q * t - 0.05364639004433673;
+  q = q * t + 0.1184391272407524;
+  q = q * t - 0.11789789501917438;
+  q = q * t + 0.04930509977688804;
+  q = q * t - 0.027986399804715534;
+  q = q * t + 0.013292126438845341;
+  q = q * t + 0.033011687973272856;
+  q = q * t + 0.06082717082829332;
+  q = q * t + 0.0857635098091793;
+  q = q * t + 0.10381036390080491;
+  q = q * t + 0.11283792962537757;
+  q = q * t + 0.11283791665947903;
+  gauss = exp2_64(x * x * -0.72134752044448170);   // -1 / (2 ln 2)
+  const double tail = t * q * gauss;
+  return a < 0.0f ? tail : 1.0 - tail;
 }
 
 // as logistic
-__device__ __forceinline__ double logistic64(double a, double& c) {
-  const double e = exp64(-fabs(a)), r = rcp64(1.0 + e);
-  c = a < 0.0 ? r : e * r;
-  return a < 0.0 ? e * r : r;
+__device__ __forceinline__ double logistic64(float a, double& c) {
+  const double e = exp2_64(size_to(a, 1000.0f) * -1.4426950408889634), r = rcp64(1.0 + e);
+  c = a < 0.0f ? r : e * r;
+  return a < 0.0f ? e * r : r;
 }
-
-// a, where it is beside a factor that is 0 beyond `most`
-__device__ __forceinline__ double bounded64(double a, double most) { return fabs(a) < most ? a : copysign(most, a); }
 
 // ---------------------------------------------------------------------------
 // of results of type TO
@@ -183,7 +180,7 @@ __device__ __forceinline__ float act_slope(float a) {
     if constexpr (X64) {
       double g;
       const double p = normal_cdf64(a, g);
-      return (float)(p + bounded64(a, 64.0) * g * 0.3989422804014327);   // 1 / sqrt(2 pi)
+      return (float)(p + copysignf(size_to(a, 57.0f), a) * (g * 0.3989422804014327));   // 1 / sqrt(2 pi)
     } else {
       float g;
       const float p = normal_cdf(a, g);
@@ -193,7 +190,7 @@ __device__ __forceinline__ float act_slope(float a) {
     if constexpr (X64) {
       double c;
       const double s = logistic64(a, c);
-      return (float)(s + bounded64(a, 1000.0) * s * c);
+      return (float)(s + copysignf(size_to(a, 1000.0f), a) * (s * c));
     } else {
       float c;
       const float s = logistic(a, c);
