@@ -50,17 +50,25 @@ __device__ __forceinline__ double other_group(double v) {
 
 // Sums over the TPR threads of a row, in a fixed order; every one of them gets
 // them.  Above a wave, `red` (K entries per wave) passes the waves' sums on; the
-// caller alternates between two of them, so one barrier is enough.
-template <int TPR, int K, class S>
+// caller alternates between two of them, so one barrier is enough.  MOVES: by lane
+// moves (between them the compiler puts other work, and holds its registers).
+template <int TPR, bool MOVES = true, int K, class S>
 __device__ __forceinline__ void row_sums(S (&v)[K], S* red) {
+  if constexpr (MOVES) {
 #pragma unroll
-  for (int k = 0; k < K; ++k) {
-    v[k] += other_group<1>(v[k]);
-    v[k] += other_group<2>(v[k]);
-    v[k] += other_group<4>(v[k]);
-    if constexpr (TPR > 8) v[k] += other_group<8>(v[k]);
-    if constexpr (TPR > 16) v[k] += other_group<16>(v[k]);
-    if constexpr (TPR > 32) v[k] += other_group<32>(v[k]);
+    for (int k = 0; k < K; ++k) {
+      v[k] += other_group<1>(v[k]);
+      v[k] += other_group<2>(v[k]);
+      v[k] += other_group<4>(v[k]);
+      if constexpr (TPR > 8) v[k] += other_group<8>(v[k]);
+      if constexpr (TPR > 16) v[k] += other_group<16>(v[k]);
+      if constexpr (TPR > 32) v[k] += other_group<32>(v[k]);
+    }
+  } else {
+#pragma unroll
+    for (int o = 1; o < (TPR < 64 ? TPR : 64); o *= 2)
+#pragma unroll
+      for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], o);
   }
   if constexpr (TPR > 64) {
     constexpr int NW = TPR / 64;
@@ -324,7 +332,9 @@ __global__ void __launch_bounds__((bwd_nth<T, TPR, NV>())) k_norm_bwd(const Norm
       }
     }
     if constexpr (DX) {
-      row_sums<TPR>(s, red[turn]);
+      // (two pieces of a row of 1024 threads: 63 registers spilled with moves, 697 us at
+      // 16384 x 16384)
+      row_sums<TPR, !(TPR == 1024 && NV == 2)>(s, red[turn]);
       const float s1 = s[0] / n, s2 = s[1] / n;
       T* row = p.out.p + g * p.out.gs + r * p.out.ld;
 #pragma unroll
