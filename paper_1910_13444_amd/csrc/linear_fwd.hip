@@ -17,8 +17,8 @@ namespace {
 // Four waves and P = 1 (many strips) are held to the registers of eight waves per
 // SIMD: 2048 blocks are then on the chip at once (fp32 64 x 1024 x 8192 31 us, 34 with
 // seven).
-// Bound by the bytes of w (one row of x, 8192 -> 2048 bf16: 10.3 us, 3.3 TB/s, of
-// which a launch by itself is 2; P = 1 15.6 us).
+// Bound by the bytes of w (one row of x, 8192 -> 2048 bf16: 9.8 us, 3.4 TB/s, of
+// which a launch by itself is 2; P = 1 15.6 us; fp32 14.9 us, 4.5 TB/s).
 // ---------------------------------------------------------------------------
 template <class T> struct ShortMma;
 template <> struct ShortMma<bf16> {
@@ -111,7 +111,7 @@ k_short_fwd(const MmArgs<T, T> p, uint32_t row_tiles, uint32_t ranges) {
 // An infinity is (1, 0, inf) with its sign: x2 meets y0 alone, so it is multiplied by
 // no zero but y's own, and x0 y2 is infinite with the right sign where y is, too.
 // Bound by memory: 4 bytes read and 6 written per value (1001 x 2000, 513 x 2000 and
-// 1001 x 513 in 7.5 us, 4.7 TB/s).
+// 1001 x 513 in 7.4 us, 4.7 TB/s).
 // ---------------------------------------------------------------------------
 struct SplitSets {
   SplitSet s[3];

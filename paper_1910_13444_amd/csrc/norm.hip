@@ -100,9 +100,10 @@ __device__ __forceinline__ S row_sum(S v, S* red) {
 // value, which it does of 8 bits (bf16), and of 11 (fp16) in up to 8192 columns.
 // Blocks walk rows; the next row is requested before the present one is worked on,
 // gamma and beta stay in registers.
-//   bf16, us (TB/s)  524288 x 512: 230 (4.7), 131072 x 2048: 222 (4.8), 32768 x 8192:
-//                    215 (5.0), 16384 x 16384: 205 (5.2); 1250 of 2048 pieces a row
-//                    (26843 x 10000) 280 (3.8)
+//   bf16, us (TB/s)  524288 x 512: 222 (4.8), 131072 x 2048: 214 (5.0), 32768 x 8192:
+//                    209 (5.1), 16384 x 16384: 198 (5.4); 1250 of 2048 pieces a row
+//                    (26843 x 10000) 268 (4.0)
+//   fp32             128521 x 1152: 230 (5.2), 2048 x 8191: 25 (5.3)
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ float mean_of(float sum, float n, double) { return sum / n; }   // no rounding of 1 / n
 __device__ __forceinline__ float mean_of(double sum, float, double inv_n) { return (float)(sum * inv_n); }
@@ -186,7 +187,7 @@ __global__ void __launch_bounds__(NTH) k_norm_fwd(const NormArgs<T> p) {
 }
 
 // Rows too long for registers: the row is read three times (from L2 after the
-// first), a block of 1024 threads per row (bf16 16376 x 16392: 419 us, 2.6 TB/s).
+// first), a block of 1024 threads per row (bf16 16376 x 16392: 392 us, 2.7 TB/s).
 template <class T>
 __global__ void __launch_bounds__(1024) k_norm_fwd_long(const NormArgs<T> p) {
   constexpr int E = EPP<T>;
@@ -250,10 +251,10 @@ template <class T, int TPR, int NV> constexpr int bwd_nth() { return TPR <= 64 &
 // Several rows of more than a wave in a block leave its loop together, for its
 // barriers: past the last row they work on zeros (ROWS_JOIN).
 //   bf16, us (TB/s)   no skip      with a skip     one row per 1024 threads
-//   262144 x 1024     319 (5.1)    424 (5.1)
-//   131072 x 2048     298 (5.4)    388 (5.5)       707, 741
-//   65536 x 4096      302 (5.3)    392 (5.5)       390, 449
-//   32768 x 8192      308 (5.2)    403 (5.3)
+//   262144 x 1024     314 (5.1)    421 (5.1)
+//   131072 x 2048     287 (5.6)    388 (5.5)       707, 741
+//   65536 x 4096      289 (5.6)    390 (5.5)       390, 449
+//   32768 x 8192      300 (5.4)    401 (5.4)
 template <class T, int TPR, int NV, bool DX, bool COLS, bool WHOLE>
 __global__ void __launch_bounds__((bwd_nth<T, TPR, NV>())) k_norm_bwd(const NormArgs<T> p, float* __restrict__ d0,
                                                       float* __restrict__ d1, int64_t d_g, int64_t d_b) {
@@ -541,7 +542,8 @@ __global__ void __launch_bounds__(256) k_zeros(float* __restrict__ dst, int64_t 
 }
 
 // g = dy act'(pre), a piece per thread and turn; `vpr` pieces per row.  Bound by
-// memory: 65,536 x 1024 bf16, silu, 72 us (5.6 TB/s).
+// memory: 65,536 x 1024 bf16, silu, 72 us (5.6 TB/s), fp32, gelu, 158 (5.1); in the
+// caches by the fp64 slope (16 x 926 x 1024 fp32, gelu, 39 us, 4.7 TB/s).
 template <class T, class I>
 __global__ void __launch_bounds__(256) k_act_bwd(int act, const Mat<const T> dy, const Mat<const T> pre, const Mat<T> out,
                                                  int64_t M, int64_t N, I vpr) {

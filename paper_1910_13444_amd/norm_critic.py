@@ -1,8 +1,8 @@
 """A layer-normalised residual critic, and a run that trains one.
 
-A Wasserstein critic's gradient penalty rules out batch norm (it couples the
-samples whose gradients it penalises one by one); layer norm is what takes its
-place.  The critic here is G independent networks (one per subdomain) of
+Batch norm couples the samples of a batch, whose scores and gradients a
+Wasserstein critic takes one by one; layer norm is what takes its place.  The
+critic here is G independent networks (one per subdomain) of
 
   h   = act(x W_in^T + b_in)
   h  += act(n W_1^T + b_1) W_2^T + b_2,  n = LN(h)      `blocks` times
@@ -12,7 +12,9 @@ with any sizes.  Host logic only: every product, norm, gradient and update runs
 in libpigan.so kernels on the current stream.  Between the operators nothing is
 launched: bias, activation and residual are the forward products' epilogues, an
 activation's slope and a skip's cotangent those of the reverse ones, and each
-parameter gradient is written to its place in one flat fp32 vector.
+parameter gradient is written to its place in one flat fp32 vector.  There is no
+second-order reverse pass: the trainer bounds the weights by clipping, not by a
+gradient penalty.
 
   python -m paper_1910_13444_amd.norm_critic --steps 50
 
