@@ -518,9 +518,9 @@ pigan_status pigan_adam_update(int64_t n, float* params, const float* grads, flo
  * depend on it.
  *
  * Errors of every entry: EINVAL for null or misaligned pointers, sizes or
- * strides out of range; EWORKSPACE for a missing or small workspace; EDEVICE
- * for a launch failure.  No rows (M = 0) is valid: nothing but zero parameter
- * gradients is written.
+ * strides out of range, operands that overlap; EWORKSPACE for a missing or small
+ * workspace; EDEVICE for a launch failure.  No rows (M = 0) is valid: nothing but
+ * zero parameter gradients is written.
  */
 typedef enum {
   PIGAN_ACT_NONE = 0,
