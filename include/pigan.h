@@ -622,6 +622,162 @@ pigan_status pigan_layer_norm_forward(const pigan_norm* a, void* stream);
 size_t pigan_layer_norm_backward_workspace(const pigan_norm* a);
 pigan_status pigan_layer_norm_backward(const pigan_norm* a, void* ws, size_t ws_bytes, void* stream);
 
+/*
+ * Group norm with an activation, channels last.  A field operand is n_groups
+ * independent layers' samples of P points with C channels; channel c of point p
+ * of sample s of group g is ptr[g * gs + s * ss + p * ld + c].  ld must be at
+ * least C, ss (for more than one sample) at least the extent of a sample's
+ * points and gs (for more than one group) at least that of a group's samples; all
+ * of it spans 2^46 elements at most, no alignment beyond the element's is required.
+ * The C channels are n equal channel groups of c = C / n; each has one mean and
+ * variance per sample, over its channels and all points (P = 1: of rows; n = 1 and
+ * P = 1: layer norm).
+ *
+ * Overlaps of outputs, errors and numbers as for the layers above (sums here are
+ * held in fp64; a constant channel group normalises to beta).  No samples (S = 0)
+ * is valid: nothing but zero parameter gradients is written.  No points is EINVAL.
+ */
+typedef struct {
+  void* p;
+  int64_t ld;
+  int64_t ss;
+  int64_t gs;
+} pigan_field;
+
+typedef struct {
+  int32_t n_groups;
+  int32_t dt;                  /* a pigan_dtype value: x, y, dy, dx, add */
+  int32_t act;                 /* a pigan_act value */
+  float eps;                   /* forward: > 0 */
+  int64_t S, P, C;             /* S >= 0; P, C in [1, 2^31 - 1] */
+  int64_t n;                   /* channel groups: a divisor of C */
+  pigan_field x;
+  pigan_field y;               /* forward: output (may be x) */
+  pigan_field dy;              /* backward: cotangent of y */
+  pigan_field add;             /* backward: added to dx, or p = NULL (may be dx) */
+  pigan_field dx;              /* backward: output, or p = NULL (may be dy or add, not x) */
+  const float* gamma;          /* [n_groups, C], or NULL: ones */
+  const float* beta;           /* [n_groups, C], or NULL: zeros; backward: read where act is not NONE */
+  float* mean;                 /* [n_groups, S, n]: forward: output, or NULL; backward: input */
+  float* rstd;                 /* [n_groups, S, n]: as mean */
+  float* dgamma;               /* backward: [n_groups, C] output, or NULL */
+  float* dbeta;                /* backward: [n_groups, C] output, or NULL */
+} pigan_group_norm;
+
+/*
+ * pigan_group_norm_forward — y = act((x - mean) rstd gamma + beta), with
+ *   rstd = 1 / sqrt(variance + eps).
+ *
+ * pigan_group_norm_backward — from the cotangent dy of y, with
+ *   xhat = (x - mean) rstd, da = dy act'(xhat gamma + beta) and h = da gamma:
+ *   dx = rstd (h - mean(h) - xhat mean(h xhat)) + add (means over the channel
+ *        group's channels and points),
+ *   dgamma = sum of da xhat and dbeta = sum of da over samples and points.
+ *
+ * The workspace (256-byte aligned; NULL where none is needed) depends on the sizes,
+ * the type and which outputs are given; the queries return 0 for invalid arguments
+ * and 1 where none is needed.
+ */
+size_t pigan_group_norm_forward_workspace(const pigan_group_norm* a);
+pigan_status pigan_group_norm_forward(const pigan_group_norm* a, void* ws, size_t ws_bytes, void* stream);
+size_t pigan_group_norm_backward_workspace(const pigan_group_norm* a);
+pigan_status pigan_group_norm_backward(const pigan_group_norm* a, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * AdamW over many tensors at once: one launch updates all of them, from a table
+ * that says where they are.  The table is laid out once, in host memory
+ * (pigan_tensors_table), and copied by the caller, byte for byte, to device memory;
+ * the calls below take both copies (the host's for what a launch needs, the device's
+ * for the kernels).  It holds the tensors' addresses: it is good for as long as they
+ * are where they were.
+ *
+ * Parameters are fp32 masters; gradients are fp32, bf16 or fp16; a parameter's 16-bit
+ * copy, where there is one, is written with it.  States lie in flat arrays of the
+ * caller's, zero at first, in the order of the tensors:
+ *   bits 32: fp32 m and v, a tensor's right behind the one's before;
+ *   bits 8:  int8 m and uint8 v, codes of blocks of 256 elements (the last block of a
+ *            tensor padded with zeros), and an fp32 scale per block.  With the scale s,
+ *            the largest size in the block,
+ *              m = s q |q| / 127^2,  q = sign(m) round(127 sqrt(|m| / s)),
+ *              v = s q^4 / 255^4,    q = round(255 (v / s)^(1/4)), at least 1 for v > 0.
+ *            The step itself takes the new states before they are coded; the next one
+ *            finds what the codes stand for.  In a block with a state that is not finite
+ *            the scales are NaN.
+ *   bits 0:  none: a table of gradients alone, for pigan_grad_norm.
+ * Updates are formed in fp64, each result is rounded once.
+ */
+typedef struct {
+  float* p;                    /* [n] fp32, updated in place (bits 0: ignored) */
+  const void* g;               /* [n] of g_dt */
+  void* copy;                  /* [n] of copy_dt, or NULL */
+  int64_t n;                   /* >= 0 */
+  double decay;                /* weight decay: finite, >= 0 */
+  int32_t g_dt;                /* a pigan_dtype value */
+  int32_t copy_dt;             /* PIGAN_BF16 or PIGAN_FP16 where copy is given */
+} pigan_tensor;
+
+typedef struct {
+  int32_t n_tensors;           /* >= 0 */
+  int32_t bits;                /* 0, 8 or 32 */
+  const pigan_tensor* tensors; /* [n_tensors], host memory */
+  void* m;                     /* flat states; 8 bits: 4-byte aligned */
+  void* v;
+  float* m_scale;              /* 8 bits: [state elements / 256] */
+  float* v_scale;
+} pigan_tensors;
+
+/* Elements of a flat state (-1 for invalid arguments; m and v are not looked at). */
+int64_t pigan_tensors_states(const pigan_tensors* a);
+/* Bytes of the table (0 for invalid arguments). */
+size_t pigan_tensors_table_bytes(const pigan_tensors* a);
+/* Writes the table to host memory (8-byte aligned).  EINVAL for null or misaligned
+ * pointers, sizes, types or decays out of range, 2^40 elements and more, and for
+ * parameters, copies and states that overlap each other or a gradient. */
+pigan_status pigan_tensors_table(const pigan_tensors* a, void* table, size_t bytes);
+
+/*
+ * pigan_grad_norm — over all gradients of a table
+ *   norm = scale sqrt(sum of g^2),  coef = scale min(1, max_norm / norm),
+ *   nonfinite = 1 where a gradient is infinite or NaN (coef is then 0 or scale), else 0.
+ * scale (1 / loss scale) is finite and > 0, max_norm > 0 (may be infinite).  Outputs on
+ * the device; any of them may be NULL, not all.  Sums in fp64, in a fixed order.
+ * The workspace is 256-byte aligned.
+ */
+size_t pigan_grad_norm_workspace(const void* table);
+pigan_status pigan_grad_norm(const void* table, const void* device_table, double max_norm, double scale, float* norm,
+                             float* coef, int32_t* nonfinite, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * pigan_adamw_update — with g' = scale coef g,
+ *   m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2,
+ *   p = p - lr ((m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps) + decay p)
+ * of every tensor, and its copy.
+ *   t     : count of updates including this one, where step is NULL;
+ *   step  : device int32 or NULL: the count of updates so far.  The call adds one and
+ *           uses it as t, on the device, so that a captured call counts its replays;
+ *           it then needs a workspace of PIGAN_ADAMW_WORKSPACE bytes, 256-byte aligned;
+ *   coef  : device fp32 factor of the gradients (pigan_grad_norm's), or NULL: 1;
+ *   skip  : device int32 (a step's or pigan_grad_norm's flag) or NULL; when it holds a
+ *           non-zero value nothing is changed, the count included.
+ */
+#define PIGAN_ADAMW_WORKSPACE 256
+typedef struct {
+  const void* table;
+  const void* device_table;
+  double lr, beta1, beta2, eps;
+  double scale;                /* finite, > 0 */
+  const float* coef;
+  const int32_t* skip;
+  int32_t* step;
+  int32_t t;                   /* >= 1 where step is NULL */
+  int32_t reserved;            /* 0 */
+} pigan_adamw;
+pigan_status pigan_adamw_update(const pigan_adamw* a, void* ws, size_t ws_bytes, void* stream);
+
+/* The fp32 values of n 8-bit states (n a multiple of 256); either output may be NULL. */
+pigan_status pigan_state_values(int64_t n, const int8_t* m, const float* m_scale, const uint8_t* v, const float* v_scale,
+                                float* m_out, float* v_out, void* stream);
+
 /* Thread-local description of the last non-OK status ("" if none). */
 const char* pigan_last_error(void);
 

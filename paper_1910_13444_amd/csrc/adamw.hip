@@ -1,0 +1,347 @@
+// AdamW over many tensors at once, with states in 32 or in 8 bits, the norm of their
+// gradients, and the values of 8-bit states, for gfx950.
+//
+//   g' = coef g,  m = b1 m + (1 - b1) g',  v = b2 v + (1 - b2) g'^2,
+//   p -= lr (m c1 / (sqrt(v c2) + eps) + decay p),   c = 1 / (1 - b^t)
+//
+// A table says which piece of which tensor a block takes, so one launch does all.
+// States are fp32 values; everything between is formed in fp64 and rounded once: a step
+// moves 16 to 30 bytes an element, which leaves the time, and what an 8-bit state rounds
+// to does not depend on the order of a sum.
+//
+// 8-bit states are codes of QBLOCK elements with the largest size s among them:
+//   m = s q |q| / 127^2,  q = sign(m) round(127 sqrt(|m| / s)),
+//   v = s q^4 / 255^4,    q = round(255 (v / s)^(1/4)), at least 1 for v > 0.
+// The root of v is what divides m: in it both codes are squares, whose steps are fine near
+// the block's largest (0.8 % of it) and reach down to 2^-14 and 2^-16 of it.  A v of 0
+// beside an m that is not would divide by eps alone.  A block that holds a state that is
+// not finite has the scale NaN and codes 0.
+#include "adamw.h"
+
+#include <algorithm>
+
+#include "piece.h"
+
+namespace pigan {
+namespace {
+
+constexpr int NTH = 256;
+
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) v += __shfl_xor(v, o);
+  return v;
+}
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) v = fmaxf(v, __shfl_xor(v, o));
+  return v;
+}
+
+// four elements of a gradient, zeros past `valid`
+__device__ __forceinline__ void load_grad(const void* g, int dt, int64_t i, int64_t valid, float (&f)[4]) {
+  typedef uint32_t half4 __attribute__((ext_vector_type(2), aligned(2)));
+  if (dt == PIGAN_FP32) {
+    const float* p = (const float*)g + i;
+    if (valid >= 4) {
+      const f32x4u v = *(const f32x4u*)p;
+      for (int e = 0; e < 4; ++e) f[e] = v[e];
+    } else {
+      for (int e = 0; e < 4; ++e) f[e] = e < valid ? p[e] : 0.0f;
+    }
+    return;
+  }
+  const uint16_t* p = (const uint16_t*)g + i;
+  uint16_t h[4];
+  if (valid >= 4) {
+    const half4 v = *(const half4*)p;
+    __builtin_memcpy(h, &v, 8);
+  } else {
+    for (int e = 0; e < 4; ++e) h[e] = e < valid ? p[e] : 0;
+  }
+  for (int e = 0; e < 4; ++e)
+    f[e] = dt == PIGAN_BF16 ? __uint_as_float((uint32_t)h[e] << 16) : (float)__builtin_bit_cast(f16, h[e]);
+}
+
+__device__ __forceinline__ void load4(const float* p, int64_t valid, float (&f)[4]) {
+  if (valid >= 4) {
+    const f32x4u v = *(const f32x4u*)p;
+    for (int e = 0; e < 4; ++e) f[e] = v[e];
+  } else {
+    for (int e = 0; e < 4; ++e) f[e] = e < valid ? p[e] : 0.0f;
+  }
+}
+__device__ __forceinline__ void store4(float* p, int64_t valid, const float (&f)[4]) {
+  if (valid >= 4) {
+    f32x4u v;
+    for (int e = 0; e < 4; ++e) v[e] = f[e];
+    *(f32x4u*)p = v;
+  } else {
+    for (int e = 0; e < 4; ++e)
+      if (e < valid) p[e] = f[e];
+  }
+}
+template <class T>
+__device__ __forceinline__ void store_copy4(T* p, int64_t valid, const float (&f)[4]) {
+  typedef uint32_t half4 __attribute__((ext_vector_type(2), aligned(2)));
+  T h[4];
+  for (int e = 0; e < 4; ++e) h[e] = Elem<T>::from_f(f[e]);
+  if (valid >= 4) {
+    half4 v;
+    __builtin_memcpy(&v, h, 8);
+    *(half4*)p = v;
+  } else {
+    for (int e = 0; e < 4; ++e)
+      if (e < valid) p[e] = h[e];
+  }
+}
+__device__ __forceinline__ void store_copy(const TensorEntry& t, int64_t i, int64_t valid, const float (&f)[4]) {
+  if (!t.copy) return;
+  if (t.copy_dt == PIGAN_BF16) store_copy4((bf16*)t.copy + i, valid, f);
+  else store_copy4((f16*)t.copy + i, valid, f);
+}
+
+// ---------------------------------------------------------------------------
+// The step.
+// ---------------------------------------------------------------------------
+struct Coefs { double coef, c1, c2; };
+__device__ __forceinline__ Coefs coefs_of(const AdamwArgs& a) {
+  return {a.coef ? a.scale * (double)*a.coef : a.scale, a.corr ? a.corr[0] : a.c1, a.corr ? a.corr[1] : a.c2};
+}
+
+// the new states, as fp32 values, and the new parameter
+__device__ __forceinline__ void update(const AdamwArgs& a, const Coefs& k, double decay, float g, double m, double v, float& p,
+                                       float& mn, float& vn) {
+  const double gs = k.coef * g;
+  mn = (float)(a.b1 * m + a.nb1 * gs);
+  vn = (float)(a.b2 * v + a.nb2 * gs * gs);
+  const double u = (double)mn * k.c1 / (sqrt((double)vn * k.c2) + a.eps);
+  p = (float)((double)p - a.lr * (u + decay * (double)p));
+}
+
+__global__ void __launch_bounds__(NTH) k_adamw32(const AdamwArgs a) {
+  if (a.skip && *a.skip) return;   // one flag for the whole launch
+  const TensorPiece w = a.pieces[blockIdx.x];
+  const TensorEntry t = a.entries[w.tensor];
+  const Coefs k = coefs_of(a);
+  const int64_t first = (int64_t)w.piece * PIECE;
+  float* m = (float*)a.m + t.state;
+  float* v = (float*)a.v + t.state;
+  for (int it = 0; it < PIECE / (NTH * 4); ++it) {
+    const int64_t i = first + (it * NTH + threadIdx.x) * 4, valid = t.n - i;
+    if (valid <= 0) break;
+    float pf[4], gf[4], mf[4], vf[4];
+    load4(t.p + i, valid, pf);
+    load_grad(t.g, t.g_dt, i, valid, gf);
+    load4(m + i, valid, mf);
+    load4(v + i, valid, vf);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const double mo = mf[e], vo = vf[e];
+      update(a, k, t.decay, gf[e], mo, vo, pf[e], mf[e], vf[e]);
+    }
+    store4(t.p + i, valid, pf);
+    store4(m + i, valid, mf);
+    store4(v + i, valid, vf);
+    store_copy(t, i, valid, pf);
+  }
+}
+
+// The code of size x among a largest of s: the nearest whole root of x top / s, top the
+// largest code's power.  The fp32 root is off by less than one code; the two halfway
+// points, whole powers of halves, decide in fp64.  inv = top / s.
+__device__ __forceinline__ int code_m(float x, double inv) {
+  const double r = (double)x * inv;
+  int q = (int)rintf(sqrtf((float)r));
+  const double lo = q - 0.5, hi = q + 0.5;
+  q += (r > hi * hi) - (q > 0 && r < lo * lo);
+  return min(q, 127);
+}
+__device__ __forceinline__ int code_v(float x, double inv) {
+  const double r = (double)x * inv;
+  int q = (int)rintf(sqrtf(sqrtf((float)r)));
+  const double lo = (q - 0.5) * (q - 0.5), hi = (q + 0.5) * (q + 0.5);
+  q += (r > hi * hi) - (q > 0 && r < lo * lo);
+  return x > 0.0f ? max(min(q, 255), 1) : 0;
+}
+
+constexpr double TOP_M = 127.0 * 127.0, TOP_V = 255.0 * 255.0 * 255.0 * 255.0;
+
+// a wave takes a block of states at a time, four elements a lane
+__global__ void __launch_bounds__(NTH) k_adamw8(const AdamwArgs a) {
+  if (a.skip && *a.skip) return;
+  const TensorPiece w = a.pieces[blockIdx.x];
+  const TensorEntry t = a.entries[w.tensor];
+  const Coefs k = coefs_of(a);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t first = (int64_t)w.piece * PIECE;
+  for (int it = 0; it < PIECE / (NTH * 4); ++it) {
+    const int64_t b = first + (it * (NTH / 64) + wave) * QBLOCK;
+    if (b >= t.n) break;
+    const int64_t i = b + lane * 4, valid = t.n - i, at = t.state + i, qb = (t.state + b) / QBLOCK;
+    float pf[4] = {0, 0, 0, 0}, gf[4] = {0, 0, 0, 0}, mf[4], vf[4];
+    if (valid > 0) {
+      load4(t.p + i, valid, pf);
+      load_grad(t.g, t.g_dt, i, valid, gf);
+    }
+    // states are there to the end of the block
+    const uint32_t mq = *(const uint32_t*)((const int8_t*)a.m + at), vq = *(const uint32_t*)((const uint8_t*)a.v + at);
+    const double ms = (double)a.m_scale[qb] / TOP_M, vs = (double)a.v_scale[qb] / TOP_V;
+    float mmax = 0.0f, vmax = 0.0f;
+    bool finite = true;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int qm = (int)(int8_t)(mq >> (8 * e));
+      const uint32_t qv = (vq >> (8 * e)) & 255;
+      update(a, k, t.decay, gf[e], (double)(qm * abs(qm)) * ms, (double)(qv * qv * qv * qv) * vs, pf[e], mf[e], vf[e]);
+      if (e >= valid) mf[e] = vf[e] = 0.0f;
+      mmax = fmaxf(mmax, fabsf(mf[e]));
+      vmax = fmaxf(vmax, vf[e]);
+      finite = finite && __builtin_isfinite(mf[e]) && __builtin_isfinite(vf[e]);
+    }
+    mmax = wave_max(mmax);
+    vmax = wave_max(vmax);
+    const bool all = __all(finite);
+    const double mi = mmax > 0.0f ? TOP_M / (double)mmax : 0.0, vi = vmax > 0.0f ? TOP_V / (double)vmax : 0.0;
+    uint32_t mo = 0, vo = 0;
+    if (all) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int q = code_m(fabsf(mf[e]), mi);
+        mo |= (uint32_t)(uint8_t)(mf[e] < 0.0f ? -q : q) << (8 * e);
+        vo |= (uint32_t)code_v(vf[e], vi) << (8 * e);
+      }
+    }
+    *(uint32_t*)((int8_t*)a.m + at) = mo;
+    *(uint32_t*)((uint8_t*)a.v + at) = vo;
+    if (lane == 0) {
+      a.m_scale[qb] = all ? mmax : __builtin_nanf("");
+      a.v_scale[qb] = all ? vmax : __builtin_nanf("");
+    }
+    if (valid > 0) {
+      store4(t.p + i, valid, pf);
+      store_copy(t, i, valid, pf);
+    }
+  }
+}
+
+__global__ void k_adamw_begin(double b1, double b2, int32_t* step, const int32_t* skip, double* corr) {
+  int32_t t = *step;
+  if (!(skip && *skip)) *step = ++t;
+  const double n = t < 1 ? 1.0 : (double)t;
+  corr[0] = 1.0 / (1.0 - pow(b1, n));
+  corr[1] = 1.0 / (1.0 - pow(b2, n));
+}
+
+// ---------------------------------------------------------------------------
+// The gradients' norm: a sum of squares per block in fp64, joined in a fixed order.
+// ---------------------------------------------------------------------------
+__global__ void __launch_bounds__(NTH) k_grad_squares(const TensorEntry* __restrict__ entries,
+                                                      const TensorPiece* __restrict__ pieces, int64_t n_pieces,
+                                                      double* __restrict__ part) {
+  __shared__ double sums[NTH / 64];
+  double s = 0.0;
+  for (int64_t b = blockIdx.x; b < n_pieces; b += gridDim.x) {
+    const TensorPiece w = pieces[b];
+    const TensorEntry t = entries[w.tensor];
+    const int64_t first = (int64_t)w.piece * PIECE;
+#pragma unroll
+    for (int it = 0; it < PIECE / (NTH * 4); ++it) {
+      const int64_t i = first + (it * NTH + threadIdx.x) * 4, valid = t.n - i;
+      if (valid <= 0) break;
+      float f[4];
+      load_grad(t.g, t.g_dt, i, valid, f);
+      for (int e = 0; e < 4; ++e) s += (double)f[e] * (double)f[e];
+    }
+  }
+  s = wave_sum(s);
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < NTH / 64; ++i) s += sums[i];
+    part[blockIdx.x] = s;
+  }
+}
+
+__global__ void __launch_bounds__(1024) k_grad_norm(const double* __restrict__ part, int n, double max_norm, double scale,
+                                                    float* norm, float* coef, int32_t* nonfinite) {
+  __shared__ double sums[16];
+  double s = 0.0;
+  for (int i = threadIdx.x; i < n; i += 1024) s += part[i];
+  s = wave_sum(s);
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < 16; ++i) s += sums[i];
+    const double v = scale * sqrt(s);
+    if (norm) *norm = (float)v;
+    if (coef) *coef = (float)(v > max_norm ? scale * (max_norm / v) : scale);
+    if (nonfinite) *nonfinite = !__builtin_isfinite(v);
+  }
+}
+
+__global__ void __launch_bounds__(NTH) k_state_values(int64_t n, const int8_t* __restrict__ m, const float* __restrict__ m_scale,
+                                                      const uint8_t* __restrict__ v, const float* __restrict__ v_scale,
+                                                      float* __restrict__ m_out, float* __restrict__ v_out) {
+  for (int64_t i = ((int64_t)blockIdx.x * NTH + threadIdx.x) * 4; i < n; i += (int64_t)gridDim.x * NTH * 4) {
+    float f[4];
+    if (m_out) {
+      const uint32_t q = *(const uint32_t*)(m + i);
+      const double s = (double)m_scale[i / QBLOCK] / TOP_M;
+      for (int e = 0; e < 4; ++e) {
+        const int c = (int)(int8_t)(q >> (8 * e));
+        f[e] = (float)((double)(c * abs(c)) * s);
+      }
+      store4(m_out + i, 4, f);
+    }
+    if (v_out) {
+      const uint32_t q = *(const uint32_t*)(v + i);
+      const double s = (double)v_scale[i / QBLOCK] / TOP_V;
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t c = (q >> (8 * e)) & 255;
+        f[e] = (float)((double)(c * c * c * c) * s);
+      }
+      store4(v_out + i, 4, f);
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_adamw(const AdamwArgs& a, int bits, int64_t n_pieces, hipStream_t st) {
+  // a launch's x dimension holds fewer than 2^32 threads
+  const int64_t most = int64_t(1) << 23;
+  for (int64_t at = 0; at < n_pieces; at += most) {
+    AdamwArgs part = a;
+    part.pieces += at;
+    const unsigned blocks = (unsigned)std::min(most, n_pieces - at);
+    if (bits == 8) k_adamw8<<<blocks, NTH, 0, st>>>(part);
+    else k_adamw32<<<blocks, NTH, 0, st>>>(part);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_adamw_begin(double b1, double b2, int32_t* step, const int32_t* skip, double* corr, hipStream_t st) {
+  k_adamw_begin<<<1, 1, 0, st>>>(b1, b2, step, skip, corr);
+  return hipGetLastError();
+}
+
+int64_t grad_norm_blocks(int64_t n_pieces) { return std::max<int64_t>(1, std::min<int64_t>(n_pieces, 2048)); }
+
+hipError_t launch_grad_norm(const TensorEntry* entries, const TensorPiece* pieces, int64_t n_pieces, double max_norm,
+                            double scale, double* part, float* norm, float* coef, int32_t* nonfinite, hipStream_t st) {
+  const int blocks = (int)grad_norm_blocks(n_pieces);
+  k_grad_squares<<<blocks, NTH, 0, st>>>(entries, pieces, n_pieces, part);
+  k_grad_norm<<<1, 1024, 0, st>>>(part, blocks, max_norm, scale, norm, coef, nonfinite);
+  return hipGetLastError();
+}
+
+hipError_t launch_state_values(int64_t n, const int8_t* m, const float* m_scale, const uint8_t* v, const float* v_scale,
+                               float* m_out, float* v_out, hipStream_t st) {
+  if (n <= 0) return hipSuccess;
+  const int64_t blocks = std::min<int64_t>((n + NTH * 4 - 1) / (NTH * 4), 8192);
+  k_state_values<<<(unsigned)blocks, NTH, 0, st>>>(n, m, m_scale, v, v_scale, m_out, v_out);
+  return hipGetLastError();
+}
+
+}  // namespace pigan

@@ -7,6 +7,7 @@
 #include "api.h"
 #include "linear.h"
 #include "norm.h"
+#include "operands.h"
 
 namespace pigan {
 namespace {
@@ -29,29 +30,11 @@ pigan_status check_mat(const pigan_mat& m, const char* name, int32_t groups, int
   return PIGAN_OK;
 }
 
-pigan_status check_vec(const void* p, const char* name) {
-  if ((uintptr_t)p % 4) return fail(PIGAN_EINVAL, "%s: pointer is not aligned to its elements", name);
-  return PIGAN_OK;
-}
-
 pigan_status check_dims(int32_t groups, int32_t dt, int64_t M, int64_t N) {
   if (groups < 1 || groups > 65535) return fail(PIGAN_EINVAL, "n_groups=%d out of [1, 65535]", (int)groups);
   if (pigan_status st = check_dtype(dt)) return st;
   if (M < 0 || M > MAX_DIM) return fail(PIGAN_EINVAL, "M=%lld out of [0, 2^31 - 1]", (long long)M);
   if (N < 1 || N > MAX_DIM) return fail(PIGAN_EINVAL, "N=%lld out of [1, 2^31 - 1]", (long long)N);
-  return PIGAN_OK;
-}
-
-pigan_status check_act(int32_t act) {
-  if (act < PIGAN_ACT_NONE || act > PIGAN_ACT_SILU) return fail(PIGAN_EINVAL, "unknown activation %d", (int)act);
-  return PIGAN_OK;
-}
-
-pigan_status check_ws(const void* ws, size_t have, size_t need) {
-  if (need == 0) return PIGAN_OK;
-  if (!ws) return fail(PIGAN_EWORKSPACE, "null workspace, %zu bytes are needed", need);
-  if (have < need) return fail(PIGAN_EWORKSPACE, "workspace of %zu bytes, %zu are needed", have, need);
-  if ((uintptr_t)ws % 256) return fail(PIGAN_EINVAL, "the workspace must be 256-byte aligned");
   return PIGAN_OK;
 }
 
@@ -82,8 +65,6 @@ struct Region {
     return p == o.p && len == o.len && rows == o.rows && ld == o.ld && groups == o.groups && gs == o.gs;
   }
 };
-
-int64_t floor_div(int64_t a, int64_t b) { return a / b - (a % b < 0); }
 
 // pieces of a (from 0 on) and of b (from d on), both ld apart
 bool rows_meet(const Region& a, const Region& b, int64_t d) {
@@ -138,27 +119,8 @@ pigan_status check_apart(const Region (&outs)[NO], const Region (&ins)[NI], F&& 
   return PIGAN_OK;
 }
 
-// an exception may not leave a C entry point
-template <class F> pigan_status guarded(F&& f) noexcept {
-  try {
-    clear_error();
-    return f();
-  } catch (...) {
-    return PIGAN_EDEVICE;
-  }
-}
-
 template <class T> Mat<const T> in(const pigan_mat& m) { return {(const T*)m.p, m.ld, m.gs}; }
 template <class T> Mat<T> out(const pigan_mat& m) { return {(T*)m.p, m.ld, m.gs}; }
-
-// f(element of the storage type)
-template <class F> pigan_status by_dtype(int32_t dt, F&& f) {
-  switch (dt) {
-    case PIGAN_BF16: return f(bf16{});
-    case PIGAN_FP16: return f(f16{});
-    default: return f(float{});
-  }
-}
 
 // ---------------------------------------------------------------------------
 // linear layer: checks

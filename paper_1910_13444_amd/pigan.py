@@ -34,6 +34,14 @@ ACTS = {"none": 0, "tanh": 1, "relu": 2, "gelu": 3, "silu": 4}
 LINEAR_ARGS = struct.Struct("4i3q" + "Pqq" * 7 + "3P")
 ACT_ARGS = struct.Struct("4i2q" + "Pqq" * 3)
 NORM_ARGS = struct.Struct("2i2qfi" + "Pqq" * 5 + "6P")
+# pigan_group_norm, each field as (p, ld, ss, gs)
+GROUP_NORM_ARGS = struct.Struct("3if4q" + "Pqqq" * 5 + "6P")
+# pigan_tensor, pigan_tensors and pigan_adamw
+TENSOR = struct.Struct("3Pqd2i")
+TENSORS_ARGS = struct.Struct("2i5P")
+ADAMW_ARGS = struct.Struct("2P5d3P2i")
+ADAMW_WORKSPACE = 256   # PIGAN_ADAMW_WORKSPACE
+STATE_BLOCK = 256       # elements of a tensor that share the scale of an 8-bit state
 
 
 class PiganError(RuntimeError):
@@ -97,7 +105,7 @@ def lib():
     if not os.path.exists(LIB_PATH):
         raise RuntimeError(f"{LIB_PATH} is missing: build it with `python -m paper_1910_13444_amd.build`")
     L = C.CDLL(LIB_PATH)
-    i32, i64, f32, sz = C.c_int32, C.c_int64, C.c_float, C.c_size_t
+    i32, i64, f32, f64, sz = C.c_int32, C.c_int64, C.c_float, C.c_double, C.c_size_t
     sigs = {
         "pigan_mlp_n_params": (i64, [P]),
         "pigan_gen_forward_workspace": (sz, [P, i32, i32, i32, i32, i32]),
@@ -130,6 +138,17 @@ def lib():
         "pigan_layer_norm_forward": (i32, [P, P]),
         "pigan_layer_norm_backward_workspace": (sz, [P]),
         "pigan_layer_norm_backward": (i32, [P, P, sz, P]),
+        "pigan_group_norm_forward_workspace": (sz, [P]),
+        "pigan_group_norm_forward": (i32, [P, P, sz, P]),
+        "pigan_group_norm_backward_workspace": (sz, [P]),
+        "pigan_group_norm_backward": (i32, [P, P, sz, P]),
+        "pigan_tensors_states": (i64, [P]),
+        "pigan_tensors_table_bytes": (sz, [P]),
+        "pigan_tensors_table": (i32, [P, P, sz]),
+        "pigan_grad_norm_workspace": (sz, [P]),
+        "pigan_grad_norm": (i32, [P, P, f64, f64, P, P, P, P, sz, P]),
+        "pigan_adamw_update": (i32, [P, P, sz, P]),
+        "pigan_state_values": (i32, [i64, P, P, P, P, P, P, P]),
         "pigan_last_error": (C.c_char_p, []),
         "pigan_profile_enable": (i32, [i32]),
         "pigan_profile_read": (i32, [P, i32, P]),
@@ -758,6 +777,271 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, r
                           _vec(mean, "mean", dy, rows), _vec(rstd, "rstd", dy, rows), pg, pb)
     _call_ws(L.pigan_layer_norm_backward, L.pigan_layer_norm_backward_workspace, args, dy, ws)
     return dx, dgamma, dbeta
+
+
+# ---------------------------------------------------------------------------
+# group norm: fields [S, P, C] of S samples, P points and C channels, or
+# [G, S, P, C] for G independent layers, with unit stride along the channels and
+# any strides above
+# ---------------------------------------------------------------------------
+_NO_FIELD = (0, 0, 0, 0)
+
+
+def _field(t: torch.Tensor, name: str, like: torch.Tensor, shape) -> tuple[int, int, int, int]:
+    """(pointer, point stride, sample stride, group stride) of a field operand."""
+    if t.dtype != like.dtype:
+        raise ValueError(f"{name} must be {like.dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.device != like.device:
+        raise ValueError(f"{name} is on {t.device}, expected {like.device}")
+    st = t.stride()
+    extent = shape[-1]
+    if st[-1] != 1 and extent > 1:
+        raise ValueError(f"{name} must have unit stride along its channels")
+    out = []
+    for axis, what in ((-2, "points"), (-3, "samples"), (-4, "groups")):
+        if -axis > len(shape) or shape[axis] < 2:
+            out.append(extent)   # not used
+            continue
+        if st[axis] < extent:
+            raise ValueError(f"{name} has overlapping {what} (stride {st[axis]}, {extent} elements)")
+        out.append(st[axis])
+        extent += (shape[axis] - 1) * st[axis]
+    return t.data_ptr(), *out
+
+
+def _field_dims(x: torch.Tensor, name: str) -> tuple[int, int]:
+    """(groups, dtype) of the field that sets a call's type and device."""
+    if not x.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if x.dim() not in (3, 4):
+        raise ValueError(f"{name} must be [samples, points, channels] or [groups, samples, points, channels]")
+    dt = TORCH_DTYPES.get(x.dtype)
+    if dt is None:
+        raise ValueError(f"{name} must be fp32, bf16 or fp16, got {x.dtype}")
+    return (x.shape[0] if x.dim() == 4 else 1), dt
+
+
+def _new_field(need: bool, t: torch.Tensor | None, name: str, like: torch.Tensor, shape):
+    """(tensor, operand) of a result: the caller's, a new one, or none."""
+    if not need:
+        return None, _NO_FIELD
+    if t is not None:
+        return t, _field(t, name, like, shape)
+    t = torch.empty(shape, dtype=like.dtype, device=like.device)
+    return t, (t.data_ptr(), shape[-1], shape[-2] * shape[-1], shape[-3] * shape[-2] * shape[-1])
+
+
+def group_norm(x: torch.Tensor, n: int, gamma: torch.Tensor | None = None, beta: torch.Tensor | None = None,
+               act: str = "none", eps: float = 1e-5, out: torch.Tensor | None = None, mean: torch.Tensor | None = None,
+               rstd: torch.Tensor | None = None, need_stats: bool = True, ws: torch.Tensor | None = None):
+    """(y, mean, rstd): y = act((x - mean) rstd gamma + beta) of x [.., S, P, C],
+    each of the n groups of C / n neighbouring channels normalised over its
+    channels and all points of a sample, rstd = 1 / sqrt(variance + eps); gamma
+    and beta [.., C], mean and rstd [.., S, n] fp32 (None without need_stats).
+    `out` may be `x`."""
+    L = lib()
+    G, dt = _field_dims(x, "x")
+    shape = x.shape
+    *lead, S, P, C_ = shape
+    if n < 1 or C_ % n:
+        raise ValueError(f"n = {n} channel groups do not divide {C_} channels")
+    chans, stats = (*lead, C_), (*lead, S, n)
+    mx = _field(x, "x", x, shape)
+    out, mo = _new_field(True, out, "out", x, shape)
+    mean, pm = _result_vec(need_stats, mean, "mean", x, stats)
+    rstd, pr = _result_vec(need_stats, rstd, "rstd", x, stats)
+    args = GROUP_NORM_ARGS.pack(G, dt, _act(act), eps, S, P, C_, n, *mx, *mo, *_NO_FIELD, *_NO_FIELD, *_NO_FIELD,
+                                0 if gamma is None else _vec(gamma, "gamma", x, chans),
+                                0 if beta is None else _vec(beta, "beta", x, chans), pm, pr, 0, 0)
+    _call_ws(L.pigan_group_norm_forward, L.pigan_group_norm_forward_workspace, args, x, ws)
+    return out, mean, rstd
+
+
+def group_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
+                        gamma: torch.Tensor | None = None, beta: torch.Tensor | None = None, act: str = "none",
+                        add: torch.Tensor | None = None, need_dx: bool = True, need_params: bool = True,
+                        dx: torch.Tensor | None = None, dgamma: torch.Tensor | None = None,
+                        dbeta: torch.Tensor | None = None, ws: torch.Tensor | None = None):
+    """Gradients of group_norm: (dx, dgamma, dbeta), `add` (a skip's cotangent)
+    added to dx.  mean and rstd [.., S, n] say how many channel groups there are.
+    What is not needed is None.  `dx` may be `dy` or `add`."""
+    L = lib()
+    G, dt = _field_dims(dy, "dy")
+    shape = dy.shape
+    *lead, S, P, C_ = shape
+    n = mean.shape[-1] if mean.dim() else 0
+    chans, stats = (*lead, C_), (*lead, S, n)
+    dx, mdx = _new_field(need_dx, dx, "dx", dy, shape)
+    dgamma, pg = _result_vec(need_params, dgamma, "dgamma", dy, chans)
+    dbeta, pb = _result_vec(need_params, dbeta, "dbeta", dy, chans)
+    args = GROUP_NORM_ARGS.pack(G, dt, _act(act), 0.0, S, P, C_, n, *_field(x, "x", dy, shape), *_NO_FIELD,
+                                *_field(dy, "dy", dy, shape), *(_NO_FIELD if add is None else _field(add, "add", dy, shape)),
+                                *mdx, 0 if gamma is None else _vec(gamma, "gamma", dy, chans),
+                                0 if beta is None else _vec(beta, "beta", dy, chans), _vec(mean, "mean", dy, stats),
+                                _vec(rstd, "rstd", dy, stats), pg, pb)
+    _call_ws(L.pigan_group_norm_backward, L.pigan_group_norm_backward_workspace, args, dy, ws)
+    return dx, dgamma, dbeta
+
+
+# ---------------------------------------------------------------------------
+# many tensors at once: their gradients' norm and their AdamW step
+# ---------------------------------------------------------------------------
+
+def _flat(t: torch.Tensor, name: str, dtypes, device) -> int:
+    """Pointer of a contiguous device tensor."""
+    if not t.is_cuda or (device is not None and t.device != device):
+        raise ValueError(f"{name} must be a device tensor, all of them on one device")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+_F32 = (torch.float32,)
+_HALVES = (torch.bfloat16, torch.float16)
+
+
+class TensorTable:
+    """Where many tensors are, laid out once for the calls that take all of them:
+    gradients (fp32, bf16 or fp16) alone for grad_norm, or with their fp32
+    parameters, 16-bit copies (or None for single ones), weight decays (one for
+    all, or one each) and states of `bits` bits for adamw_update.
+
+    The states m and v (zero at first) are flat tensors made here, in the order of
+    the parameters: fp32, or int8 and uint8 codes with m_scale and v_scale, where
+    each tensor begins at a whole block of 256 (pigan.h has the format); `starts`
+    are the tensors' first elements in them.  The table holds the tensors, and is
+    good as long as they stay where they are: one whose memory was exchanged needs
+    a new table."""
+
+    def __init__(self, grads, params=None, copies=None, decay=0.0, bits: int = 0):
+        self.grads = [g.detach() for g in grads]
+        n = len(self.grads)
+        if (bits == 0) != (params is None) or bits not in (0, 8, 32):
+            raise ValueError("bits is 8 or 32 with params, 0 without")
+        self.params = None if params is None else [p.detach() for p in params]
+        self.copies = [None if c is None else c.detach() for c in copies] if copies is not None else [None] * n
+        self.decay = [float(d) for d in decay] if isinstance(decay, (list, tuple)) else [float(decay)] * n
+        self.bits = bits
+        if not n:
+            raise ValueError("no tensors")
+        if params is None and copies is not None:
+            raise ValueError("copies without params")
+        if any(len(v) != n for v in (self.params or self.grads, self.copies, self.decay)):
+            raise ValueError(f"{n} gradients need {n} parameters, copies and weight decays")
+        dev = self.device = self.grads[0].device
+        rows = []
+        for i, (g, c, d) in enumerate(zip(self.grads, self.copies, self.decay)):
+            pg, pp, pc = _flat(g, f"grads[{i}]", TORCH_DTYPES, dev), 0, 0
+            if self.params is not None:
+                pp = _flat(self.params[i], f"params[{i}]", _F32, dev)
+                if self.params[i].shape != g.shape:
+                    raise ValueError(f"grads[{i}] has shape {tuple(g.shape)}, expected {tuple(self.params[i].shape)}")
+            if c is not None:
+                pc = _flat(c, f"copies[{i}]", _HALVES, dev)
+                if c.shape != g.shape:
+                    raise ValueError(f"copies[{i}] has shape {tuple(c.shape)}, expected {tuple(g.shape)}")
+            rows.append(TENSOR.pack(pp, pg, pc, g.numel(), d, TORCH_DTYPES[g.dtype], 0 if c is None else TORCH_DTYPES[c.dtype]))
+        tensors = C.create_string_buffer(b"".join(rows))
+        L = lib()
+
+        def args(*states):
+            return TENSORS_ARGS.pack(n, bits, C.addressof(tensors), *states)
+
+        count = L.pigan_tensors_states(args(0, 0, 0, 0))
+        if count < 0:   # let the library report why
+            _check(L.pigan_tensors_table(args(0, 0, 0, 0), None, 0))
+        self.m = self.v = self.m_scale = self.v_scale = None
+        self.starts, at = [], 0
+        for g in self.grads:
+            self.starts.append(at)
+            at += g.numel() if bits != 8 else -(-g.numel() // STATE_BLOCK) * STATE_BLOCK
+        if bits:
+            kinds = (torch.int8, torch.uint8) if bits == 8 else (torch.float32, torch.float32)
+            self.m, self.v = (torch.zeros(count, dtype=k, device=dev) for k in kinds)
+        if bits == 8:
+            self.m_scale, self.v_scale = (torch.zeros(count // STATE_BLOCK, dtype=torch.float32, device=dev) for _ in range(2))
+        full = args(*(0 if t is None else t.data_ptr() for t in (self.m, self.v, self.m_scale, self.v_scale)))
+        size = L.pigan_tensors_table_bytes(full)
+        self._host = (C.c_uint64 * -(-size // 8))()
+        _check(L.pigan_tensors_table(full, self._host, size))
+        self._device = torch.frombuffer(self._host, dtype=torch.uint8).to(dev)
+        self.host_ptr, self.device_ptr = C.addressof(self._host), self._device.data_ptr()
+        self._norm_ws = int(L.pigan_grad_norm_workspace(self.host_ptr))
+
+
+def grad_norm(table: TensorTable, max_norm: float = float("inf"), scale: float = 1.0, ws: torch.Tensor | None = None):
+    """(norm, coef, nonfinite) of all gradients of a table, on the device:
+    norm = scale sqrt(sum of squares) and coef = scale min(1, max_norm / norm) in
+    fp32, nonfinite int32 (1 where a gradient is infinite or NaN).  scale is 1 /
+    loss scale."""
+    L = lib()
+    dev = table.device
+    if dev.index != torch.cuda.current_device():
+        with torch.cuda.device(dev):
+            return grad_norm(table, max_norm, scale, ws)
+    norm, coef = torch.empty((), dtype=torch.float32, device=dev), torch.empty((), dtype=torch.float32, device=dev)
+    flag = torch.empty((), dtype=torch.int32, device=dev)
+    if ws is None or ws.numel() < table._norm_ws:
+        ws = torch.empty(table._norm_ws, dtype=torch.uint8, device=dev)
+    elif ws.dtype != torch.uint8 or ws.device != dev or not ws.is_contiguous():
+        raise ValueError(f"ws must be a contiguous torch.uint8 tensor on {dev}")
+    st = L.pigan_grad_norm(table.host_ptr, table.device_ptr, max_norm, scale, norm.data_ptr(), coef.data_ptr(), flag.data_ptr(),
+                           ws.data_ptr(), ws.numel(), torch._C._cuda_getCurrentRawStream(dev.index))
+    if st != OK:
+        _check(st)
+    return norm, coef, flag
+
+
+def _word(t: torch.Tensor | None, name: str, dtype, device) -> int:
+    """Pointer of a single device value."""
+    if t is None:
+        return 0
+    if t.dtype != dtype or t.device != device or t.numel() != 1:
+        raise ValueError(f"{name} must be one {dtype} value on {device}")
+    return t.data_ptr()
+
+
+def adamw_update(table: TensorTable, lr: float, beta1: float, beta2: float, eps: float, t: int = 0, scale: float = 1.0,
+                 coef: torch.Tensor | None = None, skip: torch.Tensor | None = None, step: torch.Tensor | None = None,
+                 ws: torch.Tensor | None = None):
+    """One AdamW update of every parameter of a table from its gradient times
+    scale times coef (one fp32 value on the device, grad_norm's); nothing changes
+    where the int32 `skip` on the device is not 0.  The count of updates, this one
+    included, is t, or what the int32 `step` on the device is after the call has
+    added one to it (for captured calls; a ws of ADAMW_WORKSPACE bytes goes with
+    it)."""
+    dev = table.device
+    if step is not None and (ws is None or ws.numel() < ADAMW_WORKSPACE):
+        ws = torch.empty(ADAMW_WORKSPACE, dtype=torch.uint8, device=dev)
+    if ws is not None and (ws.dtype != torch.uint8 or ws.device != dev or not ws.is_contiguous()):
+        raise ValueError(f"ws must be a contiguous torch.uint8 tensor on {dev}")
+    args = ADAMW_ARGS.pack(table.host_ptr, table.device_ptr, lr, beta1, beta2, eps, scale,
+                           _word(coef, "coef", torch.float32, dev), _word(skip, "skip", torch.int32, dev),
+                           _word(step, "step", torch.int32, dev), t, 0)
+    if ws is None:
+        _call(lib().pigan_adamw_update, args, table._device, None, 0)
+    else:
+        _call(lib().pigan_adamw_update, args, table._device, ws.data_ptr(), ws.numel())
+
+
+def state_values(table: TensorTable):
+    """(m, v): a table's flat states as fp32 values (the states themselves where
+    they are fp32)."""
+    if table.bits != 8:
+        return table.m, table.v
+    dev = table.device
+    if dev.index != torch.cuda.current_device():
+        with torch.cuda.device(dev):
+            return state_values(table)
+    m, v = (torch.empty(table.m.shape, dtype=torch.float32, device=dev) for _ in range(2))
+    _check(lib().pigan_state_values(m.numel(), table.m.data_ptr(), table.m_scale.data_ptr(), table.v.data_ptr(),
+                                    table.v_scale.data_ptr(), m.data_ptr(), v.data_ptr(),
+                                    torch._C._cuda_getCurrentRawStream(dev.index)))
+    return m, v
 
 
 def profile_enable(on: bool = True):

@@ -58,6 +58,53 @@ class Adam:
             None if skip is None else pigan._ptr(skip, "skip", 1, dtype=torch.int32), pigan._stream()))
 
 
+class AdamW:
+    """AdamW over a list of fp32 device parameters and their gradients (fp32, bf16
+    or fp16, kept in place from step to step): one launch updates all of them.
+
+    weight_decay is one factor for all or one per parameter; state_bits 32 or 8
+    (codes of blocks of 256 elements, pigan.h has their format); `copies` 16-bit
+    tensors, or None for single parameters, that every step writes with the new
+    parameters.  The states are flat (m, v, with m_scale and v_scale in 8 bits), in
+    the order of the parameters, each tensor's first element at `starts`.
+
+    capturable: the count of updates is an int32 on the device (`count`) that a
+    captured step advances with every replay; otherwise it is `t`.
+    grad_norm's coef and nonfinite flag are what step takes as scale and skip: a
+    clipped step reads nothing back."""
+
+    def __init__(self, params, grads, lr: float, beta1: float = 0.5, beta2: float = 0.9, eps: float = 1e-8,
+                 weight_decay=0.0, state_bits: int = 32, copies=None, capturable: bool = False):
+        self.table = pigan.TensorTable(grads, params, copies, weight_decay, state_bits)
+        self.m, self.v = self.table.m, self.table.v
+        self.m_scale, self.v_scale = self.table.m_scale, self.table.v_scale
+        self.starts = self.table.starts
+        self.lr, self.beta1, self.beta2, self.eps = float(lr), float(beta1), float(beta2), float(eps)
+        self.t = 0
+        dev = self.table.device
+        self.count = torch.zeros((), dtype=torch.int32, device=dev) if capturable else None
+        self._ws = torch.empty(pigan.ADAMW_WORKSPACE, dtype=torch.uint8, device=dev) if capturable else None
+
+    def grad_norm(self, max_norm: float = float("inf"), scale: float = 1.0):
+        """(norm, coef, nonfinite) of all gradients, on the device (pigan.grad_norm)."""
+        return pigan.grad_norm(self.table, max_norm, scale)
+
+    def step(self, scale=1.0, skip: torch.Tensor | None = None, count: bool = True):
+        """One update from the gradients times `scale` (a number, or one fp32 value
+        on the device), skipped on the device when *skip != 0.  `count` advances t
+        (False when the host knows the step was skipped); a count on the device
+        follows the applied updates by itself."""
+        if count and self.count is None:
+            self.t += 1
+        coef = scale if isinstance(scale, torch.Tensor) else None
+        pigan.adamw_update(self.table, self.lr, self.beta1, self.beta2, self.eps, max(self.t, 1),
+                           1.0 if coef is not None else scale, coef, skip, self.count, self._ws)
+
+    def states(self):
+        """(m, v): the flat states as fp32 values."""
+        return pigan.state_values(self.table)
+
+
 class LossScaler:
     """Dynamic loss scale (halve on a non-finite step, double after
     growth_interval clean steps)."""

@@ -1,0 +1,270 @@
+"""Group norm with an activation against its 64-bit form, element by element, where
+sizes, strides and values can go wrong."""
+import pytest
+import torch
+
+from paper_1910_13444_amd import pigan
+from _fields import ACTS, EPS, backward64, field, forward64
+from _layers import DT, EPS32, check, vector
+
+pytestmark = pytest.mark.gpu
+
+# (G, S, P, C, n)
+SIZES = [(None, 1, 1, 8, 1), (None, 1, 1, 8, 8), (None, 3, 7, 24, 3), (2, 5, 64, 128, 8), (None, 2, 1000, 120, 24),
+         (None, 1, 4097, 64, 4), (None, 3, 33, 30, 3), (None, 2, 5, 10, 10), (None, 1, 300, 1, 1), (3, 2, 1, 4096, 1),
+         (None, 2, 3, 10002, 2), (None, 4, 2, 8200, 1), (None, 130, 1, 1024, 32), (None, 1, 30011, 8, 2),
+         (None, 2, 257, 2048, 2), (2, 70, 1, 96, 12), (None, 9, 16, 40, 5), (None, 3, 1024, 64, 8), (4, 3, 100, 33, 11),
+         (None, 517, 3, 16, 4), (None, 2, 1, 20000, 1), (None, 2, 5000, 48, 1), (None, 2, 2048, 32, 32)]
+
+
+def _lead(G):
+    return () if G is None else (G,)
+
+
+def _inputs(seed, size, dtype, **kw):
+    G, S, P, C, n = size
+    gen = torch.Generator().manual_seed(seed)
+    shape = (*_lead(G), S, P, C)
+    return gen, shape, field(gen, shape, dtype, 1.0, 0.5, **kw), vector(gen, G, C, 0.2, 1.0), vector(gen, G, C, 0.2)
+
+
+def _check_forward(x, n, gamma, beta, act, dtype, got):
+    y, mean, rstd = got
+    y64, m64, r64, err = forward64(x, n, gamma, beta, act)
+    check(mean, m64, 1e-13 * x.double().abs().max().cpu(), "fp32", "mean")
+    check(rstd, r64, 1e-9 * r64, "fp32", "rstd")
+    check(y, y64, err, dtype, "y")
+
+
+def _check_backward(dy, x, mean, rstd, gamma, beta, act, add, dtype, got):
+    dx, dgamma, dbeta = got
+    wdx, wga, wbe = backward64(dy, x, mean, rstd, gamma, beta, act, add)
+    check(dx, *wdx, dtype, "dx")
+    check(dgamma, *wga, "fp32", "dgamma")
+    check(dbeta, *wbe, "fp32", "dbeta")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("i", range(len(SIZES)))
+def test_sizes(i, dtype):
+    size = SIZES[i]
+    act = ACTS[(i + len(dtype)) % 5]
+    G, S, P, C, n = size
+    gen, shape, x, gamma, beta = _inputs(i, size, dtype, pad=(0, 3, 8)[i % 3], spad=(0, 5)[i % 2], offset=i % 4)
+    y, mean, rstd = pigan.group_norm(x, n, gamma, beta, act)
+    _check_forward(x, n, gamma, beta, act, dtype, (y, mean, rstd))
+    dy = field(gen, shape, dtype, 0.1, pad=i % 2, offset=(i + 1) % 4)
+    add = field(gen, shape, dtype, 0.1, spad=i % 3) if i % 2 else None
+    got = pigan.group_norm_backward(dy, x, mean, rstd, gamma, beta, act, add)
+    _check_backward(dy, x, mean, rstd, gamma, beta, act, add, dtype, got)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("act", ACTS)
+def test_activations_and_outputs(act, dtype):
+    """Every activation; results alone, in the caller's and in their inputs' memory."""
+    size = (2, 4, 50, 80, 10)
+    n = size[-1]
+    gen, shape, x, gamma, beta = _inputs(3, size, dtype, pad=8)
+    y, mean, rstd = pigan.group_norm(x, n, gamma, beta, act)
+    _check_forward(x, n, gamma, beta, act, dtype, (y, mean, rstd))
+    alone, a, b = pigan.group_norm(x, n, gamma, beta, act, need_stats=False)
+    assert a is None and b is None and torch.equal(alone, y)
+    same = x.clone()
+    assert torch.equal(pigan.group_norm(same, n, gamma, beta, act, out=same)[0], y) and torch.equal(same, y)
+    dy = field(gen, shape, dtype, 0.1)
+    add = field(gen, shape, dtype, 0.1, pad=3)
+    got = pigan.group_norm_backward(dy, x, mean, rstd, gamma, beta, act, add)
+    _check_backward(dy, x, mean, rstd, gamma, beta, act, add, dtype, got)
+    for k, keep in (("dx", dict(need_params=False)), ("dgamma", dict(need_dx=False))):
+        part = pigan.group_norm_backward(dy, x, mean, rstd, gamma, beta, act, add, **keep)
+        for whole, p in zip(got, part):
+            assert p is None or torch.equal(whole, p)
+    d2, a2 = dy.clone(), add.clone()
+    assert torch.equal(pigan.group_norm_backward(d2, x, mean, rstd, gamma, beta, act, add, dx=d2)[0], got[0])
+    assert torch.equal(pigan.group_norm_backward(dy, x, mean, rstd, gamma, beta, act, a2, dx=a2)[0], got[0])
+    # no gamma, no beta
+    ones, zeros = torch.ones_like(gamma), torch.zeros_like(beta)
+    y, mean, rstd = pigan.group_norm(x, n, act=act)
+    _check_forward(x, n, ones, zeros, act, dtype, (y, mean, rstd))
+    _check_backward(dy, x, mean, rstd, ones, zeros, act, None, dtype,
+                    pigan.group_norm_backward(dy, x, mean, rstd, act=act))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("size", [(None, 2, 40, 64, 8), (None, 1, 9000, 64, 8), (None, 40, 1, 512, 4), (None, 2, 30, 15, 5),
+                                  (None, 1, 7, 9000, 1)])
+def test_constant_group_is_beta(size, dtype):
+    """A mean is rounded once: a group of one value has it, whatever its size."""
+    _, S, P, C, n = size
+    gen, shape, x, gamma, beta = _inputs(5, size, dtype)
+    value = torch.randn((S, 1, n, 1), generator=gen, dtype=torch.float32) * 1000
+    x = x.unflatten(-1, (n, C // n)).copy_(value.to(DT[dtype]).expand(S, P, n, C // n)).flatten(-2)
+    y, mean, rstd = pigan.group_norm(x, n, gamma, beta)
+    assert torch.equal(mean, value.to(DT[dtype]).float().view(S, n).cuda())
+    assert torch.equal(y, beta.to(DT[dtype]).expand(shape))
+
+
+def test_means_far_from_zero():
+    """fp32, a mean of 10,000 spreads: what remains is the rounding of the mean and of
+    the differences, not a difference of squares."""
+    gen = torch.Generator().manual_seed(1)
+    for P in (50, 20000):
+        x = (torch.randn((2, P, 32), generator=gen, dtype=torch.float64) + 1e4).float().cuda()
+        ones, zeros = torch.ones(32).cuda(), torch.zeros(32).cuda()
+        _check_forward(x, 4, ones, zeros, "none", "fp32", pigan.group_norm(x, 4, ones, zeros))
+        first = x.clone()
+        first[:, 0, ::8] = -3e6   # the group's first value, which the sums are taken from
+        _check_forward(first, 4, ones, zeros, "none", "fp32", pigan.group_norm(first, 4, ones, zeros))
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("size,at", [((None, 3, 20, 64, 8), (1, 7, 13)), ((None, 3, 20, 64, 8), (1, 0, 8)),
+                                     ((None, 2, 9000, 64, 8), (1, 8000, 63)), ((None, 2, 30, 15, 5), (0, 2, 4)),
+                                     ((None, 30, 1, 64, 8), (11, 0, 24))])
+def test_infinities_and_nan_stay_in_their_group(size, at, bad):
+    _, S, P, C, n = size
+    for dtype in ("fp32", "bf16"):
+        gen, shape, x, gamma, beta = _inputs(2, size, dtype)
+        clean = [t.clone() for t in pigan.group_norm(x, n, gamma, beta, "silu")]
+        x[at] = bad
+        y, mean, rstd = pigan.group_norm(x, n, gamma, beta, "silu")
+        s, j = at[0], at[2] // (C // n)
+        assert torch.isnan(rstd[s, j]) and torch.isnan(y.unflatten(-1, (n, C // n))[s, :, j]).all()
+        assert (torch.isnan(mean[s, j]) if bad != bad else mean[s, j] == bad)
+        keep = torch.ones((S, n), dtype=torch.bool, device="cuda")
+        keep[s, j] = False
+        assert torch.equal(mean[keep], clean[1][keep]) and torch.equal(rstd[keep], clean[2][keep])
+        some = keep[:, None, :, None].expand(S, P, n, C // n)
+        assert torch.equal(y.unflatten(-1, (n, C // n))[some], clean[0].unflatten(-1, (n, C // n))[some])
+        # a cotangent that is not finite: its group's dx, its channel's sums
+        x[at] = 0.5
+        dy = field(gen, shape, dtype, 0.1)
+        want = [t.clone() for t in pigan.group_norm_backward(dy, x, *clean[1:], gamma, beta)]
+        dy[at] = bad
+        dx, dgamma, dbeta = pigan.group_norm_backward(dy, x, *clean[1:], gamma, beta)
+        assert not torch.isfinite(dx[at]) and not torch.isfinite(dgamma[at[2]]) and not torch.isfinite(dbeta[at[2]])
+        assert torch.equal(dx.unflatten(-1, (n, C // n))[some], want[0].unflatten(-1, (n, C // n))[some])
+        others = torch.arange(C, device="cuda") != at[2]
+        assert torch.equal(dgamma[others], want[1][others]) and torch.equal(dbeta[others], want[2][others])
+
+
+def test_memory_between_points_is_left():
+    """Gaps between points, samples and groups of the outputs keep what they hold."""
+    for dtype in ("bf16", "fp32"):
+        for C, n in ((24, 3), (30, 3)):
+            shape = (2, 3, 5, C)
+            gen = torch.Generator().manual_seed(0)
+            x, gamma, beta = field(gen, shape, dtype, pad=2, spad=3), vector(gen, 2, C), vector(gen, 2, C)
+            outs = []
+            for _ in range(2):
+                buf = torch.full((2 * 3 * 5 * 64,), 7.0, dtype=DT[dtype], device="cuda")
+                outs.append((buf, buf.as_strided(shape, (960, 320, 64, 1), 1)))
+            y, mean, rstd = pigan.group_norm(x, n, gamma, beta, "tanh", out=outs[0][1])
+            pigan.group_norm_backward(x, x, mean, rstd, gamma, beta, "tanh", dx=outs[1][1])
+            for buf, view in outs:
+                assert not torch.equal(view, torch.full_like(view, 7.0))
+                view.fill_(7.0)
+                assert torch.equal(buf, torch.full_like(buf, 7.0))
+
+
+def test_no_samples():
+    x = torch.zeros((0, 5, 16), dtype=torch.bfloat16, device="cuda")
+    gamma = torch.ones(16, device="cuda")
+    y, mean, rstd = pigan.group_norm(x, 4, gamma)
+    assert y.shape == x.shape and mean.shape == (0, 4)
+    dg, db = torch.full((16,), 3.0, device="cuda"), torch.full((16,), 3.0, device="cuda")
+    pigan.group_norm_backward(x, x, mean, rstd, gamma, dgamma=dg, dbeta=db)
+    assert not dg.any() and not db.any()
+
+
+def test_samples_far_apart():
+    """Samples 2^32 + 16 elements apart: offsets pass 32 bits."""
+    far = 2 ** 32 + 16
+    buf = torch.empty(far + 4096, dtype=torch.bfloat16, device="cuda")
+    out = torch.empty(far + 4096, dtype=torch.bfloat16, device="cuda")
+    x, y = (b.as_strided((2, 16, 64), (far, 64, 1)) for b in (buf, out))
+    gen = torch.Generator().manual_seed(4)
+    x.copy_(torch.randn((2, 16, 64), generator=gen, dtype=torch.float32).bfloat16())
+    near = x.clone()
+    gamma, beta = vector(gen, None, 64), vector(gen, None, 64)
+    want = pigan.group_norm(near, 8, gamma, beta, "gelu")
+    got = pigan.group_norm(x, 8, gamma, beta, "gelu", out=y)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    a = pigan.group_norm_backward(near, near, *want[1:], gamma, beta, "gelu")
+    b = pigan.group_norm_backward(x, x, *want[1:], gamma, beta, "gelu", dx=y)
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+def test_gradients_against_differences():
+    """fp32 gradients along random directions against central differences of the
+    64-bit form, whose errors are 1e-8 (step 1e-4 squared) and 1e-12 / 1e-4."""
+    for act in ("none", "tanh", "gelu", "silu"):
+        gen, shape, x, gamma, beta = _inputs(9, (None, 3, 17, 24, 4), "fp32")
+        y, mean, rstd = pigan.group_norm(x, 4, gamma, beta, act)
+        dy = field(gen, shape, "fp32")
+        grads = pigan.group_norm_backward(dy, x, mean, rstd, gamma, beta, act)
+        ins = [t.double().cpu() for t in (x, gamma, beta)]
+        for k in range(3):
+            v = torch.randn(ins[k].shape, generator=gen, dtype=torch.float32).double()
+            ends = []
+            for h in (1e-4, -1e-4):
+                at = list(ins)
+                at[k] = at[k] + h * v
+                ends.append((forward64(at[0], 4, at[1], at[2], act)[0] * dy.double().cpu()).sum())
+            slope = (ends[0] - ends[1]).item() / 2e-4
+            got = (grads[k].double().cpu() * v).sum().item()
+            size = (grads[k].double().cpu() * v).square().sum().sqrt().item()
+            assert abs(got - slope) <= 1e-5 * (size + abs(slope)) + 1e-6, (act, k, got, slope)
+
+
+def test_repeats_streams_and_graphs():
+    """The same call gives the same bits: again, on another stream, replayed from a
+    graph with other work between the replays."""
+    for size in ((None, 3, 9000, 64, 8), (None, 200, 16, 48, 6), (2, 300, 1, 256, 8)):
+        n = size[-1]
+        gen, shape, x, gamma, beta = _inputs(6, size, "bf16")
+        dy = field(gen, shape, "bf16", 0.1)
+
+        def both():
+            y, mean, rstd = pigan.group_norm(x, n, gamma, beta, "silu")
+            return (y, mean, rstd, *pigan.group_norm_backward(dy, x, mean, rstd, gamma, beta, "silu"))
+
+        want = [t.clone() for t in both()]
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            other = both()
+        side.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, other))
+        held = {}
+        graph = pigan.StepGraph(lambda: held.update(out=both()))
+        for k in range(4):
+            x.mul_(0.5)
+            eager = [t.clone() for t in both()]
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(eager, held["out"])), k
+
+
+def test_refusals():
+    x = torch.zeros((2, 8, 16), dtype=torch.bfloat16, device="cuda")
+    stats = torch.zeros((2, 4), device="cuda")
+    vec = torch.ones(16, device="cuda")
+    for bad in (lambda: pigan.group_norm(x, 3), lambda: pigan.group_norm(x, 0), lambda: pigan.group_norm(x[0], 4),
+                lambda: pigan.group_norm(x.double(), 4), lambda: pigan.group_norm(x, 4, vec[:8]),
+                lambda: pigan.group_norm(x, 4, vec.bfloat16()), lambda: pigan.group_norm(x, 4, act="sine"),
+                lambda: pigan.group_norm(x.transpose(1, 2), 4), lambda: pigan.group_norm(x[:1].expand(2, 8, 16), 4),
+                lambda: pigan.group_norm(x, 4, out=torch.empty_like(x).float()),
+                lambda: pigan.group_norm_backward(x, x, stats[:1], stats[:1]),
+                lambda: pigan.group_norm_backward(x, x.float(), stats, stats)):
+        with pytest.raises(ValueError):
+            bad()
+    buf = torch.zeros(400, dtype=torch.bfloat16, device="cuda")
+    a, b = buf[:256].view(2, 8, 16), buf[16:272].view(2, 8, 16)
+    for bad in (lambda: pigan.group_norm(x, 4, eps=0.0), lambda: pigan.group_norm(x[:, :0], 4),
+                lambda: pigan.group_norm(a, 4, out=b), lambda: pigan.group_norm_backward(x, a, stats, stats, dx=a),
+                lambda: pigan.group_norm_backward(a, x, stats, stats, dx=b),
+                lambda: pigan.group_norm_backward(x, x, stats, stats, need_dx=False, need_params=False)):
+        with pytest.raises(pigan.PiganError):
+            bad()
