@@ -11,7 +11,13 @@ template <class T> struct Field {
 
 // How a call's samples are cut.  A slab is the channels that a block works on: whole
 // channel groups, or a part of one that is wider than a block's threads reach.
+enum GnMode {
+  GN_ROWS = 0,          // one point a sample, a channel group in 2^i <= 64 lanes
+  GN_ONE = 1,           // a sample's slab stays in a block's registers
+  GN_SPLIT = 2          // ranges of points, a pass for sums and one for results
+};
 struct GnPlan {
+  int32_t mode;
   int64_t W;            // channels of a slab (the last may have fewer)
   int64_t slabs;        // of a sample
   int64_t ng;           // channel groups of a slab
@@ -21,7 +27,7 @@ struct GnPlan {
   int32_t rows;         // points of a block's threads at a time
   int32_t ns;           // samples of a block at a time; above 1 rows = ns P
   int32_t lanes;        // that sum one channel group of one sample
-  int64_t splits;       // 0: a sample's slab stays in registers; else ranges of its points
+  int64_t splits;       // ranges of a sample's points
   int64_t split_rows;   // points of a range
   int64_t slots;        // reverse pass: partial rows of [dgamma, dbeta]
 };
