@@ -19,9 +19,9 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libpigan.so")
 
-SOURCES = ["gemm.hip", "linear_fwd.hip", "linear_dx.hip", "linear_dw.hip", "norm.hip", "group_norm.hip",
-           "pointwise.hip", "optim.hip", "adamw.hip", "pigan_api.cpp", "layers_api.cpp", "group_norm_api.cpp",
-           "adamw_api.cpp"]
+SOURCES = ["gemm.hip", "linear_fwd.hip", "linear_dx.hip", "linear_dw.hip", "norm.hip", "group_norm_fwd.hip",
+           "group_norm_bwd.hip", "pointwise.hip", "optim.hip", "adamw.hip", "pigan_api.cpp", "layers_api.cpp", "group_norm_api.cpp",
+           "group_norm_plan.cpp", "adamw_api.cpp"]
 ARCH = "gfx950"
 
 

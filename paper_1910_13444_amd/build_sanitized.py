@@ -46,7 +46,8 @@ def _compile(src: str) -> str:
     return obj
 
 
-SANITIZED = ("pigan_api.cpp", "layers_api.cpp", "group_norm_api.cpp", "adamw_api.cpp")
+SANITIZED = ("pigan_api.cpp", "layers_api.cpp", "group_norm_api.cpp", "group_norm_plan.cpp",
+             "adamw_api.cpp")
 
 
 def _object(src: str) -> str:

@@ -86,7 +86,8 @@ pigan_status check_backward_apart(const pigan_group_norm* a, const void* ws, siz
 }
 
 GnPlan plan(const pigan_group_norm* a, bool backward) {
-  return gn_plan(backward, (int)esize(a->dt), a->n_groups, a->S, a->P, a->C, a->n);
+  const int fields = backward ? 2 + !!a->dx.p + (a->dx.p && a->add.p) : 2;
+  return gn_plan(backward, fields, (int)esize(a->dt), a->n_groups, a->S, a->P, a->C, a->n);
 }
 size_t forward_ws(const pigan_group_norm* a, const GnPlan& pl) {
   return a->S > 0 ? gn_forward_ws(pl, a->n_groups, a->S, a->n) : 0;

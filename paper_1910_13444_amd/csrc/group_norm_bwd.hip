@@ -1,0 +1,526 @@
+// Group norm with an activation, channels last, backward, for gfx950.
+#include "group_norm_parts.h"
+#include "norm.h"
+
+namespace pigan {
+namespace {
+
+// the columns' coefficients of a thread
+template <class T, int SL>
+struct Column {
+  float mean[SL], rstd[SL], ga[EPP<T>], be[EPP<T>];
+  __device__ __forceinline__ void load(const GnArgs<T>& a, const Slab& b, const Div& by_span, int64_t g, int64_t s, int col) {
+    constexpr int E = EPP<T>;
+    vec_load<E>(a.gamma ? a.gamma + g * a.C : nullptr, b.c0 + col * E, b.c0 + b.width, 1.0f, ga);
+    vec_load<E>(a.beta ? a.beta + g * a.C : nullptr, b.c0 + col * E, b.c0 + b.width, 0.0f, be);
+    load_stats(a, b, by_span, g, s, col);
+  }
+  // from LDS, [2][wide], again for every piece
+  __device__ __forceinline__ void load_scales(const float* gab, int wide, int col) {
+    constexpr int E = EPP<T>;
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < E; i += 4) {
+      const f32x4 u = *(const f32x4*)(gab + col * E + i), w = *(const f32x4*)(gab + wide + col * E + i);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) { ga[i + q] = u[q]; be[i + q] = w[q]; }
+    }
+  }
+  __device__ __forceinline__ void load_stats(const GnArgs<T>& a, const Slab& b, const Div& by_span, int64_t g, int64_t s, int col) {
+#pragma unroll
+    for (int e = 0; e < SL; ++e) {
+      const int64_t at = (g * a.S + s) * a.n + b.j0 + group_of<T, SL>(b, by_span, col, e);
+      mean[e] = a.mean[at];
+      rstd[e] = a.rstd[at];
+    }
+  }
+};
+
+// xh and da of a piece; zeros past `valid`
+template <int ACT, bool WHOLE, class T, int SL>
+__device__ __forceinline__ void slope_piece(const Column<T, SL>& c, int valid, float (&xh)[EPP<T>], float (&da)[EPP<T>]) {
+#pragma unroll
+  for (int e = 0; e < EPP<T>; ++e) {
+    xh[e] = (xh[e] - c.mean[SL > 1 ? e : 0]) * c.rstd[SL > 1 ? e : 0];
+    if constexpr (ACT != PIGAN_ACT_NONE) da[e] *= slope_of<ACT, T>(xh[e] * c.ga[e] + c.be[e]);
+    if (!WHOLE && e >= valid) xh[e] = da[e] = 0.0f;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Backward, rows and samples whose slabs fit a block's registers.  Blocks walk samples; a
+// thread keeps its columns' sums of da xhat and da over all of them, a block writes one
+// partial row of [dgamma, dbeta] (the final ones, where one block takes all samples).
+// ---------------------------------------------------------------------------
+// bytes of LDS that a group's sums, or half the columns' sums, take
+constexpr size_t bwd_sums_lds(int nth, int sl, int e) {
+  return (size_t)nth * (sl * sizeof(Pair) > (size_t)e * 4 ? sl * sizeof(Pair) : (size_t)e * 4);
+}
+
+// a block's rows of sums, added in order; fm: float [rows][pw * E]
+template <class T>
+__device__ __forceinline__ void store_columns(const GnArgs<T>& a, float* fm, const float (&sg)[EPP<T>], const float (&sb)[EPP<T>],
+                                              const Slab& b, int64_t g, int col, int row) {
+  constexpr int E = EPP<T>;
+  const GnPlan& pl = a.pl;
+  const int wide = pl.pw * E;
+  const bool last = pl.slots == 1;
+  float* d0 = last ? (a.dgamma ? a.dgamma + g * a.C : nullptr) : (float*)a.ws + (g * pl.slots + blockIdx.x) * 2 * a.C;
+  float* d1 = last ? (a.dbeta ? a.dbeta + g * a.C : nullptr) : d0 + a.C;
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    __syncthreads();
+    if (row < pl.rows)
+#pragma unroll
+      for (int e = 0; e < E; ++e) fm[row * wide + col * E + e] = half ? sb[e] : sg[e];
+    __syncthreads();
+    float* d = half ? d1 : d0;
+    for (int c = threadIdx.x; c < b.width; c += blockDim.x) {
+      double t = 0.0;
+      for (int r = 0; r < pl.rows; ++r) t += fm[r * wide + c];
+      if (d) d[b.c0 + c] = (float)t;
+    }
+  }
+  __syncthreads();
+}
+
+template <class T, int NV, int ACT>
+__global__ void __launch_bounds__(256) k_gn_rows_bwd(const GnArgs<T> a) {
+  constexpr int E = EPP<T>;
+  extern __shared__ Pair sm[];
+  const GnPlan& pl = a.pl;
+  const int row = Div(pl.pw)(threadIdx.x), col = threadIdx.x - row * pl.pw;
+  const Slab b = slab_at(a, blockIdx.y);
+  const int64_t g = blockIdx.z;
+  const int lanes = pl.span;
+  const Div by_span(lanes);
+  const float inv_n = (float)pl.inv_n;
+  const bool on = row < pl.rows && col * E < b.width;   // whole groups of lanes
+  float sg[E], sb[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) sg[e] = sb[e] = 0.0f;
+  if (on) {
+    Column<T, 1> c;
+    c.load(a, b, by_span, g, 0, col);
+    const T* x = a.x.p + g * a.x.gs + b.c0 + col * E;
+    const T* dy = a.dy.p + g * a.dy.gs + b.c0 + col * E;
+    const T* add = a.add.p ? a.add.p + g * a.add.gs + b.c0 + col * E : nullptr;
+    T* out = a.out.p ? a.out.p + g * a.out.gs + b.c0 + col * E : nullptr;
+    const int64_t stats = g * a.S * a.n + b.j0 + by_span(col);
+    const int64_t step = (int64_t)gridDim.x * pl.rows;
+    for (int64_t s0 = (int64_t)blockIdx.x * pl.rows + row; s0 < a.S; s0 += NV * step) {
+      piece_t rx[NV];
+      piece_t rd[NV];
+      piece_t ra[NV];
+      float mean[NV];
+      float rstd[NV];
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const int64_t s = s0 + v * step < a.S ? s0 + v * step : s0;
+        rx[v] = load_piece<true>(x + s * a.x.ss, E, pl.stream);
+        rd[v] = load_piece<true>(dy + s * a.dy.ss, E, pl.stream);
+        if (add) ra[v] = load_piece<true>(add + s * a.add.ss, E, pl.stream);
+        mean[v] = a.mean[stats + s * a.n];
+        rstd[v] = a.rstd[stats + s * a.n];
+      }
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const int64_t s = s0 + v * step;
+        if (s >= a.S) break;
+        float xh[E];
+        float da[E];
+        float h0 = 0.0f;
+        float h1 = 0.0f;
+        piece_floats<T>(rx[v], xh);
+        piece_floats<T>(rd[v], da);
+        c.mean[0] = mean[v];
+        c.rstd[0] = rstd[v];
+        slope_piece<ACT, true>(c, E, xh, da);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          sg[e] += da[e] * xh[e];
+          sb[e] += da[e];
+          da[e] *= c.ga[e];
+          h0 += da[e];
+          h1 += da[e] * xh[e];
+        }
+        if (out) {
+          for (int o = 1; o < lanes; o *= 2) {
+            h0 += __shfl_xor(h0, o);
+            h1 += __shfl_xor(h1, o);
+          }
+          h0 *= inv_n;
+          h1 *= inv_n;
+          float r[E];
+          if (add) piece_floats<T>(ra[v], r);
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            da[e] = c.rstd[0] * (da[e] - h0 - xh[e] * h1);
+            if (add) da[e] += r[e];
+          }
+          store_piece<true>(out + s * a.out.ss, E, da, pl.stream);
+        }
+      }
+    }
+  }
+  if (a.dgamma || a.dbeta) store_columns(a, (float*)sm, sg, sb, b, g, col, row);
+}
+
+template <class T, int NTH, int NV, int SL, bool WHOLE, int ACT>
+__global__ void __launch_bounds__(NTH) k_gn_one_bwd(const GnArgs<T> a) {
+  constexpr int E = EPP<T>;
+  extern __shared__ Pair sm[];
+  const GnPlan& pl = a.pl;
+  float* gab = (float*)((char*)sm + bwd_sums_lds(NTH, SL, E));   // gamma and beta of the slab: beside the pieces they would not fit the registers
+  float2* means = (float2*)(gab + 2 * pl.pw * E);
+  const int row = Div(pl.pw)(threadIdx.x), col = threadIdx.x - row * pl.pw;
+  const bool many = NV == 1 && pl.ns > 1;
+  const int si = many ? Div((int)a.P)(row) : 0, pr = many ? row - si * (int)a.P : row, left = (int)a.P - pr;
+  const Div by_span(pl.span);
+  const int64_t batches = (a.S + pl.ns - 1) / pl.ns, g = blockIdx.z;
+  for (uint32_t slab = blockIdx.y; slab < pl.slabs; slab += gridDim.y) {
+    const Slab b = slab_at(a, slab);
+    const int valid = b.width - col * E;
+    float sg[E], sb[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) sg[e] = sb[e] = 0.0f;
+    __syncthreads();   // the slab before may still be read
+    for (int i = threadIdx.x; i < pl.pw * E; i += NTH) {
+      gab[i] = a.gamma && i < b.width ? a.gamma[g * a.C + b.c0 + i] : 1.0f;
+      gab[pl.pw * E + i] = a.beta && i < b.width ? a.beta[g * a.C + b.c0 + i] : 0.0f;
+    }
+    __syncthreads();
+    for (int64_t bt = blockIdx.x; bt < batches; bt += gridDim.x) {
+      const int64_t s = bt * pl.ns + si;
+      const bool on = row < pl.rows && left > 0 && s < a.S && valid > 0;
+      const T* x = a.x.p + g * a.x.gs + s * a.x.ss + b.c0 + col * E;
+      const T* dy = a.dy.p + g * a.dy.gs + s * a.dy.ss + b.c0 + col * E;
+      piece_t rx[NV], rd[NV];
+      Column<T, SL> c;
+      float h0[SL], h1[SL];
+#pragma unroll
+      for (int e = 0; e < SL; ++e) h0[e] = h1[e] = 0.0f;
+      if (on) {
+        load_rows<WHOLE>(rx, x + pr * a.x.ld, pl.rows * a.x.ld, left, pl.rows, valid);
+        load_rows<WHOLE>(rd, dy + pr * a.dy.ld, pl.rows * a.dy.ld, left, pl.rows, valid);
+        c.load_stats(a, b, by_span, g, s, col);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+          if (v > 0 && v * pl.rows >= left) break;
+          float xh[E];
+          float da[E];
+          piece_floats<T>(rx[v], xh);
+          piece_floats<T>(rd[v], da);
+          c.load_scales(gab, pl.pw * E, col);
+          slope_piece<ACT, WHOLE>(c, valid, xh, da);
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const int k = SL > 1 ? e : 0;
+            const float t = da[e] * xh[e];
+            sg[e] += t;
+            sb[e] += da[e];
+            h0[k] += da[e] * c.ga[e];
+            h1[k] += t * c.ga[e];
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      if (!a.out.p) continue;   // the same for every thread
+      if (row < pl.rows)
+#pragma unroll
+        for (int e = 0; e < SL; ++e) sm[row * pl.pw * SL + col * SL + e] = {h0[e], h1[e]};
+      __syncthreads();
+      group_sums(sm, pl.ns, pl.ns > 1 ? (int)a.P : pl.rows, pl.pw * SL, b.ng, pl.span, pl.lanes, [&](int i, int j, const Pair& t) {
+        means[i * b.ng + j] = {(float)(t.s * pl.inv_n), (float)(t.q * pl.inv_n)};
+      });
+      __syncthreads();
+      if (!on) continue;
+      float2 m[SL];
+#pragma unroll
+      for (int e = 0; e < SL; ++e) m[e] = means[si * b.ng + group_of<T, SL>(b, by_span, col, e)];
+      const T* add = a.add.p ? a.add.p + g * a.add.gs + s * a.add.ss + b.c0 + col * E : nullptr;
+      T* out = a.out.p + g * a.out.gs + s * a.out.ss + b.c0 + col * E;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const int64_t p = pr + v * pl.rows;
+        if (v * pl.rows < left) {
+          float xh[E];
+          float da[E];
+          float r[E];
+          if (add) piece_floats<T>(load_piece<WHOLE>(add + p * a.add.ld, valid), r);
+          piece_floats<T>(rx[v], xh);
+          piece_floats<T>(rd[v], da);
+          c.load_scales(gab, pl.pw * E, col);
+          slope_piece<ACT, WHOLE>(c, valid, xh, da);
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const int k = SL > 1 ? e : 0;
+            da[e] = c.rstd[k] * (da[e] * c.ga[e] - m[k].x - xh[e] * m[k].y);
+            if (add) da[e] += r[e];
+          }
+          store_piece<WHOLE>(out + p * a.out.ld, valid, da, pl.stream);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    if (a.dgamma || a.dbeta) store_columns(a, (float*)sm, sg, sb, b, g, col, row);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Longer samples, backward: a channel's sums of da and da xhat over ranges of points give
+// dgamma and dbeta (summed over samples) and, with gamma, a group's sums of h and
+// h xhat; then dx.
+// ---------------------------------------------------------------------------
+// ws: Pair [G][S][n][chan_parts * splits], a group's sums of h and h xhat, and behind them
+// float [G][slots][2][C], a block's sums of da xhat and da over all of its ranges.
+// Blocks: [G][slabs][slots].
+template <class T, int SL, bool WHOLE, int ACT>
+__global__ void __launch_bounds__(SPLIT_NTH) k_gn_bwd_sums(const GnArgs<T> a, float* __restrict__ cols, uint32_t ranges) {
+  constexpr int E = EPP<T>, U = BWD_TURN;
+  extern __shared__ Pair sm[];
+  const GnPlan& pl = a.pl;
+  const int row = Div(pl.pw)(threadIdx.x), col = threadIdx.x - row * pl.pw, wide = pl.pw * E, parts = pl.chan_parts * pl.splits;
+  const Div by_span(pl.span);
+  double* all = (double*)sm;               // [2][wide]: of the block
+  double* sums = all + 2 * wide;           // [2][wide]: of the range
+  float* fm = (float*)(sums + 2 * wide);   // [rows][2][wide]
+  const int64_t g = blockIdx.z;
+  for (uint32_t slab = blockIdx.y; slab < pl.slabs; slab += gridDim.y) {
+    const Slab b = slab_at(a, slab);
+    const int valid = b.width - col * E;
+    for (int i = threadIdx.x; i < 2 * wide; i += SPLIT_NTH) all[i] = 0.0;
+    for (uint32_t it = blockIdx.x; it < ranges; it += gridDim.x) {
+      const uint32_t s = it / (uint32_t)pl.splits, split = it - s * (uint32_t)pl.splits;
+      float sg[E], sb[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) sg[e] = sb[e] = 0.0f;
+      if (valid > 0 && row < pl.rows) {
+        const Turns tn(pl, a.P, U, split, pl.splits, row);
+        const int64_t xs = pl.rows * a.x.ld, ds = pl.rows * a.dy.ld;
+        const T* x = a.x.p + g * a.x.gs + s * a.x.ss + b.c0 + col * E + tn.first * a.x.ld;
+        const T* dy = a.dy.p + g * a.dy.gs + s * a.dy.ss + b.c0 + col * E + tn.first * a.dy.ld;
+        Column<T, SL> c;
+        c.load(a, b, by_span, g, s, col);
+        for (int left = tn.left; left > 0; left -= tn.by) {
+          piece_t rx[U], rd[U];
+          load_rows<WHOLE>(rx, x, xs, left, pl.rows, valid);
+          load_rows<WHOLE>(rd, dy, ds, left, pl.rows, valid);
+          x += tn.by * a.x.ld;
+          dy += tn.by * a.dy.ld;
+#pragma unroll
+          for (int v = 0; v < U; ++v) {
+            if (v == 0 || v * pl.rows < left) {
+              float xh[E], da[E];
+              piece_floats<T>(rx[v], xh);
+              piece_floats<T>(rd[v], da);
+              slope_piece<ACT, WHOLE>(c, valid, xh, da);
+#pragma unroll
+              for (int e = 0; e < E; ++e) {
+                sg[e] += da[e] * xh[e];
+                sb[e] += da[e];
+              }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+      }
+      if (row < pl.rows)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          fm[row * 2 * wide + col * E + e] = sg[e];
+          fm[row * 2 * wide + wide + col * E + e] = sb[e];
+        }
+      __syncthreads();
+      for (int i = threadIdx.x; i < 2 * wide; i += SPLIT_NTH) {
+        double t = 0.0;
+        for (int r = 0; r < pl.rows; ++r) t += fm[r * 2 * wide + i];
+        sums[i] = t;
+        all[i] += t;   // always by this thread
+      }
+      __syncthreads();
+      if (a.out.p) {
+        // gamma times a channel's sums, over a group's channels
+        const int per = b.width / b.ng;
+        const int at = pl.chan_parts > 1 ? slab % (uint32_t)pl.chan_parts * pl.splits + split : split;
+        Pair* part = (Pair*)a.ws + ((g * a.S + s) * a.n + b.j0) * parts + at;
+        lane_sums(b.ng, pl.lanes, [&](int j, int l) {
+          Pair t = {0.0, 0.0};
+          for (int i = j * per + l; i < (j + 1) * per; i += pl.lanes) {
+            const double ga = a.gamma ? a.gamma[g * a.C + b.c0 + i] : 1.0f;
+            t.s += ga * sums[wide + i];
+            t.q += ga * sums[i];
+          }
+          return t;
+        }, [&](int j, const Pair& t) { part[(int64_t)j * parts] = t; });
+      }
+    }
+    if (cols) {
+      float* d = cols + (g * pl.slots + blockIdx.x) * 2 * a.C + b.c0;
+      for (int i = threadIdx.x; i < 2 * wide; i += SPLIT_NTH) {
+        const int c = i < wide ? i : i - wide;
+        if (c < b.width) d[(i < wide ? 0 : a.C) + c] = (float)all[i];
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// dgamma and dbeta of a slab: 16 columns of a block, 16 threads to a column, added in order
+constexpr int COLS = 16;
+inline unsigned col_blocks_of(const GnPlan& pl) { return 2 * (unsigned)((pl.W + COLS - 1) / COLS); }
+template <class T>
+__device__ __forceinline__ void sum_columns(const GnArgs<T>& a, const Slab& b, const float* __restrict__ cols, double* sm) {
+  const int cl = threadIdx.x % COLS, r = threadIdx.x / COLS;
+  const unsigned half = (unsigned)((a.pl.W + COLS - 1) / COLS), second = blockIdx.x >= half;
+  const int c = (int)(blockIdx.x - second * half) * COLS + cl;
+  const int64_t g = blockIdx.z, ld = 2 * a.C, at = b.c0 + c;
+  double t = 0.0;
+  if (c < b.width) {
+    const float* q = cols + g * a.pl.slots * ld + second * a.C + at;
+#pragma unroll 8
+    for (int k = r; k < a.pl.slots; k += SPLIT_NTH / COLS) t += (double)q[k * ld];
+  }
+  sm[r * COLS + cl] = t;
+  __syncthreads();
+  if (r == 0 && c < b.width) {
+    for (int k = 1; k < SPLIT_NTH / COLS; ++k) t += sm[k * COLS + cl];
+    float* d = second ? a.dbeta : a.dgamma;
+    if (d) d[g * a.C + at] = (float)t;
+  }
+  __syncthreads();
+}
+
+// dx, and in the first `col_blocks` blocks of a slab, which are done before the others, the
+// sums of `cols`.  Blocks: [G][slabs][col_blocks + S * splits].
+template <class T, int SL, bool WHOLE, int ACT>
+__global__ void __launch_bounds__(SPLIT_NTH, SL == 1 ? 4 : 2) k_gn_bwd_apply(const GnArgs<T> a, uint32_t ranges, const float* __restrict__ cols,
+                                                            unsigned col_blocks) {
+  constexpr int E = EPP<T>, U = BWD_TURN;
+  extern __shared__ Pair sm[];
+  const GnPlan& pl = a.pl;
+  if (blockIdx.x < col_blocks) {
+    for (uint32_t slab = blockIdx.y; slab < pl.slabs; slab += gridDim.y) sum_columns(a, slab_at(a, slab), cols, (double*)sm);
+    return;
+  }
+  float2* means = (float2*)sm;
+  const int row = Div(pl.pw)(threadIdx.x), col = threadIdx.x - row * pl.pw, parts = pl.chan_parts * pl.splits;
+  const Div by_span(pl.span);
+  const int64_t g = blockIdx.z;
+  for (uint32_t slab = blockIdx.y; slab < pl.slabs; slab += gridDim.y) {
+    const Slab b = slab_at(a, slab);
+    const int valid = b.width - col * E;
+    for (uint32_t at = blockIdx.x - col_blocks; at < ranges; at += gridDim.x - col_blocks) {
+      const uint32_t it = from_last(at, ranges), s = it / (uint32_t)pl.splits, split = it - s * (uint32_t)pl.splits;
+      const Turns tn(pl, a.P, U, split, pl.splits, row);
+      const int64_t p0 = tn.first + tn.last(), xs = pl.rows * a.x.ld, ds = pl.rows * a.dy.ld, as = pl.rows * a.add.ld;
+      int left = valid > 0 && row < pl.rows ? tn.left - tn.last() : 0;
+      const T* x = a.x.p + g * a.x.gs + s * a.x.ss + b.c0 + col * E + p0 * a.x.ld;
+      const T* dy = a.dy.p + g * a.dy.gs + s * a.dy.ss + b.c0 + col * E + p0 * a.dy.ld;
+      const T* add = a.add.p ? a.add.p + g * a.add.gs + s * a.add.ss + b.c0 + col * E + p0 * a.add.ld : nullptr;
+      piece_t rx[U], rd[U], ra[U];
+      auto load = [&](int n) {
+        load_rows<WHOLE>(rx, x, xs, n, pl.rows, valid);
+        load_rows<WHOLE>(rd, dy, ds, n, pl.rows, valid);
+        if (add) load_rows<WHOLE>(ra, add, as, n, pl.rows, valid);
+      };
+      if (left > 0) load(left);
+      range_sums((const Pair*)a.ws + ((g * a.S + s) * a.n + b.j0) * parts, b.ng, parts, pl.lanes,
+                 [&](int j, const Pair& t) { means[j] = {(float)(t.s * pl.inv_n), (float)(t.q * pl.inv_n)}; });
+      __syncthreads();
+      if (left > 0) {
+        Column<T, SL> c;
+        c.load(a, b, by_span, g, s, col);
+        float2 m[SL];
+#pragma unroll
+        for (int e = 0; e < SL; ++e) m[e] = means[group_of<T, SL>(b, by_span, col, e)];
+        T* out = a.out.p + g * a.out.gs + s * a.out.ss + b.c0 + col * E + p0 * a.out.ld;
+        const int64_t os = pl.rows * a.out.ld;
+        for (;;) {
+#pragma unroll
+          for (int v = 0; v < U; ++v) {
+            if (v == 0 || v * pl.rows < left) {
+              float xh[E], da[E], r[E];
+              piece_floats<T>(rx[v], xh);
+              piece_floats<T>(rd[v], da);
+              if (add) piece_floats<T>(ra[v], r);
+              slope_piece<ACT, WHOLE>(c, valid, xh, da);
+#pragma unroll
+              for (int e = 0; e < E; ++e) {
+                const int k = SL > 1 ? e : 0;
+                da[e] = c.rstd[k] * (da[e] * c.ga[e] - m[k].x - xh[e] * m[k].y);
+                if (add) da[e] += r[e];
+              }
+              store_piece<WHOLE>(out + v * os, valid, da, pl.stream);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          left += tn.by;
+          if (left > tn.left) break;
+          x -= tn.by * a.x.ld;
+          dy -= tn.by * a.dy.ld;
+          if (add) add -= tn.by * a.add.ld;
+          out -= tn.by * a.out.ld;
+          load(left);
+        }
+      }
+      __syncthreads();
+    }
+  }
+}
+
+template <class T> __global__ void __launch_bounds__(SPLIT_NTH) k_gn_cols(const GnArgs<T> a, const float* __restrict__ cols) {
+  __shared__ double sm[SPLIT_NTH];
+  for (uint32_t slab = blockIdx.y; slab < a.pl.slabs; slab += gridDim.y) sum_columns(a, slab_at(a, slab), cols, sm);
+}
+
+}  // namespace
+
+template <class T> hipError_t launch_gn_bwd(const GnArgs<T>& a, int G, hipStream_t st) {
+  const bool cols = a.dgamma || a.dbeta;
+  if (a.S <= 0) {
+    // sums over no samples
+    for (float* sum : {a.dgamma, a.dbeta})
+      if (sum)
+        if (const hipError_t e = launch_zeros(sum, G * a.C, st); e != hipSuccess) return e;
+    return hipSuccess;
+  }
+  const GnPlan& pl = a.pl;
+  by_act(a.act, [&](auto act) {
+    constexpr int ACT = act.value;
+    if (pl.mode == GN_ROWS) {
+      k_gn_rows_bwd<T, 2, ACT><<<dim3((unsigned)pl.slots, (unsigned)pl.slabs, G), 256, bwd_sums_lds(256, 1, EPP<T>), st>>>(a);
+    } else if (pl.mode == GN_ONE) {
+      const dim3 grid((unsigned)pl.slots, (unsigned)std::min<int64_t>(pl.slabs, 65535), G);
+      by_width(a, [&](auto sl, auto whole) {
+        by_shape<true, false>(pl, [&](auto nth, auto nv) {
+          const size_t lds = bwd_sums_lds(nth.value, sl.value, EPP<T>) + (size_t)pl.ns * pl.ng * sizeof(float2) +
+                             (size_t)pl.pw * EPP<T> * 8;
+          k_gn_one_bwd<T, nth.value, nv.value, sl.value, whole.value, ACT><<<grid, nth.value, lds, st>>>(a);
+        });
+      });
+    } else {
+      const int64_t ranges = a.S * pl.splits;
+      float* sums = cols ? (float*)(a.ws + gn_pairs_bytes(pl, G, a.S, a.n)) : nullptr;
+      const unsigned slabs = (unsigned)std::min<int64_t>(pl.slabs, 65535), col_blocks = cols ? col_blocks_of(pl) : 0;
+      by_width(a, [&](auto sl, auto whole) {
+        const size_t lds = (size_t)pl.pw * EPP<T> * 32 + SPLIT_NTH * EPP<T> * 8;
+        k_gn_bwd_sums<T, sl.value, whole.value, ACT><<<dim3((unsigned)pl.slots, slabs, G), SPLIT_NTH, lds, st>>>(a, sums, (uint32_t)ranges);
+        if (a.out.p)   // dx may overwrite dy
+          k_gn_bwd_apply<T, sl.value, whole.value, ACT><<<dim3(grid_of(ranges) + col_blocks, slabs, G), SPLIT_NTH,
+              std::max<size_t>(SPLIT_NTH * 8, (size_t)pl.ng * sizeof(float2)), st>>>(a, (uint32_t)ranges, sums, col_blocks);
+      });
+      if (!a.out.p) k_gn_cols<T><<<dim3(col_blocks, slabs, G), SPLIT_NTH, 0, st>>>(a, sums);
+    }
+  });
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !cols || pl.slots == 1 || pl.mode == GN_SPLIT) return e;
+  return launch_slot_sum((const float*)a.ws, pl.slots * 2 * a.C, (int)pl.slots, 2 * a.C, a.dgamma, a.C, a.dbeta, G, st);
+}
+
+#define PIGAN_GN_INST(T) template hipError_t launch_gn_bwd<T>(const GnArgs<T>&, int, hipStream_t);
+PIGAN_GN_INST(float)
+PIGAN_GN_INST(bf16)
+PIGAN_GN_INST(f16)
+
+}  // namespace pigan
