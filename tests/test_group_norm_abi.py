@@ -66,7 +66,7 @@ def test_forward_refuses(bad):
 @pytest.mark.parametrize("bad", BAD + [dict(dy=NONE), dict(dy=(FAKE, 3, P * C, 0)), dict(dx=(1 << 24, 3, P * C, 0)),
                                        dict(add=(FAKE + 1, C, P * C, 0)), dict(mean=0), dict(rstd=0),
                                        dict(dx=NONE, dgamma=0, dbeta=0), dict(dgamma=(1 << 25) + 2), dict(dgamma=1 << 26),
-                                       dict(dx=(FAKE + 2, C, P * C, 0)), dict(x=FAR), dict(dgamma=FAKE), dict(dbeta=1 << 30)])
+                                       dict(dx=(FAKE + 2, C, P * C, 0)), dict(x=FAR), dict(dgamma=FAKE), dict(s=1, p=4000, dbeta=1 << 30)])
 def test_backward_refuses(bad):
     L = pigan.lib()
     assert L.pigan_group_norm_backward(_args(**bad), 1 << 30, 1 << 30, None) == pigan.EINVAL
