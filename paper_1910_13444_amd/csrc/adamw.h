@@ -4,6 +4,8 @@
 
 namespace pigan {
 
+// Calls that move more leave nothing for the next one in the last-level cache (256 MiB).
+constexpr double STREAM_BYTES = 192.0 * 1048576.0;
 constexpr int QBLOCK = 256;      // elements that share the scale of an 8-bit state
 constexpr int PIECE = 4096;      // elements of a tensor that a block takes
 
@@ -37,6 +39,7 @@ struct AdamwArgs {
   const float* coef;        // multiplies scale, or null
   const double* corr;       // {c1, c2} on the device, or null
   const int32_t* skip;
+  bool stream;              // past the caches
 };
 
 hipError_t launch_adamw(const AdamwArgs& a, int bits, int64_t n_pieces, hipStream_t st);

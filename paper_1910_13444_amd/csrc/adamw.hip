@@ -19,6 +19,7 @@
 #include "adamw.h"
 
 #include <algorithm>
+#include <type_traits>
 
 #include "piece.h"
 
@@ -32,19 +33,61 @@ __device__ __forceinline__ double wave_sum(double v) {
   for (int o = 1; o < 64; o *= 2) v += __shfl_xor(v, o);
   return v;
 }
+// of values >= 0, by lane permutes: rows of 16 lanes, then rows to the ones behind them
 __device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) v = fmaxf(v, __shfl_xor(v, o));
+  auto with = [&](auto ctrl, auto rows) {
+    const int o = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), ctrl.value, rows.value, 0xf, false);
+    v = fmaxf(v, __builtin_bit_cast(float, o));
+  };
+  using std::integral_constant;
+  with(integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});   // row_shr 1, 2, 4, 8
+  with(integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});
+  with(integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});
+  with(integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});
+  with(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});   // row_bcast 15, 31
+  with(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+
+typedef uint32_t half4 __attribute__((ext_vector_type(2), aligned(2)));
+
+// an entry with the knowledge that its pointers are to global memory
+__device__ __forceinline__ TensorEntry entry_at(const TensorEntry* p) {
+  TensorEntry t = *p;
+  t.p = (float*)(__attribute__((address_space(1))) float*)t.p;
+  t.g = (const void*)(__attribute__((address_space(1))) const void*)t.g;
+  t.copy = (void*)(__attribute__((address_space(1))) void*)t.copy;
+  return t;
+}
+
+// Vectors that may start at any element.  `stream`: past the caches, AdamwArgs::stream.
+template <class V, class T> __device__ __forceinline__ V get(const T* p, bool stream) {
+  V v;
+  if (stream) {
+    asm volatile("; streamed");   // else the compiler joins both to a plain access
+    v = __builtin_nontemporal_load((const V*)p);
+    asm volatile("; streamed");
+  } else {
+    v = *(const V*)p;
+  }
   return v;
+}
+template <class V, class T> __device__ __forceinline__ void put(T* p, const V& v, bool stream) {
+  if (stream) {
+    asm volatile("; streamed");
+    __builtin_nontemporal_store(v, (V*)p);
+    asm volatile("; streamed");
+  } else {
+    *(V*)p = v;
+  }
 }
 
 // four elements of a gradient, zeros past `valid`
-__device__ __forceinline__ void load_grad(const void* g, int dt, int64_t i, int64_t valid, float (&f)[4]) {
-  typedef uint32_t half4 __attribute__((ext_vector_type(2), aligned(2)));
+__device__ __forceinline__ void load_grad(const void* g, int dt, int64_t i, int64_t valid, float (&f)[4], bool stream = false) {
   if (dt == PIGAN_FP32) {
     const float* p = (const float*)g + i;
     if (valid >= 4) {
-      const f32x4u v = *(const f32x4u*)p;
+      const f32x4u v = get<f32x4u>(p, stream);
       for (int e = 0; e < 4; ++e) f[e] = v[e];
     } else {
       for (int e = 0; e < 4; ++e) f[e] = e < valid ? p[e] : 0.0f;
@@ -54,7 +97,7 @@ __device__ __forceinline__ void load_grad(const void* g, int dt, int64_t i, int6
   const uint16_t* p = (const uint16_t*)g + i;
   uint16_t h[4];
   if (valid >= 4) {
-    const half4 v = *(const half4*)p;
+    const half4 v = get<half4>(p, stream);
     __builtin_memcpy(h, &v, 8);
   } else {
     for (int e = 0; e < 4; ++e) h[e] = e < valid ? p[e] : 0;
@@ -63,67 +106,88 @@ __device__ __forceinline__ void load_grad(const void* g, int dt, int64_t i, int6
     f[e] = dt == PIGAN_BF16 ? __uint_as_float((uint32_t)h[e] << 16) : (float)__builtin_bit_cast(f16, h[e]);
 }
 
-__device__ __forceinline__ void load4(const float* p, int64_t valid, float (&f)[4]) {
+__device__ __forceinline__ void load4(const float* p, int64_t valid, float (&f)[4], bool stream) {
   if (valid >= 4) {
-    const f32x4u v = *(const f32x4u*)p;
+    const f32x4u v = get<f32x4u>(p, stream);
     for (int e = 0; e < 4; ++e) f[e] = v[e];
   } else {
     for (int e = 0; e < 4; ++e) f[e] = e < valid ? p[e] : 0.0f;
   }
 }
-__device__ __forceinline__ void store4(float* p, int64_t valid, const float (&f)[4]) {
+__device__ __forceinline__ void store4(float* p, int64_t valid, const float (&f)[4], bool stream) {
   if (valid >= 4) {
     f32x4u v;
     for (int e = 0; e < 4; ++e) v[e] = f[e];
-    *(f32x4u*)p = v;
+    put<f32x4u>(p, v, stream);
   } else {
     for (int e = 0; e < 4; ++e)
       if (e < valid) p[e] = f[e];
   }
 }
 template <class T>
-__device__ __forceinline__ void store_copy4(T* p, int64_t valid, const float (&f)[4]) {
-  typedef uint32_t half4 __attribute__((ext_vector_type(2), aligned(2)));
+__device__ __forceinline__ void store_copy4(T* p, int64_t valid, const float (&f)[4], bool stream) {
   T h[4];
   for (int e = 0; e < 4; ++e) h[e] = Elem<T>::from_f(f[e]);
   if (valid >= 4) {
     half4 v;
     __builtin_memcpy(&v, h, 8);
-    *(half4*)p = v;
+    put<half4>(p, v, stream);
   } else {
     for (int e = 0; e < 4; ++e)
       if (e < valid) p[e] = h[e];
   }
 }
-__device__ __forceinline__ void store_copy(const TensorEntry& t, int64_t i, int64_t valid, const float (&f)[4]) {
+__device__ __forceinline__ void store_copy(const TensorEntry& t, int64_t i, int64_t valid, const float (&f)[4], bool stream) {
   if (!t.copy) return;
-  if (t.copy_dt == PIGAN_BF16) store_copy4((bf16*)t.copy + i, valid, f);
-  else store_copy4((f16*)t.copy + i, valid, f);
+  if (t.copy_dt == PIGAN_BF16) store_copy4((bf16*)t.copy + i, valid, f, stream);
+  else store_copy4((f16*)t.copy + i, valid, f, stream);
 }
 
 // ---------------------------------------------------------------------------
 // The step.
 // ---------------------------------------------------------------------------
-struct Coefs { double coef, c1, c2; };
-__device__ __forceinline__ Coefs coefs_of(const AdamwArgs& a) {
-  return {a.coef ? a.scale * (double)*a.coef : a.scale, a.corr ? a.corr[0] : a.c1, a.corr ? a.corr[1] : a.c2};
+// 1 / d in fp64 from the hardware's (2^-24): two Newton steps
+__device__ __forceinline__ double rcp64_full(double d) {
+  double r = __builtin_amdgcn_rcp(d);
+  r += r * (1.0 - d * r);
+  return r + r * (1.0 - d * r);
 }
 
-// the new states, as fp32 values, and the new parameter
-__device__ __forceinline__ void update(const AdamwArgs& a, const Coefs& k, double decay, float g, double m, double v, float& p,
-                                       float& mn, float& vn) {
+constexpr double TOP_M = 127.0 * 127.0, TOP_V = 255.0 * 255.0 * 255.0 * 255.0;
+// s / top, rounded once: top times it is s again, as sums of short numbers m and v may lie
+// halfway between two fp32 values
+__device__ __forceinline__ double unit_of(float s, double top) {
+  const double inv = 1.0 / top, q = s * inv;   // a constant
+  return __builtin_fma(__builtin_fma(-top, q, (double)s), inv, q);
+}
+
+// of a tensor: p' = keep p - by m / (sqrt(c2 v) + eps)
+struct Coefs { double coef, c2, keep, by; };
+__device__ __forceinline__ Coefs coefs_of(const AdamwArgs& a, double decay) {
+  const double c1 = a.corr ? a.corr[0] : a.c1, c2 = a.corr ? a.corr[1] : a.c2;
+  return {a.coef ? a.scale * (double)*a.coef : a.scale, c2, 1.0 - a.lr * decay, a.lr * c1};
+}
+
+// the new states, as fp32 values, and the new parameter.  Root and quotient are the
+// hardware's fp64 approximations (2^-24) with a Newton step each (1e-14).
+__device__ __forceinline__ void update(const AdamwArgs& a, const Coefs& k, float g, double m, double v, float& p, float& mn,
+                                       float& vn) {
   const double gs = k.coef * g;
   mn = (float)(a.b1 * m + a.nb1 * gs);
   vn = (float)(a.b2 * v + a.nb2 * gs * gs);
-  const double u = (double)mn * k.c1 / (sqrt((double)vn * k.c2) + a.eps);
-  p = (float)((double)p - a.lr * (u + decay * (double)p));
+  // an infinite v beside a finite m is the largest one; 0 a number with a root's reciprocal
+  const double s = (double)__builtin_amdgcn_fmed3f(vn, 0.0f, 3.4028234663852886e38f) * k.c2 + 1e-300;
+  const double r = __builtin_amdgcn_rsq(s), root = s * r, d = root + root * (0.5 - root * (0.5 * r)) + a.eps;
+  double q = __builtin_amdgcn_rcp(d);
+  q += q * (1.0 - d * q);
+  p = (float)(k.keep * (double)p - k.by * (double)mn * q);
 }
 
 __global__ void __launch_bounds__(NTH) k_adamw32(const AdamwArgs a) {
   if (a.skip && *a.skip) return;   // one flag for the whole launch
   const TensorPiece w = a.pieces[blockIdx.x];
-  const TensorEntry t = a.entries[w.tensor];
-  const Coefs k = coefs_of(a);
+  const TensorEntry t = entry_at(a.entries + w.tensor);
+  const Coefs k = coefs_of(a, t.decay);
   const int64_t first = (int64_t)w.piece * PIECE;
   float* m = (float*)a.m + t.state;
   float* v = (float*)a.v + t.state;
@@ -131,48 +195,47 @@ __global__ void __launch_bounds__(NTH) k_adamw32(const AdamwArgs a) {
     const int64_t i = first + (it * NTH + threadIdx.x) * 4, valid = t.n - i;
     if (valid <= 0) break;
     float pf[4], gf[4], mf[4], vf[4];
-    load4(t.p + i, valid, pf);
-    load_grad(t.g, t.g_dt, i, valid, gf);
-    load4(m + i, valid, mf);
-    load4(v + i, valid, vf);
+    load4(t.p + i, valid, pf, a.stream);
+    load_grad(t.g, t.g_dt, i, valid, gf, a.stream);
+    load4(m + i, valid, mf, a.stream);
+    load4(v + i, valid, vf, a.stream);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const double mo = mf[e], vo = vf[e];
-      update(a, k, t.decay, gf[e], mo, vo, pf[e], mf[e], vf[e]);
+      update(a, k, gf[e], mo, vo, pf[e], mf[e], vf[e]);
     }
-    store4(t.p + i, valid, pf);
-    store4(m + i, valid, mf);
-    store4(v + i, valid, vf);
-    store_copy(t, i, valid, pf);
+    store4(t.p + i, valid, pf, a.stream);
+    store4(m + i, valid, mf, a.stream);
+    store4(v + i, valid, vf, a.stream);
+    store_copy(t, i, valid, pf, a.stream);
   }
 }
 
 // The code of size x among a largest of s: the nearest whole root of x top / s, top the
-// largest code's power.  The fp32 root is off by less than one code; the two halfway
-// points, whole powers of halves, decide in fp64.  inv = top / s.
-__device__ __forceinline__ int code_m(float x, double inv) {
+// largest code's power; inv = top / s.  The fp32 root y is off by less than 6e-5 codes
+// (2e-7 of 255), so only within 2^-12 of a halfway point the whole powers of halves
+// decide, in fp64.
+template <bool FOURTH>
+__device__ __forceinline__ int code_of(float x, double inv) {
   const double r = (double)x * inv;
-  int q = (int)rintf(sqrtf((float)r));
-  const double lo = q - 0.5, hi = q + 0.5;
-  q += (r > hi * hi) - (q > 0 && r < lo * lo);
-  return min(q, 127);
+  float y = __builtin_amdgcn_sqrtf((float)r);
+  if constexpr (FOURTH) y = __builtin_amdgcn_sqrtf(y);
+  const float c = rintf(y);
+  int q = (int)c;
+  if (fabsf(y - c) > 0.5f - 0x1p-12f) {
+    double lo = q - 0.5, hi = q + 0.5;
+    if constexpr (FOURTH) { lo *= lo; hi *= hi; }
+    q += (r > hi * hi) - (q > 0 && r < lo * lo);
+  }
+  return q;
 }
-__device__ __forceinline__ int code_v(float x, double inv) {
-  const double r = (double)x * inv;
-  int q = (int)rintf(sqrtf(sqrtf((float)r)));
-  const double lo = (q - 0.5) * (q - 0.5), hi = (q + 0.5) * (q + 0.5);
-  q += (r > hi * hi) - (q > 0 && r < lo * lo);
-  return x > 0.0f ? max(min(q, 255), 1) : 0;
-}
-
-constexpr double TOP_M = 127.0 * 127.0, TOP_V = 255.0 * 255.0 * 255.0 * 255.0;
 
 // a wave takes a block of states at a time, four elements a lane
 __global__ void __launch_bounds__(NTH) k_adamw8(const AdamwArgs a) {
   if (a.skip && *a.skip) return;
   const TensorPiece w = a.pieces[blockIdx.x];
-  const TensorEntry t = a.entries[w.tensor];
-  const Coefs k = coefs_of(a);
+  const TensorEntry t = entry_at(a.entries + w.tensor);
+  const Coefs k = coefs_of(a, t.decay);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t first = (int64_t)w.piece * PIECE;
   for (int it = 0; it < PIECE / (NTH * 4); ++it) {
@@ -181,46 +244,46 @@ __global__ void __launch_bounds__(NTH) k_adamw8(const AdamwArgs a) {
     const int64_t i = b + lane * 4, valid = t.n - i, at = t.state + i, qb = (t.state + b) / QBLOCK;
     float pf[4] = {0, 0, 0, 0}, gf[4] = {0, 0, 0, 0}, mf[4], vf[4];
     if (valid > 0) {
-      load4(t.p + i, valid, pf);
-      load_grad(t.g, t.g_dt, i, valid, gf);
+      load4(t.p + i, valid, pf, a.stream);
+      load_grad(t.g, t.g_dt, i, valid, gf, a.stream);
     }
     // states are there to the end of the block
-    const uint32_t mq = *(const uint32_t*)((const int8_t*)a.m + at), vq = *(const uint32_t*)((const uint8_t*)a.v + at);
-    const double ms = (double)a.m_scale[qb] / TOP_M, vs = (double)a.v_scale[qb] / TOP_V;
-    float mmax = 0.0f, vmax = 0.0f;
-    bool finite = true;
+    const uint32_t mq = get<uint32_t>((const int8_t*)a.m + at, a.stream), vq = get<uint32_t>((const uint8_t*)a.v + at, a.stream);
+    const double ms = unit_of(a.m_scale[qb], TOP_M), vs = unit_of(a.v_scale[qb], TOP_V);
+    float mmax = 0.0f, vmax = 0.0f, none = 0.0f;   // `none` is 0 unless a state is not finite
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int qm = (int)(int8_t)(mq >> (8 * e));
-      const uint32_t qv = (vq >> (8 * e)) & 255;
-      update(a, k, t.decay, gf[e], (double)(qm * abs(qm)) * ms, (double)(qv * qv * qv * qv) * vs, pf[e], mf[e], vf[e]);
+      const uint32_t qv = (vq >> (8 * e)) & 255, q2 = qv * qv;
+      update(a, k, gf[e], (double)(qm * abs(qm)) * ms, (double)(q2 * q2) * vs, pf[e], mf[e], vf[e]);
       if (e >= valid) mf[e] = vf[e] = 0.0f;
       mmax = fmaxf(mmax, fabsf(mf[e]));
       vmax = fmaxf(vmax, vf[e]);
-      finite = finite && __builtin_isfinite(mf[e]) && __builtin_isfinite(vf[e]);
+      none += 0.0f * mf[e];
+      none += 0.0f * vf[e];
     }
     mmax = wave_max(mmax);
     vmax = wave_max(vmax);
-    const bool all = __all(finite);
-    const double mi = mmax > 0.0f ? TOP_M / (double)mmax : 0.0, vi = vmax > 0.0f ? TOP_V / (double)vmax : 0.0;
+    const bool all = __all(none == 0.0f);
+    const double mi = mmax > 0.0f ? TOP_M * rcp64_full((double)mmax) : 0.0, vi = vmax > 0.0f ? TOP_V * rcp64_full((double)vmax) : 0.0;
     uint32_t mo = 0, vo = 0;
     if (all) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int q = code_m(fabsf(mf[e]), mi);
+        const int q = min(code_of<false>(fabsf(mf[e]), mi), 127), u = min(code_of<true>(vf[e], vi), 255);
         mo |= (uint32_t)(uint8_t)(mf[e] < 0.0f ? -q : q) << (8 * e);
-        vo |= (uint32_t)code_v(vf[e], vi) << (8 * e);
+        vo |= (uint32_t)(vf[e] > 0.0f ? max(u, 1) : 0) << (8 * e);
       }
     }
-    *(uint32_t*)((int8_t*)a.m + at) = mo;
-    *(uint32_t*)((uint8_t*)a.v + at) = vo;
+    put<uint32_t>((int8_t*)a.m + at, mo, a.stream);
+    put<uint32_t>((uint8_t*)a.v + at, vo, a.stream);
     if (lane == 0) {
       a.m_scale[qb] = all ? mmax : __builtin_nanf("");
       a.v_scale[qb] = all ? vmax : __builtin_nanf("");
     }
     if (valid > 0) {
-      store4(t.p + i, valid, pf);
-      store_copy(t, i, valid, pf);
+      store4(t.p + i, valid, pf, a.stream);
+      store_copy(t, i, valid, pf, a.stream);
     }
   }
 }
@@ -243,7 +306,7 @@ __global__ void __launch_bounds__(NTH) k_grad_squares(const TensorEntry* __restr
   double s = 0.0;
   for (int64_t b = blockIdx.x; b < n_pieces; b += gridDim.x) {
     const TensorPiece w = pieces[b];
-    const TensorEntry t = entries[w.tensor];
+    const TensorEntry t = entry_at(entries + w.tensor);
     const int64_t first = (int64_t)w.piece * PIECE;
 #pragma unroll
     for (int it = 0; it < PIECE / (NTH * 4); ++it) {
@@ -282,26 +345,26 @@ __global__ void __launch_bounds__(1024) k_grad_norm(const double* __restrict__ p
 
 __global__ void __launch_bounds__(NTH) k_state_values(int64_t n, const int8_t* __restrict__ m, const float* __restrict__ m_scale,
                                                       const uint8_t* __restrict__ v, const float* __restrict__ v_scale,
-                                                      float* __restrict__ m_out, float* __restrict__ v_out) {
+                                                      float* __restrict__ m_out, float* __restrict__ v_out, bool stream) {
   for (int64_t i = ((int64_t)blockIdx.x * NTH + threadIdx.x) * 4; i < n; i += (int64_t)gridDim.x * NTH * 4) {
     float f[4];
     if (m_out) {
-      const uint32_t q = *(const uint32_t*)(m + i);
-      const double s = (double)m_scale[i / QBLOCK] / TOP_M;
+      const uint32_t q = get<uint32_t>(m + i, stream);
+      const double s = unit_of(m_scale[i / QBLOCK], TOP_M);
       for (int e = 0; e < 4; ++e) {
         const int c = (int)(int8_t)(q >> (8 * e));
         f[e] = (float)((double)(c * abs(c)) * s);
       }
-      store4(m_out + i, 4, f);
+      store4(m_out + i, 4, f, stream);
     }
     if (v_out) {
-      const uint32_t q = *(const uint32_t*)(v + i);
-      const double s = (double)v_scale[i / QBLOCK] / TOP_V;
+      const uint32_t q = get<uint32_t>(v + i, stream);
+      const double s = unit_of(v_scale[i / QBLOCK], TOP_V);
       for (int e = 0; e < 4; ++e) {
         const uint32_t c = (q >> (8 * e)) & 255;
         f[e] = (float)((double)(c * c * c * c) * s);
       }
-      store4(v_out + i, 4, f);
+      store4(v_out + i, 4, f, stream);
     }
   }
 }
@@ -340,7 +403,7 @@ hipError_t launch_state_values(int64_t n, const int8_t* m, const float* m_scale,
                                float* m_out, float* v_out, hipStream_t st) {
   if (n <= 0) return hipSuccess;
   const int64_t blocks = std::min<int64_t>((n + NTH * 4 - 1) / (NTH * 4), 8192);
-  k_state_values<<<(unsigned)blocks, NTH, 0, st>>>(n, m, m_scale, v, v_scale, m_out, v_out);
+  k_state_values<<<(unsigned)blocks, NTH, 0, st>>>(n, m, m_scale, v, v_scale, m_out, v_out, n * 5.0 * (!!m_out + !!v_out) > STREAM_BYTES);
   return hipGetLastError();
 }
 

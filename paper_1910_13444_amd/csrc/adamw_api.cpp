@@ -261,8 +261,9 @@ pigan_status pigan_adamw_update(const pigan_adamw* a, void* ws, size_t ws_bytes,
       k.c2 = 1.0 / (1.0 - std::pow(a->beta2, (double)a->t));
     }
     if (h.n_pieces == 0) return PIGAN_OK;
-    ProfScope prof(st, h.bits == 8 ? "adamw8" : "adamw", 0.0,
-                   (double)h.elements * 8 + h.states * (h.bits == 8 ? 4.0 + 16.0 / QBLOCK : 16.0) + h.g_bytes + h.copy_bytes);
+    const double bytes = (double)h.elements * 8 + h.states * (h.bits == 8 ? 4.0 + 16.0 / QBLOCK : 16.0) + h.g_bytes + h.copy_bytes;
+    k.stream = bytes > STREAM_BYTES;
+    ProfScope prof(st, h.bits == 8 ? "adamw8" : "adamw", 0.0, bytes);
     HIP_TRY(launch_adamw(k, h.bits, h.n_pieces, st));
     return PIGAN_OK;
   });

@@ -43,6 +43,7 @@ __device__ __forceinline__ piece_t load_piece(const T* p, int valid, bool stream
   if constexpr (WHOLE) {
     piece_t v;
     if (stream) {
+      asm volatile("; streamed");
       v = __builtin_nontemporal_load((const piece_u*)p);
       asm volatile("; streamed");
     } else {
@@ -61,8 +62,9 @@ __device__ __forceinline__ void store_piece(T* p, int valid, const float* f, boo
     for (int i = 0; i < EPP<T>; ++i) e[i] = Elem<T>::from_f(f[i]);
     piece_t v;
     __builtin_memcpy(&v, e, 16);
-    __builtin_nontemporal_store(v, (piece_u*)p);
     asm volatile("; streamed");   // else the compiler joins both stores to a plain one
+    __builtin_nontemporal_store(v, (piece_u*)p);
+    asm volatile("; streamed");
   } else {
     piece_store(p, WHOLE ? EPP<T> : valid, f);
   }
