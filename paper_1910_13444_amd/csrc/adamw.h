@@ -7,7 +7,7 @@ namespace pigan {
 // Calls that move more leave nothing for the next one in the last-level cache (256 MiB).
 constexpr double STREAM_BYTES = 192.0 * 1048576.0;
 constexpr int QBLOCK = 256;      // elements that share the scale of an 8-bit state
-constexpr int PIECE = 4096;      // elements of a tensor that a block takes
+constexpr int PIECE = 1024;      // elements of a tensor that a block takes, four a thread
 
 // A tensor as the kernels see it; `state` is its first element in the flat states.
 struct TensorEntry {

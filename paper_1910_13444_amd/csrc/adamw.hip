@@ -51,41 +51,36 @@ __device__ __forceinline__ float wave_max(float v) {
 
 typedef uint32_t half4 __attribute__((ext_vector_type(2), aligned(2)));
 
-// an entry with the knowledge that its pointers are to global memory
-__device__ __forceinline__ TensorEntry entry_at(const TensorEntry* p) {
-  TensorEntry t = *p;
-  t.p = (float*)(__attribute__((address_space(1))) float*)t.p;
-  t.g = (const void*)(__attribute__((address_space(1))) const void*)t.g;
-  t.copy = (void*)(__attribute__((address_space(1))) void*)t.copy;
-  return t;
-}
+// Pointers to global memory: those that a table holds would else be taken for any memory's,
+// whose accesses wait for LDS too.
+template <class T> using G = __attribute__((address_space(1))) T*;
 
 // Vectors that may start at any element.  `stream`: past the caches, AdamwArgs::stream.
-template <class V, class T> __device__ __forceinline__ V get(const T* p, bool stream) {
+template <class V, class T> __device__ __forceinline__ V get(G<const T> p, bool stream) {
   V v;
   if (stream) {
     asm volatile("; streamed");   // else the compiler joins both to a plain access
-    v = __builtin_nontemporal_load((const V*)p);
+    v = __builtin_nontemporal_load((G<const V>)p);
     asm volatile("; streamed");
   } else {
-    v = *(const V*)p;
+    v = *(G<const V>)p;
   }
   return v;
 }
-template <class V, class T> __device__ __forceinline__ void put(T* p, const V& v, bool stream) {
+template <class V, class T> __device__ __forceinline__ void put(G<T> p, const V& v, bool stream) {
   if (stream) {
     asm volatile("; streamed");
-    __builtin_nontemporal_store(v, (V*)p);
+    __builtin_nontemporal_store(v, (G<V>)p);
     asm volatile("; streamed");
   } else {
-    *(V*)p = v;
+    *(G<V>)p = v;
   }
 }
 
 // four elements of a gradient, zeros past `valid`
-__device__ __forceinline__ void load_grad(const void* g, int dt, int64_t i, int64_t valid, float (&f)[4], bool stream = false) {
+__device__ __forceinline__ void load_grad(G<const void> g, int dt, int64_t i, int64_t valid, float (&f)[4], bool stream = false) {
   if (dt == PIGAN_FP32) {
-    const float* p = (const float*)g + i;
+    const G<const float> p = (G<const float>)g + i;
     if (valid >= 4) {
       const f32x4u v = get<f32x4u>(p, stream);
       for (int e = 0; e < 4; ++e) f[e] = v[e];
@@ -94,7 +89,7 @@ __device__ __forceinline__ void load_grad(const void* g, int dt, int64_t i, int6
     }
     return;
   }
-  const uint16_t* p = (const uint16_t*)g + i;
+  const G<const uint16_t> p = (G<const uint16_t>)g + i;
   uint16_t h[4];
   if (valid >= 4) {
     const half4 v = get<half4>(p, stream);
@@ -106,7 +101,7 @@ __device__ __forceinline__ void load_grad(const void* g, int dt, int64_t i, int6
     f[e] = dt == PIGAN_BF16 ? __uint_as_float((uint32_t)h[e] << 16) : (float)__builtin_bit_cast(f16, h[e]);
 }
 
-__device__ __forceinline__ void load4(const float* p, int64_t valid, float (&f)[4], bool stream) {
+__device__ __forceinline__ void load4(G<const float> p, int64_t valid, float (&f)[4], bool stream) {
   if (valid >= 4) {
     const f32x4u v = get<f32x4u>(p, stream);
     for (int e = 0; e < 4; ++e) f[e] = v[e];
@@ -114,7 +109,7 @@ __device__ __forceinline__ void load4(const float* p, int64_t valid, float (&f)[
     for (int e = 0; e < 4; ++e) f[e] = e < valid ? p[e] : 0.0f;
   }
 }
-__device__ __forceinline__ void store4(float* p, int64_t valid, const float (&f)[4], bool stream) {
+__device__ __forceinline__ void store4(G<float> p, int64_t valid, const float (&f)[4], bool stream) {
   if (valid >= 4) {
     f32x4u v;
     for (int e = 0; e < 4; ++e) v[e] = f[e];
@@ -125,7 +120,7 @@ __device__ __forceinline__ void store4(float* p, int64_t valid, const float (&f)
   }
 }
 template <class T>
-__device__ __forceinline__ void store_copy4(T* p, int64_t valid, const float (&f)[4], bool stream) {
+__device__ __forceinline__ void store_copy4(G<T> p, int64_t valid, const float (&f)[4], bool stream) {
   T h[4];
   for (int e = 0; e < 4; ++e) h[e] = Elem<T>::from_f(f[e]);
   if (valid >= 4) {
@@ -139,8 +134,8 @@ __device__ __forceinline__ void store_copy4(T* p, int64_t valid, const float (&f
 }
 __device__ __forceinline__ void store_copy(const TensorEntry& t, int64_t i, int64_t valid, const float (&f)[4], bool stream) {
   if (!t.copy) return;
-  if (t.copy_dt == PIGAN_BF16) store_copy4((bf16*)t.copy + i, valid, f, stream);
-  else store_copy4((f16*)t.copy + i, valid, f, stream);
+  if (t.copy_dt == PIGAN_BF16) store_copy4((G<bf16>)t.copy + i, valid, f, stream);
+  else store_copy4((G<f16>)t.copy + i, valid, f, stream);
 }
 
 // ---------------------------------------------------------------------------
@@ -186,29 +181,25 @@ __device__ __forceinline__ void update(const AdamwArgs& a, const Coefs& k, float
 __global__ void __launch_bounds__(NTH) k_adamw32(const AdamwArgs a) {
   if (a.skip && *a.skip) return;   // one flag for the whole launch
   const TensorPiece w = a.pieces[blockIdx.x];
-  const TensorEntry t = entry_at(a.entries + w.tensor);
+  const TensorEntry t = a.entries[w.tensor];
   const Coefs k = coefs_of(a, t.decay);
-  const int64_t first = (int64_t)w.piece * PIECE;
-  float* m = (float*)a.m + t.state;
-  float* v = (float*)a.v + t.state;
-  for (int it = 0; it < PIECE / (NTH * 4); ++it) {
-    const int64_t i = first + (it * NTH + threadIdx.x) * 4, valid = t.n - i;
-    if (valid <= 0) break;
-    float pf[4], gf[4], mf[4], vf[4];
-    load4(t.p + i, valid, pf, a.stream);
-    load_grad(t.g, t.g_dt, i, valid, gf, a.stream);
-    load4(m + i, valid, mf, a.stream);
-    load4(v + i, valid, vf, a.stream);
+  const int64_t i = (int64_t)w.piece * PIECE + threadIdx.x * 4, valid = t.n - i;
+  if (valid <= 0) return;
+  const G<float> m = (G<float>)a.m + t.state, v = (G<float>)a.v + t.state;
+  float pf[4], gf[4], mf[4], vf[4];
+  load4((G<const float>)t.p + i, valid, pf, a.stream);
+  load_grad((G<const void>)t.g, t.g_dt, i, valid, gf, a.stream);
+  load4(m + i, valid, mf, a.stream);
+  load4(v + i, valid, vf, a.stream);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const double mo = mf[e], vo = vf[e];
-      update(a, k, gf[e], mo, vo, pf[e], mf[e], vf[e]);
-    }
-    store4(t.p + i, valid, pf, a.stream);
-    store4(m + i, valid, mf, a.stream);
-    store4(v + i, valid, vf, a.stream);
-    store_copy(t, i, valid, pf, a.stream);
+  for (int e = 0; e < 4; ++e) {
+    const double mo = mf[e], vo = vf[e];
+    update(a, k, gf[e], mo, vo, pf[e], mf[e], vf[e]);
   }
+  store4((G<float>)t.p + i, valid, pf, a.stream);
+  store4(m + i, valid, mf, a.stream);
+  store4(v + i, valid, vf, a.stream);
+  store_copy(t, i, valid, pf, a.stream);
 }
 
 // The code of size x among a largest of s: the nearest whole root of x top / s, top the
@@ -234,57 +225,54 @@ __device__ __forceinline__ int code_of(float x, double inv) {
 __global__ void __launch_bounds__(NTH) k_adamw8(const AdamwArgs a) {
   if (a.skip && *a.skip) return;
   const TensorPiece w = a.pieces[blockIdx.x];
-  const TensorEntry t = entry_at(a.entries + w.tensor);
+  const TensorEntry t = a.entries[w.tensor];
   const Coefs k = coefs_of(a, t.decay);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t first = (int64_t)w.piece * PIECE;
-  for (int it = 0; it < PIECE / (NTH * 4); ++it) {
-    const int64_t b = first + (it * (NTH / 64) + wave) * QBLOCK;
-    if (b >= t.n) break;
-    const int64_t i = b + lane * 4, valid = t.n - i, at = t.state + i, qb = (t.state + b) / QBLOCK;
-    float pf[4] = {0, 0, 0, 0}, gf[4] = {0, 0, 0, 0}, mf[4], vf[4];
-    if (valid > 0) {
-      load4(t.p + i, valid, pf, a.stream);
-      load_grad(t.g, t.g_dt, i, valid, gf, a.stream);
-    }
-    // states are there to the end of the block
-    const uint32_t mq = get<uint32_t>((const int8_t*)a.m + at, a.stream), vq = get<uint32_t>((const uint8_t*)a.v + at, a.stream);
-    const double ms = unit_of(a.m_scale[qb], TOP_M), vs = unit_of(a.v_scale[qb], TOP_V);
-    float mmax = 0.0f, vmax = 0.0f, none = 0.0f;   // `none` is 0 unless a state is not finite
+  const int64_t b = (int64_t)w.piece * PIECE + wave * QBLOCK;
+  if (b >= t.n) return;
+  const int64_t i = b + lane * 4, valid = t.n - i, at = t.state + i, qb = (t.state + b) / QBLOCK;
+  float pf[4] = {0, 0, 0, 0}, gf[4] = {0, 0, 0, 0}, mf[4], vf[4];
+  if (valid > 0) {
+    load4((G<const float>)t.p + i, valid, pf, a.stream);
+    load_grad((G<const void>)t.g, t.g_dt, i, valid, gf, a.stream);
+  }
+  // states are there to the end of the block
+  const uint32_t mq = get<uint32_t>((G<const int8_t>)a.m + at, a.stream), vq = get<uint32_t>((G<const uint8_t>)a.v + at, a.stream);
+  const double ms = unit_of(a.m_scale[qb], TOP_M), vs = unit_of(a.v_scale[qb], TOP_V);
+  float mmax = 0.0f, vmax = 0.0f, none = 0.0f;   // `none` is 0 unless a state is not finite
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int qm = (int)(int8_t)(mq >> (8 * e));
+    const uint32_t qv = (vq >> (8 * e)) & 255, q2 = qv * qv;
+    update(a, k, gf[e], (double)(qm * abs(qm)) * ms, (double)(q2 * q2) * vs, pf[e], mf[e], vf[e]);
+    if (e >= valid) mf[e] = vf[e] = 0.0f;
+    mmax = fmaxf(mmax, fabsf(mf[e]));
+    vmax = fmaxf(vmax, vf[e]);
+    none += 0.0f * mf[e];
+    none += 0.0f * vf[e];
+  }
+  mmax = wave_max(mmax);
+  vmax = wave_max(vmax);
+  const bool all = __all(none == 0.0f);
+  const double mi = mmax > 0.0f ? TOP_M * rcp64_full((double)mmax) : 0.0, vi = vmax > 0.0f ? TOP_V * rcp64_full((double)vmax) : 0.0;
+  uint32_t mo = 0, vo = 0;
+  if (all) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int qm = (int)(int8_t)(mq >> (8 * e));
-      const uint32_t qv = (vq >> (8 * e)) & 255, q2 = qv * qv;
-      update(a, k, gf[e], (double)(qm * abs(qm)) * ms, (double)(q2 * q2) * vs, pf[e], mf[e], vf[e]);
-      if (e >= valid) mf[e] = vf[e] = 0.0f;
-      mmax = fmaxf(mmax, fabsf(mf[e]));
-      vmax = fmaxf(vmax, vf[e]);
-      none += 0.0f * mf[e];
-      none += 0.0f * vf[e];
+      const int q = min(code_of<false>(fabsf(mf[e]), mi), 127), u = min(code_of<true>(vf[e], vi), 255);
+      mo |= (uint32_t)(uint8_t)(mf[e] < 0.0f ? -q : q) << (8 * e);
+      vo |= (uint32_t)(vf[e] > 0.0f ? max(u, 1) : 0) << (8 * e);
     }
-    mmax = wave_max(mmax);
-    vmax = wave_max(vmax);
-    const bool all = __all(none == 0.0f);
-    const double mi = mmax > 0.0f ? TOP_M * rcp64_full((double)mmax) : 0.0, vi = vmax > 0.0f ? TOP_V * rcp64_full((double)vmax) : 0.0;
-    uint32_t mo = 0, vo = 0;
-    if (all) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int q = min(code_of<false>(fabsf(mf[e]), mi), 127), u = min(code_of<true>(vf[e], vi), 255);
-        mo |= (uint32_t)(uint8_t)(mf[e] < 0.0f ? -q : q) << (8 * e);
-        vo |= (uint32_t)(vf[e] > 0.0f ? max(u, 1) : 0) << (8 * e);
-      }
-    }
-    put<uint32_t>((int8_t*)a.m + at, mo, a.stream);
-    put<uint32_t>((uint8_t*)a.v + at, vo, a.stream);
-    if (lane == 0) {
-      a.m_scale[qb] = all ? mmax : __builtin_nanf("");
-      a.v_scale[qb] = all ? vmax : __builtin_nanf("");
-    }
-    if (valid > 0) {
-      store4(t.p + i, valid, pf, a.stream);
-      store_copy(t, i, valid, pf, a.stream);
-    }
+  }
+  put<uint32_t>((G<int8_t>)a.m + at, mo, a.stream);
+  put<uint32_t>((G<uint8_t>)a.v + at, vo, a.stream);
+  if (lane == 0) {
+    a.m_scale[qb] = all ? mmax : __builtin_nanf("");
+    a.v_scale[qb] = all ? vmax : __builtin_nanf("");
+  }
+  if (valid > 0) {
+    store4((G<float>)t.p + i, valid, pf, a.stream);
+    store_copy(t, i, valid, pf, a.stream);
   }
 }
 
@@ -303,19 +291,21 @@ __global__ void __launch_bounds__(NTH) k_grad_squares(const TensorEntry* __restr
                                                       const TensorPiece* __restrict__ pieces, int64_t n_pieces,
                                                       double* __restrict__ part) {
   __shared__ double sums[NTH / 64];
+  constexpr int U = 4;   // pieces under way
   double s = 0.0;
-  for (int64_t b = blockIdx.x; b < n_pieces; b += gridDim.x) {
-    const TensorPiece w = pieces[b];
-    const TensorEntry t = entry_at(entries + w.tensor);
-    const int64_t first = (int64_t)w.piece * PIECE;
+  for (int64_t b = (int64_t)blockIdx.x * U; b < n_pieces; b += (int64_t)gridDim.x * U) {
+    float f[U][4];
 #pragma unroll
-    for (int it = 0; it < PIECE / (NTH * 4); ++it) {
-      const int64_t i = first + (it * NTH + threadIdx.x) * 4, valid = t.n - i;
-      if (valid <= 0) break;
-      float f[4];
-      load_grad(t.g, t.g_dt, i, valid, f);
-      for (int e = 0; e < 4; ++e) s += (double)f[e] * (double)f[e];
+    for (int u = 0; u < U; ++u) {
+      const TensorPiece w = pieces[min(b + u, n_pieces - 1)];
+      const TensorEntry& t = entries[w.tensor];
+      const int64_t i = (int64_t)w.piece * PIECE + threadIdx.x * 4;
+      load_grad((G<const void>)t.g, t.g_dt, i, b + u < n_pieces ? t.n - i : 0, f[u]);
     }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s += (double)f[u][e] * (double)f[u][e];
   }
   s = wave_sum(s);
   if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
@@ -349,22 +339,22 @@ __global__ void __launch_bounds__(NTH) k_state_values(int64_t n, const int8_t* _
   for (int64_t i = ((int64_t)blockIdx.x * NTH + threadIdx.x) * 4; i < n; i += (int64_t)gridDim.x * NTH * 4) {
     float f[4];
     if (m_out) {
-      const uint32_t q = get<uint32_t>(m + i, stream);
+      const uint32_t q = get<uint32_t>((G<const int8_t>)m + i, stream);
       const double s = unit_of(m_scale[i / QBLOCK], TOP_M);
       for (int e = 0; e < 4; ++e) {
         const int c = (int)(int8_t)(q >> (8 * e));
         f[e] = (float)((double)(c * abs(c)) * s);
       }
-      store4(m_out + i, 4, f, stream);
+      store4((G<float>)m_out + i, 4, f, stream);
     }
     if (v_out) {
-      const uint32_t q = get<uint32_t>(v + i, stream);
+      const uint32_t q = get<uint32_t>((G<const uint8_t>)v + i, stream);
       const double s = unit_of(v_scale[i / QBLOCK], TOP_V);
       for (int e = 0; e < 4; ++e) {
         const uint32_t c = (q >> (8 * e)) & 255;
         f[e] = (float)((double)(c * c * c * c) * s);
       }
-      store4(v_out + i, 4, f, stream);
+      store4((G<float>)v_out + i, 4, f, stream);
     }
   }
 }
@@ -389,7 +379,7 @@ hipError_t launch_adamw_begin(double b1, double b2, int32_t* step, const int32_t
   return hipGetLastError();
 }
 
-int64_t grad_norm_blocks(int64_t n_pieces) { return std::max<int64_t>(1, std::min<int64_t>(n_pieces, 2048)); }
+int64_t grad_norm_blocks(int64_t n_pieces) { return std::max<int64_t>(1, std::min<int64_t>((n_pieces + 3) / 4, 2048)); }
 
 hipError_t launch_grad_norm(const TensorEntry* entries, const TensorPiece* pieces, int64_t n_pieces, double max_norm,
                             double scale, double* part, float* norm, float* coef, int32_t* nonfinite, hipStream_t st) {
@@ -402,7 +392,7 @@ hipError_t launch_grad_norm(const TensorEntry* entries, const TensorPiece* piece
 hipError_t launch_state_values(int64_t n, const int8_t* m, const float* m_scale, const uint8_t* v, const float* v_scale,
                                float* m_out, float* v_out, hipStream_t st) {
   if (n <= 0) return hipSuccess;
-  const int64_t blocks = std::min<int64_t>((n + NTH * 4 - 1) / (NTH * 4), 8192);
+  const int64_t blocks = std::min<int64_t>((n + NTH * 4 - 1) / (NTH * 4), 1 << 20);
   k_state_values<<<(unsigned)blocks, NTH, 0, st>>>(n, m, m_scale, v, v_scale, m_out, v_out, n * 5.0 * (!!m_out + !!v_out) > STREAM_BYTES);
   return hipGetLastError();
 }
