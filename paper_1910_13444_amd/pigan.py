@@ -789,12 +789,16 @@ _NO_FIELD = (0, 0, 0, 0)
 
 def _field(t: torch.Tensor, name: str, like: torch.Tensor, shape) -> tuple[int, int, int, int]:
     """(pointer, point stride, sample stride, group stride) of a field operand."""
-    if t.dtype != like.dtype:
-        raise ValueError(f"{name} must be {like.dtype}, got {t.dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.device != like.device:
-        raise ValueError(f"{name} is on {t.device}, expected {like.device}")
+    if t is not like:
+        if t.dtype != like.dtype:
+            raise ValueError(f"{name} must be {like.dtype}, got {t.dtype}")
+        if t.shape != shape:
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+        if t.device != like.device:
+            raise ValueError(f"{name} is on {t.device}, expected {like.device}")
+    if t.is_contiguous():
+        *_, S, P, C_ = shape
+        return t.data_ptr(), C_, P * C_, S * P * C_
     st = t.stride()
     extent = shape[-1]
     if st[-1] != 1 and extent > 1:
@@ -829,7 +833,7 @@ def _new_field(need: bool, t: torch.Tensor | None, name: str, like: torch.Tensor
         return None, _NO_FIELD
     if t is not None:
         return t, _field(t, name, like, shape)
-    t = torch.empty(shape, dtype=like.dtype, device=like.device)
+    t = torch.empty_like(like) if like.is_contiguous() else torch.empty(shape, dtype=like.dtype, device=like.device)
     return t, (t.data_ptr(), shape[-1], shape[-2] * shape[-1], shape[-3] * shape[-2] * shape[-1])
 
 
@@ -851,7 +855,11 @@ def group_norm(x: torch.Tensor, n: int, gamma: torch.Tensor | None = None, beta:
     mx = _field(x, "x", x, shape)
     out, mo = _new_field(True, out, "out", x, shape)
     mean, pm = _result_vec(need_stats, mean, "mean", x, stats)
-    rstd, pr = _result_vec(need_stats, rstd, "rstd", x, stats)
+    if need_stats and rstd is None:
+        rstd = torch.empty_like(mean)
+        pr = rstd.data_ptr()
+    else:
+        rstd, pr = _result_vec(need_stats, rstd, "rstd", x, stats)
     args = GROUP_NORM_ARGS.pack(G, dt, _act(act), eps, S, P, C_, n, *mx, *mo, *_NO_FIELD, *_NO_FIELD, *_NO_FIELD,
                                 0 if gamma is None else _vec(gamma, "gamma", x, chans),
                                 0 if beta is None else _vec(beta, "beta", x, chans), pm, pr, 0, 0)
@@ -983,8 +991,8 @@ def grad_norm(table: TensorTable, max_norm: float = float("inf"), scale: float =
     if dev.index != torch.cuda.current_device():
         with torch.cuda.device(dev):
             return grad_norm(table, max_norm, scale, ws)
-    norm, coef = torch.empty((), dtype=torch.float32, device=dev), torch.empty((), dtype=torch.float32, device=dev)
-    flag = torch.empty((), dtype=torch.int32, device=dev)
+    norm = torch.empty((), dtype=torch.float32, device=dev)
+    coef, flag = torch.empty_like(norm), torch.empty_like(norm, dtype=torch.int32)
     if ws is None or ws.numel() < table._norm_ws:
         ws = torch.empty(table._norm_ws, dtype=torch.uint8, device=dev)
     elif ws.dtype != torch.uint8 or ws.device != dev or not ws.is_contiguous():
@@ -1037,7 +1045,8 @@ def state_values(table: TensorTable):
     if dev.index != torch.cuda.current_device():
         with torch.cuda.device(dev):
             return state_values(table)
-    m, v = (torch.empty(table.m.shape, dtype=torch.float32, device=dev) for _ in range(2))
+    m = torch.empty_like(table.m, dtype=torch.float32)
+    v = torch.empty_like(m)
     _check(lib().pigan_state_values(m.numel(), table.m.data_ptr(), table.m_scale.data_ptr(), table.v.data_ptr(),
                                     table.v_scale.data_ptr(), m.data_ptr(), v.data_ptr(),
                                     torch._C._cuda_getCurrentRawStream(dev.index)))

@@ -65,10 +65,11 @@ def test_a_table_covers_every_tensor(bits, states):
     assert st == pigan.OK and count == states
     raw = bytes(table)[:size]
     n_tensors, tbits, n_pieces, got = struct.unpack_from("2i2q", raw, 8)
-    assert (n_tensors, tbits, n_pieces, got) == (4, bits, 1 + 2 + 1, states)
+    assert (n_tensors, tbits, n_pieces, got) == (4, bits, 1 + 5 + 1, states)   # pieces of 1024 elements
     entries_at, pieces_at, total = struct.unpack_from("3q", raw, 32)
     assert total == size and pieces_at - entries_at == 4 * 56
-    assert [struct.unpack_from("2I", raw, pieces_at + 8 * k) for k in range(4)] == [(0, 0), (2, 0), (2, 1), (3, 0)]
+    assert [struct.unpack_from("2I", raw, pieces_at + 8 * k) for k in range(7)] == \
+        [(0, 0), *((2, k) for k in range(5)), (3, 0)]
     starts = [struct.unpack_from("3P2qd2i", raw, entries_at + 56 * k)[4] for k in range(4)]
     assert starts == {8: [0, 256, 256, 256 + 17 * 256], 32: [0, 1, 1, 4098], 0: [0, 1, 1, 4098]}[bits]
 
