@@ -10,21 +10,13 @@ template <class T, int SL>
 struct Column {
   float mean[SL], rstd[SL], ga[EPP<T>], be[EPP<T>];
   __device__ __forceinline__ void load(const GnArgs<T>& a, const Slab& b, const Div& by_span, int64_t g, int64_t s, int col) {
+    load_scales(a, b, g, col);
+    load_stats(a, b, by_span, g, s, col);
+  }
+  __device__ __forceinline__ void load_scales(const GnArgs<T>& a, const Slab& b, int64_t g, int col) {
     constexpr int E = EPP<T>;
     vec_load<E>(a.gamma ? a.gamma + g * a.C : nullptr, b.c0 + col * E, b.c0 + b.width, 1.0f, ga);
     vec_load<E>(a.beta ? a.beta + g * a.C : nullptr, b.c0 + col * E, b.c0 + b.width, 0.0f, be);
-    load_stats(a, b, by_span, g, s, col);
-  }
-  // from LDS, [2][wide], again for every piece
-  __device__ __forceinline__ void load_scales(const float* gab, int wide, int col) {
-    constexpr int E = EPP<T>;
-    asm volatile("" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < E; i += 4) {
-      const f32x4 u = *(const f32x4*)(gab + col * E + i), w = *(const f32x4*)(gab + wide + col * E + i);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) { ga[i + q] = u[q]; be[i + q] = w[q]; }
-    }
   }
   __device__ __forceinline__ void load_stats(const GnArgs<T>& a, const Slab& b, const Div& by_span, int64_t g, int64_t s, int col) {
 #pragma unroll
@@ -54,7 +46,7 @@ __device__ __forceinline__ void slope_piece(const Column<T, SL>& c, int valid, f
 // ---------------------------------------------------------------------------
 // bytes of LDS that a group's sums, or half the columns' sums, take
 constexpr size_t bwd_sums_lds(int nth, int sl, int e) {
-  return (size_t)nth * (sl * sizeof(Pair) > (size_t)e * 4 ? sl * sizeof(Pair) : (size_t)e * 4);
+  return (size_t)nth * ((sl + 1) * sizeof(PairF) > (size_t)e * 4 ? (sl + 1) * sizeof(PairF) : (size_t)e * 4);
 }
 
 // a block's rows of sums, added in order; fm: float [rows][pw * E]
@@ -77,6 +69,7 @@ __device__ __forceinline__ void store_columns(const GnArgs<T>& a, float* fm, con
     float* d = half ? d1 : d0;
     for (int c = threadIdx.x; c < b.width; c += blockDim.x) {
       double t = 0.0;
+#pragma unroll 8
       for (int r = 0; r < pl.rows; ++r) t += fm[r * wide + c];
       if (d) d[b.c0 + c] = (float)t;
     }
@@ -166,103 +159,82 @@ __global__ void __launch_bounds__(256) k_gn_rows_bwd(const GnArgs<T> a) {
   if (a.dgamma || a.dbeta) store_columns(a, (float*)sm, sg, sb, b, g, col, row);
 }
 
-template <class T, int NTH, int NV, int SL, bool WHOLE, int ACT>
-__global__ void __launch_bounds__(NTH) k_gn_one_bwd(const GnArgs<T> a) {
+// Short samples: a thread has one point's piece of a batch of samples, and the next batch's on
+// its way.
+template <class T, int SL, bool WHOLE, int ACT>
+__global__ void __launch_bounds__(ONE_NTH) k_gn_one_bwd(const GnArgs<T> a) {
   constexpr int E = EPP<T>;
   extern __shared__ Pair sm[];
   const GnPlan& pl = a.pl;
-  float* gab = (float*)((char*)sm + bwd_sums_lds(NTH, SL, E));   // gamma and beta of the slab: beside the pieces they would not fit the registers
-  float2* means = (float2*)(gab + 2 * pl.pw * E);
-  const int row = Div(pl.pw)(threadIdx.x), col = threadIdx.x - row * pl.pw;
-  const bool many = NV == 1 && pl.ns > 1;
-  const int si = many ? Div((int)a.P)(row) : 0, pr = many ? row - si * (int)a.P : row, left = (int)a.P - pr;
+  PairF* hs = (PairF*)sm;
+  float2* means = (float2*)((char*)sm + bwd_sums_lds(ONE_NTH, SL, E));
+  const int row = Div(pl.pw)(threadIdx.x), col = threadIdx.x - row * pl.pw, per = row_of(pl.pw * SL);
+  const int si = pl.ns > 1 ? Div((int)a.P)(row) : 0, p = row - si * (int)a.P;
   const Div by_span(pl.span);
   const int64_t batches = (a.S + pl.ns - 1) / pl.ns, g = blockIdx.z;
   for (uint32_t slab = blockIdx.y; slab < pl.slabs; slab += gridDim.y) {
     const Slab b = slab_at(a, slab);
     const int valid = b.width - col * E;
+    const bool here = row < pl.rows && p < a.P && valid > 0;
+    const int64_t at = b.c0 + col * E;
+    const T* x = a.x.p + g * a.x.gs + p * a.x.ld + at;
+    const T* dy = a.dy.p + g * a.dy.gs + p * a.dy.ld + at;
     float sg[E], sb[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) sg[e] = sb[e] = 0.0f;
-    __syncthreads();   // the slab before may still be read
-    for (int i = threadIdx.x; i < pl.pw * E; i += NTH) {
-      gab[i] = a.gamma && i < b.width ? a.gamma[g * a.C + b.c0 + i] : 1.0f;
-      gab[pl.pw * E + i] = a.beta && i < b.width ? a.beta[g * a.C + b.c0 + i] : 0.0f;
-    }
-    __syncthreads();
+    Column<T, SL> c;
+    c.load_scales(a, b, g, col);
+    piece_t rx, rd;
+    auto load = [&](int64_t s) {
+      if (here && s < a.S) {
+        rx = load_piece<WHOLE>(x + s * a.x.ss, valid, pl.stream);
+        rd = load_piece<WHOLE>(dy + s * a.dy.ss, valid, pl.stream);
+      }
+    };
+    load(blockIdx.x * (int64_t)pl.ns + si);
     for (int64_t bt = blockIdx.x; bt < batches; bt += gridDim.x) {
       const int64_t s = bt * pl.ns + si;
-      const bool on = row < pl.rows && left > 0 && s < a.S && valid > 0;
-      const T* x = a.x.p + g * a.x.gs + s * a.x.ss + b.c0 + col * E;
-      const T* dy = a.dy.p + g * a.dy.gs + s * a.dy.ss + b.c0 + col * E;
-      piece_t rx[NV], rd[NV];
-      Column<T, SL> c;
-      float h0[SL], h1[SL];
+      const bool on = here && s < a.S;
+      float xh[E], da[E], h0[SL], h1[SL];
 #pragma unroll
       for (int e = 0; e < SL; ++e) h0[e] = h1[e] = 0.0f;
       if (on) {
-        load_rows<WHOLE>(rx, x + pr * a.x.ld, pl.rows * a.x.ld, left, pl.rows, valid);
-        load_rows<WHOLE>(rd, dy + pr * a.dy.ld, pl.rows * a.dy.ld, left, pl.rows, valid);
         c.load_stats(a, b, by_span, g, s, col);
+        piece_floats<T>(rx, xh);
+        piece_floats<T>(rd, da);
+        slope_piece<ACT, WHOLE>(c, valid, xh, da);
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-          if (v > 0 && v * pl.rows >= left) break;
-          float xh[E];
-          float da[E];
-          piece_floats<T>(rx[v], xh);
-          piece_floats<T>(rd[v], da);
-          c.load_scales(gab, pl.pw * E, col);
-          slope_piece<ACT, WHOLE>(c, valid, xh, da);
-#pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const int k = SL > 1 ? e : 0;
-            const float t = da[e] * xh[e];
-            sg[e] += t;
-            sb[e] += da[e];
-            h0[k] += da[e] * c.ga[e];
-            h1[k] += t * c.ga[e];
-          }
-          __builtin_amdgcn_sched_barrier(0);
+        for (int e = 0; e < E; ++e) {
+          const int k = SL > 1 ? e : 0;
+          const float t = da[e] * xh[e];
+          sg[e] += t;
+          sb[e] += da[e];
+          h0[k] += da[e] * c.ga[e];
+          h1[k] += t * c.ga[e];
         }
       }
+      load(s + (int64_t)gridDim.x * pl.ns);
       if (!a.out.p) continue;   // the same for every thread
       if (row < pl.rows)
 #pragma unroll
-        for (int e = 0; e < SL; ++e) sm[row * pl.pw * SL + col * SL + e] = {h0[e], h1[e]};
+        for (int e = 0; e < SL; ++e) hs[row * per + col * SL + e] = {h0[e], h1[e]};
       __syncthreads();
-      group_sums(sm, pl.ns, pl.ns > 1 ? (int)a.P : pl.rows, pl.pw * SL, b.ng, pl.span, pl.lanes, [&](int i, int j, const Pair& t) {
+      group_sums(hs, pl.ns, pl.ns > 1 ? (int)a.P : pl.rows, per, b.ng, pl.span, pl.lanes, [&](int i, int j, const Pair& t) {
         means[i * b.ng + j] = {(float)(t.s * pl.inv_n), (float)(t.q * pl.inv_n)};
       });
       __syncthreads();
       if (!on) continue;
-      float2 m[SL];
+      float r[E];
+      if (a.add.p) piece_floats<T>(load_piece<WHOLE>(a.add.p + g * a.add.gs + s * a.add.ss + p * a.add.ld + at, valid, pl.stream), r);
 #pragma unroll
-      for (int e = 0; e < SL; ++e) m[e] = means[si * b.ng + group_of<T, SL>(b, by_span, col, e)];
-      const T* add = a.add.p ? a.add.p + g * a.add.gs + s * a.add.ss + b.c0 + col * E : nullptr;
-      T* out = a.out.p + g * a.out.gs + s * a.out.ss + b.c0 + col * E;
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        const int64_t p = pr + v * pl.rows;
-        if (v * pl.rows < left) {
-          float xh[E];
-          float da[E];
-          float r[E];
-          if (add) piece_floats<T>(load_piece<WHOLE>(add + p * a.add.ld, valid), r);
-          piece_floats<T>(rx[v], xh);
-          piece_floats<T>(rd[v], da);
-          c.load_scales(gab, pl.pw * E, col);
-          slope_piece<ACT, WHOLE>(c, valid, xh, da);
-#pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const int k = SL > 1 ? e : 0;
-            da[e] = c.rstd[k] * (da[e] * c.ga[e] - m[k].x - xh[e] * m[k].y);
-            if (add) da[e] += r[e];
-          }
-          store_piece<WHOLE>(out + p * a.out.ld, valid, da, pl.stream);
-        }
-        __builtin_amdgcn_sched_barrier(0);
+      for (int e = 0; e < E; ++e) {
+        const float2 m = means[si * b.ng + group_of<T, SL>(b, by_span, col, SL > 1 ? e : 0)];
+        da[e] = c.rstd[SL > 1 ? e : 0] * (da[e] * c.ga[e] - m.x - xh[e] * m.y);
+        if (a.add.p) da[e] += r[e];
       }
+      store_piece<WHOLE>(a.out.p + g * a.out.gs + s * a.out.ss + p * a.out.ld + at, valid, da, pl.stream);
     }
+    __syncthreads();   // the sums' place is the columns', and the next slab's
     if (a.dgamma || a.dbeta) store_columns(a, (float*)sm, sg, sb, b, g, col, row);
   }
 }
@@ -334,6 +306,7 @@ __global__ void __launch_bounds__(SPLIT_NTH) k_gn_bwd_sums(const GnArgs<T> a, fl
       __syncthreads();
       for (int i = threadIdx.x; i < 2 * wide; i += SPLIT_NTH) {
         double t = 0.0;
+#pragma unroll 8
         for (int r = 0; r < pl.rows; ++r) t += fm[r * 2 * wide + i];
         sums[i] = t;
         all[i] += t;   // always by this thread
@@ -493,11 +466,8 @@ template <class T> hipError_t launch_gn_bwd(const GnArgs<T>& a, int G, hipStream
     } else if (pl.mode == GN_ONE) {
       const dim3 grid((unsigned)pl.slots, (unsigned)std::min<int64_t>(pl.slabs, 65535), G);
       by_width(a, [&](auto sl, auto whole) {
-        by_shape<true, false>(pl, [&](auto nth, auto nv) {
-          const size_t lds = bwd_sums_lds(nth.value, sl.value, EPP<T>) + (size_t)pl.ns * pl.ng * sizeof(float2) +
-                             (size_t)pl.pw * EPP<T> * 8;
-          k_gn_one_bwd<T, nth.value, nv.value, sl.value, whole.value, ACT><<<grid, nth.value, lds, st>>>(a);
-        });
+        const size_t lds = bwd_sums_lds(ONE_NTH, sl.value, EPP<T>) + (size_t)pl.ns * pl.ng * sizeof(float2);
+        k_gn_one_bwd<T, sl.value, whole.value, ACT><<<grid, ONE_NTH, lds, st>>>(a);
       });
     } else {
       const int64_t ranges = a.S * pl.splits;

@@ -71,12 +71,13 @@ __global__ void __launch_bounds__(NTH, NV < 8 ? 1 : SL == 1 && WHOLE ? 4 : 3) k_
   constexpr int E = EPP<T>;
   extern __shared__ Pair sm[];
   const GnPlan& pl = a.pl;
-  Stat* stat = (Stat*)(sm + NTH * SL);
+  Stat* stat = (Stat*)(sm + NTH * (SL + 1));
   float* shift = (float*)(stat + pl.ns * pl.ng);
   const int row = Div(pl.pw)(threadIdx.x), col = threadIdx.x - row * pl.pw;
   const bool many = NV == 1 && pl.ns > 1;
   const int si = many ? Div((int)a.P)(row) : 0, pr = many ? row - si * (int)a.P : row;
   const Div by_span(pl.span);
+  const int per = row_of(pl.pw * SL);
   const int64_t g = blockIdx.z;
   const Slab b = slab_at(a, blockIdx.x);
   const int valid = b.width - col * E, left = (int)min(a.P, (int64_t)INT32_MAX) - pr;
@@ -114,11 +115,11 @@ __global__ void __launch_bounds__(NTH, NV < 8 ? 1 : SL == 1 && WHOLE ? 4 : 3) k_
 #pragma unroll
       for (int e = 0; e < SL; ++e) {
         const int slot = col * SL + e, j = by_span(slot);
-        sm[row * pl.pw * SL + slot] = acc[e];
+        sm[row * per + slot] = acc[e];
         if (on && pr == 0 && j < b.ng && slot == j * pl.span) shift[si * b.ng + j] = k[e];
       }
     __syncthreads();
-    group_sums(sm, pl.ns, pl.ns > 1 ? (int)a.P : pl.rows, pl.pw * SL, b.ng, pl.span, pl.lanes, [&](int i, int j, const Pair& t) {
+    group_sums(sm, pl.ns, pl.ns > 1 ? (int)a.P : pl.rows, per, b.ng, pl.span, pl.lanes, [&](int i, int j, const Pair& t) {
       const Stat st = stat_of(t, shift[i * b.ng + j], pl.inv_n, a.eps);
       stat[i * b.ng + j] = st;
       const int64_t at = (g * a.S + s0 + i) * a.n + b.j0 + j;
@@ -167,6 +168,7 @@ __global__ void __launch_bounds__(SPLIT_NTH) k_gn_sums(const GnArgs<T> a, uint32
   const GnPlan& pl = a.pl;
   const int row = Div(pl.pw)(threadIdx.x), col = threadIdx.x - row * pl.pw, parts = pl.chan_parts * pl.splits;
   const Div by_span(pl.span);
+  const int per = row_of(pl.pw * SL);
   const int64_t g = blockIdx.z;
   for (uint32_t slab = blockIdx.y; slab < pl.slabs; slab += gridDim.y) {
     const Slab b = slab_at(a, slab);
@@ -207,13 +209,13 @@ __global__ void __launch_bounds__(SPLIT_NTH) k_gn_sums(const GnArgs<T> a, uint32
       }
       if (row < pl.rows)
 #pragma unroll
-        for (int e = 0; e < SL; ++e) sm[(row * pl.pw + col) * SL + e] = acc[e];
+        for (int e = 0; e < SL; ++e) sm[row * per + col * SL + e] = acc[e];
       __syncthreads();
       Pair* part = (Pair*)a.ws;
       float* shifts = (float*)(part + all_groups * parts);
       const int64_t i0 = (g * a.S + s) * a.n + b.j0;
       const int at = pl.chan_parts > 1 ? slab % (uint32_t)pl.chan_parts * pl.splits + split : split;
-      group_sums(sm, 1, pl.rows, pl.pw * SL, b.ng, pl.span, pl.lanes, [&](int, int j, const Pair& t) {
+      group_sums(sm, 1, pl.rows, per, b.ng, pl.span, pl.lanes, [&](int, int j, const Pair& t) {
         part[(i0 + j) * parts + at] = t;
         if (at == 0) shifts[i0 + j] = shift_of(Elem<T>::to_f(first[(b.j0 + j) * pl.cg]));
       });
@@ -309,8 +311,8 @@ template <class T> hipError_t launch_gn_fwd(const GnArgs<T>& a, int G, hipStream
       const int64_t batches = cdiv(a.S, pl.ns);
       const dim3 grid((unsigned)pl.slabs, (unsigned)std::min<int64_t>(batches, 65535), G);
       by_width(a, [&](auto sl, auto whole) {
-        by_shape<false, sl.value == 1 && whole.value>(pl, [&](auto nth, auto nv) {
-          const size_t lds = nth.value * sl.value * sizeof(Pair) + (size_t)pl.ns * pl.ng * (sizeof(Stat) + 4);
+        by_shape<sl.value == 1 && whole.value>(pl, [&](auto nth, auto nv) {
+          const size_t lds = nth.value * (sl.value + 1) * sizeof(Pair) + (size_t)pl.ns * pl.ng * (sizeof(Stat) + 4);
           k_gn_one<T, nth.value, nv.value, sl.value, whole.value, ACT><<<grid, nth.value, lds, st>>>(a, batches);
         });
       });
@@ -318,7 +320,7 @@ template <class T> hipError_t launch_gn_fwd(const GnArgs<T>& a, int G, hipStream
       const int64_t groups = (int64_t)G * a.S * a.n, ranges = a.S * pl.splits;
       const unsigned slabs = (unsigned)std::min<int64_t>(pl.slabs, 65535);
       by_width(a, [&](auto sl, auto whole) {
-        k_gn_sums<T, sl.value, whole.value><<<dim3(grid_of(ranges), slabs, G), SPLIT_NTH, SPLIT_NTH * sl.value * sizeof(Pair), st>>>(a, (uint32_t)ranges, groups);
+        k_gn_sums<T, sl.value, whole.value><<<dim3(grid_of(ranges), slabs, G), SPLIT_NTH, SPLIT_NTH * (sl.value + 1) * sizeof(Pair), st>>>(a, (uint32_t)ranges, groups);
         k_gn_apply<T, sl.value, whole.value, ACT><<<dim3(grid_of(ranges), slabs, G), SPLIT_NTH, (size_t)pl.ng * sizeof(Stat), st>>>(a, (uint32_t)ranges, groups);
       });
     }

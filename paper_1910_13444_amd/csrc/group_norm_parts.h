@@ -115,19 +115,25 @@ __device__ __forceinline__ void lane_sums(int all, int lanes, A&& add, F&& f) {
   }
 }
 
+// Sums in LDS lie in rows of an odd number of entries, so that a slot's are in banks of their
+// own; a block of N threads has N (slots + 1) entries at most.
+__device__ __forceinline__ int row_of(int slots) { return slots | 1; }
+struct PairF { float s, q; };
+
 // sm[row][slot] of each of `ns` samples of `rows` rows: f(sample, group, sums) of each of its
 // `ng` groups of `span` neighbouring slots
-template <class F>
-__device__ __forceinline__ void group_sums(const Pair* sm, int ns, int rows, int per_row, int ng, int span, int lanes, F&& f) {
+template <class P, class F>
+__device__ __forceinline__ void group_sums(const P* sm, int ns, int rows, int per_row, int ng, int span, int lanes, F&& f) {
   const Div by_ng(ng), by_span(span);
   const int n = rows * span;
   lane_sums(ns * ng, lanes, [&](int k, int l) {
     const int i = ns > 1 ? by_ng(k) : 0, j = k - i * ng;
-    const Pair* p = sm + i * rows * per_row + j * span;
+    const P* p = sm + i * rows * per_row + j * span;
     Pair t = {0.0, 0.0};
+#pragma unroll 4
     for (int q = l; q < n; q += lanes) {
       const int r = by_span(q);
-      const Pair v = p[r * per_row + (q - r * span)];
+      const P v = p[r * per_row + (q - r * span)];
       t.s += v.s;
       t.q += v.q;
     }
@@ -268,11 +274,10 @@ template <class T, class F> void by_width(const GnArgs<T>& a, F&& f) {
   else f(std::integral_constant<int, E>{}, std::false_type{});
 }
 
-// f(NTH, NV) of a plan; the lists' shapes
-template <bool BACKWARD, bool ALIGNED, class F> void by_shape(const GnPlan& pl, F&& f) {
+// f(NTH, NV) of a forward plan; the lists' shapes
+template <bool ALIGNED, class F> void by_shape(const GnPlan& pl, F&& f) {
   constexpr const auto& list = [] () -> const auto& {
-    if constexpr (BACKWARD) return BWD_SHAPES;
-    else if constexpr (ALIGNED) return FWD_SHAPES;
+    if constexpr (ALIGNED) return FWD_SHAPES;
     else return FWD_ODD;
   }();
   constexpr int N = (int)(sizeof(list) / sizeof(Shape));

@@ -37,13 +37,18 @@ GnPlan gn_plan(bool backward, int fields, int elem_bytes, int64_t G, int64_t S, 
     // as many lanes as entries, and no more groups in turns than need be
     while (pl.lanes > 1 && (pl.lanes / 2 >= entries || pl.lanes * pl.ng * pl.ns > pl.nth)) pl.lanes /= 2;
   };
+  // blocks beside each other over a reverse pass's samples, four to a CU; few batches are one
+  // block's, as the sum of several blocks' columns is a launch of its own (3.4 us)
+  auto slots = [&](int64_t batches) {
+    if (batches <= 6) return (int32_t)1;
+    return (int32_t)std::min<int64_t>(batches, std::max<int64_t>(1, 1024 / std::min<int64_t>(1024, G * pl.slabs)));
+  };
   const int64_t lanes = cg / E;
   if (P == 1 && whole_pieces && lanes <= 64 && (lanes & (lanes - 1)) == 0 && cdiv(n, 256 / lanes) <= 65535) {
     slab(std::min<int64_t>(n, 256 / lanes));
     finish(256, 4);
     pl.mode = GN_ROWS;
-    const int64_t blocks = cdiv(S, pl.rows), most = std::max<int64_t>(1, 1024 / std::min<int64_t>(1024, G * pl.slabs));
-    pl.slots = (int32_t)std::min(blocks, most);
+    pl.slots = slots(cdiv(S, pl.rows));
     return pl;
   }
   // one pass: slabs of 128 bytes of a point, 64 where those do not fit
@@ -54,8 +59,7 @@ GnPlan gn_plan(bool backward, int fields, int elem_bytes, int64_t G, int64_t S, 
     const size_t count = backward ? std::size(BWD_SHAPES) : whole_pieces ? std::size(FWD_SHAPES) : std::size(FWD_ODD);
     for (size_t i = 0; i < count; ++i) {
       const Shape f = list[i];
-      // backward: gamma and beta in LDS
-      if (f.nth < pl.pw || (int64_t)(f.nth / pl.pw) * f.nv < P || (backward && pl.pw * E > 2048)) continue;
+      if (f.nth < pl.pw || (int64_t)(f.nth / pl.pw) * f.nv < P) continue;
       const int64_t items = G * S * pl.slabs;
       if (items < 256 && (int64_t)f.nth * f.nv > 4096) break;   // few blocks with much to do: ranges of points
       finish(f.nth, f.nv);
@@ -70,8 +74,7 @@ GnPlan gn_plan(bool backward, int fields, int elem_bytes, int64_t G, int64_t S, 
       }
       fit_lanes((pl.ns > 1 ? P : pl.rows) * (mixed ? cg : std::max<int64_t>(1, pl.pw / pl.ng)));
       pl.mode = GN_ONE;
-      const int64_t batches = cdiv(S, pl.ns), most = std::max<int64_t>(1, 1024 / std::min<int64_t>(1024, G * pl.slabs));
-      pl.slots = (int32_t)std::min(batches, most);
+      pl.slots = slots(cdiv(S, pl.ns));
       return pl;
     }
   }
