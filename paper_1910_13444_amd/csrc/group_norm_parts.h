@@ -149,6 +149,7 @@ template <class F>
 __device__ __forceinline__ void range_sums(const Pair* __restrict__ part, int ng, int parts, int lanes, F&& f) {
   lane_sums(ng, lanes, [&](int k, int l) {
     Pair t = {0.0, 0.0};
+#pragma unroll 4
     for (int q = l; q < parts; q += lanes) {
       const Pair v = part[(int64_t)k * parts + q];
       t.s += v.s;
