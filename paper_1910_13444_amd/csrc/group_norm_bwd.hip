@@ -367,7 +367,7 @@ __device__ __forceinline__ void sum_columns(const GnArgs<T>& a, const Slab& b, c
 // dx, and in the first `col_blocks` blocks of a slab, which are done before the others, the
 // sums of `cols`.  Blocks: [G][slabs][col_blocks + S * splits].
 template <class T, int SL, bool WHOLE, int ACT>
-__global__ void __launch_bounds__(SPLIT_NTH, SL == 1 ? 4 : 2) k_gn_bwd_apply(const GnArgs<T> a, uint32_t ranges, const float* __restrict__ cols,
+__global__ void __launch_bounds__(SPLIT_NTH, SL == 1 ? 3 : 2) k_gn_bwd_apply(const GnArgs<T> a, uint32_t ranges, const float* __restrict__ cols,
                                                             unsigned col_blocks) {
   constexpr int E = EPP<T>, U = BWD_TURN;
   extern __shared__ Pair sm[];

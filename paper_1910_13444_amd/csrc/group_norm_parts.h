@@ -247,10 +247,10 @@ __device__ __forceinline__ float slope_of(float a) {
     const float tail = normal_tail(a, g);
     return (a > 0.0f ? 1.0f - tail : tail) + __builtin_amdgcn_fmed3f(a, -64.0f, 64.0f) * 0.3989422804014327f * g;
   } else if constexpr (sizeof(T) == 2 && ACT == PIGAN_ACT_SILU) {
-    // below -60 the slope is less than 2^-80
-    const float b = __builtin_amdgcn_fmed3f(a, -60.0f, 200.0f);
+    // below -60 the slope is less than 2^-80; a NaN stays one
+    const float b = a < -60.0f ? -60.0f : a;
     const float e = __builtin_amdgcn_exp2f(b * -1.4426950408889634f), s = __builtin_amdgcn_rcpf(1.0f + e);
-    return s + b * s * (e * s);
+    return s + fminf(b, 200.0f) * (s * (e * s));
   } else {
     return act_slope<ACT, T>(a);
   }

@@ -286,6 +286,28 @@ def test_captured_steps_count_their_replays(bits):
         assert all(torch.equal(c, p.half()) for c, p in zip(cs, ps))
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_steps_beyond_the_caches(bits):
+    """A step that moves more than 192 MiB gives the bits of the same step in parts."""
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    parts, n = 8, 256 * 8001
+    ps, gs, cs = [], [], []
+    for _ in range(2):
+        ps.append(torch.empty(parts * n, dtype=torch.float32, device="cuda").normal_(0.0, 0.1, generator=gen.manual_seed(7)))
+        cs.append(torch.empty(parts * n, dtype=torch.bfloat16, device="cuda"))
+    g = torch.empty(parts * n, dtype=torch.float32, device="cuda")
+    whole = AdamW([ps[0]], [g], LR, B1, B2, EPS, 0.01, bits, [cs[0]])
+    split = [AdamW([p], [q], LR, B1, B2, EPS, 0.01, bits, [c]) for p, q, c in zip(ps[1].split(n), g.split(n), cs[1].split(n))]
+    for _ in range(2):
+        g.normal_(0.0, 1e-3, generator=gen)
+        whole.step()
+        for opt in split:
+            opt.step()
+        assert torch.equal(ps[0], ps[1]) and torch.equal(cs[0], cs[1])
+        for k in range(2):
+            assert torch.equal(whole.states()[k], torch.cat([opt.states()[k] for opt in split]))
+
+
 def test_another_stream():
     gen, ps, gs, cs, decay, _ = _case(6, [100000, 77])
     other = [p.clone() for p in ps]

@@ -5,7 +5,7 @@ import torch
 
 from paper_1910_13444_amd import pigan
 from _fields import ACTS, EPS, backward64, field, forward64
-from _layers import DT, EPS32, check, vector
+from _layers import DT, EPS32, check, sum_error, vector
 
 pytestmark = pytest.mark.gpu
 
@@ -14,7 +14,10 @@ SIZES = [(None, 1, 1, 8, 1), (None, 1, 1, 8, 8), (None, 3, 7, 24, 3), (2, 5, 64,
          (None, 1, 4097, 64, 4), (None, 3, 33, 30, 3), (None, 2, 5, 10, 10), (None, 1, 300, 1, 1), (3, 2, 1, 4096, 1),
          (None, 2, 3, 10002, 2), (None, 4, 2, 8200, 1), (None, 130, 1, 1024, 32), (None, 1, 30011, 8, 2),
          (None, 2, 257, 2048, 2), (2, 70, 1, 96, 12), (None, 9, 16, 40, 5), (None, 3, 1024, 64, 8), (4, 3, 100, 33, 11),
-         (None, 517, 3, 16, 4), (None, 2, 1, 20000, 1), (None, 2, 5000, 48, 1), (None, 2, 2048, 32, 32)]
+         (None, 517, 3, 16, 4), (None, 2, 1, 20000, 1), (None, 2, 5000, 48, 1), (None, 2, 2048, 32, 32),
+         (None, 70, 300, 64, 8), (None, 40, 200, 512, 8), (2, 130, 600, 64, 4), (None, 300, 130, 48, 16), (None, 20, 130, 40, 8),
+         (None, 300, 40, 120, 3), (3, 7, 19, 264, 3), (None, 5, 1000, 70, 7), (None, 700, 5, 37, 37), (None, 2, 30000, 20, 20),
+         (None, 1500, 9, 24, 2), (None, 2000, 1, 600, 4)]
 
 
 def _lead(G):
@@ -149,6 +152,22 @@ def test_infinities_and_nan_stay_in_their_group(size, at, bad):
         assert torch.equal(dgamma[others], want[1][others]) and torch.equal(dbeta[others], want[2][others])
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("act", ["tanh", "gelu", "silu"])
+def test_a_nan_reaches_the_gradients(act, dtype):
+    """A saved input that is NaN: its group's dx and its channel's sums, no others'."""
+    for size in ((None, 3, 20, 64, 8), (None, 2, 3000, 64, 8), (None, 30, 1, 64, 8)):
+        gen, shape, x, gamma, beta = _inputs(4, size, dtype)
+        dy = field(gen, shape, dtype, 0.1)
+        _, mean, rstd = pigan.group_norm(x, 8, gamma, beta, act)
+        x[1, 0, 9] = float("nan")
+        dx, dgamma, dbeta = pigan.group_norm_backward(dy, x, mean, rstd, gamma, beta, act)
+        bad = torch.isnan(dx.unflatten(-1, (8, 8)))
+        assert bad[1, :, 1].all() and int(bad.sum()) == shape[1] * 8
+        for t in (dgamma, dbeta):
+            assert torch.isnan(t[9]) and int(torch.isnan(t).sum()) == 1
+
+
 def test_memory_between_points_is_left():
     """Gaps between points, samples and groups of the outputs keep what they hold."""
     for dtype in ("bf16", "fp32"):
@@ -194,6 +213,38 @@ def test_samples_far_apart():
     a = pigan.group_norm_backward(near, near, *want[1:], gamma, beta, "gelu")
     b = pigan.group_norm_backward(x, x, *want[1:], gamma, beta, "gelu", dx=y)
     assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+@pytest.mark.parametrize("size", [(None, 200, 1024, 512, 8), (None, 6, 40000, 512, 16), (None, 120000, 1, 1024, 32),
+                                  (None, 30000, 4, 1024, 4)])
+def test_fields_beyond_the_caches(size):
+    """Fields of more than 192 MiB: some samples element by element, the parameters'
+    gradients against sums in 64 bits."""
+    _, S, P, C, n = size
+    gen = torch.Generator(device="cuda").manual_seed(8)
+
+    def normal(scale, shift=0.0):
+        return torch.empty((S, P, C), dtype=torch.bfloat16, device="cuda").normal_(shift, scale, generator=gen)
+
+    x, dy, add = normal(1.0, 0.5), normal(0.1), normal(0.1)
+    gamma, beta = (torch.randn(C, device="cuda", generator=gen, dtype=torch.float32) * 0.2 + k for k in (1, 0))
+    y, mean, rstd = pigan.group_norm(x, n, gamma, beta, "gelu")
+    _, mean0, _ = pigan.group_norm(x, n)
+    assert torch.equal(mean, mean0)
+    dx, dgamma, dbeta = pigan.group_norm_backward(dy, x, mean, rstd, gamma, beta, "none", add)
+    some = [0, 1, S // 2, S - 1]
+    _check_forward(x[some], n, gamma, beta, "gelu", "bf16", (y[some], mean[some], rstd[some]))
+    want = backward64(dy[some], x[some], mean[some], rstd[some], gamma, beta, "none", add[some])
+    check(dx[some], *want[0], "bf16", "dx")
+    sums = torch.zeros((4, C), dtype=torch.float64, device="cuda")
+    for part in range(0, S, max(1, 2 ** 24 // (P * C))):
+        k = slice(part, part + max(1, 2 ** 24 // (P * C)))
+        xh = ((x[k].double().unflatten(-1, (n, C // n)) - mean[k].double()[:, None, :, None]) * rstd[k].double()[:, None, :, None]).flatten(-2)
+        t = dy[k].double() * xh
+        sums += torch.stack([t.sum((0, 1)), t.square().sum((0, 1)), dy[k].double().sum((0, 1)), dy[k].double().square().sum((0, 1))])
+    for got, k, what in ((dgamma, 0, "dgamma"), (dbeta, 2, "dbeta")):
+        # xhat's two roundings of every term and the product's, and fp32 sums
+        check(got, sums[k].cpu(), (3 * EPS32 + sum_error(S * P, 1.0)) * (S * P) ** 0.5 * sums[k + 1].sqrt().cpu(), "fp32", what)
 
 
 def test_gradients_against_differences():
