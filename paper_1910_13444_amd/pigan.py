@@ -897,19 +897,24 @@ def group_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, r
 # many tensors at once: their gradients' norm and their AdamW step
 # ---------------------------------------------------------------------------
 
-def _flat(t: torch.Tensor, name: str, dtypes, device) -> int:
+def _flat(t: torch.Tensor, name: str, i: int, dtypes, device) -> int:
     """Pointer of a contiguous device tensor."""
-    if not t.is_cuda or (device is not None and t.device != device):
+    if t.dtype in dtypes and t.is_cuda and t.device == device and t.is_contiguous():
+        return t.data_ptr()
+    name = f"{name}[{i}]"
+    if not t.is_cuda or t.device != device:
         raise ValueError(f"{name} must be a device tensor, all of them on one device")
     if t.dtype not in dtypes:
         raise ValueError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return t.data_ptr()
+    raise ValueError(f"{name} must be contiguous")
 
 
 _F32 = (torch.float32,)
 _HALVES = (torch.bfloat16, torch.float16)
+
+
+def _leaf(t: torch.Tensor) -> torch.Tensor:
+    return t.detach() if t.requires_grad else t
 
 
 class TensorTable:
@@ -926,12 +931,12 @@ class TensorTable:
     a new table."""
 
     def __init__(self, grads, params=None, copies=None, decay=0.0, bits: int = 0):
-        self.grads = [g.detach() for g in grads]
+        self.grads = [_leaf(g) for g in grads]
         n = len(self.grads)
         if (bits == 0) != (params is None) or bits not in (0, 8, 32):
             raise ValueError("bits is 8 or 32 with params, 0 without")
-        self.params = None if params is None else [p.detach() for p in params]
-        self.copies = [None if c is None else c.detach() for c in copies] if copies is not None else [None] * n
+        self.params = None if params is None else [_leaf(p) for p in params]
+        self.copies = [None if c is None else _leaf(c) for c in copies] if copies is not None else [None] * n
         self.decay = [float(d) for d in decay] if isinstance(decay, (list, tuple)) else [float(decay)] * n
         self.bits = bits
         if not n:
@@ -943,13 +948,13 @@ class TensorTable:
         dev = self.device = self.grads[0].device
         rows = []
         for i, (g, c, d) in enumerate(zip(self.grads, self.copies, self.decay)):
-            pg, pp, pc = _flat(g, f"grads[{i}]", TORCH_DTYPES, dev), 0, 0
+            pg, pp, pc = _flat(g, "grads", i, TORCH_DTYPES, dev), 0, 0
             if self.params is not None:
-                pp = _flat(self.params[i], f"params[{i}]", _F32, dev)
+                pp = _flat(self.params[i], "params", i, _F32, dev)
                 if self.params[i].shape != g.shape:
                     raise ValueError(f"grads[{i}] has shape {tuple(g.shape)}, expected {tuple(self.params[i].shape)}")
             if c is not None:
-                pc = _flat(c, f"copies[{i}]", _HALVES, dev)
+                pc = _flat(c, "copies", i, _HALVES, dev)
                 if c.shape != g.shape:
                     raise ValueError(f"copies[{i}] has shape {tuple(c.shape)}, expected {tuple(g.shape)}")
             rows.append(TENSOR.pack(pp, pg, pc, g.numel(), d, TORCH_DTYPES[g.dtype], 0 if c is None else TORCH_DTYPES[c.dtype]))
