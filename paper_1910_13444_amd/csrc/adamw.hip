@@ -202,21 +202,29 @@ __global__ void __launch_bounds__(NTH) k_adamw32(const AdamwArgs a) {
   store_copy(t, i, valid, pf, a.stream);
 }
 
-// The code of size x among a largest of s: the nearest whole root of x top / s, top the
-// largest code's power; inv = top / s.  The fp32 root y is off by less than 6e-5 codes
-// (2e-7 of 255), so only within 2^-12 of a halfway point the whole powers of halves
-// decide, in fp64.
+// a b - c d, its sign exact: |a|, |c| are fp32 values and b, d whole numbers below 2^53
+__device__ __forceinline__ double difference(double a, double b, double c, double d) {
+#pragma clang fp contract(off)
+  const double p = a * b, q = c * d;
+  return (p - q) + (__builtin_fma(a, b, -p) - __builtin_fma(c, d, -q));
+}
+
+// The code of size x among a largest of s: the nearest whole number to top (x / s)^(1/2), or
+// 255 (x / s)^(1/4), an even one where two are as near (x = s / 4 is halfway between 63 and
+// 64, s / 16 between 127 and 128); inv = top^2 / s or top^4 / s.  The fp32 root y is off by
+// less than 6e-5 codes (2e-7 of 255), so only within 2^-12 of a halfway point n + 1/2 the
+// whole powers decide, x (2 top)^2 against s (2 n + 1)^2.
 template <bool FOURTH>
-__device__ __forceinline__ int code_of(float x, double inv) {
-  const double r = (double)x * inv;
-  float y = __builtin_amdgcn_sqrtf((float)r);
+__device__ __forceinline__ int code_of(float x, float s, double inv) {
+  float y = __builtin_amdgcn_sqrtf((float)((double)x * inv));
   if constexpr (FOURTH) y = __builtin_amdgcn_sqrtf(y);
   const float c = rintf(y);
   int q = (int)c;
   if (fabsf(y - c) > 0.5f - 0x1p-12f) {
-    double lo = q - 0.5, hi = q + 0.5;
-    if constexpr (FOURTH) { lo *= lo; hi *= hi; }
-    q += (r > hi * hi) - (q > 0 && r < lo * lo);
+    const int n = (int)floorf(y);
+    const double h = 2 * n + 1, h2 = h * h;
+    const double d = FOURTH ? difference(x, 16.0 * TOP_V, s, h2 * h2) : difference(x, 4.0 * TOP_M, s, h2);
+    q = d > 0.0 || (d == 0.0 && (n & 1)) ? n + 1 : n;
   }
   return q;
 }
@@ -259,7 +267,7 @@ __global__ void __launch_bounds__(NTH) k_adamw8(const AdamwArgs a) {
   if (all) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int q = min(code_of<false>(fabsf(mf[e]), mi), 127), u = min(code_of<true>(vf[e], vi), 255);
+      const int q = min(code_of<false>(fabsf(mf[e]), mmax, mi), 127), u = min(code_of<true>(vf[e], vmax, vi), 255);
       mo |= (uint32_t)(uint8_t)(mf[e] < 0.0f ? -q : q) << (8 * e);
       vo |= (uint32_t)(vf[e] > 0.0f ? max(u, 1) : 0) << (8 * e);
     }

@@ -236,6 +236,22 @@ def test_zero_gradients_and_range_of_the_codes():
     assert ((p - before).abs() <= 4.4 * LR).all()
 
 
+def test_halfway_codes_are_even():
+    """m = s / 4 lies halfway between the codes 63 and 64, v = s / 16 between 127 and 128."""
+    n = 4000
+    gen = torch.Generator().manual_seed(9)
+    tops = torch.randn(n, generator=gen, dtype=torch.float32) * torch.exp2(torch.randint(-20, 4, (n,), generator=gen).float())
+    g = (tops[:, None] * torch.full((256,), 2.0 ** -6)).contiguous()
+    g[:, 0], g[:, 1], g[:, 200] = tops, tops / 4, -tops / 4
+    g = g.view(-1).cuda()
+    opt = AdamW([torch.zeros_like(g)], [g], LR, B1, B2, EPS, state_bits=8)
+    opt.step()
+    m, v = (t.view(n, 256).cpu().int() for t in (opt.m, opt.v))
+    sign = tops.sign().int()
+    assert torch.equal(m[:, 0], 127 * sign) and torch.equal(m[:, 1], 64 * sign) and torch.equal(m[:, 200], -64 * sign)
+    assert (v[:, 0] == 255).all() and (v[:, 1] == 128).all() and (v[:, 200] == 128).all()
+
+
 def test_gradients_that_are_not_finite():
     for bad in (float("nan"), float("inf"), -float("inf")):
         p = torch.zeros(1024, device="cuda")
