@@ -178,6 +178,9 @@ __device__ __forceinline__ void update(const AdamwArgs& a, const Coefs& k, float
   p = (float)(k.keep * (double)p - k.by * (double)mn * q);
 }
 
+// Four elements a thread, one turn a block, in order: as a copy, which is fastest that way
+// (1 GiB: 6.2 TB/s, blocks of four turns 4.9).  Bound by memory: 33.6 M parameters with bf16
+// copies 174 us (5.8 TB/s; in blocks of 4096 elements 190).
 __global__ void __launch_bounds__(NTH) k_adamw32(const AdamwArgs a) {
   if (a.skip && *a.skip) return;   // one flag for the whole launch
   const TensorPiece w = a.pieces[blockIdx.x];
@@ -229,7 +232,10 @@ __device__ __forceinline__ int code_of(float x, float s, double inv) {
   return q;
 }
 
-// a wave takes a block of states at a time, four elements a lane
+// A wave takes a block of states at a time, four elements a lane.  Memory and the vector units
+// (a hundred instructions an element, most in fp64) take the same time: 21.2 M parameters with
+// bf16 copies 72 us (5.3 TB/s); with library roots and quotients and every code's borders in
+// fp64 131 us.
 __global__ void __launch_bounds__(NTH) k_adamw8(const AdamwArgs a) {
   if (a.skip && *a.skip) return;
   const TensorPiece w = a.pieces[blockIdx.x];
@@ -293,7 +299,8 @@ __global__ void k_adamw_begin(double b1, double b2, int32_t* step, const int32_t
 }
 
 // ---------------------------------------------------------------------------
-// The gradients' norm: a sum of squares per block in fp64, joined in a fixed order.
+// The gradients' norm: a sum of squares per block in fp64, joined in a fixed order.  Bound by
+// memory: 33.6 M fp32 24 us (5.6 TB/s) and 4 us for the join, a launch of one block.
 // ---------------------------------------------------------------------------
 __global__ void __launch_bounds__(NTH) k_grad_squares(const TensorEntry* __restrict__ entries,
                                                       const TensorPiece* __restrict__ pieces, int64_t n_pieces,
@@ -341,6 +348,7 @@ __global__ void __launch_bounds__(1024) k_grad_norm(const double* __restrict__ p
   }
 }
 
+// Bound by memory: 21.2 M values of m and v 38 us (5.6 TB/s).
 __global__ void __launch_bounds__(NTH) k_state_values(int64_t n, const int8_t* __restrict__ m, const float* __restrict__ m_scale,
                                                       const uint8_t* __restrict__ v, const float* __restrict__ v_scale,
                                                       float* __restrict__ m_out, float* __restrict__ v_out, bool stream) {

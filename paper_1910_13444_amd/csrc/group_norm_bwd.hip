@@ -40,9 +40,10 @@ __device__ __forceinline__ void slope_piece(const Column<T, SL>& c, int valid, f
 }
 
 // ---------------------------------------------------------------------------
-// Backward, rows and samples whose slabs fit a block's registers.  Blocks walk samples; a
-// thread keeps its columns' sums of da xhat and da over all of them, a block writes one
-// partial row of [dgamma, dbeta] (the final ones, where one block takes all samples).
+// Backward, rows and short samples.  Blocks walk samples; a thread keeps its columns' sums
+// of da xhat and da over all of them, a block writes one partial row of [dgamma, dbeta] (the
+// final ones, where one block takes all samples).  Rows as forward: 47,020 x 176 bf16, 22
+// groups, tanh, 16 us and 5 for the sum of the blocks' rows.
 // ---------------------------------------------------------------------------
 // bytes of LDS that a group's sums, or half the columns' sums, take
 constexpr size_t bwd_sums_lds(int nth, int sl, int e) {
@@ -160,7 +161,10 @@ __global__ void __launch_bounds__(256) k_gn_rows_bwd(const GnArgs<T> a) {
 }
 
 // Short samples: a thread has one point's piece of a batch of samples, and the next batch's on
-// its way.
+// its way; xhat and da stay in registers from the sums to dx.  Bound by the two barriers of a
+// batch at four blocks to a CU (two where pieces are of several groups): 30,078 x 9 x 144 fp16,
+// two groups, gelu, 112 us (2.1 TB/s).  With more pieces a thread the compiler spills (128 x
+// 1024 x 256 bf16: 217 us where two passes take 76).
 template <class T, int SL, bool WHOLE, int ACT>
 __global__ void __launch_bounds__(ONE_NTH) k_gn_one_bwd(const GnArgs<T> a) {
   constexpr int E = EPP<T>;
@@ -242,7 +246,10 @@ __global__ void __launch_bounds__(ONE_NTH) k_gn_one_bwd(const GnArgs<T> a) {
 // ---------------------------------------------------------------------------
 // Longer samples, backward: a channel's sums of da and da xhat over ranges of points give
 // dgamma and dbeta (summed over samples) and, with gamma, a group's sums of h and
-// h xhat; then dx.
+// h xhat; then dx, whose blocks join the ranges' sums themselves (a launch between cost 5 us)
+// while others sum the columns (9 us).  128 x 1024 x 256 bf16, silu, with `add`: sums 32 us
+// (4.2 TB/s), dx 45 us (5.9 TB/s); 4 x 21 x 1000 x 120 fp32, groups of five, tanh in fp64:
+// 20 + 25 us, vector units 75 % busy.
 // ---------------------------------------------------------------------------
 // ws: Pair [G][S][n][chan_parts * splits], a group's sums of h and h xhat, and behind them
 // float [G][slots][2][C], a block's sums of da xhat and da over all of its ranges.
