@@ -155,7 +155,7 @@ def test_calls_that_are_refused():
 
 @needs_lib
 def test_binding_refuses():
-    z = torch.zeros(8)
+    z = torch.zeros(8, dtype=torch.float32)
     with pytest.raises(ValueError, match="device tensor"):
         pigan.TensorTable([z])
     with pytest.raises(ValueError, match="bits"):

@@ -28,7 +28,7 @@ def _case(seed, counts, gdt=("fp32",), copy=(None,), gap=1):
     gen = torch.Generator().manual_seed(seed)
     sizes, total = counts, sum(counts) + gap * (len(counts) + 1)
     flat = {k: torch.full((total,), 7.0, dtype=DT[k]).cuda() for k in ("fp32", "bf16", "fp16")}
-    masters = torch.full((total,), 7.0).cuda()
+    masters = torch.full((total,), 7.0, dtype=torch.float32).cuda()
     lows = {k: torch.full((total,), 7.0, dtype=DT[k]).cuda() for k in ("bf16", "fp16")}
     ps, gs, cs, at = [], [], [], gap
     for i, n in enumerate(sizes):
@@ -153,7 +153,7 @@ def test_clipped_steps():
             norm, coef, flag = opt.grad_norm(most, 0.25)
             want = 0.25 * torch.cat([g.double().cpu() for g in gs]).norm()
             check(norm, want, 1e-14 * want, "fp32", "norm")
-            check(coef, 0.25 * (most / want if want > most else torch.ones_like(want)), torch.tensor(1e-15), "fp32", "coef")
+            check(coef, 0.25 * (most / want if want > most else torch.ones_like(want)), torch.tensor(1e-15, dtype=torch.float64), "fp32", "coef")
             assert flag.item() == 0 and norm.shape == coef.shape == flag.shape == ()
             opt.step(coef, flag)
             _check_step(opt, ps, cs, oracle, oracle.step(gs, t, decay, coef.item()))
@@ -193,7 +193,7 @@ def test_sizes_beyond_fp32_squares():
         norm, coef, flag = pigan.grad_norm(pigan.TensorTable([g]), 1e-30)
         want = g.double().cpu().norm()
         assert flag.item() == 0
-        check(coef, (1e-30 / want).clamp(max=1), torch.tensor(1e-60), "fp32", "coef")
+        check(coef, (1e-30 / want).clamp(max=1), torch.tensor(1e-60, dtype=torch.float64), "fp32", "coef")
         check(norm, want, 1e-13 * want, "fp32", "norm") if want < 3e38 else None
 
 
@@ -215,8 +215,8 @@ def test_a_skipped_step_changes_nothing():
 
 
 def test_zero_gradients_and_range_of_the_codes():
-    p = torch.ones(600, device="cuda")
-    g = torch.zeros(600, device="cuda")
+    p = torch.ones(600, dtype=torch.float32, device="cuda")
+    g = torch.zeros(600, dtype=torch.float32, device="cuda")
     opt = AdamW([p], [g], LR, B1, B2, EPS, 0.1, state_bits=8)
     opt.step()
     assert torch.equal(p, torch.full_like(p, 1 - LR * 0.1))
@@ -225,7 +225,7 @@ def test_zero_gradients_and_range_of_the_codes():
     # (half a code, squared, is taken for one) and at least (1 / 1.5)^4 of v.  So in the
     # second step m <= B1 4 (0.5 g) = g, over 1 - B1^2, and v >= B2 0.197 (0.1 g^2), over
     # 1 - B2^2: a step of at most 1.34 / 0.305 lr, where a v of 0 would give m / eps.
-    g.copy_(torch.logspace(-12, 0, 600))
+    g.copy_(torch.logspace(-12, 0, 600, dtype=torch.float32))
     p.zero_()
     opt = AdamW([p], [g], LR, B1, B2, EPS, state_bits=8)
     opt.step()
@@ -240,8 +240,8 @@ def test_halfway_codes_are_even():
     """m = s / 4 lies halfway between the codes 63 and 64, v = s / 16 between 127 and 128."""
     n = 4000
     gen = torch.Generator().manual_seed(9)
-    tops = torch.randn(n, generator=gen, dtype=torch.float32) * torch.exp2(torch.randint(-20, 4, (n,), generator=gen).float())
-    g = (tops[:, None] * torch.full((256,), 2.0 ** -6)).contiguous()
+    tops = torch.randn(n, generator=gen, dtype=torch.float32) * torch.exp2(torch.randint(-20, 4, (n,), generator=gen).to(torch.float32))
+    g = (tops[:, None] * torch.full((256,), 2.0 ** -6, dtype=torch.float32)).contiguous()
     g[:, 0], g[:, 1], g[:, 200] = tops, tops / 4, -tops / 4
     g = g.view(-1).cuda()
     opt = AdamW([torch.zeros_like(g)], [g], LR, B1, B2, EPS, state_bits=8)
@@ -254,8 +254,8 @@ def test_halfway_codes_are_even():
 
 def test_gradients_that_are_not_finite():
     for bad in (float("nan"), float("inf"), -float("inf")):
-        p = torch.zeros(1024, device="cuda")
-        g = torch.full((1024,), 0.5, device="cuda")
+        p = torch.zeros(1024, dtype=torch.float32, device="cuda")
+        g = torch.full((1024,), 0.5, dtype=torch.float32, device="cuda")
         want = p.clone()
         opt8, opt32 = (AdamW([t], [g], LR, state_bits=b) for t, b in ((p, 8), (want, 32)))
         g[300] = bad
@@ -339,7 +339,7 @@ def test_another_stream():
 
 
 def test_refusals():
-    p, g = torch.zeros(8, device="cuda"), torch.zeros(8, device="cuda")
+    p, g = (torch.zeros(8, dtype=torch.float32, device="cuda") for _ in range(2))
     for bad in (dict(params=[p], grads=[]), dict(params=[p], grads=[g, g]), dict(params=[p.half()], grads=[g]),
                 dict(params=[p], grads=[g.double()]), dict(params=[p], grads=[g[:4]]), dict(params=[p[::2]], grads=[g[:4]]),
                 dict(params=[p], grads=[g.cpu()]), dict(params=[p], grads=[g], copies=[p]), dict(params=[], grads=[]),

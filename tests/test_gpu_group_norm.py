@@ -114,7 +114,7 @@ def test_means_far_from_zero():
     gen = torch.Generator().manual_seed(1)
     for P in (50, 20000):
         x = (torch.randn((2, P, 32), generator=gen, dtype=torch.float64) + 1e4).float().cuda()
-        ones, zeros = torch.ones(32).cuda(), torch.zeros(32).cuda()
+        ones, zeros = (torch.full((32,), v, dtype=torch.float32).cuda() for v in (1.0, 0.0))
         _check_forward(x, 4, ones, zeros, "none", "fp32", pigan.group_norm(x, 4, ones, zeros))
         first = x.clone()
         first[:, 0, ::8] = -3e6   # the group's first value, which the sums are taken from
@@ -189,10 +189,10 @@ def test_memory_between_points_is_left():
 
 def test_no_samples():
     x = torch.zeros((0, 5, 16), dtype=torch.bfloat16, device="cuda")
-    gamma = torch.ones(16, device="cuda")
+    gamma = torch.ones(16, dtype=torch.float32, device="cuda")
     y, mean, rstd = pigan.group_norm(x, 4, gamma)
     assert y.shape == x.shape and mean.shape == (0, 4)
-    dg, db = torch.full((16,), 3.0, device="cuda"), torch.full((16,), 3.0, device="cuda")
+    dg, db = (torch.full((16,), 3.0, dtype=torch.float32, device="cuda") for _ in range(2))
     pigan.group_norm_backward(x, x, mean, rstd, gamma, dgamma=dg, dbeta=db)
     assert not dg.any() and not db.any()
 
@@ -300,8 +300,8 @@ def test_repeats_streams_and_graphs():
 
 def test_refusals():
     x = torch.zeros((2, 8, 16), dtype=torch.bfloat16, device="cuda")
-    stats = torch.zeros((2, 4), device="cuda")
-    vec = torch.ones(16, device="cuda")
+    stats = torch.zeros((2, 4), dtype=torch.float32, device="cuda")
+    vec = torch.ones(16, dtype=torch.float32, device="cuda")
     for bad in (lambda: pigan.group_norm(x, 3), lambda: pigan.group_norm(x, 0), lambda: pigan.group_norm(x[0], 4),
                 lambda: pigan.group_norm(x.double(), 4), lambda: pigan.group_norm(x, 4, vec[:8]),
                 lambda: pigan.group_norm(x, 4, vec.bfloat16()), lambda: pigan.group_norm(x, 4, act="sine"),
