@@ -41,9 +41,8 @@ struct GnPlan {
 // Threads and pieces of a thread of the one-pass kernels, by what they hold.
 struct Shape { int nth, nv; };
 constexpr Shape FWD_SHAPES[] = {{256, 1}, {256, 4}, {1024, 2}, {256, 8}, {512, 8}, {1024, 8}};
-constexpr Shape FWD_ODD[] = {{256, 1}, {256, 4}, {256, 8}};   // channel groups that are no whole pieces
-constexpr Shape BWD_SHAPES[] = {{256, 1}};   // short samples
-constexpr int ONE_NTH = 256;     // threads of its blocks
+constexpr Shape FWD_ODD[] = {{256, 1}, {512, 1}, {256, 4}, {256, 8}};   // channel groups that are no whole pieces
+constexpr Shape BWD_SHAPES[] = {{256, 1}, {512, 1}};
 constexpr int SPLIT_NTH = 256;   // threads of a block that takes a range of points
 
 struct Pair { double s, q; };    // of two sums

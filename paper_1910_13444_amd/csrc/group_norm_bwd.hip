@@ -165,13 +165,13 @@ __global__ void __launch_bounds__(256) k_gn_rows_bwd(const GnArgs<T> a) {
 // batch at four blocks to a CU (two where pieces are of several groups): 30,078 x 9 x 144 fp16,
 // two groups, gelu, 112 us (2.1 TB/s).  With more pieces a thread the compiler spills (128 x
 // 1024 x 256 bf16: 217 us where two passes take 76).
-template <class T, int SL, bool WHOLE, int ACT>
-__global__ void __launch_bounds__(ONE_NTH) k_gn_one_bwd(const GnArgs<T> a) {
+template <class T, int NTH, int SL, bool WHOLE, int ACT>
+__global__ void __launch_bounds__(NTH) k_gn_one_bwd(const GnArgs<T> a) {
   constexpr int E = EPP<T>;
   extern __shared__ Pair sm[];
   const GnPlan& pl = a.pl;
   PairF* hs = (PairF*)sm;
-  float2* means = (float2*)((char*)sm + bwd_sums_lds(ONE_NTH, SL, E));
+  float2* means = (float2*)((char*)sm + bwd_sums_lds(NTH, SL, E));
   const int row = Div(pl.pw)(threadIdx.x), col = threadIdx.x - row * pl.pw, per = row_of(pl.pw * SL);
   const int si = pl.ns > 1 ? Div((int)a.P)(row) : 0, p = row - si * (int)a.P;
   const Div by_span(pl.span);
@@ -473,8 +473,12 @@ template <class T> hipError_t launch_gn_bwd(const GnArgs<T>& a, int G, hipStream
     } else if (pl.mode == GN_ONE) {
       const dim3 grid((unsigned)pl.slots, (unsigned)std::min<int64_t>(pl.slabs, 65535), G);
       by_width(a, [&](auto sl, auto whole) {
-        const size_t lds = bwd_sums_lds(ONE_NTH, sl.value, EPP<T>) + (size_t)pl.ns * pl.ng * sizeof(float2);
-        k_gn_one_bwd<T, sl.value, whole.value, ACT><<<grid, ONE_NTH, lds, st>>>(a);
+        auto launch = [&](auto nth) {
+          const size_t lds = bwd_sums_lds(nth.value, sl.value, EPP<T>) + (size_t)pl.ns * pl.ng * sizeof(float2);
+          k_gn_one_bwd<T, nth.value, sl.value, whole.value, ACT><<<grid, nth.value, lds, st>>>(a);
+        };
+        if (pl.nth == 512) launch(std::integral_constant<int, 512>{});
+        else launch(std::integral_constant<int, 256>{});
       });
     } else {
       const int64_t ranges = a.S * pl.splits;

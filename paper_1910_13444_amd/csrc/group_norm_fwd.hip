@@ -70,12 +70,21 @@ __global__ void __launch_bounds__(256) k_gn_rows(const GnArgs<T> a) {
 // all write, with the vector units busy for three quarters of it: 256 x 1024 x 128 bf16,
 // silu, 32 us (4.2 TB/s; 512 threads on 64 bytes of a point 37 us, two passes 42).
 // ---------------------------------------------------------------------------
+// Whether a block's values lie in LDS for the sums, 4 bytes each: where a thread has one piece
+// of several groups, whose sums would be 16 bytes an element.  Else bytes of the sums.
+constexpr bool one_values(int nv, int sl) { return nv == 1 && sl > 1; }
+constexpr size_t one_lds(int nth, int nv, int sl) {
+  return one_values(nv, sl) ? (size_t)nth * (sl + 1) * 4 : (size_t)nth * (sl + 1) * sizeof(Pair);
+}
+
 template <class T, int NTH, int NV, int SL, bool WHOLE, int ACT>
 __global__ void __launch_bounds__(NTH, NV < 8 ? 1 : SL == 1 && WHOLE ? 4 : 3) k_gn_one(const GnArgs<T> a, int64_t batches) {
   constexpr int E = EPP<T>;
+  constexpr bool VALUES = one_values(NV, SL);
   extern __shared__ Pair sm[];
   const GnPlan& pl = a.pl;
-  Stat* stat = (Stat*)(sm + NTH * (SL + 1));
+  float* values = (float*)sm;
+  Stat* stat = (Stat*)((char*)sm + one_lds(NTH, NV, SL));
   float* shift = (float*)(stat + pl.ns * pl.ng);
   const int row = Div(pl.pw)(threadIdx.x), col = threadIdx.x - row * pl.pw;
   const bool many = NV == 1 && pl.ns > 1;
@@ -84,7 +93,7 @@ __global__ void __launch_bounds__(NTH, NV < 8 ? 1 : SL == 1 && WHOLE ? 4 : 3) k_
   const int per = row_of(pl.pw * SL);
   const int64_t g = blockIdx.z;
   const Slab b = slab_at(a, blockIdx.x);
-  const int valid = b.width - col * E, left = (int)min(a.P, (int64_t)INT32_MAX) - pr;
+  const int valid = b.width - col * E, left = (int)a.P - pr;
   for (int64_t bt = blockIdx.y; bt < batches; bt += gridDim.y) {
     const int64_t s0 = bt * pl.ns, s = s0 + si;
     const bool on = row < pl.rows && left > 0 && s < a.S && valid > 0;
@@ -92,46 +101,78 @@ __global__ void __launch_bounds__(NTH, NV < 8 ? 1 : SL == 1 && WHOLE ? 4 : 3) k_
     piece_t raw[NV];
     load_rows<WHOLE>(raw, on ? first + b.c0 + col * E + pr * a.x.ld : first + b.c0, pl.rows * a.x.ld, on ? left : 1, pl.rows,
                      on ? valid : b.width);
-    float k[SL];
-    Pair acc[SL];
-#pragma unroll
-    for (int e = 0; e < SL; ++e) {
-      k[e] = shift_of(Elem<T>::to_f(first[(b.j0 + group_of<T, SL>(b, by_span, col, e)) * pl.cg]));
-      acc[e] = {0.0, 0.0};
-    }
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      if (on && v * pl.rows < left) {
-        float f[E];
-        piece_floats<T>(raw[v], f);
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const double d = (double)f[e] - k[SL > 1 ? e : 0];
-          if (WHOLE || e < valid) {
-            acc[SL > 1 ? e : 0].s += d;
-            acc[SL > 1 ? e : 0].q += d * d;
-          }
-        }
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    if (row < pl.rows)
-#pragma unroll
-      for (int e = 0; e < SL; ++e) {
-        const int slot = col * SL + e, j = by_span(slot);
-        sm[row * per + slot] = acc[e];
-        if (on && pr == 0 && j < b.ng && slot == j * pl.span) shift[si * b.ng + j] = k[e];
-      }
-    __syncthreads();
-    group_sums(sm, pl.ns, pl.ns > 1 ? (int)a.P : pl.rows, per, b.ng, pl.span, pl.lanes, [&](int i, int j, const Pair& t) {
-      const Stat st = stat_of(t, shift[i * b.ng + j], pl.inv_n, a.eps);
+    auto tell = [&](int i, int j, const Pair& t, float k) {
+      const Stat st = stat_of(t, k, pl.inv_n, a.eps);
       stat[i * b.ng + j] = st;
       const int64_t at = (g * a.S + s0 + i) * a.n + b.j0 + j;
       if (s0 + i < a.S) {
         if (a.mean) a.mean[at] = st.mean;
         if (a.rstd) a.rstd[at] = st.rstd;
       }
-    });
+    };
+    if constexpr (VALUES) {
+      // one piece of several groups: the values themselves, which the groups' lanes sum
+      if (on) {
+        float f[E];
+        piece_floats<T>(raw[0], f);
+#pragma unroll
+        for (int e = 0; e < E; ++e) values[row * per + col * E + e] = f[e];
+      }
+      __syncthreads();
+      const int rows = min((int)a.P, pl.rows);
+      const Div by_ng(b.ng);
+      auto at = [&](int k) { return values + (pl.ns > 1 ? by_ng(k) : 0) * rows * per + (pl.ns > 1 ? k - by_ng(k) * b.ng : k) * pl.span; };
+      lane_sums(pl.ns * b.ng, pl.lanes, [&](int k, int l) {
+        const float* v = at(k);
+        const double base = shift_of(v[0]);
+        Pair t = {0.0, 0.0};
+#pragma unroll 4
+        for (int q = l; q < rows * pl.span; q += pl.lanes) {
+          const int r = by_span(q);
+          const double d = v[r * per + (q - r * pl.span)] - base;
+          t.s += d;
+          t.q += d * d;
+        }
+        return t;
+      }, [&](int k, const Pair& t) {
+        const int i = pl.ns > 1 ? by_ng(k) : 0;
+        tell(i, k - i * b.ng, t, shift_of(at(k)[0]));
+      });
+    } else {
+      float k[SL];
+      Pair acc[SL];
+#pragma unroll
+      for (int e = 0; e < SL; ++e) {
+        k[e] = shift_of(Elem<T>::to_f(first[(b.j0 + group_of<T, SL>(b, by_span, col, e)) * pl.cg]));
+        acc[e] = {0.0, 0.0};
+      }
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        if (on && v * pl.rows < left) {
+          float f[E];
+          piece_floats<T>(raw[v], f);
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const double d = (double)f[e] - k[SL > 1 ? e : 0];
+            if (WHOLE || e < valid) {
+              acc[SL > 1 ? e : 0].s += d;
+              acc[SL > 1 ? e : 0].q += d * d;
+            }
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (row < pl.rows)
+#pragma unroll
+        for (int e = 0; e < SL; ++e) {
+          const int slot = col * SL + e, j = by_span(slot);
+          sm[row * per + slot] = acc[e];
+          if (on && pr == 0 && j < b.ng && slot == j * pl.span) shift[si * b.ng + j] = k[e];
+        }
+      __syncthreads();
+      group_sums(sm, pl.ns, pl.ns > 1 ? (int)a.P : pl.rows, per, b.ng, pl.span, pl.lanes,
+                 [&](int i, int j, const Pair& t) { tell(i, j, t, shift[i * b.ng + j]); });
+    }
     __syncthreads();
     if (!on) continue;
     float mean[SL], sc[E], be[E];
@@ -318,7 +359,7 @@ template <class T> hipError_t launch_gn_fwd(const GnArgs<T>& a, int G, hipStream
       const dim3 grid((unsigned)pl.slabs, (unsigned)std::min<int64_t>(batches, 65535), G);
       by_width(a, [&](auto sl, auto whole) {
         by_shape<sl.value == 1 && whole.value>(pl, [&](auto nth, auto nv) {
-          const size_t lds = nth.value * (sl.value + 1) * sizeof(Pair) + (size_t)pl.ns * pl.ng * (sizeof(Stat) + 4);
+          const size_t lds = one_lds(nth.value, nv.value, sl.value) + (size_t)pl.ns * pl.ng * (sizeof(Stat) + 4);
           k_gn_one<T, nth.value, nv.value, sl.value, whole.value, ACT><<<grid, nth.value, lds, st>>>(a, batches);
         });
       });

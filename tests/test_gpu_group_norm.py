@@ -17,7 +17,8 @@ SIZES = [(None, 1, 1, 8, 1), (None, 1, 1, 8, 8), (None, 3, 7, 24, 3), (2, 5, 64,
          (None, 517, 3, 16, 4), (None, 2, 1, 20000, 1), (None, 2, 5000, 48, 1), (None, 2, 2048, 32, 32),
          (None, 70, 300, 64, 8), (None, 40, 200, 512, 8), (2, 130, 600, 64, 4), (None, 300, 130, 48, 16), (None, 20, 130, 40, 8),
          (None, 300, 40, 120, 3), (3, 7, 19, 264, 3), (None, 5, 1000, 70, 7), (None, 700, 5, 37, 37), (None, 2, 30000, 20, 20),
-         (None, 1500, 9, 24, 2), (None, 2000, 1, 600, 4)]
+         (None, 1500, 9, 24, 2), (None, 2000, 1, 600, 4),
+         (None, 500, 66, 32, 1), (None, 300, 90, 19, 19), (2, 130, 24, 156, 13), (None, 200, 33, 52, 4)]
 
 
 def _lead(G):
