@@ -639,6 +639,14 @@ def _result_vec(need: bool, t: torch.Tensor | None, name: str, like: torch.Tenso
     return _new_vec(shape, like) if t is None else (t, _vec(t, name, like, shape))
 
 
+def _second_vec(need: bool, t: torch.Tensor | None, name: str, like: torch.Tensor, shape, first: torch.Tensor | None):
+    """_result_vec beside a first one of its shape, which a new one is made like (the shorter call)"""
+    if not need or t is not None:
+        return _result_vec(need, t, name, like, shape)
+    t = torch.empty_like(first)
+    return t, t.data_ptr()
+
+
 def _act(act: str) -> int:
     if act not in ACTS:
         raise ValueError(f"unknown activation {act!r}: one of {', '.join(ACTS)}")
@@ -855,11 +863,7 @@ def group_norm(x: torch.Tensor, n: int, gamma: torch.Tensor | None = None, beta:
     mx = _field(x, "x", x, shape)
     out, mo = _new_field(True, out, "out", x, shape)
     mean, pm = _result_vec(need_stats, mean, "mean", x, stats)
-    if need_stats and rstd is None:
-        rstd = torch.empty_like(mean)
-        pr = rstd.data_ptr()
-    else:
-        rstd, pr = _result_vec(need_stats, rstd, "rstd", x, stats)
+    rstd, pr = _second_vec(need_stats, rstd, "rstd", x, stats, mean)
     args = GROUP_NORM_ARGS.pack(G, dt, _act(act), eps, S, P, C_, n, *mx, *mo, *_NO_FIELD, *_NO_FIELD, *_NO_FIELD,
                                 0 if gamma is None else _vec(gamma, "gamma", x, chans),
                                 0 if beta is None else _vec(beta, "beta", x, chans), pm, pr, 0, 0)
@@ -883,7 +887,7 @@ def group_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, r
     chans, stats = (*lead, C_), (*lead, S, n)
     dx, mdx = _new_field(need_dx, dx, "dx", dy, shape)
     dgamma, pg = _result_vec(need_params, dgamma, "dgamma", dy, chans)
-    dbeta, pb = _result_vec(need_params, dbeta, "dbeta", dy, chans)
+    dbeta, pb = _second_vec(need_params, dbeta, "dbeta", dy, chans, dgamma)
     args = GROUP_NORM_ARGS.pack(G, dt, _act(act), 0.0, S, P, C_, n, *_field(x, "x", dy, shape), *_NO_FIELD,
                                 *_field(dy, "dy", dy, shape), *(_NO_FIELD if add is None else _field(add, "add", dy, shape)),
                                 *mdx, 0 if gamma is None else _vec(gamma, "gamma", dy, chans),
@@ -984,6 +988,8 @@ class TensorTable:
         self._device = torch.frombuffer(self._host, dtype=torch.uint8).to(dev)
         self.host_ptr, self.device_ptr = C.addressof(self._host), self._device.data_ptr()
         self._norm_ws = int(L.pigan_grad_norm_workspace(self.host_ptr))
+        # results of grad_norm are made like these
+        self._value, self._flag = (torch.empty((), dtype=k, device=dev) for k in (torch.float32, torch.int32))
 
 
 def grad_norm(table: TensorTable, max_norm: float = float("inf"), scale: float = 1.0, ws: torch.Tensor | None = None):
@@ -996,10 +1002,9 @@ def grad_norm(table: TensorTable, max_norm: float = float("inf"), scale: float =
     if dev.index != torch.cuda.current_device():
         with torch.cuda.device(dev):
             return grad_norm(table, max_norm, scale, ws)
-    norm = torch.empty((), dtype=torch.float32, device=dev)
-    coef, flag = torch.empty_like(norm), torch.empty_like(norm, dtype=torch.int32)
+    norm, coef, flag = torch.empty_like(table._value), torch.empty_like(table._value), torch.empty_like(table._flag)
     if ws is None or ws.numel() < table._norm_ws:
-        ws = torch.empty(table._norm_ws, dtype=torch.uint8, device=dev)
+        ws = table._device.new_empty(table._norm_ws)
     elif ws.dtype != torch.uint8 or ws.device != dev or not ws.is_contiguous():
         raise ValueError(f"ws must be a contiguous torch.uint8 tensor on {dev}")
     st = L.pigan_grad_norm(table.host_ptr, table.device_ptr, max_norm, scale, norm.data_ptr(), coef.data_ptr(), flag.data_ptr(),
