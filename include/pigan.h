@@ -633,8 +633,9 @@ pigan_status pigan_layer_norm_backward(const pigan_norm* a, void* ws, size_t ws_
  * variance per sample, over its channels and all points (P = 1: of rows; n = 1 and
  * P = 1: layer norm).
  *
- * Overlaps of outputs, errors and numbers as for the layers above (sums here are
- * held in fp64; a constant channel group normalises to beta).  No samples (S = 0)
+ * Overlaps of outputs, errors and numbers as for the layers above (statistics are
+ * summed in fp64, a constant channel group normalises to beta; the reverse pass sums
+ * in fp32 within a thread and joins in fp64, in a fixed order).  No samples (S = 0)
  * is valid: nothing but zero parameter gradients is written.  No points is EINVAL.
  */
 typedef struct {
