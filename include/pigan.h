@@ -752,7 +752,8 @@ pigan_status pigan_grad_norm(const void* table, const void* device_table, double
  * pigan_adamw_update — with g' = scale coef g,
  *   m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2,
  *   p = p - lr ((m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps) + decay p)
- * of every tensor, and its copy.
+ * of every tensor, and its copy.  The quotient is that of the stored m and v: 0 where v
+ * has passed fp32 (an infinity) beside a finite m, NaN beside an infinite one.
  *   t     : count of updates including this one, where step is NULL;
  *   step  : device int32 or NULL: the count of updates so far.  The call adds one and
  *           uses it as t, on the device, so that a captured call counts its replays;

@@ -170,11 +170,15 @@ __device__ __forceinline__ void update(const AdamwArgs& a, const Coefs& k, float
   const double gs = k.coef * g;
   mn = (float)(a.b1 * m + a.nb1 * gs);
   vn = (float)(a.b2 * v + a.nb2 * gs * gs);
-  // an infinite v beside a finite m is the largest one; 0 a number with a root's reciprocal
-  const double s = (double)__builtin_amdgcn_fmed3f(vn, 0.0f, 3.4028234663852886e38f) * k.c2 + 1e-300;
-  const double r = __builtin_amdgcn_rsq(s), root = s * r, d = root + root * (0.5 - root * (0.5 * r)) + a.eps;
-  double q = __builtin_amdgcn_rcp(d);
-  q += q * (1.0 - d * q);
+  // the quotient is 0 where v has passed fp32; an infinite m beside it, and a v that is NaN,
+  // give NaN.  A v of 0 is a number with a root's reciprocal
+  double q = 0.0;
+  if (!(vn > 3.4028234663852886e38f)) {
+    const double s = (double)vn * k.c2 + 1e-300;
+    const double r = __builtin_amdgcn_rsq(s), root = s * r, d = root + root * (0.5 - root * (0.5 * r)) + a.eps;
+    q = __builtin_amdgcn_rcp(d);
+    q += q * (1.0 - d * q);
+  }
   p = (float)(k.keep * (double)p - k.by * (double)mn * q);
 }
 
