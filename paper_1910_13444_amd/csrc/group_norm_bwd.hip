@@ -435,8 +435,8 @@ __global__ void __launch_bounds__(SPLIT_NTH, SL == 1 ? 3 : 2) k_gn_bwd_apply(con
             }
             __builtin_amdgcn_sched_barrier(0);
           }
+          if (!tn.before(left)) break;
           left += tn.by;
-          if (left > tn.left) break;
           x -= tn.by * a.x.ld;
           dy -= tn.by * a.dy.ld;
           if (add) add -= tn.by * a.add.ld;

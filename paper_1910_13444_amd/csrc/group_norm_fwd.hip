@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(SPLIT_NTH) k_gn_apply(const GnArgs<T> a, uint3
         for (;;) {
           // the next turn's loads before this one's stores: a wait for them is one for the stores too
           piece_t next[U];
-          const bool more = left + tn.by <= tn.left;
+          const bool more = tn.before(left);
           q -= tn.by * a.x.ld;
           if (more) load_rows<WHOLE>(next, q, step, left + tn.by, pl.rows, valid);
 #pragma unroll

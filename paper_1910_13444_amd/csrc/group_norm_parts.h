@@ -193,10 +193,13 @@ __device__ __forceinline__ void load_rows(piece_t (&raw)[NV], const T* q, int64_
 struct Turns {
   int64_t first;   // a thread's first point
   int left, by;    // points from there on
-  __device__ __forceinline__ Turns(const GnPlan& pl, int64_t P, int U, uint32_t split, int splits, int row)
+  __host__ __device__ __forceinline__ Turns(const GnPlan& pl, int64_t P, int U, uint32_t split, int splits, int row)
       : first((int64_t)split * U * pl.rows + row), left((int)(P - first)), by(splits * U * pl.rows) {}
   // from the first turn's begin to the last one's; 0 without any
-  __device__ __forceinline__ int last() const { return left > by ? (left - 1) / by * by : 0; }
+  __host__ __device__ __forceinline__ int last() const { return left > by ? (left - 1) / by * by : 0; }
+  // whether a turn lies before the one with `at` points from its begin on.  A sample has up to
+  // 2^31 - 1 points: at + by may pass that, the difference does not
+  __host__ __device__ __forceinline__ bool before(int at) const { return left - at >= by; }
 };
 // of eight neighbours each stays on its XCD
 __device__ __forceinline__ uint32_t from_last(uint32_t i, uint32_t n) {
