@@ -78,7 +78,7 @@ constexpr size_t one_lds(int nth, int nv, int sl) {
 }
 
 template <class T, int NTH, int NV, int SL, bool WHOLE, int ACT>
-__global__ void __launch_bounds__(NTH, NV < 8 ? 1 : SL == 1 && WHOLE ? 4 : 3) k_gn_one(const GnArgs<T> a, int64_t batches) {
+__global__ void __launch_bounds__(NTH, NV < 8 ? 1 : SL == 1 && WHOLE ? 4 : 3) k_gn_one(const GnArgs<T> a, int64_t batches, uint32_t slab0) {
   constexpr int E = EPP<T>;
   constexpr bool VALUES = one_values(NV, SL);
   extern __shared__ Pair sm[];
@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(NTH, NV < 8 ? 1 : SL == 1 && WHOLE ? 4 : 3) k_
   const Div by_span(pl.span);
   const int per = row_of(pl.pw * SL);
   const int64_t g = blockIdx.z;
-  const Slab b = slab_at(a, blockIdx.x);
+  const Slab b = slab_at(a, slab0 + blockIdx.x);
   const int valid = b.width - col * E, left = (int)a.P - pr;
   for (int64_t bt = blockIdx.y; bt < batches; bt += gridDim.y) {
     const int64_t s0 = bt * pl.ns, s = s0 + si;
@@ -356,11 +356,14 @@ template <class T> hipError_t launch_gn_fwd(const GnArgs<T>& a, int G, hipStream
       k_gn_rows<T, 4, ACT><<<dim3((unsigned)std::min(turns, most), (unsigned)pl.slabs, G), 256, 0, st>>>(a);
     } else if (pl.mode == GN_ONE) {
       const int64_t batches = cdiv(a.S, pl.ns);
-      const dim3 grid((unsigned)pl.slabs, (unsigned)std::min<int64_t>(batches, 65535), G);
+      const int64_t most = int64_t(1) << 21;   // a launch's x dimension holds fewer than 2^32 threads
       by_width(a, [&](auto sl, auto whole) {
         by_shape<sl.value == 1 && whole.value>(pl, [&](auto nth, auto nv) {
           const size_t lds = one_lds(nth.value, nv.value, sl.value) + (size_t)pl.ns * pl.ng * (sizeof(Stat) + 4);
-          k_gn_one<T, nth.value, nv.value, sl.value, whole.value, ACT><<<grid, nth.value, lds, st>>>(a, batches);
+          for (int64_t at = 0; at < pl.slabs; at += most) {
+            const dim3 grid((unsigned)std::min(most, pl.slabs - at), (unsigned)std::min<int64_t>(batches, 65535), G);
+            k_gn_one<T, nth.value, nv.value, sl.value, whole.value, ACT><<<grid, nth.value, lds, st>>>(a, batches, (uint32_t)at);
+          }
         });
       });
     } else {

@@ -75,3 +75,21 @@ def test_the_longest_samples(P):
         h = 1.25 * dy[k].double()
         err = r * (e_m * (1 + xh.abs()) + 8 * EPS32 * (h.abs() + m1.abs() + (xh * m2).abs()))
         assert _near(y[k], r * (h - m1 - xh * m2), err, "bf16"), k
+
+
+def test_more_slabs_than_a_launch_holds():
+    """4,198,400 slabs of 64 channels whose 130 points take 1024 threads: more than 2^32.  A
+    field of one tile repeated gives the tile's results everywhere, in place (70 GB)."""
+    P, W, K = 130, 64 * 4096, 1025
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    tile = torch.empty((P, W), dtype=torch.bfloat16, device="cuda").normal_(0.5, 1.0, generator=gen)
+    gamma, beta = (torch.empty(W, dtype=torch.float32, device="cuda").normal_(v, 0.2, generator=gen) for v in (1.0, 0.0))
+    want, mean, rstd = pigan.group_norm(tile.view(1, P, W), W // 64, gamma, beta)
+    x = torch.empty((1, P, K * W), dtype=torch.bfloat16, device="cuda")
+    wide = x.view(P, K, W)
+    wide.copy_(tile[:, None, :].expand(P, K, W))
+    y, m, r = pigan.group_norm(x, K * W // 64, gamma.repeat(K), beta.repeat(K), out=x)
+    torch.cuda.synchronize()
+    assert torch.equal(m.view(K, -1), mean.expand(K, -1)) and torch.equal(r.view(K, -1), rstd.expand(K, -1))
+    for p in range(P):
+        assert torch.equal(wide[p], want[0, p].expand(K, W)), p
