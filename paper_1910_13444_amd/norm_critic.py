@@ -181,7 +181,8 @@ class CriticTrainer:
 
     optimizer "adamw" takes the tensors one by one: weight_decay of the matrices,
     states in state_bits (32 or 8), gradients clipped to max_norm (None: as they
-    are; an update with a gradient that is not finite is then skipped)."""
+    are).  With max_norm an update with a gradient that is not finite is skipped, and
+    not counted, on the device."""
 
     def __init__(self, critic: NormCritic, lr: float = 1e-4, clip: float | None = None, optimizer: str = "adam",
                  weight_decay: float = 0.0, state_bits: int = 32, max_norm: float | None = None):
@@ -191,7 +192,7 @@ class CriticTrainer:
             names = list(c.p)
             self.opt = AdamW([c.p[n] for n in names], [c.g[n] for n in names], lr,
                              weight_decay=[weight_decay if n in c.w else 0.0 for n in names], state_bits=state_bits,
-                             copies=None if c.low is None else [c.w.get(n) for n in names])
+                             copies=None if c.low is None else [c.w.get(n) for n in names], capturable=max_norm is not None)
         elif optimizer != "adam":
             raise ValueError(f"unknown optimizer {optimizer!r}: adam or adamw")
         elif weight_decay or state_bits != 32 or max_norm is not None:

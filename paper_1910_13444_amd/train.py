@@ -68,10 +68,11 @@ class AdamW:
     parameters.  The states are flat (m, v, with m_scale and v_scale in 8 bits), in
     the order of the parameters, each tensor's first element at `starts`.
 
-    capturable: the count of updates is an int32 on the device (`count`) that a
-    captured step advances with every replay; otherwise it is `t`.
-    grad_norm's coef and nonfinite flag are what step takes as scale and skip: a
-    clipped step reads nothing back."""
+    t is the count of updates.  capturable: it is an int32 on the device (`count`),
+    which the applied updates alone advance: a captured step with every replay, and
+    no step that its flag skips.  grad_norm's coef and nonfinite flag are what such a
+    step takes as scale and skip, and nothing is read back (reading t waits for the
+    device).  Otherwise the host counts, and has to know of a skipped step."""
 
     def __init__(self, params, grads, lr: float, beta1: float = 0.5, beta2: float = 0.9, eps: float = 1e-8,
                  weight_decay=0.0, state_bits: int = 32, copies=None, capturable: bool = False):
@@ -80,10 +81,21 @@ class AdamW:
         self.m_scale, self.v_scale = self.table.m_scale, self.table.v_scale
         self.starts = self.table.starts
         self.lr, self.beta1, self.beta2, self.eps = float(lr), float(beta1), float(beta2), float(eps)
-        self.t = 0
+        self._t = 0
         dev = self.table.device
         self.count = torch.zeros((), dtype=torch.int32, device=dev) if capturable else None
         self._ws = torch.empty(pigan.ADAMW_WORKSPACE, dtype=torch.uint8, device=dev) if capturable else None
+
+    @property
+    def t(self) -> int:
+        return self._t if self.count is None else int(self.count)
+
+    @t.setter
+    def t(self, t: int):
+        if self.count is None:
+            self._t = t
+        else:
+            self.count.fill_(t)
 
     def grad_norm(self, max_norm: float = float("inf"), scale: float = 1.0):
         """(norm, coef, nonfinite) of all gradients, on the device (pigan.grad_norm)."""
@@ -91,13 +103,13 @@ class AdamW:
 
     def step(self, scale=1.0, skip: torch.Tensor | None = None, count: bool = True):
         """One update from the gradients times `scale` (a number, or one fp32 value
-        on the device), skipped on the device when *skip != 0.  `count` advances t
-        (False when the host knows the step was skipped); a count on the device
-        follows the applied updates by itself."""
+        on the device), skipped on the device when *skip != 0.  `count` advances a t
+        that the host counts (False when the host knows the step is skipped); one on
+        the device follows the applied updates by itself."""
         if count and self.count is None:
-            self.t += 1
+            self._t += 1
         coef = scale if isinstance(scale, torch.Tensor) else None
-        pigan.adamw_update(self.table, self.lr, self.beta1, self.beta2, self.eps, max(self.t, 1),
+        pigan.adamw_update(self.table, self.lr, self.beta1, self.beta2, self.eps, max(self._t, 1),
                            1.0 if coef is not None else scale, coef, skip, self.count, self._ws)
 
     def states(self):
