@@ -742,7 +742,8 @@ pigan_status pigan_tensors_table(const pigan_tensors* a, void* table, size_t byt
  *   nonfinite = 1 where a gradient is infinite or NaN (coef is then 0 or scale), else 0.
  * scale (1 / loss scale) is finite and > 0, max_norm > 0 (may be infinite).  Outputs on
  * the device; any of them may be NULL, not all.  Sums in fp64, in a fixed order.
- * The workspace is 256-byte aligned.
+ * The workspace is 256-byte aligned.  Outputs and workspace share no memory with each
+ * other, the gradients or the table (EINVAL).
  */
 size_t pigan_grad_norm_workspace(const void* table);
 pigan_status pigan_grad_norm(const void* table, const void* device_table, double max_norm, double scale, float* norm,
@@ -761,6 +762,8 @@ pigan_status pigan_grad_norm(const void* table, const void* device_table, double
  *   coef  : device fp32 factor of the gradients (pigan_grad_norm's), or NULL: 1;
  *   skip  : device int32 (a step's or pigan_grad_norm's flag) or NULL; when it holds a
  *           non-zero value nothing is changed, the count included.
+ * step, coef, skip and the workspace share no memory with a parameter, copy or state, step
+ * and the workspace none with each other, coef, skip, a gradient or the table (EINVAL).
  */
 #define PIGAN_ADAMW_WORKSPACE 256
 typedef struct {

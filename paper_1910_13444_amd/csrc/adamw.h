@@ -20,8 +20,13 @@ struct TensorEntry {
 // A piece of work: elements [piece * PIECE, ...) of tensor `tensor`.
 struct TensorPiece { uint32_t tensor; uint32_t piece; };
 
+// Memory [from, to) of a table's tensors.
+struct Extent { uint64_t from; uint64_t to; };
+
 // A table, in host memory and, byte for byte, in device memory: the header, the
-// entries, the pieces.
+// entries, the pieces, and, for the host's checks of a call's other operands, what the
+// tensors' outputs (parameters, copies, states) and their gradients take, joined and in
+// the order of the addresses.
 struct TableHeader {
   uint64_t magic;
   int32_t n_tensors; int32_t bits;      // bits 0: gradients alone
@@ -29,6 +34,7 @@ struct TableHeader {
   int64_t entries_at; int64_t pieces_at; int64_t bytes;
   void* m; void* v; float* m_scale; float* v_scale;
   int64_t elements; int64_t g_bytes; int64_t copy_bytes;
+  int64_t extents_at; int64_t n_written; int64_t n_read;
 };
 constexpr uint64_t TABLE_MAGIC = 0x656c626174676970ull;
 

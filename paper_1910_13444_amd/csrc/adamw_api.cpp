@@ -63,13 +63,13 @@ pigan_status check_states(const pigan_tensors* a, const Counts& c) {
 
 struct Span { uintptr_t from, to; const char* what; int32_t tensor; };
 
-// every output lies apart from every other one and from every gradient
-pigan_status check_spans(const pigan_tensors* a, const Counts& c) {
+// parameters, copies and states
+std::vector<Span> written(const pigan_tensors* a, const Counts& c) {
   std::vector<Span> outs;
   auto add = [&](const void* p, int64_t bytes, const char* what, int32_t i) {
     if (p && bytes > 0) outs.push_back({(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes, what, i});
   };
-  if (!a->bits) return PIGAN_OK;
+  if (!a->bits) return outs;
   for (int32_t i = 0; i < a->n_tensors; ++i) {
     add(a->tensors[i].p, a->tensors[i].n * 4, "parameter", i);
     add(a->tensors[i].copy, a->tensors[i].n * 2, "copy", i);
@@ -81,19 +81,47 @@ pigan_status check_spans(const pigan_tensors* a, const Counts& c) {
     add(a->m_scale, c.states / QBLOCK * 4, "m_scale", -1);
     add(a->v_scale, c.states / QBLOCK * 4, "v_scale", -1);
   }
-  std::sort(outs.begin(), outs.end(), [](const Span& x, const Span& y) { return x.from < y.from; });
+  return outs;
+}
+
+std::vector<Span> gradients(const pigan_tensors* a) {
+  std::vector<Span> ins;
+  for (int32_t i = 0; i < a->n_tensors; ++i) {
+    const pigan_tensor& t = a->tensors[i];
+    if (t.n > 0) ins.push_back({(uintptr_t)t.g, (uintptr_t)t.g + (uintptr_t)(t.n * (int64_t)esize(t.g_dt)), "gradient", i});
+  }
+  return ins;
+}
+
+void sort(std::vector<Span>& v) {
+  std::sort(v.begin(), v.end(), [](const Span& x, const Span& y) { return x.from < y.from; });
+}
+
+// joined, in order, behind each other to `to`; their number
+int64_t extents(std::vector<Span> v, Extent* to) {
+  sort(v);
+  int64_t n = 0;
+  for (const Span& s : v) {
+    if (n > 0 && s.from <= to[n - 1].to) to[n - 1].to = std::max<uint64_t>(to[n - 1].to, s.to);
+    else to[n++] = {s.from, s.to};
+  }
+  return n;
+}
+
+// every output lies apart from every other one and from every gradient
+pigan_status check_spans(const pigan_tensors* a, const Counts& c) {
+  if (!a->bits) return PIGAN_OK;
+  std::vector<Span> outs = written(a, c);
+  sort(outs);
   for (size_t i = 1; i < outs.size(); ++i)
     if (outs[i].from < outs[i - 1].to)
       return fail(PIGAN_EINVAL, "%s (tensor %d) overlaps %s (tensor %d)", outs[i].what, (int)outs[i].tensor, outs[i - 1].what,
                   (int)outs[i - 1].tensor);
-  for (int32_t i = 0; i < a->n_tensors; ++i) {
-    const pigan_tensor& t = a->tensors[i];
-    if (t.n == 0) continue;
-    const uintptr_t from = (uintptr_t)t.g, to = from + (uintptr_t)(t.n * (int64_t)esize(t.g_dt));
+  for (const Span& g : gradients(a)) {
     // the last output that begins before the gradient ends
-    auto it = std::lower_bound(outs.begin(), outs.end(), to, [](const Span& s, uintptr_t v) { return s.from < v; });
-    if (it != outs.begin() && (--it)->to > from)
-      return fail(PIGAN_EINVAL, "gradient of tensor %d overlaps %s (tensor %d)", (int)i, it->what, (int)it->tensor);
+    auto it = std::lower_bound(outs.begin(), outs.end(), g.to, [](const Span& s, uintptr_t v) { return s.from < v; });
+    if (it != outs.begin() && (--it)->to > g.from)
+      return fail(PIGAN_EINVAL, "gradient of tensor %d overlaps %s (tensor %d)", (int)g.tensor, it->what, (int)it->tensor);
   }
   return PIGAN_OK;
 }
@@ -107,7 +135,9 @@ TableHeader header_of(const pigan_tensors* a, const Counts& c) {
   h.states = c.states;
   h.entries_at = round_up(sizeof(TableHeader), 16);
   h.pieces_at = h.entries_at + (int64_t)a->n_tensors * (int64_t)sizeof(TensorEntry);
-  h.bytes = h.pieces_at + c.pieces * (int64_t)sizeof(TensorPiece);
+  h.extents_at = h.pieces_at + c.pieces * (int64_t)sizeof(TensorPiece);
+  // as many as there are where none are joined
+  h.bytes = h.extents_at + ((int64_t)a->n_tensors * (a->bits ? 3 : 1) + (a->bits ? 4 : 0)) * (int64_t)sizeof(Extent);
   h.m = a->m;
   h.v = a->v;
   h.m_scale = a->m_scale;
@@ -126,6 +156,26 @@ pigan_status check_table(const void* table, const void* device_table) {
 }
 
 template <class T> const T* at(const void* table, int64_t off) { return (const T*)((const char*)table + off); }
+
+bool meets(const Extent* e, int64_t n, const Runs& r) {
+  const uint64_t from = (uint64_t)r.p, to = from + (uint64_t)r.len;
+  const Extent* it = std::upper_bound(e, e + n, from, [](uint64_t v, const Extent& x) { return v < x.to; });
+  return it != e + n && it->from < to;
+}
+
+// `r` apart from the tables' tensors: those that a call writes, and their gradients, and, where
+// the call writes r, from the table
+pigan_status check_off_tensors(const void* table, const void* device_table, const Runs& r, bool is_written, bool with_written,
+                               bool with_gradients) {
+  if (!r.p) return PIGAN_OK;
+  const TableHeader& h = *(const TableHeader*)table;
+  const Extent* e = at<Extent>(table, h.extents_at);
+  if (with_written && meets(e, h.n_written, r)) return fail(PIGAN_EINVAL, "%s overlaps a parameter, copy or state", r.name);
+  if (with_gradients && meets(e + h.n_written, h.n_read, r)) return fail(PIGAN_EINVAL, "%s overlaps a gradient", r.name);
+  const Extent own = {(uint64_t)(uintptr_t)device_table, (uint64_t)(uintptr_t)device_table + (uint64_t)h.bytes};
+  if (is_written && meets(&own, 1, r)) return fail(PIGAN_EINVAL, "%s overlaps the table", r.name);
+  return PIGAN_OK;
+}
 
 pigan_status check_device_word(const void* p, const char* name) {
   if ((uintptr_t)p % 4) return fail(PIGAN_EINVAL, "%s: not aligned to its elements", name);
@@ -167,9 +217,13 @@ pigan_status pigan_tensors_table(const pigan_tensors* a, void* table, size_t byt
     if (pigan_status st = check_tensors(a, c)) return st;
     if (pigan_status st = check_states(a, c)) return st;
     if (pigan_status st = check_spans(a, c)) return st;
-    const TableHeader h = header_of(a, c);
+    TableHeader h = header_of(a, c);
     if (!table || (uintptr_t)table % 8) return fail(PIGAN_EINVAL, "the table must be 8-byte aligned");
     if (bytes < (size_t)h.bytes) return fail(PIGAN_EINVAL, "table of %zu bytes, %lld are needed", bytes, (long long)h.bytes);
+    Extent* const to = (Extent*)((char*)table + h.extents_at);
+    h.n_written = extents(written(a, c), to);
+    h.n_read = extents(gradients(a), to + h.n_written);
+    memset(to + h.n_written + h.n_read, 0, (size_t)(h.bytes - h.extents_at) - (size_t)(h.n_written + h.n_read) * sizeof(Extent));
     memcpy(table, &h, sizeof h);
     TensorEntry* entries = (TensorEntry*)((char*)table + h.entries_at);
     TensorPiece* pieces = (TensorPiece*)((char*)table + h.pieces_at);
@@ -209,6 +263,8 @@ pigan_status pigan_grad_norm(const void* table, const void* device_table, double
     if (pigan_status st = check_ws(ws, ws_bytes, need)) return st;
     const Runs none[] = {{"the workspace", ws, (int64_t)need}};
     if (pigan_status st = check_apart(outs, none, [](int, int) { return false; })) return st;
+    for (const Runs& o : {outs[0], outs[1], outs[2], none[0]})
+      if (pigan_status st = check_off_tensors(table, device_table, o, true, false, true)) return st;
     const hipStream_t st = (hipStream_t)stream;
     ProfScope prof(st, "grad_norm", 0.0, (double)h.g_bytes);
     HIP_TRY(launch_grad_norm(at<TensorEntry>(device_table, h.entries_at), at<TensorPiece>(device_table, h.pieces_at), h.n_pieces,
@@ -233,9 +289,14 @@ pigan_status pigan_adamw_update(const pigan_adamw* a, void* ws, size_t ws_bytes,
     if (pigan_status st = check_device_word(a->coef, "coef")) return st;
     if (pigan_status st = check_device_word(a->skip, "skip")) return st;
     if (pigan_status st = check_device_word(a->step, "step")) return st;
-    if (a->step && (a->step == a->skip || (const void*)a->step == (const void*)a->coef))
-      return fail(PIGAN_EINVAL, "step overlaps skip or coef");
     if (pigan_status st = check_ws(ws, ws_bytes, a->step ? PIGAN_ADAMW_WORKSPACE : 0)) return st;
+    const Runs outs[] = {{"step", a->step, 4}, {"the workspace", a->step ? ws : nullptr, PIGAN_ADAMW_WORKSPACE}};
+    const Runs ins[] = {{"coef", a->coef, 4}, {"skip", a->skip, 4}};
+    if (pigan_status st = check_apart(outs, ins, [](int, int) { return false; })) return st;
+    for (const Runs& r : ins)
+      if (pigan_status st = check_off_tensors(a->table, a->device_table, r, false, true, false)) return st;
+    for (const Runs& r : outs)
+      if (pigan_status st = check_off_tensors(a->table, a->device_table, r, true, true, true)) return st;
     const hipStream_t st = (hipStream_t)stream;
     AdamwArgs k{};
     k.entries = at<TensorEntry>(a->device_table, h.entries_at);

@@ -8,6 +8,7 @@ import math
 import pytest
 import torch
 
+from paper_1910_13444_amd import pigan
 from paper_1910_13444_amd.train import AdamW
 from _layers import check
 
@@ -73,3 +74,30 @@ def test_states_that_are_not_finite():
         before = p.double().cpu()
         opt.step()
         _check_step(p, before, *_states(m.double(), v.double(), g.double().cpu()), 1)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_words_beside_the_tensors(bits):
+    """Count, factor, flag and norms in the elements between parameters and gradients of one
+    buffer: taken as others, one element further refused."""
+    n = 300
+    flat = torch.zeros(3 * n + 8, dtype=torch.float32, device="cuda")
+    ints = flat.view(torch.int32)
+    gen = torch.Generator().manual_seed(2)
+    start, grad = (torch.randn(n, generator=gen, dtype=torch.float32).cuda() for _ in range(2))
+    # coef | p | step, skip | g | norm words
+    p, g = flat[1:1 + n], flat[n + 3:2 * n + 3]
+    coef, step, skip = flat[0:1], ints[n + 1:n + 2], ints[n + 2:n + 3]
+    p.copy_(start), g.copy_(grad), coef.fill_(0.5)
+    table = pigan.TensorTable([g], [p], bits=bits)
+    pigan.adamw_update(table, LR, B1, B2, EPS, coef=coef, step=step, skip=skip)
+    want = start.clone()
+    other = AdamW([want], [grad], LR, B1, B2, EPS, state_bits=bits)
+    other.step(0.5)
+    assert torch.equal(p, want) and torch.equal(g, grad) and step.item() == 1
+    assert (coef.item(), skip.item()) == (0.5, 0) and not flat[2 * n + 3:].any()
+    for bad in (dict(coef=flat[1:2]), dict(coef=flat[n:n + 1]), dict(skip=ints[n:n + 1]), dict(step=ints[1:2]),
+                dict(step=ints[n + 3:n + 4]), dict(coef=coef, step=coef.view(torch.int32))):
+        with pytest.raises(pigan.PiganError):
+            pigan.adamw_update(table, LR, B1, B2, EPS, 1, **bad)
+    assert torch.equal(p, want) and step.item() == 1
