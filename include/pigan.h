@@ -635,7 +635,7 @@ pigan_status pigan_layer_norm_backward(const pigan_norm* a, void* ws, size_t ws_
  *
  * Overlaps of outputs, errors and numbers as for the layers above (statistics are
  * summed in fp64, a constant channel group normalises to beta; the reverse pass sums
- * in fp32 within a thread and joins in fp64, in a fixed order).  No samples (S = 0)
+ * up to 512 terms in fp32 and joins those sums in fp64, in a fixed order).  No samples (S = 0)
  * is valid: nothing but zero parameter gradients is written.  No points is EINVAL.
  */
 typedef struct {

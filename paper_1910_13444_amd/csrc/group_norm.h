@@ -44,6 +44,10 @@ constexpr Shape FWD_SHAPES[] = {{256, 1}, {256, 4}, {1024, 2}, {256, 8}, {512, 8
 constexpr Shape FWD_ODD[] = {{256, 1}, {512, 1}, {256, 4}, {256, 8}};   // channel groups that are no whole pieces
 constexpr Shape BWD_SHAPES[] = {{256, 1}, {512, 1}};
 constexpr int SPLIT_NTH = 256;   // threads of a block that takes a range of points
+// Terms that the reverse pass sums in fp32 at most, before it joins in fp64: of a channel's
+// gradients those of a thread, of a channel group's means those of a row's lanes (64 pieces).
+// A sum is off by BWD_TERMS 2^-24 of its terms' sizes at most.
+constexpr int64_t BWD_TERMS = 512;
 
 struct Pair { double s, q; };    // of two sums
 

@@ -37,11 +37,13 @@ GnPlan gn_plan(bool backward, int fields, int elem_bytes, int64_t G, int64_t S, 
     // as many lanes as entries, and no more groups in turns than need be
     while (pl.lanes > 1 && (pl.lanes / 2 >= entries || pl.lanes * pl.ng * pl.ns > pl.nth)) pl.lanes /= 2;
   };
-  // blocks beside each other over a reverse pass's samples, four to a CU; few batches are one
-  // block's, as the sum of several blocks' columns is a launch of its own (3.4 us)
+  // blocks beside each other over a reverse pass's samples, four to a CU, and more where a
+  // thread would have more than BWD_TERMS; few batches are one block's, as the sum of several
+  // blocks' columns is a launch of its own (3.4 us)
   auto slots = [&](int64_t batches) {
     if (batches <= 6) return (int32_t)1;
-    return (int32_t)std::min<int64_t>(batches, std::max<int64_t>(1, 1024 / std::min<int64_t>(1024, G * pl.slabs)));
+    const int64_t each = std::max<int64_t>(1, 1024 / std::min<int64_t>(1024, G * pl.slabs));
+    return (int32_t)std::min(batches, std::max(each, cdiv(batches, BWD_TERMS)));
   };
   const int64_t lanes = cg / E;
   if (P == 1 && whole_pieces && lanes <= 64 && (lanes & (lanes - 1)) == 0 && cdiv(n, 256 / lanes) <= 65535) {
@@ -104,6 +106,7 @@ GnPlan gn_plan(bool backward, int fields, int elem_bytes, int64_t G, int64_t S, 
   const int64_t blocks = 256 * (backward ? 3 : 5), base = G * S * pl.slabs, least = cdiv(P, 4 * pl.rows);
   const int64_t each = base < blocks ? blocks / base : cdiv(4 * blocks, base);
   pl.splits = (int32_t)std::max<int64_t>(1, std::min(each, least));
+  if (backward) pl.splits = (int32_t)std::max<int64_t>(pl.splits, cdiv(P, BWD_TERMS * pl.rows));
   pl.slots = (int32_t)std::min(S * pl.splits, std::max<int64_t>(1, blocks / std::min(blocks, G * pl.slabs)));
   return pl;
 }

@@ -93,3 +93,22 @@ def test_more_slabs_than_a_launch_holds():
     assert torch.equal(m.view(K, -1), mean.expand(K, -1)) and torch.equal(r.view(K, -1), rstd.expand(K, -1))
     for p in range(P):
         assert torch.equal(wide[p], want[0, p].expand(K, W)), p
+
+
+@pytest.mark.parametrize("size", [(1024, 16384, 1, 256, 1), (1024, 172032, 3, 8, 1), (None, 1, 768 * 256 * 4096, 1, 1),
+                                  (None, 3072, 4096 * 256, 1, 1)])
+def test_long_sums_of_one_sign(size):
+    """fp32 gradients of gamma and beta of up to 3e9 equal terms.  The pass sums up to 512
+    terms in fp32 (half a unit of the partial sum each) and joins in fp64; 4096 terms of this
+    value in a row would be off by 1000 half units."""
+    G, S, P, C, n = size
+    c = 1.0216064453125
+    shape, lead = ((S, P, C), ()) if G is None else ((G, S, P, C), (G,))
+    x = torch.full(shape, c, dtype=torch.float32, device="cuda")
+    mean, rstd = (torch.full((*lead, S, n), v, dtype=torch.float32, device="cuda") for v in (0.0, 1.0))
+    _, dgamma, dbeta = pigan.group_norm_backward(x, x, mean, rstd, need_dx=False)
+    torch.cuda.synchronize()
+    del x
+    for got, term in ((dgamma, c * c), (dbeta, c)):
+        want = torch.full((*lead, C), S * P * term, dtype=torch.float64)
+        check(got, want, 514 * EPS32 * want, "fp32", "sum")   # and the term's own roundings
