@@ -62,8 +62,17 @@ pigan_status check_backward(const pigan_group_norm* a) {
   return a->dx.p ? check_field(a->dx, "dx", a) : PIGAN_OK;
 }
 
-Runs runs(const char* name, const pigan_field& f, const pigan_group_norm* a) {
+// strides of what there is one of may be any: 0, so that no product with them passes 64 bits
+pigan_field used(pigan_field f, const pigan_group_norm* a) {
+  if (a->P < 2) f.ld = 0;
+  if (a->S < 2) f.ss = 0;
+  if (a->n_groups < 2) f.gs = 0;
+  return f;
+}
+
+Runs runs(const char* name, const pigan_field& field, const pigan_group_norm* a) {
   const int64_t es = (int64_t)esize(a->dt);
+  const pigan_field f = used(field, a);
   return Runs(name, f.p, a->C * es).repeat(a->P, f.ld * es).repeat(a->S, f.ss * es).repeat(a->n_groups, f.gs * es);
 }
 
@@ -96,12 +105,14 @@ size_t backward_ws(const pigan_group_norm* a, const GnPlan& pl) {
   return a->S > 0 ? gn_backward_ws(pl, a->n_groups, a->S, a->C, a->n, a->dgamma || a->dbeta) : 0;
 }
 
-template <class T> Field<const T> in(const pigan_field& f) { return {(const T*)f.p, f.ld, f.ss, f.gs}; }
-template <class T> Field<T> out(const pigan_field& f) { return {(T*)f.p, f.ld, f.ss, f.gs}; }
+template <class T> Field<T> field(const pigan_field& f, const pigan_group_norm* a) {
+  const pigan_field u = used(f, a);
+  return {(T*)u.p, u.ld, u.ss, u.gs};
+}
 
 template <class T> GnArgs<T> args(const pigan_group_norm* a, const GnPlan& pl, void* ws) {
   GnArgs<T> k{};
-  k.x = in<T>(a->x);
+  k.x = field<const T>(a->x, a);
   k.gamma = a->gamma;
   k.beta = a->beta;
   k.mean = a->mean;
@@ -151,7 +162,7 @@ pigan_status pigan_group_norm_forward(const pigan_group_norm* a, void* ws, size_
     return by_dtype(a->dt, [&](auto t) -> pigan_status {
       typedef decltype(t) T;
       GnArgs<T> k = args<T>(a, pl, ws);
-      k.out = out<T>(a->y);
+      k.out = field<T>(a->y, a);
       HIP_TRY(launch_gn_fwd(k, a->n_groups, st));
       return PIGAN_OK;
     });
@@ -181,9 +192,9 @@ pigan_status pigan_group_norm_backward(const pigan_group_norm* a, void* ws, size
     return by_dtype(a->dt, [&](auto t) -> pigan_status {
       typedef decltype(t) T;
       GnArgs<T> k = args<T>(a, pl, ws);
-      k.dy = in<T>(a->dy);
-      k.add = in<T>(a->add);
-      k.out = out<T>(a->dx);
+      k.dy = field<const T>(a->dy, a);
+      k.add = field<const T>(a->add, a);
+      k.out = field<T>(a->dx, a);
       k.dgamma = a->dgamma;
       k.dbeta = a->dbeta;
       HIP_TRY(launch_gn_bwd(k, a->n_groups, st));
