@@ -334,8 +334,8 @@ pigan_status pigan_state_values(int64_t n, const int8_t* m, const float* m_scale
                                 float* m_out, float* v_out, void* stream) {
   return guarded([&]() -> pigan_status {
     if (n < 0 || n % QBLOCK || n > MOST) return fail(PIGAN_EINVAL, "n=%lld must be a multiple of 256 in [0, 2^40]", (long long)n);
+    if (n == 0) return PIGAN_OK;   // outputs of no elements may have no address
     if (!m_out && !v_out) return fail(PIGAN_EINVAL, "no output: m_out and v_out are null");
-    if (n == 0) return PIGAN_OK;
     if ((m_out && (!m || !m_scale)) || (v_out && (!v || !v_scale))) return fail(PIGAN_EINVAL, "null codes or scales");
     if ((uintptr_t)m % 4 || (uintptr_t)v % 4) return fail(PIGAN_EINVAL, "m and v must be 4-byte aligned");
     if ((uintptr_t)m_scale % 4 || (uintptr_t)v_scale % 4 || (uintptr_t)m_out % 4 || (uintptr_t)v_out % 4)

@@ -101,3 +101,17 @@ def test_words_beside_the_tensors(bits):
         with pytest.raises(pigan.PiganError):
             pigan.adamw_update(table, LR, B1, B2, EPS, 1, **bad)
     assert torch.equal(p, want) and step.item() == 1
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_tensors_of_no_elements(bits):
+    """A network's tensors may all be empty: every call is valid and changes nothing."""
+    p, g = (torch.empty((0, 3), dtype=torch.float32, device="cuda") for _ in range(2))
+    for n in (1, 3):
+        opt = AdamW([p] * n, [g] * n, LR, state_bits=bits, capturable=True)
+        norm, coef, flag = opt.grad_norm(0.5, 0.25)
+        assert (norm.item(), coef.item(), flag.item()) == (0.0, 0.25, 0)
+        opt.step(coef, flag)
+        assert opt.t == 1
+        m, v = opt.states()
+        assert m.shape == v.shape == (0,) and m.dtype == v.dtype == torch.float32
