@@ -93,13 +93,13 @@ std::vector<Span> gradients(const pigan_tensors* a) {
   return ins;
 }
 
-void sort(std::vector<Span>& v) {
+std::vector<Span> in_order(std::vector<Span> v) {
   std::sort(v.begin(), v.end(), [](const Span& x, const Span& y) { return x.from < y.from; });
+  return v;
 }
 
-// joined, in order, behind each other to `to`; their number
-int64_t extents(std::vector<Span> v, Extent* to) {
-  sort(v);
+// joined, behind each other to `to`; their number
+int64_t extents(const std::vector<Span>& v, Extent* to) {
   int64_t n = 0;
   for (const Span& s : v) {
     if (n > 0 && s.from <= to[n - 1].to) to[n - 1].to = std::max<uint64_t>(to[n - 1].to, s.to);
@@ -109,15 +109,12 @@ int64_t extents(std::vector<Span> v, Extent* to) {
 }
 
 // every output lies apart from every other one and from every gradient
-pigan_status check_spans(const pigan_tensors* a, const Counts& c) {
-  if (!a->bits) return PIGAN_OK;
-  std::vector<Span> outs = written(a, c);
-  sort(outs);
+pigan_status check_spans(const std::vector<Span>& outs, const std::vector<Span>& grads) {
   for (size_t i = 1; i < outs.size(); ++i)
     if (outs[i].from < outs[i - 1].to)
       return fail(PIGAN_EINVAL, "%s (tensor %d) overlaps %s (tensor %d)", outs[i].what, (int)outs[i].tensor, outs[i - 1].what,
                   (int)outs[i - 1].tensor);
-  for (const Span& g : gradients(a)) {
+  for (const Span& g : grads) {
     // the last output that begins before the gradient ends
     auto it = std::lower_bound(outs.begin(), outs.end(), g.to, [](const Span& s, uintptr_t v) { return s.from < v; });
     if (it != outs.begin() && (--it)->to > g.from)
@@ -216,13 +213,14 @@ pigan_status pigan_tensors_table(const pigan_tensors* a, void* table, size_t byt
     Counts c;
     if (pigan_status st = check_tensors(a, c)) return st;
     if (pigan_status st = check_states(a, c)) return st;
-    if (pigan_status st = check_spans(a, c)) return st;
+    const std::vector<Span> outs = in_order(written(a, c)), grads = in_order(gradients(a));
+    if (pigan_status st = check_spans(outs, grads)) return st;
     TableHeader h = header_of(a, c);
     if (!table || (uintptr_t)table % 8) return fail(PIGAN_EINVAL, "the table must be 8-byte aligned");
     if (bytes < (size_t)h.bytes) return fail(PIGAN_EINVAL, "table of %zu bytes, %lld are needed", bytes, (long long)h.bytes);
     Extent* const to = (Extent*)((char*)table + h.extents_at);
-    h.n_written = extents(written(a, c), to);
-    h.n_read = extents(gradients(a), to + h.n_written);
+    h.n_written = extents(outs, to);
+    h.n_read = extents(grads, to + h.n_written);
     memset(to + h.n_written + h.n_read, 0, (size_t)(h.bytes - h.extents_at) - (size_t)(h.n_written + h.n_read) * sizeof(Extent));
     memcpy(table, &h, sizeof h);
     TensorEntry* entries = (TensorEntry*)((char*)table + h.entries_at);
