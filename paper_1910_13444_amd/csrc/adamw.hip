@@ -164,7 +164,7 @@ __device__ __forceinline__ Coefs coefs_of(const AdamwArgs& a, double decay) {
 }
 
 // the new states, as fp32 values, and the new parameter.  Root and quotient are the
-// hardware's fp64 approximations (2^-24) with a Newton step each (1e-14).
+// hardware's fp64 approximations (2^-24.2, 2^-24.4) with a Newton step each (1e-14).
 __device__ __forceinline__ void update(const AdamwArgs& a, const Coefs& k, float g, double m, double v, float& p, float& mn,
                                        float& vn) {
   const double gs = k.coef * g;

@@ -1,4 +1,5 @@
-// Launchers of group norm with an activation (group_norm.hip).
+// Launchers of group norm with an activation (group_norm_fwd.hip, group_norm_bwd.hip) and how
+// a call is cut (group_norm_plan.cpp).
 #pragma once
 #include "common.h"
 

@@ -932,7 +932,8 @@ class TensorTable:
     each tensor begins at a whole block of 256 (pigan.h has the format); `starts`
     are the tensors' first elements in them.  The table holds the tensors, and is
     good as long as they stay where they are: one whose memory was exchanged needs
-    a new table."""
+    a new table, whose states take the values of the old one's (`new.m.copy_(old.m)`;
+    v, and in 8 bits the scales, alike)."""
 
     def __init__(self, grads, params=None, copies=None, decay=0.0, bits: int = 0):
         self.grads = [_leaf(g) for g in grads]
